@@ -525,6 +525,73 @@ int32_t rtp_local_attn_ring(const rtp_layer_desc* layer, const void* q,
                             const int32_t* ctx_len, int32_t B, int64_t max_ctx, void* out, float* lse,
                             void* ws, size_t ws_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * A K/V cache held in 4 bits, in pages -- a storage format (the equations of Sec. 3.2 unchanged, on the values that the
+ * cache stands for): 136 bytes per token and KV head where a 16-bit cache has 512.
+ *
+ * A row of 128 values is four blocks of 32 consecutive ones.  A block is a scale byte s, which stands for 2^(s - 127), and 32
+ * codes of sign, 2 exponent bits and 1 mantissa bit: +-{0, .5, 1, 1.5, 2, 3, 4, 6}.  rtp_kv4_append chooses, with
+ * amax = max |x| of the block = (1 + M) 2^(E - 127),  s = max(2, E - 2 + [M >= 0.75]),  and rounds x 2^(127 - s) to the nearest
+ * code, ties to the even one: the largest value of a block lies in [3.5, 7) steps and is off by at most half a step of the
+ * codes, like every other.  A block that holds an infinity or a NaN gets s = 255, and all its values read as NaN.
+ *
+ * Position t of sequence b lives in slot r = t % page_size of pool page P = page_table[b * pt_stride + t / page_size]:
+ *   codes   128 bytes at  codes + P * code_page_stride + kvh * code_head_stride + r * 128:  K in the first 64 (dims 2i and
+ *           2i + 1 in the low and the high half of byte i), V in the other 64
+ *   scales  one byte per block j at  scales + P * scale_page_stride + kvh * scale_head_stride + (r / 4) * 32 + 4 j + r % 4
+ *           for K, 16 bytes further for V
+ * codes, scales and all four strides (in BYTES) are multiples of 16; pages and heads may be nested either way (head-major or
+ * page-major) but must not overlap.  page_size: a power of two in [16, 2^20].  A page is page_size * 128 bytes of codes and
+ * page_size * 8 of scales per KV head: 16-byte pieces that rtp_kv_pages_copy moves.
+ *
+ * An entry of page_table that is not in [0, n_pages), and a position behind pt_stride * page_size, are never followed: rtp_kv4_append
+ * drops such a token, rtp_kv4_read gives zeros for it, and the attention leaves it out.  The struct is HOST memory, read during the call.
+ */
+typedef struct rtp_kv4_cache {
+  void* codes;
+  int64_t code_page_stride, code_head_stride;
+  void* scales;
+  int64_t scale_page_stride, scale_head_stride;
+  const int32_t* page_table;   /* device int32 [B, pt_stride] */
+  int64_t pt_stride;
+  int32_t page_size;
+  int32_t n_pages;             /* pages of the pool */
+} rtp_kv4_cache;
+
+/* Stores new tokens: token t < count[b] (count NULL: T; never more than T) of sequence b goes to position start[b] + t.
+ * k, v: the layer's 16-bit type, element (b, t, kvh, c) at base[b * batch_stride + t * token_stride + kvh * head_stride + c], strides
+ * in ELEMENTS, multiples of 8, 16-byte aligned bases -- a slice of a fused projection, or rows of a head-major cache.  start: device
+ * int32 [B], start[b] < 0 skips the sequence.  Positions that the call does not name keep their bytes.  No workspace.
+ * A sequence may stand in one call once; the pages written to must belong to one sequence each. */
+int32_t rtp_kv4_append(const rtp_layer_desc* layer, const rtp_kv4_cache* cache, const void* k, const void* v,
+                       int64_t batch_stride, int64_t token_stride, int64_t head_stride, const int32_t* start,
+                       const int32_t* count, int32_t B, int32_t T, void* stream);
+
+/* Gives stored tokens back in the layer's 16-bit type (bf16: exactly; fp16: rounded once) -- what a further prefill chunk's attention,
+ * which reads 16-bit rows, needs of a context that is held in 4 bits.  Positions start[b] .. start[b] + count[b] - 1 go to rows
+ * 0 .. count[b] - 1 of sequence b, laid out like the inputs of rtp_kv4_append; rows behind them are left as they are.  No workspace. */
+int32_t rtp_kv4_read(const rtp_layer_desc* layer, const rtp_kv4_cache* cache, const int32_t* start, const int32_t* count,
+                     int32_t B, int32_t T, void* k, void* v, int64_t batch_stride, int64_t token_stride, int64_t head_stride,
+                     void* stream);
+
+/* rtp_sparse_attn_decode, rtp_local_attn (n_q = 1) and rtp_dense_attn (n_q = 1) with the 4-bit cache as the source of K and V; the
+ * other arguments, the rows that are written and lse are theirs.  Contexts and selections longer than max_ctx / max_sel are cut
+ * there (both in [1, 2^30]); selected positions may come in any order.  K and V are taken as the values that the codes
+ * stand for, exactly; products and sums are fp32, and probabilities enter the product with V with 16 bits of mantissa.  A row whose
+ * set is empty writes zeros and lse = -inf; a token whose K block is NaN makes its row NaN.
+ * rtp_local_attn_kv4 and rtp_dense_attn_kv4 serve any batch with B * n_kv_heads <= 2^20, rtp_sparse_attn_decode_kv4 up to 1024 rows
+ * (B * n_ret <= 1024): RTP_ERR_UNSUPPORTED beyond that. */
+size_t rtp_sparse_attn_decode_kv4_workspace_bytes(const rtp_layer_desc* layer, int32_t B, int64_t max_sel);
+int32_t rtp_sparse_attn_decode_kv4(const rtp_layer_desc* layer, const void* q, const rtp_kv4_cache* cache,
+                                   const int32_t* sel_idx, int64_t sel_stride, const int32_t* sel_count, int64_t max_sel,
+                                   int32_t B, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+size_t rtp_local_attn_kv4_workspace_bytes(const rtp_layer_desc* layer, int32_t B, int64_t max_ctx);
+int32_t rtp_local_attn_kv4(const rtp_layer_desc* layer, const void* q, const rtp_kv4_cache* cache, const int32_t* ctx_len,
+                           int32_t B, int64_t max_ctx, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+size_t rtp_dense_attn_kv4_workspace_bytes(const rtp_layer_desc* layer, int32_t B, int64_t max_ctx);
+int32_t rtp_dense_attn_kv4(const rtp_layer_desc* layer, const void* q, const rtp_kv4_cache* cache, const int32_t* ctx_len,
+                           int32_t B, int64_t max_ctx, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

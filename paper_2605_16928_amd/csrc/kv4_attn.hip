@@ -1,0 +1,632 @@
+// Decode attention over the 4-bit cache: rtp_sparse_attn_decode_kv4 (selected tokens, retrieval heads), rtp_local_attn_kv4 (sink +
+// window, the other heads) and rtp_dense_attn_kv4 (every token, every head).
+//
+//   out_h = sum_n p_n v_n / sum_n p_n,   p_n = 2^(c <q_h, k_n> - m),   c = softmax scale * log2(e)
+// over the tokens n of the set, K and V as the values that their codes stand for.
+//
+// Bound: 136 bytes per token and KV head.  At that size the vector ALU is as near a limit as HBM is, so both products go to the matrix
+// cores, 32 tokens (two tiles of 16) per wave and step:
+//   S = K q^T    v_mfma_f32_16x16x32_bf16, A = 16 tokens: lane (token c, quarter g) holds the dims 32 g .. + 31 of its token -- one
+//                16-byte load, one scale -- as bf16, which every code times its scale is exactly.  B = the queries in 8 columns.
+//   O += P V     A = P, whose rows are the columns of S: lane (head c, rows g) has the tokens 4 g + i of both tiles in registers and
+//                takes them for the k positions 8 g .. + 7, so no probability changes its lane.  B = V: lane (c, g) loads the dims
+//                8 c .. + 7 (one word) of the tokens 4 g + i, and pairs of converted values are regrouped to pairs of tokens.
+// A GQA group has at most 8 heads, so the other 8 columns and rows are free.  They carry what 16 bits lose: P is the sum of its
+// bf16 rounding (rows 0 - 7) and the bf16 rounding of the rest (rows 8 - 15; the columns 8 - 15 of S repeat the heads, so the lane
+// that needs the rest has p itself), and an fp16 query is split over the columns the same way.  P keeps 16 bits of mantissa thereby,
+// and one kernel serves both types.
+//
+// Work split: a unit (sequence and KV head, or sequence and retrieval head) is cut into items, an item goes to a workgroup of four
+// waves, which leaves a partial (max, sum, 128 outputs) per head for the merge launch, or the result where a unit is one item.
+#include "attn_decode_shared.h"
+#include "kv4_cache.h"
+
+namespace rtp {
+
+struct Kv4AttnArgs {
+  AttnDecodeArgs d;            // (K, V, strides, seq_start, ring and table fields are not used)
+  Kv4Cache c;
+  int32_t max_len;             // upper bound of a context / a selection: longer ones are cut there
+  int32_t direct;              // range sources: a unit is one item and writes its result
+};
+
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  bf16x2_t v;
+  v[0] = (__bf16)lo;
+  v[1] = (__bf16)hi;
+  return __builtin_bit_cast(uint32_t, v);
+}
+__device__ __forceinline__ uint16_t out16(float x, bool f16) {       // (NaN stays NaN)
+  return f16 ? __builtin_bit_cast(uint16_t, (_Float16)x) : __builtin_bit_cast(uint16_t, (__bf16)x);
+}
+
+// One wave's share of 32 tokens, as loaded.
+struct Kv4Tiles {
+  u32x4 k[2];                  // tile s: token c, dims 32 g .. + 31
+  uint32_t v[2][4];            // tile s: token 4 g + i, dims 8 c .. + 7
+  uint32_t ks[2];              // scale byte of k[s]
+  uint32_t vs[2];              // scale bytes of v[s][0 .. 3]
+};
+
+// A wave's running state: m of head c & 7 (the same in the four lanes of a column and in column c + 8), l per lane, outputs of
+// rows 4 g + i at dims 8 c + n.
+struct Kv4State {
+  float m, l;
+  f32x4_t o[8];
+};
+
+constexpr float kLateMax = 8.f;   // the reference m follows the maximum only when it is left behind by more than this: p <= 2^8
+
+// valid: bit t = token t of the 32 takes part.  Tokens that do not are masked out of S; their V scales have to be finite.
+template <bool F16>
+__device__ __forceinline__ void kv4_step(const Kv4Tiles& t, const uint32_t valid, const u32x4 (&qB)[4], const float scale_log2,
+                                         Kv4State& st) {
+  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+  float x[2][4];
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    const float f = __uint_as_float(t.ks[s] << 23);
+    f32x4_t S = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+      u32x4 a;
+      a[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(t.k[s][kk], f, 0));
+      a[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(t.k[s][kk], f, 1));
+      a[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(t.k[s][kk], f, 2));
+      a[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(t.k[s][kk], f, 3));
+      S = mfma16<false>(a, qB[kk], S);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float y = S[i];
+      if (F16) y += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), 0x128, 0xf, 0xf, true));   // row_ror:8
+      x[s][i] = y * scale_log2;
+    }
+  }
+  const float ninf = -__builtin_huge_valf();
+  if (valid != 0xffffffffu) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const uint32_t mine = valid >> (16 * s + 4 * g);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[s][i] = (mine >> i) & 1u ? x[s][i] : ninf;
+    }
+  }
+  float mx = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])), fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
+  mx = max_over_rows(mx);
+  if (__ballot(mx > st.m + kLateMax) != 0ull) {          // (also where m is still -inf)
+    const float m_new = fmaxf(st.m, mx);
+    const float corr = m_new == ninf ? 1.f : fast_exp2(st.m - m_new);
+    st.l *= corr;
+    st.m = m_new;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float ci = __shfl(corr, (lane & 48) | ((4 * g + i) & 7));
+#pragma unroll
+      for (int n = 0; n < 8; ++n) st.o[n][i] *= ci;
+    }
+  }
+  const float ref = st.m == ninf ? 0.f : st.m;           // (a row without a finite logit so far: NaN stays NaN, -inf gives 0)
+  u32x4 pA;
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    float p[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      p[i] = fast_exp2(x[s][i] - ref);
+      st.l += p[i];
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t hi = pack_bf16(p[2 * h], p[2 * h + 1]);
+      const uint32_t rest = pack_bf16(p[2 * h] - bf16_lo(hi), p[2 * h + 1] - bf16_hi(hi));
+      pA[2 * s + h] = c < 8 ? hi : rest;
+    }
+  }
+  float fv[2][4];
+#pragma unroll
+  for (int s = 0; s < 2; ++s)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) fv[s][i] = kv4_scale(t.vs[s], i);
+#define RTP_KV4_PV(B)                                                                                                        \
+  {                                                                                                                          \
+    u32x4 even, odd;                                                                                                         \
+    _Pragma("unroll") for (int s = 0; s < 2; ++s) _Pragma("unroll") for (int h = 0; h < 2; ++h) {                             \
+      const uint32_t a = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(t.v[s][2 * h], fv[s][2 * h], B));          \
+      const uint32_t b = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(t.v[s][2 * h + 1], fv[s][2 * h + 1], B));  \
+      even[2 * s + h] = __builtin_amdgcn_perm(b, a, 0x05040100u);                                                             \
+      odd[2 * s + h] = __builtin_amdgcn_perm(b, a, 0x07060302u);                                                              \
+    }                                                                                                                        \
+    st.o[2 * B] = mfma16<false>(pA, even, st.o[2 * B]);                                                                       \
+    st.o[2 * B + 1] = mfma16<false>(pA, odd, st.o[2 * B + 1]);                                                                \
+  }
+  RTP_KV4_PV(0)
+  RTP_KV4_PV(1)
+  RTP_KV4_PV(2)
+  RTP_KV4_PV(3)
+#undef RTP_KV4_PV
+}
+
+// The queries of heads h0 .. h0 + heads - 1 as the B operand: column c = head c & 7 (zero beyond `heads`); the columns 8 - 15 repeat
+// them, or hold what bf16 leaves of an fp16 query.
+template <bool F16>
+__device__ __forceinline__ void kv4_queries(const AttnDecodeArgs& a, int b, int h0, int heads, u32x4 (&qB)[4]) {
+  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+#pragma unroll
+  for (int kk = 0; kk < 4; ++kk) {
+    qB[kk] = (u32x4){0u, 0u, 0u, 0u};
+    if ((c & 7) < heads) qB[kk] = *reinterpret_cast<const u32x4*>(a.q + ((int64_t)b * a.n_q_heads + h0 + (c & 7)) * kHeadDim + 32 * g + 8 * kk);
+    if (F16) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float lo = lo16<true>(qB[kk][i]), hi = hi16<true>(qB[kk][i]);
+        const uint32_t top = pack_bf16(lo, hi);
+        qB[kk][i] = c < 8 ? top : pack_bf16(lo - bf16_lo(top), hi - bf16_hi(top));
+      }
+    }
+  }
+}
+
+// Joins the four waves' states of an item through LDS and writes the partials of its heads, or, `direct`, their results.
+// skip: heads (of the unit's) that the call does not serve.
+__device__ __forceinline__ void kv4_finish(const Kv4AttnArgs& a, Kv4State& st, int item, int b, int h0, int heads, bool direct,
+                                           uint32_t skip) {
+  __shared__ float sh_m[4][8], sh_l[4][8];
+  __shared__ float sh_o[4][8][kHeadDim];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 15, g = lane >> 4;
+  const float ninf = -__builtin_huge_valf();
+  st.l = sum_rows(st.l, st.l, st.l, st.l);
+  if (lane < 8) { sh_m[wave][lane] = st.m; sh_l[wave][lane] = st.l; }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {                // rows r and r + 8 are 32 lanes apart
+    float o[8];
+#pragma unroll
+    for (int n = 0; n < 8; ++n) o[n] = st.o[n][i] + __shfl_xor(st.o[n][i], 32);
+    if (g < 2 && 4 * g + i < heads) {
+      *reinterpret_cast<float4*>(&sh_o[wave][4 * g + i][8 * c]) = make_float4(o[0], o[1], o[2], o[3]);
+      *reinterpret_cast<float4*>(&sh_o[wave][4 * g + i][8 * c + 4]) = make_float4(o[4], o[5], o[6], o[7]);
+    }
+  }
+  __syncthreads();
+  float* part = a.d.part + (int64_t)item * heads * kPartStride;
+  for (int e = tid; e < heads * kHeadDim; e += kAdThreads) {
+    const int hh = e >> 7, dim = e & 127;
+    if ((skip >> hh) & 1u) continue;
+    const float M = fmaxf(fmaxf(sh_m[0][hh], sh_m[1][hh]), fmaxf(sh_m[2][hh], sh_m[3][hh]));
+    const float ref = M == ninf ? 0.f : M;
+    float L = 0.f, A = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float cw = fast_exp2(sh_m[w][hh] - ref);
+      L += sh_l[w][hh] * (sh_m[w][hh] == ninf ? 1.f : cw);       // (a wave without a finite logit: its sum is 0, or NaN)
+      A += sh_o[w][hh][dim] * (sh_m[w][hh] == ninf ? 1.f : cw);
+    }
+    if (direct) {
+      const int64_t o = (int64_t)b * a.d.n_q_heads + h0 + hh;
+      a.d.out[o * kHeadDim + dim] = out16(L == 0.f ? 0.f : A / L, a.d.f16 != 0);
+      if (a.d.lse && dim == 0) a.d.lse[o] = L == 0.f ? ninf : (ref + log2f(L)) * 0.6931471805599453f;
+    } else {
+      part[hh * kPartStride + 4 + dim] = A;
+      if (dim == 0) { part[hh * kPartStride] = M; part[hh * kPartStride + 1] = L; }
+    }
+  }
+}
+
+__device__ __forceinline__ void kv4_clear(Kv4State& st) {
+  st.m = -__builtin_huge_valf();
+  st.l = 0.f;
+#pragma unroll
+  for (int n = 0; n < 8; ++n) st.o[n] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+}
+
+// ---- every token, or sink + window --------------------------------------------------------------------------------------------
+// A unit's tokens as blocks of 16 positions (a block lies in one page): the sink's blocks, then the window's.
+struct Kv4Range {
+  int n, s0, w0;          // tokens; token t takes part if t < n and (t < s0 or t >= w0)
+  int sb, wb0, blocks;    // block j < sb is block j of the sequence, block j >= sb is block wb0 + j - sb
+};
+__device__ __forceinline__ Kv4Range kv4_range(const Kv4AttnArgs& a, int b, bool local) {
+  Kv4Range r;
+  r.n = min(max(a.d.ctx_len[b], 0), a.max_len);
+  r.s0 = local ? min(a.d.sink, r.n) : r.n;
+  r.w0 = local ? max(a.d.sink, r.n - a.d.window) : r.n;
+  r.sb = (r.s0 + 15) >> 4;
+  r.wb0 = max(r.sb, r.w0 >> 4);
+  r.blocks = r.sb + max(0, ((r.n + 15) >> 4) - r.wb0);
+  return r;
+}
+__device__ __forceinline__ uint32_t low16(int n) { return n >= 16 ? 0xffffu : n <= 0 ? 0u : (1u << n) - 1u; }
+
+// Blocks per item of a unit of `blocks` blocks that is cut into at most n_splits items: whole rounds of the four waves.
+constexpr int kKv4Round = 8;
+__device__ __forceinline__ int kv4_item_blocks(int blocks, int n_splits, int shortest) {
+  const int per = max((blocks + n_splits - 1) / n_splits, shortest);
+  return (per + kKv4Round - 1) / kKv4Round * kKv4Round;
+}
+
+template <bool LOCAL, bool F16>
+__global__ __launch_bounds__(kAdThreads) void kv4_range_kernel(const Kv4AttnArgs a) {
+  const int item = blockIdx.x, unit = item / a.d.n_splits, split = item - unit * a.d.n_splits;
+  const int b = unit / a.d.n_kv_heads, kvh = unit - b * a.d.n_kv_heads;
+  const int heads = a.d.n_q_heads / a.d.n_kv_heads, h0 = kvh * heads;
+  uint32_t skip = 0;
+  if (LOCAL) {
+    for (int h = 0; h < heads; ++h) skip |= (uint32_t)(a.d.is_ret[h0 + h] != 0) << h;
+    if (skip == (1u << heads) - 1u) return;
+  }
+  const Kv4Range r = kv4_range(a, b, LOCAL);
+  const int per = kv4_item_blocks(r.blocks, a.d.n_splits, a.d.split_tokens);
+  const int j0 = split * per, j1 = min(r.blocks, j0 + per);
+  if (j0 >= j1 && !(a.direct && split == 0)) return;
+  const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  u32x4 qB[4];
+  kv4_queries<F16>(a.d, b, h0, heads, qB);
+  Kv4State st;
+  kv4_clear(st);
+  const int32_t* pt = a.c.page_table + b * a.c.pt_stride;
+  const uint8_t* codes = a.c.codes + kvh * a.c.code_head_stride;
+  const uint8_t* scales = a.c.scales + kvh * a.c.scale_head_stride;
+  const int bshift = a.c.page_shift - 4, bmask = (1 << bshift) - 1;
+
+  // two blocks, clamped to the item's last one; bits of the tokens that take part
+  auto load = [&](int j, Kv4Tiles& t) -> uint32_t {
+    uint32_t valid = 0;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const int jj = min(j + s, j1 - 1);
+      const int blk = jj < r.sb ? jj : r.wb0 + (jj - r.sb);
+      const int page = kv4_page(a.c, pt, blk << 4);
+      uint32_t v = low16(r.n - 16 * blk) & (low16(r.s0 - 16 * blk) | ~low16(r.w0 - 16 * blk));
+      if (page < 0 || j + s >= j1) v = 0;
+      const int64_t pg = max(page, 0);
+      const uint8_t* cp = codes + pg * a.c.code_page_stride + (int64_t)(blk & bmask) * (16 * kKv4Row);
+      const uint8_t* sp = scales + pg * a.c.scale_page_stride + (int64_t)(blk & bmask) * (4 * kKv4Group);
+      t.k[s] = *reinterpret_cast<const u32x4*>(cp + c * kKv4Row + g * 16);
+      t.ks[s] = sp[(c >> 2) * kKv4Group + g * 4 + (c & 3)];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) t.v[s][i] = *reinterpret_cast<const uint32_t*>(cp + (4 * g + i) * kKv4Row + 64 + c * 4);
+      t.vs[s] = *reinterpret_cast<const uint32_t*>(sp + g * kKv4Group + 16 + (c & ~3));
+      valid |= v << (16 * s);
+    }
+    return valid;
+  };
+  // tokens that do not take part may hold anything: their V scales become 2^-127
+  auto clean = [&](uint32_t valid, Kv4Tiles& t) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const uint32_t mine = valid >> (16 * s + 4 * g);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (!((mine >> i) & 1u)) t.vs[s] &= ~(0xffu << (8 * i));
+    }
+  };
+
+  const int step = 2 * (kAdThreads / 64);
+  int j = j0 + 2 * wave;
+  if (j < j1) {
+    Kv4Tiles t[2];
+    uint32_t valid[2];
+    valid[0] = load(j, t[0]);
+    for (; j < j1; j += 2 * step) {
+      valid[1] = load(j + step, t[1]);
+      if (valid[0] != 0xffffffffu) clean(valid[0], t[0]);
+      if (valid[0]) kv4_step<F16>(t[0], valid[0], qB, a.d.scale_log2, st);
+      valid[0] = load(j + 2 * step, t[0]);
+      if (valid[1] != 0xffffffffu) clean(valid[1], t[1]);
+      if (valid[1]) kv4_step<F16>(t[1], valid[1], qB, a.d.scale_log2, st);
+    }
+  }
+  kv4_finish(a, st, item, b, h0, heads, a.direct != 0, skip);
+}
+
+// Merges partials i0 .. i1 - 1 of head slot hh (of `heads` in each) into the output row of query head h: 256 threads, 8 slices of 32
+// lanes with four dims each.
+__device__ __forceinline__ void kv4_merge(const Kv4AttnArgs& a, int heads, int hh, int b, int h, int i0, int i1) {
+  __shared__ float sh_m[8], sh_l[8];
+  __shared__ float sh_o[8][kHeadDim];
+  const int tid = threadIdx.x, d4 = tid & 31, slice = tid >> 5;
+  const float ninf = -__builtin_huge_valf();
+  float M = ninf, L = 0.f;
+  float4 A = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i = i0 + slice; i < i1; i += 8) {
+    const float* p = a.d.part + ((int64_t)i * heads + hh) * kPartStride;
+    const float m = p[0], l = p[1];
+    const float4 v = *reinterpret_cast<const float4*>(p + 4 + d4 * 4);
+    const float Mn = fmaxf(M, m);
+    const float c0 = M == ninf ? 1.f : fast_exp2(M - Mn), c1 = m == ninf ? 1.f : fast_exp2(m - Mn);   // (-inf: 0, or NaN, as it is)
+    L = L * c0 + l * c1;
+    A.x = A.x * c0 + v.x * c1; A.y = A.y * c0 + v.y * c1;
+    A.z = A.z * c0 + v.z * c1; A.w = A.w * c0 + v.w * c1;
+    M = Mn;
+  }
+  if (d4 == 0) { sh_m[slice] = M; sh_l[slice] = L; }
+  *reinterpret_cast<float4*>(&sh_o[slice][d4 * 4]) = A;
+  __syncthreads();
+  if (tid < kHeadDim) {
+    float Mt = sh_m[0];
+#pragma unroll
+    for (int s = 1; s < 8; ++s) Mt = fmaxf(Mt, sh_m[s]);
+    const float ref = Mt == ninf ? 0.f : Mt;
+    float Lt = 0.f, At = 0.f;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      const float cs = sh_m[s] == ninf ? 1.f : fast_exp2(sh_m[s] - ref);
+      Lt += sh_l[s] * cs;
+      At += sh_o[s][tid] * cs;
+    }
+    const int64_t o = (int64_t)b * a.d.n_q_heads + h;
+    a.d.out[o * kHeadDim + tid] = out16(Lt == 0.f ? 0.f : At / Lt, a.d.f16 != 0);
+    if (a.d.lse && tid == 0) a.d.lse[o] = Lt == 0.f ? ninf : (ref + log2f(Lt)) * 0.6931471805599453f;
+  }
+}
+
+template <bool LOCAL>
+__global__ __launch_bounds__(kAdThreads) void kv4_range_merge_kernel(const Kv4AttnArgs a) {
+  const int heads = a.d.n_q_heads / a.d.n_kv_heads;
+  const int unit = blockIdx.x / heads, hh = blockIdx.x - unit * heads;
+  const int b = unit / a.d.n_kv_heads, h = (unit - b * a.d.n_kv_heads) * heads + hh;
+  if (LOCAL && a.d.is_ret[h]) return;
+  const Kv4Range r = kv4_range(a, b, LOCAL);
+  const int per = kv4_item_blocks(r.blocks, a.d.n_splits, a.d.split_tokens), i0 = unit * a.d.n_splits;
+  kv4_merge(a, heads, hh, b, h, i0, i0 + (r.blocks + per - 1) / per);
+}
+
+// LDS words that only the own wave writes and reads: its accesses stay in program order, no workgroup barrier is needed.
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// ---- selected tokens ------------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ int kv4_selected(const Kv4AttnArgs& a, int unit) { return min(max(a.d.sel_count[unit], 0), a.max_len); }
+
+template <bool F16>
+__global__ __launch_bounds__(kAdThreads) void kv4_sparse_kernel(const Kv4AttnArgs a) {
+  __shared__ int sh_prefix[kAdMaxUnits + 1];
+  __shared__ int sh_w[2 * (kAdThreads / 64)];
+  __shared__ int64_t sh_at[kAdThreads / 64][64];          // per wave: a token's bytes of codes, from the pool's start
+  __shared__ uint32_t sh_ks[kAdThreads / 64][64];         // its four K scales
+  __shared__ __attribute__((aligned(16))) uint8_t sh_vs[kAdThreads / 64][4][64];       // V scales by block
+  int per, n_items;
+  build_plan([&](int u) { return kv4_selected(a, u); }, a.d.units, a.d.target_items, sh_prefix, sh_w, &per, &n_items);
+  const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int group = a.d.n_q_heads / a.d.n_kv_heads;
+  for (int item = blockIdx.x; item < n_items; item += gridDim.x) {
+    const int unit = find_unit(sh_prefix, a.d.units, item), split = item - sh_prefix[unit];
+    const int b = unit / a.d.n_ret, h = a.d.ret_heads[unit - b * a.d.n_ret], kvh = h / group;
+    const int t0 = split * per, t1 = min(kv4_selected(a, unit), t0 + per);
+    const int32_t* idx = a.d.sel_idx + (int64_t)unit * a.d.sel_stride;
+    const int32_t* pt = a.c.page_table + b * a.c.pt_stride;
+    const uint8_t* codes = a.c.codes + kvh * a.c.code_head_stride;
+    const uint8_t* scales = a.c.scales + kvh * a.c.scale_head_stride;
+    u32x4 qB[4];
+    kv4_queries<F16>(a.d, b, h, 1, qB);
+    Kv4State st;
+    kv4_clear(st);
+    for (int base = t0 + wave * 64; base < t1; base += kAdThreads) {
+      // a lane looks one token up; the tiles' lanes fetch its bytes by its offset
+      const int i = base + lane;
+      const int pos = i < t1 ? idx[i] : -1;
+      const int page = kv4_page(a.c, pt, pos);
+      const uint64_t there = __ballot(page >= 0);
+      uint32_t ks = 0, vs = 0;
+      int64_t at = 0;
+      if (page >= 0) {
+        const int slot = pos & ((1 << a.c.page_shift) - 1);
+        at = page * a.c.code_page_stride + (int64_t)slot * kKv4Row;
+        const uint8_t* sp = scales + page * a.c.scale_page_stride + (int64_t)(slot >> 2) * kKv4Group;
+        const u32x4 k4 = *reinterpret_cast<const u32x4*>(sp), v4 = *reinterpret_cast<const u32x4*>(sp + 16);
+        const int sh = 8 * (slot & 3);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          ks |= ((k4[q] >> sh) & 255u) << (8 * q);
+          vs |= ((v4[q] >> sh) & 255u) << (8 * q);
+        }
+      }
+      sh_at[wave][lane] = at;
+      sh_ks[wave][lane] = ks;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) sh_vs[wave][q][lane] = (uint8_t)(vs >> (8 * q));
+      wave_lds_fence();
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const uint32_t valid = (uint32_t)(there >> (32 * half));
+        if (!valid) continue;
+        Kv4Tiles t;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const int first = 32 * half + 16 * s;
+          t.k[s] = *reinterpret_cast<const u32x4*>(codes + sh_at[wave][first + c] + g * 16);
+          t.ks[s] = (sh_ks[wave][first + c] >> (8 * g)) & 255u;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) t.v[s][q] = *reinterpret_cast<const uint32_t*>(codes + sh_at[wave][first + 4 * g + q] + 64 + c * 4);
+          t.vs[s] = *reinterpret_cast<const uint32_t*>(&sh_vs[wave][c >> 2][first + 4 * g]);
+        }
+        kv4_step<F16>(t, valid, qB, a.d.scale_log2, st);
+      }
+      wave_lds_fence();
+    }
+    __syncthreads();                           // (the previous item's readers of the joining buffers are done)
+    kv4_finish(a, st, item, b, h, 1, false, 0);
+  }
+}
+
+__global__ __launch_bounds__(kAdThreads) void kv4_sparse_merge_kernel(const Kv4AttnArgs a) {
+  __shared__ int sh_prefix[kAdMaxUnits + 1];
+  __shared__ int sh_w[2 * (kAdThreads / 64)];
+  int per, n_items;
+  build_plan([&](int u) { return kv4_selected(a, u); }, a.d.units, a.d.target_items, sh_prefix, sh_w, &per, &n_items);
+  const int unit = blockIdx.x, b = unit / a.d.n_ret;
+  kv4_merge(a, 1, 0, b, a.d.ret_heads[unit - b * a.d.n_ret], sh_prefix[unit], unit + 1 < a.d.units ? sh_prefix[unit + 1] : n_items);
+}
+
+constexpr int64_t kMaxLen = (int64_t)1 << 30;      // (positions and counts, rounded up, stay inside an int)
+
+// ---- host -----------------------------------------------------------------------------------------------------------------------
+struct Kv4RangePlan {
+  int32_t units, n_splits, shortest;
+  size_t ws_bytes;
+};
+static Kv4RangePlan plan_range(const rtp_layer_desc* L, bool local, int32_t B, int64_t max_ctx) {
+  Kv4RangePlan p = {};
+  const int G = L->n_q_heads / L->n_kv_heads;
+  p.units = B * L->n_kv_heads;
+  int64_t blocks = (max_ctx + 15) / 16;
+  if (local) {                                 // sink blocks, window blocks, one more where the window starts inside a block
+    const int64_t set = ((int64_t)L->sink + 15) / 16 + ((int64_t)L->window + 15) / 16 + 1;
+    if (set < blocks) blocks = set;
+  }
+  p.shortest = 16;
+  int64_t n = 1024 / p.units, most = (blocks + p.shortest - 1) / p.shortest;
+  if (n > most) n = most;
+  if (n < 1) n = 1;
+  p.n_splits = (int32_t)n;
+  p.ws_bytes = n == 1 ? 0 : align_up((size_t)p.units * n * G * kPartStride * sizeof(float), 256);
+  return p;
+}
+
+static size_t range_ws(const rtp_layer_desc* L, bool local, int32_t B, int64_t max_ctx) {
+  if (!L || B <= 0 || max_ctx <= 0 || L->n_kv_heads <= 0 || L->n_q_heads < L->n_kv_heads) return 256;
+  const size_t w = plan_range(L, local, B, max_ctx).ws_bytes;
+  return w ? w : 256;
+}
+
+static int32_t check_io(const char* who, const void* q, const void* out, const void* ws, size_t ws_bytes, size_t need) {
+  if (!q || !out) return fail(RTP_ERR_INVALID_ARG, "%s: NULL tensor pointer", who);
+  if (((uintptr_t)q & 15) || ((uintptr_t)out & 15)) return fail(RTP_ERR_INVALID_ARG, "%s: q and out must be 16-byte aligned", who);
+  if (need && (!ws || ((uintptr_t)ws & 255) || ws_bytes < need))
+    return fail(RTP_ERR_WORKSPACE, "%s: workspace of %zu bytes (256-byte aligned) required, got %zu", who, need, ws_bytes);
+  return RTP_OK;
+}
+
+static void fill_attn(Kv4AttnArgs& a, const rtp_layer_desc* L, const HeadTable& ht, const void* q, void* out, float* lse, void* ws) {
+  a.d = AttnDecodeArgs{};
+  a.d.q = (const uint16_t*)q;
+  a.d.n_q_heads = L->n_q_heads;
+  a.d.n_kv_heads = L->n_kv_heads;
+  a.d.n_ret = L->n_ret;
+  a.d.sink = L->sink;
+  a.d.window = L->window;
+  a.d.scale_log2 = softmax_scale_of(L) * 1.4426950408889634f;
+  a.d.part = (float*)ws;
+  a.d.out = (uint16_t*)out;
+  a.d.lse = lse;
+  a.d.f16 = L->kv_dtype == RTP_DTYPE_FP16;
+  for (int j = 0; j < 64; ++j) a.d.ret_heads[j] = ht.ret_heads[j];
+  for (int h = 0; h < 128; ++h) a.d.is_ret[h] = ht.is_ret[h];
+}
+
+template <bool LOCAL>
+static int32_t range_attn_kv4(const char* who, const rtp_layer_desc* layer, const void* q, const rtp_kv4_cache* cache,
+                              const int32_t* ctx_len, int32_t B, int64_t max_ctx, void* out, float* lse, void* ws,
+                              size_t ws_bytes, hipStream_t s) {
+  HeadTable ht;
+  int32_t rc = fill_head_table(layer, &ht, who);
+  if (rc != RTP_OK) return rc;
+  if (B <= 0 || max_ctx <= 0 || max_ctx > kMaxLen)
+    return fail(RTP_ERR_INVALID_ARG, "%s: B must be positive, max_ctx in [1, 2^30]", who);
+  if (!ctx_len) return fail(RTP_ERR_INVALID_ARG, "%s: NULL ctx_len", who);
+  Kv4AttnArgs a;
+  rc = check_kv4_cache(who, layer, cache, max_ctx, &a.c);
+  if (rc != RTP_OK) return rc;
+  if ((int64_t)B * layer->n_kv_heads > (1 << 20))
+    return fail(RTP_ERR_UNSUPPORTED, "%s: B * n_kv_heads = %lld exceeds %d", who, (long long)B * layer->n_kv_heads, 1 << 20);
+  const Kv4RangePlan p = plan_range(layer, LOCAL, B, max_ctx);
+  rc = check_io(who, q, out, ws, ws_bytes, p.ws_bytes);
+  if (rc != RTP_OK) return rc;
+  clear_error();
+  if (LOCAL && layer->n_ret == layer->n_q_heads) return RTP_OK;   // no local head
+  fill_attn(a, layer, ht, q, out, lse, ws);
+  a.d.ctx_len = ctx_len;
+  a.d.units = p.units;
+  a.d.n_splits = p.n_splits;
+  a.d.split_tokens = p.shortest;
+  a.max_len = (int32_t)max_ctx;
+  a.direct = p.n_splits == 1;
+  const dim3 grid((unsigned)p.units * p.n_splits), block(kAdThreads);
+  if (a.d.f16) RTP_LAUNCH((kv4_range_kernel<LOCAL, true>), grid, block, 0, s, a);
+  else RTP_LAUNCH((kv4_range_kernel<LOCAL, false>), grid, block, 0, s, a);
+  if (!a.direct)
+    RTP_LAUNCH(kv4_range_merge_kernel<LOCAL>, dim3((unsigned)B * layer->n_q_heads), block, 0, s, a);
+  return check_launch(who);
+}
+
+struct Kv4SparsePlan {
+  int32_t target;
+  size_t ws_bytes;
+};
+static Kv4SparsePlan plan_sparse(int64_t units, int64_t max_sel) {
+  const int64_t blocks = units * ((max_sel + 127) / 128);
+  Kv4SparsePlan p;
+  p.target = (int32_t)(blocks < 1024 ? blocks : 1024);
+  // items <= total / ceil(total / target) + units <= target + units
+  p.ws_bytes = align_up((size_t)(p.target + units) * kPartStride * sizeof(float), 256);
+  return p;
+}
+
+}  // namespace rtp
+
+using namespace rtp;
+
+extern "C" size_t rtp_sparse_attn_decode_kv4_workspace_bytes(const rtp_layer_desc* layer, int32_t B, int64_t max_sel) {
+  if (!layer || B <= 0 || max_sel <= 0 || layer->n_ret <= 0) return 256;
+  return plan_sparse((int64_t)B * layer->n_ret, max_sel).ws_bytes;
+}
+
+extern "C" int32_t rtp_sparse_attn_decode_kv4(const rtp_layer_desc* layer, const void* q, const rtp_kv4_cache* cache,
+                                              const int32_t* sel_idx, int64_t sel_stride, const int32_t* sel_count,
+                                              int64_t max_sel, int32_t B, void* out, float* lse, void* ws, size_t ws_bytes,
+                                              void* stream) {
+  const char* who = "rtp_sparse_attn_decode_kv4";
+  HeadTable ht;
+  int32_t rc = fill_head_table(layer, &ht, who);
+  if (rc != RTP_OK) return rc;
+  Kv4AttnArgs a;
+  rc = check_kv4_cache(who, layer, cache, 0, &a.c);
+  if (rc != RTP_OK) return rc;
+  if (!sel_idx || !sel_count) return fail(RTP_ERR_INVALID_ARG, "%s: NULL sel_idx/sel_count", who);
+  if (B <= 0 || max_sel <= 0 || max_sel > kMaxLen)
+    return fail(RTP_ERR_INVALID_ARG, "%s: B must be positive, max_sel in [1, 2^30]", who);
+  if (sel_stride < max_sel) return fail(RTP_ERR_INVALID_ARG, "%s: sel_stride must be >= max_sel", who);
+  const int64_t units = (int64_t)B * layer->n_ret;
+  if (units > kAdMaxUnits) return fail(RTP_ERR_UNSUPPORTED, "%s: B * n_ret = %lld exceeds %d", who, (long long)units, kAdMaxUnits);
+  const Kv4SparsePlan p = plan_sparse(units, max_sel);
+  rc = check_io(who, q, out, ws, ws_bytes, units ? p.ws_bytes : 0);
+  if (rc != RTP_OK) return rc;
+  clear_error();
+  if (units == 0) return RTP_OK;
+  fill_attn(a, layer, ht, q, out, lse, ws);
+  a.d.sel_idx = sel_idx;
+  a.d.sel_stride = sel_stride;
+  a.d.sel_count = sel_count;
+  a.d.units = (int32_t)units;
+  a.d.target_items = p.target;
+  a.max_len = (int32_t)max_sel;
+  a.direct = 0;
+  hipStream_t s = (hipStream_t)stream;
+  if (a.d.f16) RTP_LAUNCH(kv4_sparse_kernel<true>, dim3((unsigned)p.target), dim3(kAdThreads), 0, s, a);
+  else RTP_LAUNCH(kv4_sparse_kernel<false>, dim3((unsigned)p.target), dim3(kAdThreads), 0, s, a);
+  RTP_LAUNCH(kv4_sparse_merge_kernel, dim3((unsigned)units), dim3(kAdThreads), 0, s, a);
+  return check_launch(who);
+}
+
+extern "C" size_t rtp_local_attn_kv4_workspace_bytes(const rtp_layer_desc* layer, int32_t B, int64_t max_ctx) {
+  return range_ws(layer, true, B, max_ctx);
+}
+extern "C" size_t rtp_dense_attn_kv4_workspace_bytes(const rtp_layer_desc* layer, int32_t B, int64_t max_ctx) {
+  return range_ws(layer, false, B, max_ctx);
+}
+extern "C" int32_t rtp_local_attn_kv4(const rtp_layer_desc* layer, const void* q, const rtp_kv4_cache* cache,
+                                      const int32_t* ctx_len, int32_t B, int64_t max_ctx, void* out, float* lse, void* ws,
+                                      size_t ws_bytes, void* stream) {
+  return range_attn_kv4<true>("rtp_local_attn_kv4", layer, q, cache, ctx_len, B, max_ctx, out, lse, ws, ws_bytes, (hipStream_t)stream);
+}
+extern "C" int32_t rtp_dense_attn_kv4(const rtp_layer_desc* layer, const void* q, const rtp_kv4_cache* cache,
+                                      const int32_t* ctx_len, int32_t B, int64_t max_ctx, void* out, float* lse, void* ws,
+                                      size_t ws_bytes, void* stream) {
+  return range_attn_kv4<false>("rtp_dense_attn_kv4", layer, q, cache, ctx_len, B, max_ctx, out, lse, ws, ws_bytes, (hipStream_t)stream);
+}

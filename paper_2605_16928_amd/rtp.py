@@ -32,6 +32,10 @@ EXPORTS = [
     "rtp_decode_attention", "rtp_decode_attention_paged", "rtp_sparse_attn_decode_paged",
     "rtp_kv_ring_heads", "rtp_kv_ring_append", "rtp_kv_ring_fill",
     "rtp_local_attn_ring_workspace_bytes", "rtp_local_attn_ring",
+    "rtp_kv4_append", "rtp_kv4_read",
+    "rtp_sparse_attn_decode_kv4_workspace_bytes", "rtp_sparse_attn_decode_kv4",
+    "rtp_local_attn_kv4_workspace_bytes", "rtp_local_attn_kv4",
+    "rtp_dense_attn_kv4_workspace_bytes", "rtp_dense_attn_kv4",
 ]
 RTP_SIDE_QUERY, RTP_SIDE_KEY = 0, 1
 RTP_DTYPE_BF16, RTP_DTYPE_FP16 = 0, 1
@@ -54,6 +58,31 @@ class rtp_layer_desc(C.Structure):
         ("sink", C.c_int32), ("window", C.c_int32),
         ("softmax_scale", C.c_float), ("index_scale", C.c_float), ("kv_dtype", C.c_int32),
     ]
+
+
+class rtp_kv4_cache(C.Structure):
+    _fields_ = [
+        ("codes", C.c_void_p), ("code_page_stride", C.c_int64), ("code_head_stride", C.c_int64),
+        ("scales", C.c_void_p), ("scale_page_stride", C.c_int64), ("scale_head_stride", C.c_int64),
+        ("page_table", C.c_void_p), ("pt_stride", C.c_int64), ("page_size", C.c_int32), ("n_pages", C.c_int32),
+    ]
+
+
+def kv4_cache(codes, scales, page_table) -> rtp_kv4_cache:
+    """Descriptor of a 4-bit cache in torch tensors: codes uint8 [n_kv_heads, n_pages, page_size, 128], scales uint8 with
+    n_kv_heads and n_pages in front and page_size * 8 bytes behind them, page_table int32 [B, pages].  The first two dims of codes
+    and scales may have any strides (a page-major pool as a transposed view)."""
+    ok = codes.dim() == 4 and codes.shape[3] == 128 and min(codes.shape) > 0 and codes.element_size() == 1 \
+        and scales.dim() >= 3 and scales.shape[:2] == codes.shape[:2] and scales.element_size() == 1 \
+        and scales[0, 0].numel() == 8 * codes.shape[2] and codes[0, 0].is_contiguous() and scales[0, 0].is_contiguous() \
+        and page_table.dim() == 2 and page_table.element_size() == 4 and page_table.is_contiguous()
+    if not ok:
+        raise RtpError(RTP_ERR_INVALID_ARG, "kv4_cache: bytes in codes [heads, pages, page_size, 128] and scales [heads, pages, "
+                                            "8 * page_size], a page's own contiguous, and a contiguous int32 page_table [B, pages]")
+    c = rtp_kv4_cache(codes.data_ptr(), codes.stride(1), codes.stride(0), scales.data_ptr(), scales.stride(1), scales.stride(0),
+                      page_table.data_ptr(), page_table.shape[1], codes.shape[2], codes.shape[1])
+    c._keepalive = (codes, scales, page_table)
+    return c
 
 
 def layer_desc(n_q_heads: int, n_kv_heads: int, ret_heads: Sequence[int], sink: int, window: int,
@@ -148,6 +177,20 @@ def lib() -> C.CDLL:
     L.rtp_local_attn_ring_workspace_bytes.argtypes = [dp, i32, i64]
     L.rtp_local_attn_ring.restype = i32
     L.rtp_local_attn_ring.argtypes = [dp, vp, vp, vp, i64, i64, vp, vp, vp, i64, i64, vp, vp, i32, i64, vp, vp, vp, sz, vp]
+    cp = C.POINTER(rtp_kv4_cache)
+    L.rtp_kv4_append.restype = i32
+    L.rtp_kv4_append.argtypes = [dp, cp, vp, vp, i64, i64, i64, vp, vp, i32, i32, vp]
+    L.rtp_kv4_read.restype = i32
+    L.rtp_kv4_read.argtypes = [dp, cp, vp, vp, i32, i32, vp, vp, i64, i64, i64, vp]
+    L.rtp_sparse_attn_decode_kv4_workspace_bytes.restype = sz
+    L.rtp_sparse_attn_decode_kv4_workspace_bytes.argtypes = [dp, i32, i64]
+    L.rtp_sparse_attn_decode_kv4.restype = i32
+    L.rtp_sparse_attn_decode_kv4.argtypes = [dp, vp, cp, vp, i64, vp, i64, i32, vp, vp, vp, sz, vp]
+    for name in ("rtp_local_attn_kv4", "rtp_dense_attn_kv4"):
+        getattr(L, name + "_workspace_bytes").restype = sz
+        getattr(L, name + "_workspace_bytes").argtypes = [dp, i32, i64]
+        getattr(L, name).restype = i32
+        getattr(L, name).argtypes = [dp, vp, cp, vp, i32, i64, vp, vp, vp, sz, vp]
     L.rtp_sparsity_stats.restype = i32
     L.rtp_sparsity_stats.argtypes = [dp, vp, vp, i64, vp, vp, vp, i32, vp, vp, vp]
     _lib = L
@@ -409,3 +452,40 @@ def rtp_sparsity_stats(layer, ctx_len, sel_idx, sel_stride, sel_count, lse_selec
     _check(lib().rtp_sparsity_stats(C.byref(layer), _ptr(ctx_len), _ptr(sel_idx), sel_stride, _ptr(sel_count),
                                     _ptr(lse_selected), _ptr(lse_full), B, _ptr(stats), _ptr(union_size),
                                     _stream(stream)))
+
+
+def rtp_kv4_append(layer, cache, k, v, batch_stride, token_stride, head_stride, start, count, B, T, stream=None):
+    _check(lib().rtp_kv4_append(C.byref(layer), C.byref(cache), _ptr(k), _ptr(v), batch_stride, token_stride, head_stride,
+                                _ptr(start), _ptr(count), B, T, _stream(stream)))
+
+
+def rtp_kv4_read(layer, cache, start, count, B, T, k, v, batch_stride, token_stride, head_stride, stream=None):
+    _check(lib().rtp_kv4_read(C.byref(layer), C.byref(cache), _ptr(start), _ptr(count), B, T, _ptr(k), _ptr(v), batch_stride,
+                              token_stride, head_stride, _stream(stream)))
+
+
+def rtp_sparse_attn_decode_kv4_workspace_bytes(layer, B, max_sel) -> int:
+    return lib().rtp_sparse_attn_decode_kv4_workspace_bytes(C.byref(layer), B, max_sel)
+
+
+def rtp_sparse_attn_decode_kv4(layer, q, cache, sel_idx, sel_stride, sel_count, max_sel, B, out, lse, ws, stream=None):
+    _check(lib().rtp_sparse_attn_decode_kv4(C.byref(layer), _ptr(q), C.byref(cache), _ptr(sel_idx), sel_stride, _ptr(sel_count),
+                                            max_sel, B, _ptr(out), _ptr(lse), _ptr(ws), _nbytes(ws), _stream(stream)))
+
+
+def rtp_local_attn_kv4_workspace_bytes(layer, B, max_ctx) -> int:
+    return lib().rtp_local_attn_kv4_workspace_bytes(C.byref(layer), B, max_ctx)
+
+
+def rtp_local_attn_kv4(layer, q, cache, ctx_len, B, max_ctx, out, lse, ws, stream=None):
+    _check(lib().rtp_local_attn_kv4(C.byref(layer), _ptr(q), C.byref(cache), _ptr(ctx_len), B, max_ctx, _ptr(out), _ptr(lse),
+                                    _ptr(ws), _nbytes(ws), _stream(stream)))
+
+
+def rtp_dense_attn_kv4_workspace_bytes(layer, B, max_ctx) -> int:
+    return lib().rtp_dense_attn_kv4_workspace_bytes(C.byref(layer), B, max_ctx)
+
+
+def rtp_dense_attn_kv4(layer, q, cache, ctx_len, B, max_ctx, out, lse, ws, stream=None):
+    _check(lib().rtp_dense_attn_kv4(C.byref(layer), _ptr(q), C.byref(cache), _ptr(ctx_len), B, max_ctx, _ptr(out), _ptr(lse),
+                                    _ptr(ws), _nbytes(ws), _stream(stream)))
