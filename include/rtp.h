@@ -592,6 +592,63 @@ size_t rtp_dense_attn_kv4_workspace_bytes(const rtp_layer_desc* layer, int32_t B
 int32_t rtp_dense_attn_kv4(const rtp_layer_desc* layer, const void* q, const rtp_kv4_cache* cache, const int32_t* ctx_len,
                            int32_t B, int64_t max_ctx, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Pages of a cache: handing out, sharing (fork), releasing, compacting, copying -- what a server does to the page table that
+ * rtp_decode_attention_paged and the 4-bit cache read (the paper keeps the retrieval heads' whole cache, Sec. 2.1, and gives no
+ * storage for it).
+ *
+ * A page map is the page table int32 [n_seqs, pt_stride] and a reference count per pool page, int32 [n_pages] (both device memory of
+ * the caller): how many table entries name the page; a page is free when its count is 0.  Entries that name no page are -1.  One map
+ * serves all pools (layers, K and V, codes and scales) that are cut into pages alike.  All calls are stream-ordered; nothing is copied to the
+ * host: lengths, results and lists of page pairs stay on the device.  Lists of sequences are device int32 [n]; an id outside
+ * [0, n_seqs) is passed over, and a table entry outside [0, n_pages) is never followed.
+ *
+ *   rtp_kv_pages_init      every entry -1, every count 0.
+ *   rtp_kv_pages_extend    sequence seq[i] grows from old_len[i] to new_len[i] tokens: entries ceil(old / page_size) ..
+ *                          ceil(new / page_size) - 1 receive fresh pages.  If it grows, and its last page is partly filled and shared (count > 1
+ *                          before the call), the sequence gets a page of its own for that entry too, and the pair (copy_src[i],
+ *                          copy_dst[i]) says which bytes to copy before they are appended to; otherwise the pair is (-1, -1).  Fresh
+ *                          pages are the lowest free ones, in the order of i (a sequence's own page before its new ones).
+ *                          status: device int32 [2] = { pages that are lacking (2^29 at most), what is left of the free pages }.  If pages (or entries of a table row)
+ *                          are lacking, nothing else has changed, and the pairs are all (-1, -1).  A sequence stands in the list once;
+ *                          n <= 4096.
+ *   rtp_kv_pages_fork      sequence dst_seq[i], whose row holds no page, shares the pages of the first len[i] tokens of src_seq[i].  A
+ *                          source may be shared any number of times; a destination is no other's source or destination.  n <= 65535.
+ *   rtp_kv_pages_truncate  sequence seq[i] keeps the pages of its first keep_len[i] tokens (keep_len NULL: none) and releases the
+ *                          rest of its row, for a rejected draft or a sequence that has ended.  n <= 65535.
+ *   rtp_kv_pages_compact   moves the pages in use to the front of the pool: with U pages in use, the r-th free page below U takes
+ *                          the r-th page in use from the top, r = 0 .. moves - 1.  Table and counts are rewritten; the pairs are in
+ *                          move_src / move_dst (int32 [n_pages], the first `moves` of each), status = { U, moves }.
+ *   rtp_kv_pages_copy      copies pages src[i] -> dst[i], i < n (and i < *count, device int32, if count is not NULL), in every
+ *                          pool: page p of head h of a pool is the page_bytes bytes at base + h * head_stride + p * page_stride (bytes, multiples
+ *                          of 16).  Pairs with an id outside [0, n_pages) are passed over.  No destination is another pair's source
+ *                          or destination (the lists of the two calls above are such).  pools: HOST array of n_pools.
+ *
+ * ws: rtp_kv_pages_workspace_bytes(map, n) bytes for rtp_kv_pages_extend of n sequences; n = 0 for rtp_kv_pages_compact.  At most 2^26 pages.
+ */
+typedef struct rtp_page_map {
+  int32_t* page_table;
+  int64_t pt_stride;
+  int32_t* page_refs;
+  int32_t n_seqs, n_pages, page_size;
+} rtp_page_map;
+typedef struct rtp_page_pool {
+  void* base;
+  int64_t page_stride, head_stride, page_bytes;
+  int32_t n_heads;
+} rtp_page_pool;
+size_t rtp_kv_pages_workspace_bytes(const rtp_page_map* map, int32_t n);
+int32_t rtp_kv_pages_init(const rtp_page_map* map, void* stream);
+int32_t rtp_kv_pages_extend(const rtp_page_map* map, const int32_t* seq, const int32_t* old_len, const int32_t* new_len, int32_t n,
+                            int32_t* copy_src, int32_t* copy_dst, int32_t* status, void* ws, size_t ws_bytes, void* stream);
+int32_t rtp_kv_pages_fork(const rtp_page_map* map, const int32_t* src_seq, const int32_t* dst_seq, const int32_t* len, int32_t n,
+                          void* stream);
+int32_t rtp_kv_pages_truncate(const rtp_page_map* map, const int32_t* seq, const int32_t* keep_len, int32_t n, void* stream);
+int32_t rtp_kv_pages_compact(const rtp_page_map* map, int32_t* move_src, int32_t* move_dst, int32_t* status, void* ws,
+                             size_t ws_bytes, void* stream);
+int32_t rtp_kv_pages_copy(const rtp_page_pool* pools, int32_t n_pools, int32_t n_pages, const int32_t* src, const int32_t* dst,
+                          int32_t n, const int32_t* count, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

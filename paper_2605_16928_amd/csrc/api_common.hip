@@ -68,6 +68,15 @@ int32_t fill_head_table(const rtp_layer_desc* L, HeadTable* t, const char* who) 
   return RTP_OK;
 }
 
+bool strides_apart(int64_t s0, int64_t n0, int64_t s1, int64_t n1, int64_t unit) {
+  if (s0 < 0 || s1 < 0 || s0 > ((int64_t)1 << 46) || s1 > ((int64_t)1 << 46)) return false;
+  if (n0 > 1 && s0 < unit) return false;
+  if (n1 > 1 && s1 < unit) return false;
+  if (n0 == 1 || n1 == 1) return true;
+  // (quotients: the products may exceed 64 bits)
+  return s0 <= s1 ? (s1 - unit) / s0 >= n0 - 1 : (s0 - unit) / s1 >= n1 - 1;
+}
+
 int32_t check_launch(const char* who) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(RTP_ERR_HIP, "%s: launch failed: %s", who, hipGetErrorString(e));

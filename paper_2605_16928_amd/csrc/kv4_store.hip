@@ -181,14 +181,6 @@ __global__ __launch_bounds__(kStoreThreads) void kv4_read_kernel(const Kv4StoreA
   }
 }
 
-// Two regular strides over n0 and n1 pieces of `unit` bytes that do not overlap.
-static bool apart(int64_t s0, int64_t n0, int64_t s1, int64_t n1, int64_t unit) {
-  if (n0 > 1 && s0 < unit) return false;
-  if (n1 > 1 && s1 < unit) return false;
-  if (n0 == 1 || n1 == 1) return true;
-  return s0 <= s1 ? s1 >= (n0 - 1) * s0 + unit : s0 >= (n1 - 1) * s1 + unit;
-}
-
 int32_t check_kv4_cache(const char* who, const rtp_layer_desc* L, const rtp_kv4_cache* c, int64_t max_tokens, Kv4Cache* out) {
   if (!c) return fail(RTP_ERR_INVALID_ARG, "%s: cache descriptor is NULL", who);
   if (!c->codes || !c->scales || !c->page_table) return fail(RTP_ERR_INVALID_ARG, "%s: NULL codes/scales/page_table", who);
@@ -199,11 +191,8 @@ int32_t check_kv4_cache(const char* who, const rtp_layer_desc* L, const rtp_kv4_
   if (((uintptr_t)c->codes & 15) || ((uintptr_t)c->scales & 15) || (c->code_page_stride & 15) || (c->code_head_stride & 15) ||
       (c->scale_page_stride & 15) || (c->scale_head_stride & 15))
     return fail(RTP_ERR_INVALID_ARG, "%s: codes, scales and their strides must be 16-byte aligned", who);
-  const int64_t most = (int64_t)1 << 46;
-  if (c->code_page_stride < 0 || c->code_head_stride < 0 || c->scale_page_stride < 0 || c->scale_head_stride < 0 ||
-      c->code_page_stride > most || c->code_head_stride > most || c->scale_page_stride > most || c->scale_head_stride > most ||
-      !apart(c->code_page_stride, c->n_pages, c->code_head_stride, L->n_kv_heads, (int64_t)ps * kKv4Row) ||
-      !apart(c->scale_page_stride, c->n_pages, c->scale_head_stride, L->n_kv_heads, (int64_t)ps / 4 * kKv4Group))
+  if (!strides_apart(c->code_page_stride, c->n_pages, c->code_head_stride, L->n_kv_heads, (int64_t)ps * kKv4Row) ||
+      !strides_apart(c->scale_page_stride, c->n_pages, c->scale_head_stride, L->n_kv_heads, (int64_t)ps / 4 * kKv4Group))
     return fail(RTP_ERR_INVALID_ARG, "%s: strides let pages or heads overlap", who);
   if (c->pt_stride < (max_tokens + ps - 1) / ps) return fail(RTP_ERR_INVALID_ARG, "%s: pt_stride must cover %lld tokens", who, (long long)max_tokens);
   int sh = 4;

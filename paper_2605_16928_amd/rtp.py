@@ -36,6 +36,8 @@ EXPORTS = [
     "rtp_sparse_attn_decode_kv4_workspace_bytes", "rtp_sparse_attn_decode_kv4",
     "rtp_local_attn_kv4_workspace_bytes", "rtp_local_attn_kv4",
     "rtp_dense_attn_kv4_workspace_bytes", "rtp_dense_attn_kv4",
+    "rtp_kv_pages_workspace_bytes", "rtp_kv_pages_init", "rtp_kv_pages_extend", "rtp_kv_pages_fork",
+    "rtp_kv_pages_truncate", "rtp_kv_pages_compact", "rtp_kv_pages_copy",
 ]
 RTP_SIDE_QUERY, RTP_SIDE_KEY = 0, 1
 RTP_DTYPE_BF16, RTP_DTYPE_FP16 = 0, 1
@@ -83,6 +85,40 @@ def kv4_cache(codes, scales, page_table) -> rtp_kv4_cache:
                       page_table.data_ptr(), page_table.shape[1], codes.shape[2], codes.shape[1])
     c._keepalive = (codes, scales, page_table)
     return c
+
+
+class rtp_page_map(C.Structure):
+    _fields_ = [("page_table", C.c_void_p), ("pt_stride", C.c_int64), ("page_refs", C.c_void_p),
+                ("n_seqs", C.c_int32), ("n_pages", C.c_int32), ("page_size", C.c_int32)]
+
+
+class rtp_page_pool(C.Structure):
+    _fields_ = [("base", C.c_void_p), ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("page_bytes", C.c_int64),
+                ("n_heads", C.c_int32)]
+
+
+def page_map(page_table, page_refs, page_size: int) -> rtp_page_map:
+    """Descriptor of a page table int32 [n_seqs, pages] and reference counts int32 [n_pages], both contiguous."""
+    if page_table.dim() != 2 or page_refs.dim() != 1 or page_table.element_size() != 4 or page_refs.element_size() != 4 \
+            or not page_table.is_contiguous() or not page_refs.is_contiguous():
+        raise RtpError(RTP_ERR_INVALID_ARG, "page_map: contiguous int32 page_table [n_seqs, pages] and page_refs [n_pages] expected")
+    m = rtp_page_map(page_table.data_ptr(), page_table.shape[1], page_refs.data_ptr(), page_table.shape[0], page_refs.shape[0], page_size)
+    m._keepalive = (page_table, page_refs)
+    return m
+
+
+def page_pools(pools: Sequence):
+    """Descriptors of pools in torch tensors [heads, n_pages, ...]: a page's own bytes contiguous, the first two dims of any
+    strides (the K and V pools of the paged calls as [n_kv_heads, n_pages, page_size * 128], a 4-bit cache's codes and scales)."""
+    arr = (rtp_page_pool * max(len(pools), 1))()
+    for i, t in enumerate(pools):
+        if t.dim() < 3 or min(t.shape) == 0 or not t[0, 0].is_contiguous():
+            raise RtpError(RTP_ERR_INVALID_ARG, "page_pools: tensors [heads, n_pages, ...] with contiguous pages expected")
+        e = t.element_size()
+        arr[i] = rtp_page_pool(t.data_ptr(), t.stride(1) * e, t.stride(0) * e, t[0, 0].numel() * e, t.shape[0])
+    arr._keepalive = list(pools)
+    arr.n_pools = len(pools)
+    return arr
 
 
 def layer_desc(n_q_heads: int, n_kv_heads: int, ret_heads: Sequence[int], sink: int, window: int,
@@ -191,6 +227,15 @@ def lib() -> C.CDLL:
         getattr(L, name + "_workspace_bytes").argtypes = [dp, i32, i64]
         getattr(L, name).restype = i32
         getattr(L, name).argtypes = [dp, vp, cp, vp, i32, i64, vp, vp, vp, sz, vp]
+    mp = C.POINTER(rtp_page_map)
+    L.rtp_kv_pages_workspace_bytes.restype = sz
+    L.rtp_kv_pages_workspace_bytes.argtypes = [mp, i32]
+    for name, args in (("init", [mp, vp]), ("extend", [mp, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]),
+                       ("fork", [mp, vp, vp, vp, i32, vp]), ("truncate", [mp, vp, vp, i32, vp]),
+                       ("compact", [mp, vp, vp, vp, vp, sz, vp]),
+                       ("copy", [C.POINTER(rtp_page_pool), i32, i32, vp, vp, i32, vp, vp])):
+        getattr(L, "rtp_kv_pages_" + name).restype = i32
+        getattr(L, "rtp_kv_pages_" + name).argtypes = args
     L.rtp_sparsity_stats.restype = i32
     L.rtp_sparsity_stats.argtypes = [dp, vp, vp, i64, vp, vp, vp, i32, vp, vp, vp]
     _lib = L
@@ -489,3 +534,34 @@ def rtp_dense_attn_kv4_workspace_bytes(layer, B, max_ctx) -> int:
 def rtp_dense_attn_kv4(layer, q, cache, ctx_len, B, max_ctx, out, lse, ws, stream=None):
     _check(lib().rtp_dense_attn_kv4(C.byref(layer), _ptr(q), C.byref(cache), _ptr(ctx_len), B, max_ctx, _ptr(out), _ptr(lse),
                                     _ptr(ws), _nbytes(ws), _stream(stream)))
+
+
+def rtp_kv_pages_workspace_bytes(map, n) -> int:
+    return lib().rtp_kv_pages_workspace_bytes(C.byref(map), n)
+
+
+def rtp_kv_pages_init(map, stream=None):
+    _check(lib().rtp_kv_pages_init(C.byref(map), _stream(stream)))
+
+
+def rtp_kv_pages_extend(map, seq, old_len, new_len, n, copy_src, copy_dst, status, ws, stream=None):
+    _check(lib().rtp_kv_pages_extend(C.byref(map), _ptr(seq), _ptr(old_len), _ptr(new_len), n, _ptr(copy_src), _ptr(copy_dst),
+                                     _ptr(status), _ptr(ws), _nbytes(ws), _stream(stream)))
+
+
+def rtp_kv_pages_fork(map, src_seq, dst_seq, len, n, stream=None):
+    _check(lib().rtp_kv_pages_fork(C.byref(map), _ptr(src_seq), _ptr(dst_seq), _ptr(len), n, _stream(stream)))
+
+
+def rtp_kv_pages_truncate(map, seq, keep_len, n, stream=None):
+    _check(lib().rtp_kv_pages_truncate(C.byref(map), _ptr(seq), _ptr(keep_len), n, _stream(stream)))
+
+
+def rtp_kv_pages_compact(map, move_src, move_dst, status, ws, stream=None):
+    _check(lib().rtp_kv_pages_compact(C.byref(map), _ptr(move_src), _ptr(move_dst), _ptr(status), _ptr(ws), _nbytes(ws),
+                                      _stream(stream)))
+
+
+def rtp_kv_pages_copy(pools, n_pages, src, dst, n, count=None, stream=None):
+    """pools: what page_pools returned."""
+    _check(lib().rtp_kv_pages_copy(pools, pools.n_pools, n_pages, _ptr(src), _ptr(dst), n, _ptr(count), _stream(stream)))
