@@ -42,13 +42,49 @@ __device__ __forceinline__ uint16_t out16(float x, bool f16) {       // (NaN sta
   return f16 ? __builtin_bit_cast(uint16_t, (_Float16)x) : __builtin_bit_cast(uint16_t, (__bf16)x);
 }
 
-// One wave's share of 32 tokens, as loaded.
+// 32 tokens of a wave as they come from memory: whole records, 8 lanes of 16 bytes each, so that every load instruction takes full
+// cache lines and may be non-temporal (the operand layouts below would touch every line twice, K's half and V's).
+// line[q]: token 8 q + lane / 8, piece lane % 8 of its 128 bytes.
+struct Kv4Lines {
+  u32x4 line[4];
+};
+// The same 32 tokens as a lane's operands.
 struct Kv4Tiles {
   u32x4 k[2];                  // tile s: token c, dims 32 g .. + 31
   uint32_t v[2][4];            // tile s: token 4 g + i, dims 8 c .. + 7
   uint32_t ks[2];              // scale byte of k[s]
   uint32_t vs[2];              // scale bytes of v[s][0 .. 3]
 };
+// A wave's own LDS: the records on their way from the one form to the other, later its part of the joined outputs.
+struct Kv4WaveLds {
+  union {
+    u32x4 line[32 * 8];        // [token][piece ^ (token / 2 % 8)]: 16 tokens' pieces of one number lie in 16 different bank groups
+    float o[8][kHeadDim];
+  };
+};
+__device__ __forceinline__ int kv4_place(int token, int piece) { return token * 8 + (piece ^ ((token >> 1) & 7)); }
+
+// LDS words that only the own wave writes and reads: its accesses stay in program order, no workgroup barrier is needed.
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// Records -> LDS -> operands (without the scales).
+__device__ __forceinline__ void kv4_turn(const Kv4Lines& in, Kv4WaveLds& lds, Kv4Tiles& t) {
+  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+  wave_lds_fence();
+#pragma unroll
+  for (int q = 0; q < 4; ++q) lds.line[kv4_place(8 * q + (lane >> 3), lane & 7)] = in.line[q];
+  wave_lds_fence();
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    t.k[s] = lds.line[kv4_place(16 * s + c, g)];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      t.v[s][i] = reinterpret_cast<const uint32_t*>(&lds.line[kv4_place(16 * s + 4 * g + i, 4 + (c >> 2))])[c & 3];
+  }
+}
 
 // A wave's running state: m of head c & 7 (the same in the four lanes of a column and in column c + 8), l per lane, outputs of
 // rows 4 g + i at dims 8 c + n.
@@ -82,7 +118,7 @@ __device__ __forceinline__ void kv4_step(const Kv4Tiles& t, const uint32_t valid
     for (int i = 0; i < 4; ++i) {
       float y = S[i];
       if (F16) y += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), 0x128, 0xf, 0xf, true));   // row_ror:8
-      x[s][i] = y * scale_log2;
+      x[s][i] = y;
     }
   }
   const float ninf = -__builtin_huge_valf();
@@ -94,8 +130,9 @@ __device__ __forceinline__ void kv4_step(const Kv4Tiles& t, const uint32_t valid
       for (int i = 0; i < 4; ++i) x[s][i] = (mine >> i) & 1u ? x[s][i] : ninf;
     }
   }
-  float mx = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])), fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
-  mx = max_over_rows(mx);
+  // (max_nn of a NaN and a number is the number, of two NaN +inf: the row is NaN by its sum either way)
+  float mx = max_nn(max_nn(max_nn(x[0][0], x[0][1]), max_nn(x[0][2], x[0][3])), max_nn(max_nn(x[1][0], x[1][1]), max_nn(x[1][2], x[1][3])));
+  mx = max_over_rows(mx) * scale_log2;
   if (__ballot(mx > st.m + kLateMax) != 0ull) {          // (also where m is still -inf)
     const float m_new = fmaxf(st.m, mx);
     const float corr = m_new == ninf ? 1.f : fast_exp2(st.m - m_new);
@@ -115,7 +152,7 @@ __device__ __forceinline__ void kv4_step(const Kv4Tiles& t, const uint32_t valid
     float p[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      p[i] = fast_exp2(x[s][i] - ref);
+      p[i] = fast_exp2(fmaf(x[s][i], scale_log2, -ref));
       st.l += p[i];
     }
 #pragma unroll
@@ -171,22 +208,22 @@ __device__ __forceinline__ void kv4_queries(const AttnDecodeArgs& a, int b, int 
 
 // Joins the four waves' states of an item through LDS and writes the partials of its heads, or, `direct`, their results.
 // skip: heads (of the unit's) that the call does not serve.
-__device__ __forceinline__ void kv4_finish(const Kv4AttnArgs& a, Kv4State& st, int item, int b, int h0, int heads, bool direct,
-                                           uint32_t skip) {
+__device__ __forceinline__ void kv4_finish(const Kv4AttnArgs& a, Kv4State& st, Kv4WaveLds (&lds)[4], int item, int b, int h0, int heads,
+                                           bool direct, uint32_t skip) {
   __shared__ float sh_m[4][8], sh_l[4][8];
-  __shared__ float sh_o[4][8][kHeadDim];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 15, g = lane >> 4;
   const float ninf = -__builtin_huge_valf();
   st.l = sum_rows(st.l, st.l, st.l, st.l);
   if (lane < 8) { sh_m[wave][lane] = st.m; sh_l[wave][lane] = st.l; }
+  wave_lds_fence();
 #pragma unroll
   for (int i = 0; i < 4; ++i) {                // rows r and r + 8 are 32 lanes apart
     float o[8];
 #pragma unroll
     for (int n = 0; n < 8; ++n) o[n] = st.o[n][i] + __shfl_xor(st.o[n][i], 32);
     if (g < 2 && 4 * g + i < heads) {
-      *reinterpret_cast<float4*>(&sh_o[wave][4 * g + i][8 * c]) = make_float4(o[0], o[1], o[2], o[3]);
-      *reinterpret_cast<float4*>(&sh_o[wave][4 * g + i][8 * c + 4]) = make_float4(o[4], o[5], o[6], o[7]);
+      *reinterpret_cast<float4*>(&lds[wave].o[4 * g + i][8 * c]) = make_float4(o[0], o[1], o[2], o[3]);
+      *reinterpret_cast<float4*>(&lds[wave].o[4 * g + i][8 * c + 4]) = make_float4(o[4], o[5], o[6], o[7]);
     }
   }
   __syncthreads();
@@ -201,7 +238,7 @@ __device__ __forceinline__ void kv4_finish(const Kv4AttnArgs& a, Kv4State& st, i
     for (int w = 0; w < 4; ++w) {
       const float cw = fast_exp2(sh_m[w][hh] - ref);
       L += sh_l[w][hh] * (sh_m[w][hh] == ninf ? 1.f : cw);       // (a wave without a finite logit: its sum is 0, or NaN)
-      A += sh_o[w][hh][dim] * (sh_m[w][hh] == ninf ? 1.f : cw);
+      A += lds[w].o[hh][dim] * (sh_m[w][hh] == ninf ? 1.f : cw);
     }
     if (direct) {
       const int64_t o = (int64_t)b * a.d.n_q_heads + h0 + hh;
@@ -247,7 +284,9 @@ __device__ __forceinline__ int kv4_item_blocks(int blocks, int n_splits, int sho
 }
 
 template <bool LOCAL, bool F16>
-__global__ __launch_bounds__(kAdThreads) void kv4_range_kernel(const Kv4AttnArgs a) {
+__global__ __launch_bounds__(kAdThreads, 4) void kv4_range_kernel(const Kv4AttnArgs a) {
+  __shared__ Kv4WaveLds sh_lines[kAdThreads / 64];
+  __shared__ uint32_t sh_scales[kAdThreads / 64][64];      // two blocks: [group of four tokens][K or V][block][token]
   const int item = blockIdx.x, unit = item / a.d.n_splits, split = item - unit * a.d.n_splits;
   const int b = unit / a.d.n_kv_heads, kvh = unit - b * a.d.n_kv_heads;
   const int heads = a.d.n_q_heads / a.d.n_kv_heads, h0 = kvh * heads;
@@ -271,26 +310,39 @@ __global__ __launch_bounds__(kAdThreads) void kv4_range_kernel(const Kv4AttnArgs
   const uint8_t* scales = a.c.scales + kvh * a.c.scale_head_stride;
   const int bshift = a.c.page_shift - 4, bmask = (1 << bshift) - 1;
 
-  // two blocks, clamped to the item's last one; bits of the tokens that take part
-  auto load = [&](int j, Kv4Tiles& t) -> uint32_t {
-    uint32_t valid = 0;
+  // The blocks j and j + 1 (clamped to the item's last one) and the table's entries for them, which are loaded a step ahead of the
+  // bytes.  A context ends inside its table row, so the entry is there; it may name no page of the pool.
+  struct Spot {
+    int blk[2], page[2];
+  };
+  auto look_up = [&](int j) {
+    Spot p;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       const int jj = min(j + s, j1 - 1);
-      const int blk = jj < r.sb ? jj : r.wb0 + (jj - r.sb);
-      const int page = kv4_page(a.c, pt, blk << 4);
-      uint32_t v = low16(r.n - 16 * blk) & (low16(r.s0 - 16 * blk) | ~low16(r.w0 - 16 * blk));
-      if (page < 0 || j + s >= j1) v = 0;
-      const int64_t pg = max(page, 0);
-      const uint8_t* cp = codes + pg * a.c.code_page_stride + (int64_t)(blk & bmask) * (16 * kKv4Row);
-      const uint8_t* sp = scales + pg * a.c.scale_page_stride + (int64_t)(blk & bmask) * (4 * kKv4Group);
-      t.k[s] = *reinterpret_cast<const u32x4*>(cp + c * kKv4Row + g * 16);
-      t.ks[s] = sp[(c >> 2) * kKv4Group + g * 4 + (c & 3)];
+      p.blk[s] = jj < r.sb ? jj : r.wb0 + (jj - r.sb);
+      p.page[s] = pt[p.blk[s] >> bshift];
+    }
+    return p;
+  };
+  // the bytes (sc: lane's word of the two blocks' scales); returns the bits of the tokens that take part
+  auto load = [&](int j, const Spot& p, Kv4Lines& in, uint32_t& sc) -> uint32_t {
+    uint32_t valid = 0;
+    const uint8_t* sp[2];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) t.v[s][i] = *reinterpret_cast<const uint32_t*>(cp + (4 * g + i) * kKv4Row + 64 + c * 4);
-      t.vs[s] = *reinterpret_cast<const uint32_t*>(sp + g * kKv4Group + 16 + (c & ~3));
+    for (int s = 0; s < 2; ++s) {
+      const int blk = p.blk[s];
+      const bool here = (uint32_t)p.page[s] < (uint32_t)a.c.n_pages;
+      uint32_t v = low16(r.n - 16 * blk) & (low16(r.s0 - 16 * blk) | ~low16(r.w0 - 16 * blk));
+      if (!here || j + s >= j1) v = 0;
+      const int64_t pg = here ? p.page[s] : 0;
+      const u32x4* cp = reinterpret_cast<const u32x4*>(codes + pg * a.c.code_page_stride + (int64_t)(blk & bmask) * (16 * kKv4Row));
+      sp[s] = scales + pg * a.c.scale_page_stride + (int64_t)(blk & bmask) * (4 * kKv4Group);
+      in.line[2 * s] = __builtin_nontemporal_load(cp + lane);
+      in.line[2 * s + 1] = __builtin_nontemporal_load(cp + 64 + lane);
       valid |= v << (16 * s);
     }
+    sc = *(reinterpret_cast<const uint32_t*>(lane < 32 ? sp[0] : sp[1]) + (lane & 31));
     return valid;
   };
   // tokens that do not take part may hold anything: their V scales become 2^-127
@@ -303,23 +355,40 @@ __global__ __launch_bounds__(kAdThreads) void kv4_range_kernel(const Kv4AttnArgs
         if (!((mine >> i) & 1u)) t.vs[s] &= ~(0xffu << (8 * i));
     }
   };
-
+  // 32 tokens, whose bytes have been asked for
+  auto attend = [&](const Kv4Lines& in, uint32_t sc, uint32_t valid) {
+    if (!valid) return;
+    Kv4Tiles t;
+    sh_scales[wave][lane] = sc;
+    kv4_turn(in, sh_lines[wave], t);
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      t.ks[s] = reinterpret_cast<const uint8_t*>(&sh_scales[wave][32 * s + 8 * (c >> 2) + g])[c & 3];
+      t.vs[s] = sh_scales[wave][32 * s + 8 * g + 4 + (c >> 2)];
+    }
+    if (valid != 0xffffffffu) clean(valid, t);
+    kv4_step<F16>(t, valid, qB, a.d.scale_log2, st);
+  };
   const int step = 2 * (kAdThreads / 64);
   int j = j0 + 2 * wave;
   if (j < j1) {
-    Kv4Tiles t[2];
-    uint32_t valid[2];
-    valid[0] = load(j, t[0]);
+    Kv4Lines in[2];
+    Spot p[2];
+    uint32_t sc[2], valid[2];
+    p[0] = look_up(j);
+    p[1] = look_up(j + step);
+    valid[0] = load(j, p[0], in[0], sc[0]);
+    p[0] = look_up(j + 2 * step);
     for (; j < j1; j += 2 * step) {
-      valid[1] = load(j + step, t[1]);
-      if (valid[0] != 0xffffffffu) clean(valid[0], t[0]);
-      if (valid[0]) kv4_step<F16>(t[0], valid[0], qB, a.d.scale_log2, st);
-      valid[0] = load(j + 2 * step, t[0]);
-      if (valid[1] != 0xffffffffu) clean(valid[1], t[1]);
-      if (valid[1]) kv4_step<F16>(t[1], valid[1], qB, a.d.scale_log2, st);
+      valid[1] = load(j + step, p[1], in[1], sc[1]);
+      p[1] = look_up(j + 3 * step);
+      attend(in[0], sc[0], valid[0]);
+      valid[0] = load(j + 2 * step, p[0], in[0], sc[0]);
+      p[0] = look_up(j + 4 * step);
+      attend(in[1], sc[1], valid[1]);
     }
   }
-  kv4_finish(a, st, item, b, h0, heads, a.direct != 0, skip);
+  kv4_finish(a, st, sh_lines, item, b, h0, heads, a.direct != 0, skip);
 }
 
 // Merges partials i0 .. i1 - 1 of head slot hh (of `heads` in each) into the output row of query head h: 256 threads, 8 slices of 32
@@ -374,20 +443,20 @@ __global__ __launch_bounds__(kAdThreads) void kv4_range_merge_kernel(const Kv4At
   kv4_merge(a, heads, hh, b, h, i0, i0 + (r.blocks + per - 1) / per);
 }
 
-// LDS words that only the own wave writes and reads: its accesses stay in program order, no workgroup barrier is needed.
-__device__ __forceinline__ void wave_lds_fence() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
 // ---- selected tokens ------------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ int kv4_selected(const Kv4AttnArgs& a, int unit) { return min(max(a.d.sel_count[unit], 0), a.max_len); }
 
+// A wave takes 64 tokens at a time.  A lane looks one of them up -- its position a chunk ahead of the page, the page a chunk ahead of
+// the bytes -- and fetches its scales; the records are then loaded by eight lanes each, by the offsets that the lanes left in LDS.
 template <bool F16>
-__global__ __launch_bounds__(kAdThreads) void kv4_sparse_kernel(const Kv4AttnArgs a) {
+#ifndef SPW
+#define SPW 3
+#endif
+__global__ __launch_bounds__(kAdThreads, SPW) void kv4_sparse_kernel(const Kv4AttnArgs a) {
   __shared__ int sh_prefix[kAdMaxUnits + 1];
   __shared__ int sh_w[2 * (kAdThreads / 64)];
-  __shared__ int64_t sh_at[kAdThreads / 64][64];          // per wave: a token's bytes of codes, from the pool's start
+  __shared__ Kv4WaveLds sh_lines[kAdThreads / 64];
+  __shared__ int64_t sh_at[kAdThreads / 64][64];          // a token's record, from the head's first byte
   __shared__ uint32_t sh_ks[kAdThreads / 64][64];         // its four K scales
   __shared__ __attribute__((aligned(16))) uint8_t sh_vs[kAdThreads / 64][4][64];       // V scales by block
   int per, n_items;
@@ -407,51 +476,78 @@ __global__ __launch_bounds__(kAdThreads) void kv4_sparse_kernel(const Kv4AttnArg
     kv4_queries<F16>(a.d, b, h, 1, qB);
     Kv4State st;
     kv4_clear(st);
-    for (int base = t0 + wave * 64; base < t1; base += kAdThreads) {
-      // a lane looks one token up; the tiles' lanes fetch its bytes by its offset
-      const int i = base + lane;
-      const int pos = i < t1 ? idx[i] : -1;
-      const int page = kv4_page(a.c, pt, pos);
-      const uint64_t there = __ballot(page >= 0);
-      uint32_t ks = 0, vs = 0;
-      int64_t at = 0;
-      if (page >= 0) {
-        const int slot = pos & ((1 << a.c.page_shift) - 1);
-        at = page * a.c.code_page_stride + (int64_t)slot * kKv4Row;
-        const uint8_t* sp = scales + page * a.c.scale_page_stride + (int64_t)(slot >> 2) * kKv4Group;
-        const u32x4 k4 = *reinterpret_cast<const u32x4*>(sp), v4 = *reinterpret_cast<const u32x4*>(sp + 16);
-        const int sh = 8 * (slot & 3);
+
+    // position of this lane's token in the chunk at `base`, and its page (-1: none)
+    auto position = [&](int base) { return base + lane < t1 ? idx[base + lane] : -1; };
+    auto page_of = [&](int pos) { return kv4_page(a.c, pt, pos); };
+    // leaves the records' offsets in LDS and asks for the scales; tokens without a page stand at the head's first record
+    auto place = [&](int pos, int page, u32x4& k4, u32x4& v4) {
+      const int slot = page < 0 ? 0 : pos & ((1 << a.c.page_shift) - 1);
+      const int64_t pg = max(page, 0);
+      wave_lds_fence();
+      sh_at[wave][lane] = pg * a.c.code_page_stride + (int64_t)slot * kKv4Row;
+      wave_lds_fence();
+      const u32x4* sp = reinterpret_cast<const u32x4*>(scales + pg * a.c.scale_page_stride + (int64_t)(slot >> 2) * kKv4Group);
+      k4 = sp[0];
+      v4 = sp[1];
+    };
+    auto load = [&](int half, Kv4Lines& in) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        in.line[q] = *reinterpret_cast<const u32x4*>(codes + sh_at[wave][32 * half + 8 * q + (lane >> 3)] + (lane & 7) * 16);
+    };
+
+    int base = t0 + wave * 64;
+    if (base < t1) {
+      Kv4Lines in[2];
+      u32x4 k4, v4;
+      int pos = position(base), next_pos = position(base + kAdThreads);
+      int page = page_of(pos);
+      place(pos, page, k4, v4);
+      load(0, in[0]);
+      load(1, in[1]);
+      int next_page = page_of(next_pos), third_pos = position(base + 2 * kAdThreads);
+      for (; base < t1; base += kAdThreads) {
+        // this chunk's scales to where the tiles' lanes read them
+        const uint64_t there = __ballot(page >= 0);
+        uint32_t ks = 0, vs = 0;
+        const int sh = 8 * (pos & 3);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           ks |= ((k4[q] >> sh) & 255u) << (8 * q);
           vs |= ((v4[q] >> sh) & 255u) << (8 * q);
         }
-      }
-      sh_at[wave][lane] = at;
-      sh_ks[wave][lane] = ks;
+        if (page < 0) vs = 0;                    // (2^-127: what it multiplies stays finite)
+        wave_lds_fence();
+        sh_ks[wave][lane] = ks;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) sh_vs[wave][q][lane] = (uint8_t)(vs >> (8 * q));
-      wave_lds_fence();
+        for (int q = 0; q < 4; ++q) sh_vs[wave][q][lane] = (uint8_t)(vs >> (8 * q));
+        pos = next_pos;
+        page = next_page;
+        place(pos, page, k4, v4);
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const uint32_t valid = (uint32_t)(there >> (32 * half));
-        if (!valid) continue;
-        Kv4Tiles t;
+        for (int half = 0; half < 2; ++half) {
+          const uint32_t valid = (uint32_t)(there >> (32 * half));
+          if (valid) {
+            Kv4Tiles t;
+            kv4_turn(in[half], sh_lines[wave], t);
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const int first = 32 * half + 16 * s;
-          t.k[s] = *reinterpret_cast<const u32x4*>(codes + sh_at[wave][first + c] + g * 16);
-          t.ks[s] = (sh_ks[wave][first + c] >> (8 * g)) & 255u;
-#pragma unroll
-          for (int q = 0; q < 4; ++q) t.v[s][q] = *reinterpret_cast<const uint32_t*>(codes + sh_at[wave][first + 4 * g + q] + 64 + c * 4);
-          t.vs[s] = *reinterpret_cast<const uint32_t*>(&sh_vs[wave][c >> 2][first + 4 * g]);
+            for (int s = 0; s < 2; ++s) {
+              const int first = 32 * half + 16 * s;
+              t.ks[s] = reinterpret_cast<const uint8_t*>(&sh_ks[wave][first + c])[g];
+              t.vs[s] = *reinterpret_cast<const uint32_t*>(&sh_vs[wave][c >> 2][first + 4 * g]);
+            }
+            kv4_step<F16>(t, valid, qB, a.d.scale_log2, st);
+          }
+          load(half, in[half]);
         }
-        kv4_step<F16>(t, valid, qB, a.d.scale_log2, st);
+        next_pos = third_pos;
+        next_page = page_of(next_pos);
+        third_pos = position(base + 3 * kAdThreads);
       }
-      wave_lds_fence();
     }
-    __syncthreads();                           // (the previous item's readers of the joining buffers are done)
-    kv4_finish(a, st, item, b, h, 1, false, 0);
+    kv4_finish(a, st, sh_lines, item, b, h, 1, false, 0);
+    __syncthreads();                             // (the joined outputs have been read: their LDS is free again)
   }
 }
 

@@ -41,7 +41,7 @@ __device__ __forceinline__ int kv4_page(const Kv4Cache& c, const int32_t* pt, in
 // Scale byte of lane field i (0 .. 3) of a word of four, as the fp32 power of two that the conversions take (0 stands for 2^-127
 // there, 255 makes every converted value NaN).
 __device__ __forceinline__ float kv4_scale(uint32_t word, int i) {
-  return __uint_as_float(i < 3 ? (word << (23 - 8 * i)) & 0x7f800000u : (word >> 1) & 0x7f800000u);
+  return __uint_as_float(((word >> (8 * i)) & 255u) << 23);      // (one instruction: a shift with a byte select)
 }
 
 }  // namespace rtp
