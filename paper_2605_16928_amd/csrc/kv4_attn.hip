@@ -23,11 +23,16 @@
 
 namespace rtp {
 
+constexpr int kKv4MaxHeads = 128;
+
 struct Kv4AttnArgs {
   AttnDecodeArgs d;            // (K, V, strides, seq_start, ring and table fields are not used)
   Kv4Cache c;
   int32_t max_len;             // upper bound of a context / a selection: longer ones are cut there
-  int32_t direct;              // range sources: a unit is one item and writes its result
+  int32_t direct;              // a unit is one item and writes its result
+  int32_t B;
+  int32_t balanced;            // range sources: items are shared out by the lengths on the device, else n_splits to a unit
+  uint32_t skip[kKv4MaxHeads / 4];   // local source: byte kvh = bits of the group's heads that the call does not serve
 };
 
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
@@ -131,10 +136,10 @@ __device__ __forceinline__ void kv4_step(const Kv4Tiles& t, const uint32_t valid
     }
   }
   // (max_nn of a NaN and a number is the number, of two NaN +inf: the row is NaN by its sum either way)
-  float mx = max_nn(max_nn(max_nn(x[0][0], x[0][1]), max_nn(x[0][2], x[0][3])), max_nn(max_nn(x[1][0], x[1][1]), max_nn(x[1][2], x[1][3])));
-  mx = max_over_rows(mx) * scale_log2;
-  if (__ballot(mx > st.m + kLateMax) != 0ull) {          // (also where m is still -inf)
-    const float m_new = fmaxf(st.m, mx);
+  const float mine = scale_log2 * max_nn(max_nn(max_nn(x[0][0], x[0][1]), max_nn(x[0][2], x[0][3])),
+                                         max_nn(max_nn(x[1][0], x[1][1]), max_nn(x[1][2], x[1][3])));
+  if (__ballot(mine > st.m + kLateMax) != 0ull) {        // (also where m is still -inf)
+    const float m_new = fmaxf(st.m, max_over_rows(mine));
     const float corr = m_new == ninf ? 1.f : fast_exp2(st.m - m_new);
     st.l *= corr;
     st.m = m_new;
@@ -147,6 +152,7 @@ __device__ __forceinline__ void kv4_step(const Kv4Tiles& t, const uint32_t valid
   }
   const float ref = st.m == ninf ? 0.f : st.m;           // (a row without a finite logit so far: NaN stays NaN, -inf gives 0)
   u32x4 pA;
+  const bf16x2_t minus_lo = __builtin_bit_cast(bf16x2_t, c < 8 ? 0u : 0x0000bf80u), minus_hi = __builtin_bit_cast(bf16x2_t, c < 8 ? 0u : 0xbf800000u);
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
     float p[4];
@@ -157,9 +163,10 @@ __device__ __forceinline__ void kv4_step(const Kv4Tiles& t, const uint32_t valid
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const uint32_t hi = pack_bf16(p[2 * h], p[2 * h + 1]);
-      const uint32_t rest = pack_bf16(p[2 * h] - bf16_lo(hi), p[2 * h + 1] - bf16_hi(hi));
-      pA[2 * s + h] = c < 8 ? hi : rest;
+      // rows 0 - 7: p rounded; rows 8 - 15: what that leaves (p - 1 * lo - 0 * hi as one dot product, factors 0 in the rows below)
+      const bf16x2_t hi = __builtin_bit_cast(bf16x2_t, pack_bf16(p[2 * h], p[2 * h + 1]));
+      pA[2 * s + h] = pack_bf16(__builtin_amdgcn_fdot2_f32_bf16(hi, minus_lo, p[2 * h], false),
+                                __builtin_amdgcn_fdot2_f32_bf16(hi, minus_hi, p[2 * h + 1], false));
     }
   }
   float fv[2][4];
@@ -276,29 +283,82 @@ __device__ __forceinline__ Kv4Range kv4_range(const Kv4AttnArgs& a, int b, bool 
 }
 __device__ __forceinline__ uint32_t low16(int n) { return n >= 16 ? 0xffffu : n <= 0 ? 0u : (1u << n) - 1u; }
 
-// Blocks per item of a unit of `blocks` blocks that is cut into at most n_splits items: whole rounds of the four waves.
-constexpr int kKv4Round = 8;
-__device__ __forceinline__ int kv4_item_blocks(int blocks, int n_splits, int shortest) {
-  const int per = max((blocks + n_splits - 1) / n_splits, shortest);
-  return (per + kKv4Round - 1) / kKv4Round * kKv4Round;
+constexpr int kKv4Round = 8;           // blocks that the four waves take at a time
+constexpr int kKv4Shortest = 8;        // blocks of the shortest item (dense, 1 x 4096 tokens, 2 KV heads, both launches: 8 blocks 9.2 us,
+                                       // 16 9.8, 24 11.1)
+constexpr int kKv4Items = 1024;        // items that are resident together: 4 workgroups on each of 256 compute units
+__device__ __forceinline__ int whole_rounds(int blocks) { return (max(blocks, kKv4Shortest) + kKv4Round - 1) / kKv4Round * kKv4Round; }
+
+// Where an item lies: sequence and its tokens, KV head, blocks j0 .. j1 - 1, and the partials of its unit.
+struct Kv4Item {
+  int b, kvh, j0, j1;
+  int first, count;
+  Kv4Range r;
+};
+
+// Balanced: every item of the call takes the same number of blocks, by the lengths that the device holds, so that a ragged batch keeps
+// all workgroups busy to the end.  Each wave makes the plan for itself, a lane per sequence: the items of a sequence's KV heads are
+// consecutive, KV head by KV head.  want: an item's number, or (by_unit) a unit's; false: there is none.
+template <bool LOCAL>
+__device__ __forceinline__ bool kv4_balanced_item(const Kv4AttnArgs& a, int want, bool by_unit, Kv4Item* it) {
+  const int lane = threadIdx.x & 63;
+  int total = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 64) total += wave_sum(b0 + lane < a.B ? kv4_range(a, b0 + lane, LOCAL).blocks : 0);
+  const int per = whole_rounds((int)(((int64_t)total * a.d.n_kv_heads + a.d.target_items - 1) / a.d.target_items));
+  int base = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    const int blocks = b0 + lane < a.B ? kv4_range(a, b0 + lane, LOCAL).blocks : 0;
+    const int splits = (blocks + per - 1) / per, incl = wave_incl_scan(splits * a.d.n_kv_heads);
+    const int before = base + incl - splits * a.d.n_kv_heads;
+    const uint64_t mine = by_unit ? __ballot(b0 + lane == want / a.d.n_kv_heads) : __ballot(want >= before && want < base + incl);
+    if (mine) {
+      const int l = __ffsll((unsigned long long)mine) - 1;
+      const int sp = __builtin_amdgcn_readlane(splits, l), at = __builtin_amdgcn_readlane(before, l);
+      it->b = b0 + l;
+      it->kvh = by_unit ? want % a.d.n_kv_heads : (want - at) / sp;
+      it->first = at + it->kvh * sp;
+      it->r = kv4_range(a, it->b, LOCAL);
+      // (a unit's items are equal, or the last one would often be a small one)
+      const int each = whole_rounds((it->r.blocks + sp - 1) / max(sp, 1)), split = by_unit ? 0 : want - it->first;
+      it->count = (it->r.blocks + each - 1) / each;
+      it->j0 = split * each;
+      it->j1 = min(it->r.blocks, it->j0 + each);
+      return it->j0 < it->j1;
+    }
+    base += __builtin_amdgcn_readlane(incl, 63);
+  }
+  return false;
 }
+
+// Fixed: n_splits items to a unit, the trailing ones of a short unit empty.
+template <bool LOCAL>
+__device__ __forceinline__ bool kv4_fixed_item(const Kv4AttnArgs& a, int want, bool by_unit, Kv4Item* it) {
+  const int unit = by_unit ? want : want / a.d.n_splits, split = by_unit ? 0 : want - unit * a.d.n_splits;
+  it->b = unit / a.d.n_kv_heads;
+  it->kvh = unit - it->b * a.d.n_kv_heads;
+  it->r = kv4_range(a, it->b, LOCAL);
+  const int per = whole_rounds((it->r.blocks + a.d.n_splits - 1) / a.d.n_splits);
+  it->first = unit * a.d.n_splits;
+  it->count = (it->r.blocks + per - 1) / per;
+  it->j0 = split * per;
+  it->j1 = min(it->r.blocks, it->j0 + per);
+  return it->j0 < it->j1 || (a.direct && split == 0);
+}
+
+__device__ __forceinline__ uint32_t kv4_skip(const Kv4AttnArgs& a, int kvh) { return (a.skip[kvh >> 2] >> (8 * (kvh & 3))) & 255u; }
 
 template <bool LOCAL, bool F16>
 __global__ __launch_bounds__(kAdThreads, 4) void kv4_range_kernel(const Kv4AttnArgs a) {
   __shared__ Kv4WaveLds sh_lines[kAdThreads / 64];
   __shared__ uint32_t sh_scales[kAdThreads / 64][64];      // two blocks: [group of four tokens][K or V][block][token]
-  const int item = blockIdx.x, unit = item / a.d.n_splits, split = item - unit * a.d.n_splits;
-  const int b = unit / a.d.n_kv_heads, kvh = unit - b * a.d.n_kv_heads;
+  const int item = blockIdx.x;
+  Kv4Item it;
+  if (!(a.balanced ? kv4_balanced_item<LOCAL>(a, item, false, &it) : kv4_fixed_item<LOCAL>(a, item, false, &it))) return;
+  const int b = it.b, kvh = it.kvh, j0 = it.j0, j1 = it.j1;
+  const Kv4Range r = it.r;
   const int heads = a.d.n_q_heads / a.d.n_kv_heads, h0 = kvh * heads;
-  uint32_t skip = 0;
-  if (LOCAL) {
-    for (int h = 0; h < heads; ++h) skip |= (uint32_t)(a.d.is_ret[h0 + h] != 0) << h;
-    if (skip == (1u << heads) - 1u) return;
-  }
-  const Kv4Range r = kv4_range(a, b, LOCAL);
-  const int per = kv4_item_blocks(r.blocks, a.d.n_splits, a.d.split_tokens);
-  const int j0 = split * per, j1 = min(r.blocks, j0 + per);
-  if (j0 >= j1 && !(a.direct && split == 0)) return;
+  const uint32_t skip = LOCAL ? kv4_skip(a, kvh) : 0;
+  if (skip == (1u << heads) - 1u) return;
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   u32x4 qB[4];
@@ -313,34 +373,39 @@ __global__ __launch_bounds__(kAdThreads, 4) void kv4_range_kernel(const Kv4AttnA
   // The blocks j and j + 1 (clamped to the item's last one) and the table's entries for them, which are loaded a step ahead of the
   // bytes.  A context ends inside its table row, so the entry is there; it may name no page of the pool.
   struct Spot {
-    int blk[2], page[2];
+    int blk[2];
+    uint32_t page[2];
   };
   auto look_up = [&](int j) {
     Spot p;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       const int jj = min(j + s, j1 - 1);
-      p.blk[s] = jj < r.sb ? jj : r.wb0 + (jj - r.sb);
-      p.page[s] = pt[p.blk[s] >> bshift];
+      p.blk[s] = jj + (jj < r.sb ? 0 : r.wb0 - r.sb);
+      p.page[s] = (uint32_t)pt[p.blk[s] >> bshift];
     }
     return p;
   };
   // the bytes (sc: lane's word of the two blocks' scales); returns the bits of the tokens that take part
   auto load = [&](int j, const Spot& p, Kv4Lines& in, uint32_t& sc) -> uint32_t {
-    uint32_t valid = 0;
+    uint32_t valid = 0xffffffffu;
     const uint8_t* sp[2];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       const int blk = p.blk[s];
-      const bool here = (uint32_t)p.page[s] < (uint32_t)a.c.n_pages;
-      uint32_t v = low16(r.n - 16 * blk) & (low16(r.s0 - 16 * blk) | ~low16(r.w0 - 16 * blk));
-      if (!here || j + s >= j1) v = 0;
-      const int64_t pg = here ? p.page[s] : 0;
-      const u32x4* cp = reinterpret_cast<const u32x4*>(codes + pg * a.c.code_page_stride + (int64_t)(blk & bmask) * (16 * kKv4Row));
-      sp[s] = scales + pg * a.c.scale_page_stride + (int64_t)(blk & bmask) * (4 * kKv4Group);
+      const bool here = p.page[s] < (uint32_t)a.c.n_pages;
+      const uint32_t pg = here ? p.page[s] : 0u;
+      const uint32_t row = (uint32_t)(blk & bmask);
+      const u32x4* cp = reinterpret_cast<const u32x4*>(codes + ((uint64_t)pg * a.c.code_page16 + row * (16 * kKv4Row / 16)) * 16);
+      sp[s] = scales + ((uint64_t)pg * a.c.scale_page16 + row * (4 * kKv4Group / 16)) * 16;
       in.line[2 * s] = __builtin_nontemporal_load(cp + lane);
       in.line[2 * s + 1] = __builtin_nontemporal_load(cp + 64 + lane);
-      valid |= v << (16 * s);
+      // whole blocks, but for the last one of the sequence, the sink's last and the window's first
+      const int jj = j + s;
+      if (!here || jj >= j1 || jj == r.blocks - 1 || jj == r.sb || jj == r.sb - 1) {
+        const uint32_t v = low16(r.n - 16 * blk) & (low16(r.s0 - 16 * blk) | ~low16(r.w0 - 16 * blk));
+        valid &= ~(((here && jj < j1 ? v : 0u) ^ 0xffffu) << (16 * s));
+      }
     }
     sc = *(reinterpret_cast<const uint32_t*>(lane < 32 ? sp[0] : sp[1]) + (lane & 31));
     return valid;
@@ -436,11 +501,11 @@ template <bool LOCAL>
 __global__ __launch_bounds__(kAdThreads) void kv4_range_merge_kernel(const Kv4AttnArgs a) {
   const int heads = a.d.n_q_heads / a.d.n_kv_heads;
   const int unit = blockIdx.x / heads, hh = blockIdx.x - unit * heads;
-  const int b = unit / a.d.n_kv_heads, h = (unit - b * a.d.n_kv_heads) * heads + hh;
-  if (LOCAL && a.d.is_ret[h]) return;
-  const Kv4Range r = kv4_range(a, b, LOCAL);
-  const int per = kv4_item_blocks(r.blocks, a.d.n_splits, a.d.split_tokens), i0 = unit * a.d.n_splits;
-  kv4_merge(a, heads, hh, b, h, i0, i0 + (r.blocks + per - 1) / per);
+  if (LOCAL && (kv4_skip(a, unit % a.d.n_kv_heads) >> hh) & 1u) return;
+  Kv4Item it;
+  if (a.balanced) kv4_balanced_item<LOCAL>(a, unit, true, &it);
+  else kv4_fixed_item<LOCAL>(a, unit, true, &it);
+  kv4_merge(a, heads, hh, it.b, it.kvh * heads + hh, it.first, it.first + it.count);
 }
 
 // ---- selected tokens ------------------------------------------------------------------------------------------------------------
@@ -485,9 +550,9 @@ __global__ __launch_bounds__(kAdThreads, SPW) void kv4_sparse_kernel(const Kv4At
       const int slot = page < 0 ? 0 : pos & ((1 << a.c.page_shift) - 1);
       const int64_t pg = max(page, 0);
       wave_lds_fence();
-      sh_at[wave][lane] = pg * a.c.code_page_stride + (int64_t)slot * kKv4Row;
+      sh_at[wave][lane] = pg * ((int64_t)a.c.code_page16 * 16) + (int64_t)slot * kKv4Row;
       wave_lds_fence();
-      const u32x4* sp = reinterpret_cast<const u32x4*>(scales + pg * a.c.scale_page_stride + (int64_t)(slot >> 2) * kKv4Group);
+      const u32x4* sp = reinterpret_cast<const u32x4*>(scales + pg * ((int64_t)a.c.scale_page16 * 16) + (int64_t)(slot >> 2) * kKv4Group);
       k4 = sp[0];
       v4 = sp[1];
     };
@@ -564,7 +629,8 @@ constexpr int64_t kMaxLen = (int64_t)1 << 30;      // (positions and counts, rou
 
 // ---- host -----------------------------------------------------------------------------------------------------------------------
 struct Kv4RangePlan {
-  int32_t units, n_splits, shortest;
+  int32_t units, n_splits, target, grid;
+  bool balanced;
   size_t ws_bytes;
 };
 static Kv4RangePlan plan_range(const rtp_layer_desc* L, bool local, int32_t B, int64_t max_ctx) {
@@ -576,12 +642,22 @@ static Kv4RangePlan plan_range(const rtp_layer_desc* L, bool local, int32_t B, i
     const int64_t set = ((int64_t)L->sink + 15) / 16 + ((int64_t)L->window + 15) / 16 + 1;
     if (set < blocks) blocks = set;
   }
-  p.shortest = 16;
-  int64_t n = 1024 / p.units, most = (blocks + p.shortest - 1) / p.shortest;
+  const int64_t most = (blocks + kKv4Shortest - 1) / kKv4Shortest;       // items of the longest unit
+  int64_t n = kKv4Items / p.units;
   if (n > most) n = most;
   if (n < 1) n = 1;
   p.n_splits = (int32_t)n;
-  p.ws_bytes = n == 1 ? 0 : align_up((size_t)p.units * n * G * kPartStride * sizeof(float), 256);
+  p.grid = p.units * p.n_splits;
+  // Lengths can differ, and a unit is more than one item: shared out by the lengths.  (Beyond 256 sequences the plan, a pass over the
+  // lengths in every wave, costs more than it saves: there are at least 256 units then, of four items at most.)
+  p.balanced = n > 1 && B > 1 && B <= 256;
+  if (p.balanced) {
+    p.target = kKv4Items - p.units / 2;                                  // (a unit's number of items is rounded up, by a half on average)
+    int64_t grid = (int64_t)p.target + p.units;                          // items <= total / ceil(total / target) + units
+    if (grid > p.units * most) grid = p.units * most;
+    p.grid = (int32_t)grid;
+  }
+  p.ws_bytes = n == 1 ? 0 : align_up((size_t)p.grid * G * kPartStride * sizeof(float), 256);
   return p;
 }
 
@@ -601,6 +677,9 @@ static int32_t check_io(const char* who, const void* q, const void* out, const v
 
 static void fill_attn(Kv4AttnArgs& a, const rtp_layer_desc* L, const HeadTable& ht, const void* q, void* out, float* lse, void* ws) {
   a.d = AttnDecodeArgs{};
+  for (uint32_t& w : a.skip) w = 0;
+  a.B = 0;
+  a.balanced = 0;
   a.d.q = (const uint16_t*)q;
   a.d.n_q_heads = L->n_q_heads;
   a.d.n_kv_heads = L->n_kv_heads;
@@ -613,7 +692,6 @@ static void fill_attn(Kv4AttnArgs& a, const rtp_layer_desc* L, const HeadTable& 
   a.d.lse = lse;
   a.d.f16 = L->kv_dtype == RTP_DTYPE_FP16;
   for (int j = 0; j < 64; ++j) a.d.ret_heads[j] = ht.ret_heads[j];
-  for (int h = 0; h < 128; ++h) a.d.is_ret[h] = ht.is_ret[h];
 }
 
 template <bool LOCAL>
@@ -640,10 +718,16 @@ static int32_t range_attn_kv4(const char* who, const rtp_layer_desc* layer, cons
   a.d.ctx_len = ctx_len;
   a.d.units = p.units;
   a.d.n_splits = p.n_splits;
-  a.d.split_tokens = p.shortest;
+  a.d.target_items = p.target;
   a.max_len = (int32_t)max_ctx;
   a.direct = p.n_splits == 1;
-  const dim3 grid((unsigned)p.units * p.n_splits), block(kAdThreads);
+  a.B = B;
+  a.balanced = p.balanced;
+  if (LOCAL) {
+    const int G = layer->n_q_heads / layer->n_kv_heads;
+    for (int j = 0; j < layer->n_ret; ++j) a.skip[ht.ret_heads[j] / G / 4] |= 1u << (8 * (ht.ret_heads[j] / G % 4) + ht.ret_heads[j] % G);
+  }
+  const dim3 grid((unsigned)p.grid), block(kAdThreads);
   if (a.d.f16) RTP_LAUNCH((kv4_range_kernel<LOCAL, true>), grid, block, 0, s, a);
   else RTP_LAUNCH((kv4_range_kernel<LOCAL, false>), grid, block, 0, s, a);
   if (!a.direct)

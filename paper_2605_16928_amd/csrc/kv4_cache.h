@@ -20,7 +20,8 @@ constexpr int kKv4Group = 32;         // bytes of scales per four tokens and KV 
 struct Kv4Cache {
   uint8_t* codes;
   uint8_t* scales;
-  int64_t code_page_stride, code_head_stride, scale_page_stride, scale_head_stride;   // bytes
+  int64_t code_head_stride, scale_head_stride;     // bytes
+  uint32_t code_page16, scale_page16;              // pages' strides in 16 bytes
   const int32_t* page_table;
   int64_t pt_stride;
   int32_t page_shift, n_pages;

@@ -124,8 +124,8 @@ __global__ __launch_bounds__(kStoreThreads) void kv4_append_kernel(const Kv4Stor
       vx[i] = *reinterpret_cast<const u32x4*>(a.v + at);
     }
   }
-  uint8_t* codes = a.c.codes + page * a.c.code_page_stride + s.kvh * a.c.code_head_stride + (int64_t)slot * kKv4Row + piece * 4;
-  uint8_t* scales = a.c.scales + page * a.c.scale_page_stride + s.kvh * a.c.scale_head_stride + (int64_t)(slot >> 2) * kKv4Group + (piece & ~3);
+  uint8_t* codes = a.c.codes + (int64_t)page * a.c.code_page16 * 16 + s.kvh * a.c.code_head_stride + (int64_t)slot * kKv4Row + piece * 4;
+  uint8_t* scales = a.c.scales + (int64_t)page * a.c.scale_page16 * 16 + s.kvh * a.c.scale_head_stride + (int64_t)(slot >> 2) * kKv4Group + (piece & ~3);
   uint32_t ks = 0, vs = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -161,8 +161,8 @@ __global__ __launch_bounds__(kStoreThreads) void kv4_read_kernel(const Kv4StoreA
   const int slot = s.pos0 & ((1 << a.c.page_shift) - 1);
   uint32_t kc[4] = {0u, 0u, 0u, 0u}, vc[4] = {0u, 0u, 0u, 0u}, ks = 0, vs = 0;
   if (page >= 0) {                            // (tokens without a page come back as zeros)
-    const uint8_t* codes = a.c.codes + page * a.c.code_page_stride + s.kvh * a.c.code_head_stride + (int64_t)slot * kKv4Row + piece * 4;
-    const uint8_t* scales = a.c.scales + page * a.c.scale_page_stride + s.kvh * a.c.scale_head_stride + (int64_t)(slot >> 2) * kKv4Group + (piece & ~3);
+    const uint8_t* codes = a.c.codes + (int64_t)page * a.c.code_page16 * 16 + s.kvh * a.c.code_head_stride + (int64_t)slot * kKv4Row + piece * 4;
+    const uint8_t* scales = a.c.scales + (int64_t)page * a.c.scale_page16 * 16 + s.kvh * a.c.scale_head_stride + (int64_t)(slot >> 2) * kKv4Group + (piece & ~3);
     ks = *reinterpret_cast<const uint32_t*>(scales);
     vs = *reinterpret_cast<const uint32_t*>(scales + 16);
 #pragma unroll
@@ -195,10 +195,13 @@ int32_t check_kv4_cache(const char* who, const rtp_layer_desc* L, const rtp_kv4_
       !strides_apart(c->scale_page_stride, c->n_pages, c->scale_head_stride, L->n_kv_heads, (int64_t)ps / 4 * kKv4Group))
     return fail(RTP_ERR_INVALID_ARG, "%s: strides let pages or heads overlap", who);
   if (c->pt_stride < (max_tokens + ps - 1) / ps) return fail(RTP_ERR_INVALID_ARG, "%s: pt_stride must cover %lld tokens", who, (long long)max_tokens);
+  const int64_t page16_most = ((int64_t)1 << 32) - 1;
+  if (c->code_page_stride / 16 > page16_most || c->scale_page_stride / 16 > page16_most)
+    return fail(RTP_ERR_UNSUPPORTED, "%s: page strides of 2^36 bytes and more", who);
   int sh = 4;
   while ((1 << sh) < ps) ++sh;
-  *out = Kv4Cache{(uint8_t*)c->codes, (uint8_t*)c->scales, c->code_page_stride, c->code_head_stride, c->scale_page_stride,
-                  c->scale_head_stride, c->page_table, c->pt_stride, sh, c->n_pages};
+  *out = Kv4Cache{(uint8_t*)c->codes, (uint8_t*)c->scales, c->code_head_stride, c->scale_head_stride, (uint32_t)(c->code_page_stride / 16),
+                  (uint32_t)(c->scale_page_stride / 16), c->page_table, c->pt_stride, sh, c->n_pages};
   return RTP_OK;
 }
 
