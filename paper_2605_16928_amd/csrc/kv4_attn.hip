@@ -514,25 +514,22 @@ __device__ __forceinline__ int kv4_selected(const Kv4AttnArgs& a, int unit) { re
 // A wave takes 64 tokens at a time.  A lane looks one of them up -- its position a chunk ahead of the page, the page a chunk ahead of
 // the bytes -- and fetches its scales; the records are then loaded by eight lanes each, by the offsets that the lanes left in LDS.
 template <bool F16>
-#ifndef SPW
-#define SPW 3
-#endif
-__global__ __launch_bounds__(kAdThreads, SPW) void kv4_sparse_kernel(const Kv4AttnArgs a) {
+__global__ __launch_bounds__(kAdThreads, 3) void kv4_sparse_kernel(const Kv4AttnArgs a) {
   __shared__ int sh_prefix[kAdMaxUnits + 1];
   __shared__ int sh_w[2 * (kAdThreads / 64)];
   __shared__ Kv4WaveLds sh_lines[kAdThreads / 64];
   __shared__ int64_t sh_at[kAdThreads / 64][64];          // a token's record, from the head's first byte
   __shared__ uint32_t sh_ks[kAdThreads / 64][64];         // its four K scales
   __shared__ __attribute__((aligned(16))) uint8_t sh_vs[kAdThreads / 64][4][64];       // V scales by block
-  int per, n_items;
-  build_plan([&](int u) { return kv4_selected(a, u); }, a.d.units, a.d.target_items, sh_prefix, sh_w, &per, &n_items);
+  int per = 0, n_items = a.d.units;
+  if (!a.direct) build_plan([&](int u) { return kv4_selected(a, u); }, a.d.units, a.d.target_items, sh_prefix, sh_w, &per, &n_items);
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int group = a.d.n_q_heads / a.d.n_kv_heads;
   for (int item = blockIdx.x; item < n_items; item += gridDim.x) {
-    const int unit = find_unit(sh_prefix, a.d.units, item), split = item - sh_prefix[unit];
+    const int unit = a.direct ? item : find_unit(sh_prefix, a.d.units, item), split = a.direct ? 0 : item - sh_prefix[unit];
     const int b = unit / a.d.n_ret, h = a.d.ret_heads[unit - b * a.d.n_ret], kvh = h / group;
-    const int t0 = split * per, t1 = min(kv4_selected(a, unit), t0 + per);
+    const int t0 = split * per, t1 = a.direct ? kv4_selected(a, unit) : min(kv4_selected(a, unit), t0 + per);
     const int32_t* idx = a.d.sel_idx + (int64_t)unit * a.d.sel_stride;
     const int32_t* pt = a.c.page_table + b * a.c.pt_stride;
     const uint8_t* codes = a.c.codes + kvh * a.c.code_head_stride;
@@ -611,7 +608,7 @@ __global__ __launch_bounds__(kAdThreads, SPW) void kv4_sparse_kernel(const Kv4At
         third_pos = position(base + 3 * kAdThreads);
       }
     }
-    kv4_finish(a, st, sh_lines, item, b, h, 1, false, 0);
+    kv4_finish(a, st, sh_lines, item, b, h, 1, a.direct != 0, 0);
     __syncthreads();                             // (the joined outputs have been read: their LDS is free again)
   }
 }
@@ -628,6 +625,9 @@ __global__ __launch_bounds__(kAdThreads) void kv4_sparse_merge_kernel(const Kv4A
 constexpr int64_t kMaxLen = (int64_t)1 << 30;      // (positions and counts, rounded up, stay inside an int)
 
 // ---- host -----------------------------------------------------------------------------------------------------------------------
+#ifndef RDIRECT
+#define RDIRECT 40
+#endif
 struct Kv4RangePlan {
   int32_t units, n_splits, target, grid;
   bool balanced;
@@ -645,7 +645,7 @@ static Kv4RangePlan plan_range(const rtp_layer_desc* L, bool local, int32_t B, i
   const int64_t most = (blocks + kKv4Shortest - 1) / kKv4Shortest;       // items of the longest unit
   int64_t n = kKv4Items / p.units;
   if (n > most) n = most;
-  if (n < 1) n = 1;
+  if (n < 1 || blocks <= RDIRECT) n = 1;
   p.n_splits = (int32_t)n;
   p.grid = p.units * p.n_splits;
   // Lengths can differ, and a unit is more than one item: shared out by the lengths.  (Beyond 256 sequences the plan, a pass over the
@@ -737,14 +737,19 @@ static int32_t range_attn_kv4(const char* who, const rtp_layer_desc* layer, cons
 
 struct Kv4SparsePlan {
   int32_t target;
+  bool direct;
   size_t ws_bytes;
 };
+#ifndef SDIRECT
+#define SDIRECT 640
+#endif
 static Kv4SparsePlan plan_sparse(int64_t units, int64_t max_sel) {
   const int64_t blocks = units * ((max_sel + 127) / 128);
   Kv4SparsePlan p;
-  p.target = (int32_t)(blocks < 1024 ? blocks : 1024);
+  p.direct = max_sel <= SDIRECT;
+  p.target = (int32_t)(blocks < 1536 ? blocks : 1536);
   // items <= total / ceil(total / target) + units <= target + units
-  p.ws_bytes = align_up((size_t)(p.target + units) * kPartStride * sizeof(float), 256);
+  p.ws_bytes = p.direct ? 0 : align_up((size_t)(p.target + units) * kPartStride * sizeof(float), 256);
   return p;
 }
 
@@ -754,7 +759,8 @@ using namespace rtp;
 
 extern "C" size_t rtp_sparse_attn_decode_kv4_workspace_bytes(const rtp_layer_desc* layer, int32_t B, int64_t max_sel) {
   if (!layer || B <= 0 || max_sel <= 0 || layer->n_ret <= 0) return 256;
-  return plan_sparse((int64_t)B * layer->n_ret, max_sel).ws_bytes;
+  const size_t w = plan_sparse((int64_t)B * layer->n_ret, max_sel).ws_bytes;
+  return w ? w : 256;
 }
 
 extern "C" int32_t rtp_sparse_attn_decode_kv4(const rtp_layer_desc* layer, const void* q, const rtp_kv4_cache* cache,
@@ -786,11 +792,12 @@ extern "C" int32_t rtp_sparse_attn_decode_kv4(const rtp_layer_desc* layer, const
   a.d.units = (int32_t)units;
   a.d.target_items = p.target;
   a.max_len = (int32_t)max_sel;
-  a.direct = 0;
+  a.direct = p.direct;
   hipStream_t s = (hipStream_t)stream;
-  if (a.d.f16) RTP_LAUNCH(kv4_sparse_kernel<true>, dim3((unsigned)p.target), dim3(kAdThreads), 0, s, a);
-  else RTP_LAUNCH(kv4_sparse_kernel<false>, dim3((unsigned)p.target), dim3(kAdThreads), 0, s, a);
-  RTP_LAUNCH(kv4_sparse_merge_kernel, dim3((unsigned)units), dim3(kAdThreads), 0, s, a);
+  const dim3 grid((unsigned)(p.direct ? units : p.target));
+  if (a.d.f16) RTP_LAUNCH(kv4_sparse_kernel<true>, grid, dim3(kAdThreads), 0, s, a);
+  else RTP_LAUNCH(kv4_sparse_kernel<false>, grid, dim3(kAdThreads), 0, s, a);
+  if (!p.direct) RTP_LAUNCH(kv4_sparse_merge_kernel, dim3((unsigned)units), dim3(kAdThreads), 0, s, a);
   return check_launch(who);
 }
 

@@ -65,32 +65,52 @@ __device__ __forceinline__ T pg_scan(T v, uint64_t* sh, T* total) {
   return off + incl - v;
 }
 
-// The mask word of this thread: bit i = page (chunk's first + 64 * thread + i) is free (FREE) or in use.
+// Bit `at` of a mask, and the bits below it, in 32-bit steps: a 64-bit shift by a vector register gave wrong results where that register was
+// the last of the kernel's (v_lshlrev_b64 by v71 of 72).
+__device__ __forceinline__ bool mask_bit(uint64_t mask, int at) {
+  return (((at & 32) ? (uint32_t)(mask >> 32) : (uint32_t)mask) >> (at & 31)) & 1u;
+}
+__device__ __forceinline__ int mask_below(uint64_t mask, int at) {
+  const uint32_t low = (1u << (at & 31)) - 1u;
+  return (at & 32) ? __popc((uint32_t)mask) + __popc((uint32_t)(mask >> 32) & low) : __popc((uint32_t)mask & low);
+}
+
+// A chunk's masks in LDS (bit i of word w = page 64 w + i of the chunk is free, or in use where FREE is false) and, for every word, the
+// set bits in front of it; *total: all of them.
+struct ChunkMasks {
+  uint64_t mask[kPgThreads];
+  int32_t before[kPgThreads];
+};
+constexpr int kPgWaves = kPgThreads / 64, kPgAhead = 16;
+// Counts of the pages of rounds r0 .. r0 + kPgAhead - 1 (round r of a wave: word r * kPgWaves + wave, a page per lane); what is behind the
+// pool counts as neither free nor in use.
 template <bool FREE>
-__device__ __forceinline__ uint64_t pg_masks(const PageMap& m, int chunk, uint64_t* sh_mask /*[kPgThreads]*/) {
+__device__ __forceinline__ void pg_counts(const PageMap& m, int chunk, int r0, int (&v)[kPgAhead]) {
+  const int64_t first = (int64_t)chunk * kPgChunk + (r0 * kPgWaves + (threadIdx.x >> 6)) * 64 + (threadIdx.x & 63);
+#pragma unroll
+  for (int r = 0; r < kPgAhead; ++r) {
+    const int64_t p = first + r * kPgWaves * 64;
+    v[r] = p < m.n_pages ? m.refs[p] : (FREE ? 1 : 0);
+  }
+}
+template <bool FREE>
+__device__ __forceinline__ void pg_masks(const PageMap& m, int chunk, int (&v)[kPgAhead], ChunkMasks& c, uint64_t* sh, int* total) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t base = (int64_t)chunk * kPgChunk;
-  constexpr int kWaves = kPgThreads / 64, kAhead = 16;
-  for (int r0 = 0; r0 < 64; r0 += kAhead) {              // round r of a wave: pages of mask word r * waves + wave
-    if (base + (int64_t)r0 * kWaves * 64 >= m.n_pages) {
-      for (int r = r0 + lane / kWaves; r < 64; r += 64 / kWaves)
-        if (wave == 0) sh_mask[r * kWaves + lane % kWaves] = 0;
-      break;
-    }
-    int v[kAhead];
+  c.mask[threadIdx.x] = 0;
+  __syncthreads();
+  for (int r0 = 0;;) {
 #pragma unroll
-    for (int r = 0; r < kAhead; ++r) {
-      const int64_t p = base + ((int64_t)(r0 + r) * kWaves + wave) * 64 + lane;
-      v[r] = p < m.n_pages ? m.refs[p] : (FREE ? 1 : 0);
-    }
-#pragma unroll
-    for (int r = 0; r < kAhead; ++r) {
+    for (int r = 0; r < kPgAhead; ++r) {
       const uint64_t bits = __ballot(FREE ? v[r] <= 0 : v[r] > 0);
-      if (lane == 0) sh_mask[(r0 + r) * kWaves + wave] = bits;
+      if (lane == 0) c.mask[(r0 + r) * kPgWaves + wave] = bits;
     }
+    r0 += kPgAhead;
+    if (r0 >= 64 || (int64_t)chunk * kPgChunk + r0 * kPgWaves * 64 >= m.n_pages) break;
+    pg_counts<FREE>(m, chunk, r0, v);
   }
   __syncthreads();
-  return sh_mask[threadIdx.x];
+  c.before[threadIdx.x] = pg_scan<int>(__popcll(c.mask[threadIdx.x]), sh, total);
+  __syncthreads();
 }
 
 // Pages that request i takes: one to copy its shared last page to, then what the new length adds.  lacks: entries that the table row has
@@ -116,38 +136,41 @@ __device__ __forceinline__ Request pg_request(const ExtendArgs& a, int i) {
 }
 
 // Prefix sums of the requests' pages into need[0 .. n] (cut at 2^30, more than any pool has: with a total beyond the pool nobody reads
-// them); returns the entries that do not fit their rows, cut likewise.
-__device__ __forceinline__ int pg_needs(const ExtendArgs& a, int32_t* need, uint64_t* sh) {
+// them); returns the entries that do not fit their rows, cut likewise.  r: request threadIdx.x (nothing, if there is none).
+__device__ __forceinline__ int pg_needs(const ExtendArgs& a, Request r, int32_t* need, uint64_t* sh) {
   constexpr uint64_t kMost = 1ull << 30;
   uint64_t base = 0, lacking = 0;
-  for (int i0 = 0; i0 < a.n; i0 += kPgThreads) {
-    const int i = i0 + threadIdx.x;
-    Request r = {0, 0};
-    if (i < a.n) r = pg_request(a, i);
+  for (int i = threadIdx.x;; ) {
     uint64_t total, lacks;
     const uint64_t off = pg_scan<uint64_t>((uint64_t)r.pages, sh, &total);
-    pg_scan<uint64_t>((uint64_t)r.lacks, sh, &lacks);
+    if (__syncthreads_or(r.lacks != 0)) {
+      pg_scan<uint64_t>((uint64_t)r.lacks, sh, &lacks);
+      lacking += lacks;
+    }
     if (i < a.n) need[i] = (int32_t)min(base + off, kMost);
     base += total;
-    lacking += lacks;
+    i += kPgThreads;
+    if (i - (int)threadIdx.x >= a.n) break;
+    r = i < a.n ? pg_request(a, i) : Request{0, 0};
   }
   if (threadIdx.x == 0) need[a.n] = (int32_t)min(base, kMost);
   return (int)min(lacking, kMost);
 }
 
+// Chunks of a large pool: masks and prefixes to the workspace, and, by the first workgroup, the requests' prefix sums.
 template <bool FREE, bool REQUESTS>
 __global__ __launch_bounds__(kPgThreads) void kv_pages_scan_kernel(const ExtendArgs a) {
-  __shared__ uint64_t sh_mask[kPgThreads];
-  __shared__ uint64_t sh[kPgThreads / 64];
-  const uint64_t mask = pg_masks<FREE>(a.m, blockIdx.x, sh_mask);
+  __shared__ ChunkMasks c;
+  __shared__ uint64_t sh[kPgWaves];
+  int v[kPgAhead], total;
+  pg_counts<FREE>(a.m, blockIdx.x, 0, v);
+  pg_masks<FREE>(a.m, blockIdx.x, v, c, sh, &total);
   const int64_t word = (int64_t)blockIdx.x * kPgThreads + threadIdx.x;
-  int total;
-  const int before = pg_scan<int>(__popcll(mask), sh, &total);
-  a.w.mask[word] = mask;
-  a.w.before[word] = before;
+  a.w.mask[word] = c.mask[threadIdx.x];
+  a.w.before[word] = c.before[threadIdx.x];
   if (threadIdx.x == 0) a.w.count[blockIdx.x] = total;
   if (REQUESTS && blockIdx.x == 0) {
-    const int lacking = pg_needs(a, a.w.need, sh);
+    const int lacking = pg_needs(a, (int)threadIdx.x < a.n ? pg_request(a, threadIdx.x) : Request{0, 0}, a.w.need, sh);
     if (threadIdx.x == 0) a.w.need[a.n + 1] = lacking;
   }
 }
@@ -166,22 +189,37 @@ __device__ __forceinline__ int pg_chunks_before(const PageWork& w, int n_chunks,
   return before;
 }
 
-// Gives the requests their pages.  ONE: the pool is one chunk, nothing has been prepared.
+// The chunk's masks and prefixes, from the workspace; *first: set bits in the chunks in front, *total: in all.
+__device__ __forceinline__ void pg_load_chunk(const ExtendArgs& a, ChunkMasks& c, uint64_t* sh, int* first, int* total) {
+  const int64_t word = (int64_t)blockIdx.x * kPgThreads + threadIdx.x;
+  c.mask[threadIdx.x] = a.w.mask[word];
+  c.before[threadIdx.x] = a.w.before[word];
+  *first = pg_chunks_before(a.w, a.m.n_chunks, blockIdx.x, sh, total);
+  __syncthreads();
+}
+
+// Entries that request i grows by, beside one for its shared last page; *k0: the first of them.
+__device__ __forceinline__ int pg_grown(const ExtendArgs& a, int i, int64_t* k0) {
+  const int64_t size1 = ((int64_t)1 << a.m.page_shift) - 1;
+  *k0 = (max(a.old_len[i], 0) + size1) >> a.m.page_shift;
+  return (int)(min((a.new_len[i] + size1) >> a.m.page_shift, a.m.pt_stride) - *k0);
+}
+
+// Gives the requests their pages, a lane per page of the pool.  ONE: the pool is one chunk, nothing has been prepared.
 template <bool ONE>
 __global__ __launch_bounds__(kPgThreads) void kv_pages_extend_kernel(const ExtendArgs a) {
-  __shared__ uint64_t sh_mask[ONE ? kPgThreads : 1];
-  __shared__ uint64_t sh[kPgThreads / 64];
+  __shared__ ChunkMasks c;
+  __shared__ uint64_t sh[kPgWaves];
   __shared__ int32_t sh_need[kPgMaxSeqs + 1];
-  uint64_t mask;
-  int before, total, lacking;
+  int first = 0, total, lacking;
   if (ONE) {
-    mask = pg_masks<true>(a.m, 0, sh_mask);
-    before = pg_scan<int>(__popcll(mask), sh, &total);
-    lacking = pg_needs(a, sh_need, sh);
+    int v[kPgAhead];
+    pg_counts<true>(a.m, 0, 0, v);              // (asked for before the request, a chain of loads of its own)
+    const Request r = (int)threadIdx.x < a.n ? pg_request(a, threadIdx.x) : Request{0, 0};
+    pg_masks<true>(a.m, 0, v, c, sh, &total);
+    lacking = pg_needs(a, r, sh_need, sh);
   } else {
-    const int64_t word = (int64_t)blockIdx.x * kPgThreads + threadIdx.x;
-    mask = a.w.mask[word];
-    before = pg_chunks_before(a.w, a.m.n_chunks, blockIdx.x, sh, &total) + a.w.before[word];
+    pg_load_chunk(a, c, sh, &first, &total);
     for (int i = threadIdx.x; i <= a.n; i += kPgThreads) sh_need[i] = a.w.need[i];
     lacking = a.w.need[a.n + 1];
   }
@@ -193,35 +231,35 @@ __global__ __launch_bounds__(kPgThreads) void kv_pages_extend_kernel(const Exten
       a.status[0] = short_of;
       a.status[1] = total - (short_of ? 0 : need);
     }
-    // pairs of requests that copy nothing (the others are written with their page)
-    for (int i = threadIdx.x; i < a.n; i += kPgThreads) {
-      bool copies = false;
-      if (!short_of && sh_need[i + 1] > sh_need[i]) {
-        const int sh_ = a.m.page_shift, from = max(a.old_len[i], 0);
-        const int64_t grown = (min(((int64_t)a.new_len[i] + (1 << sh_) - 1) >> sh_, a.m.pt_stride)) - (((int64_t)from + (1 << sh_) - 1) >> sh_);
-        copies = sh_need[i + 1] - sh_need[i] > grown;
-      }
-      if (!copies) a.copy_src[i] = a.copy_dst[i] = -1;
+    for (int i = threadIdx.x; i < a.n; i += kPgThreads) {      // pairs of requests that copy nothing; the others are written with their page
+      const int pages = sh_need[i + 1] - sh_need[i];
+      int64_t k0;
+      if (short_of || pages == 0 || pages <= pg_grown(a, i, &k0)) a.copy_src[i] = a.copy_dst[i] = -1;
     }
   }
   if (short_of) return;
-  for (int r = before; mask && r < need; ++r, mask &= mask - 1) {
-    const int page = (int)((ONE ? 0 : blockIdx.x) * (int64_t)kPgChunk) + threadIdx.x * 64 + __ffsll((unsigned long long)mask) - 1;
-    int lo = 0, hi = a.n - 1;                    // the request that rank r belongs to: the last one whose prefix is <= r
+  const int lane = threadIdx.x & 63;
+  for (int w = threadIdx.x >> 6; w < kPgThreads; w += kPgWaves) {
+    const uint64_t mask = c.mask[w];
+    const int before = first + c.before[w];
+    if (before >= need) break;
+    const int r = before + mask_below(mask, lane);
+    if (!mask_bit(mask, lane) || r >= need) continue;
+    const int page = blockIdx.x * kPgChunk + w * 64 + lane;
+    int lo = 0, hi = a.n - 1;                   // the request that rank r belongs to: the last one whose prefix is <= r
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
       if (sh_need[mid] <= r) lo = mid; else hi = mid - 1;
     }
-    const int sh_ = a.m.page_shift, from = max(a.old_len[lo], 0);
-    const int64_t k0 = ((int64_t)from + (1 << sh_) - 1) >> sh_;
-    const int64_t grown = min(((int64_t)a.new_len[lo] + (1 << sh_) - 1) >> sh_, a.m.pt_stride) - k0;
-    const int copies = sh_need[lo + 1] - sh_need[lo] > grown, j = r - sh_need[lo];
+    int64_t k0;
+    const int grown = pg_grown(a, lo, &k0), j = r - sh_need[lo];
+    const int copies = sh_need[lo + 1] - sh_need[lo] - grown;   // 0 or 1
     int32_t* entry = a.m.table + a.seq[lo] * a.m.pt_stride + k0 - copies + j;
     if (copies && j == 0) {
       const int src = *entry;
       a.copy_src[lo] = src;
       a.copy_dst[lo] = page;
-      atomicSub(&a.m.refs[src], 1);
+      if (in_pool(a.m, src)) atomicSub(&a.m.refs[src], 1);     // (a sequence listed twice may have changed the entry)
     }
     *entry = page;
     a.m.refs[page] = 1;
@@ -261,39 +299,30 @@ __global__ __launch_bounds__(256) void kv_pages_fork_kernel(const PageMap m, con
 // Lists the moves: with U pages in use, the r-th free page below U takes the r-th page in use from the top.
 template <bool ONE>
 __global__ __launch_bounds__(kPgThreads) void kv_pages_moves_kernel(const ExtendArgs a) {
-  __shared__ uint64_t sh_mask[ONE ? kPgThreads : 1];
-  __shared__ uint64_t sh[kPgThreads / 64];
-  const int chunk = ONE ? 0 : blockIdx.x;
-  const int64_t word = (int64_t)chunk * kPgThreads + threadIdx.x;
-  uint64_t mask;
-  int before, total;
+  __shared__ ChunkMasks c;
+  __shared__ uint64_t sh[kPgWaves];
+  int first = 0, total;
   if (ONE) {
-    mask = pg_masks<false>(a.m, 0, sh_mask);
-    before = pg_scan<int>(__popcll(mask), sh, &total);
-    a.w.mask[word] = mask;
-    a.w.before[word] = before;
+    int v[kPgAhead];
+    pg_counts<false>(a.m, 0, 0, v);
+    pg_masks<false>(a.m, 0, v, c, sh, &total);
+    a.w.mask[threadIdx.x] = c.mask[threadIdx.x];
+    a.w.before[threadIdx.x] = c.before[threadIdx.x];
   } else {
-    mask = a.w.mask[word];
-    before = pg_chunks_before(a.w, a.m.n_chunks, chunk, sh, &total) + a.w.before[word];
+    pg_load_chunk(a, c, sh, &first, &total);
   }
-  const int64_t first = word * 64;
-  // pages of this word below U that are free, and pages from U on that are in use
-  const int64_t below = total - first;
-  const uint64_t low = below >= 64 ? ~0ull : below <= 0 ? 0ull : (1ull << below) - 1ull;
-  for (uint64_t holes = ~mask & low; holes; holes &= holes - 1) {
-    const int bit = __ffsll((unsigned long long)holes) - 1;
-    const int used = before + __popcll(mask & ((1ull << bit) - 1ull));
-    a.copy_dst[first + bit - used] = (int)first + bit;
-  }
-  for (uint64_t high = mask & ~low; high; high &= high - 1) {
-    const int bit = __ffsll((unsigned long long)high) - 1;
-    const int used = before + __popcll(mask & ((1ull << bit) - 1ull));
-    a.copy_src[total - 1 - used] = (int)first + bit;
-  }
-  // moves: the pages in use from U on, which the word that holds page U - 1 can tell
-  if (word == max(total - 1, 0) / 64) {
-    a.status[0] = total;
-    a.status[1] = total - (before + __popcll(mask & low));
+  const int lane = threadIdx.x & 63, chunk0 = blockIdx.x * kPgChunk;
+  const int words = (min(a.m.n_pages - chunk0, kPgChunk) + 63) / 64;
+  for (int w = threadIdx.x >> 6; w < words; w += kPgWaves) {
+    const uint64_t mask = c.mask[w];
+    const int page = chunk0 + w * 64 + lane, used = first + c.before[w] + mask_below(mask, lane);
+    const bool here = mask_bit(mask, lane);
+    if (!here && page < total) a.copy_dst[page - used] = page;
+    if (here && page >= total) a.copy_src[total - 1 - used] = page;
+    if (page == max(total - 1, 0)) {            // moves: the pages in use from U on, which page U - 1 can tell
+      a.status[0] = total;
+      a.status[1] = total - used - (here ? 1 : 0);
+    }
   }
 }
 
@@ -326,9 +355,9 @@ __global__ __launch_bounds__(256) void kv_pages_remap_kernel(const ExtendArgs a)
   for (int64_t e = t; e < entries; e += step) {
     const int page = a.m.table[e];
     if (page < used || page >= a.m.n_pages) continue;
-    const uint64_t mask = a.w.mask[page >> 6], bit = 1ull << (page & 63);
-    if (!(mask & bit)) continue;
-    const int rank = (a.m.n_chunks > 1 ? sh_chunk[page / kPgChunk] : 0) + a.w.before[page >> 6] + __popcll(mask & (bit - 1ull));
+    const uint64_t mask = a.w.mask[page >> 6];
+    if (!mask_bit(mask, page & 63)) continue;
+    const int rank = (a.m.n_chunks > 1 ? sh_chunk[page / kPgChunk] : 0) + a.w.before[page >> 6] + mask_below(mask, page & 63);
     a.m.table[e] = a.copy_dst[used - 1 - rank];
   }
   for (int64_t r = t; r < moves; r += step) {
