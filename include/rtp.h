@@ -533,7 +533,8 @@ int32_t rtp_local_attn_ring(const rtp_layer_desc* layer, const void* q,
  * codes of sign, 2 exponent bits and 1 mantissa bit: +-{0, .5, 1, 1.5, 2, 3, 4, 6}.  rtp_kv4_append chooses, with
  * amax = max |x| of the block = (1 + M) 2^(E - 127),  s = max(2, E - 2 + [M >= 0.75]),  and rounds x 2^(127 - s) to the nearest
  * code, ties to the even one: the largest value of a block lies in [3.5, 7) steps and is off by at most half a step of the
- * codes, like every other.  A block that holds an infinity or a NaN gets s = 255, and all its values read as NaN.
+ * codes, like every other (a bf16 maximum above 1.75 * 2^127 rounds up to 2^128 and reads as infinite).  A block that holds an
+ * infinity or a NaN gets s = 255, and all its values read as NaN.
  *
  * Position t of sequence b lives in slot r = t % page_size of pool page P = page_table[b * pt_stride + t / page_size]:
  *   codes   128 bytes at  codes + P * code_page_stride + kvh * code_head_stride + r * 128:  K in the first 64 (dims 2i and
@@ -576,7 +577,7 @@ int32_t rtp_kv4_read(const rtp_layer_desc* layer, const rtp_kv4_cache* cache, co
 
 /* rtp_sparse_attn_decode, rtp_local_attn (n_q = 1) and rtp_dense_attn (n_q = 1) with the 4-bit cache as the source of K and V; the
  * other arguments, the rows that are written and lse are theirs.  Contexts and selections longer than max_ctx / max_sel are cut
- * there (both in [1, 2^30]); selected positions may come in any order.  K and V are taken as the values that the codes
+ * there (both in [1, 2^26]); selected positions may come in any order.  K and V are taken as the values that the codes
  * stand for, exactly; products and sums are fp32, and probabilities enter the product with V with 16 bits of mantissa.  A row whose
  * set is empty writes zeros and lse = -inf; a token whose K block is NaN makes its row NaN.
  * rtp_local_attn_kv4 and rtp_dense_attn_kv4 serve any batch with B * n_kv_heads <= 2^20, rtp_sparse_attn_decode_kv4 up to 1024 rows

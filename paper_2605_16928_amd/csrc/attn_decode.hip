@@ -20,10 +20,86 @@
 // kernel merges the partials of a unit (the split-KV reduction of Sec. 3.4, as a separate launch).
 // Algorithmic traffic: 512 B per attended token and KV head (+ 4 B per token for the index list).
 #include "attn_decode_shared.h"
+#include "split_plan.h"
 
 #include <stdlib.h>
 
 namespace rtp {
+
+// Exclusive prefix sum over the block (256 threads); *total gets the block sum.
+__device__ __forceinline__ int block_excl_scan(int v, int* sh_w /*[4]*/, int* total) {
+  int incl = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int t = __shfl_up(incl, o);
+    if ((threadIdx.x & 63) >= o) incl += t;
+  }
+  __syncthreads();
+  if ((threadIdx.x & 63) == 63) sh_w[threadIdx.x >> 6] = incl;
+  __syncthreads();
+  int off = 0, tot = 0;
+#pragma unroll
+  for (int i = 0; i < kAdThreads / 64; ++i) {
+    if (i < (int)(threadIdx.x >> 6)) off += sh_w[i];
+    tot += sh_w[i];
+  }
+  *total = tot;
+  return off + incl - v;
+}
+
+// Every workgroup computes the same plan: split length and the exclusive item prefix per unit.
+template <int SRC>
+__device__ __forceinline__ void build_plan(const AttnDecodeArgs& a, int* sh_prefix /*[kAdMaxUnits+1]*/, int* sh_w /*[2 * waves]*/,
+                                           int* split_tokens, int* n_items) {
+  const int tid = threadIdx.x;
+  int cnt[kAdMaxUnits / kAdThreads];
+  int total128 = 0, longest128 = 0;       // in blocks of 128 tokens, so the total cannot overflow int
+#pragma unroll
+  for (int i = 0; i < kAdMaxUnits / kAdThreads; ++i) {
+    const int u = tid * (kAdMaxUnits / kAdThreads) + i;
+    cnt[i] = u < a.units ? unit_tokens<SRC>(a, u) : 0;
+    total128 += (cnt[i] + 127) >> 7;
+    longest128 = max(longest128, (cnt[i] + 127) >> 7);
+  }
+  total128 = wave_sum(total128);
+  longest128 = wave_max_ge_m1(longest128);
+  if ((tid & 63) == 0) { sh_w[2 * (tid >> 6)] = total128; sh_w[2 * (tid >> 6) + 1] = longest128; }
+  __syncthreads();
+  total128 = longest128 = 0;
+#pragma unroll
+  for (int w = 0; w < kAdThreads / 64; ++w) {
+    total128 += sh_w[2 * w];
+    longest128 = max(longest128, sh_w[2 * w + 1]);
+  }
+  const int st = split_blocks(total128, longest128, a.target_items) * 128;
+  int items = 0;
+#pragma unroll
+  for (int i = 0; i < kAdMaxUnits / kAdThreads; ++i) {
+    cnt[i] = (cnt[i] + st - 1) / st;
+    items += cnt[i];
+  }
+  int tot;
+  int off = block_excl_scan(items, sh_w, &tot);
+#pragma unroll
+  for (int i = 0; i < kAdMaxUnits / kAdThreads; ++i) {
+    const int u = tid * (kAdMaxUnits / kAdThreads) + i;
+    sh_prefix[u] = off;
+    off += cnt[i];
+  }
+  if (tid == kAdThreads - 1) sh_prefix[kAdMaxUnits] = off;
+  __syncthreads();
+  *split_tokens = st;
+  *n_items = tot;
+}
+
+__device__ __forceinline__ int find_unit(const int* sh_prefix, int units, int item) {
+  int lo = 0, hi = units - 1;             // largest u with prefix[u] <= item
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (sh_prefix[mid] <= item) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
 
 // Merge online-softmax state (mo, lo, acco) into (m, l, acc); log2-domain maxima.
 __device__ __forceinline__ void merge_state(float& m, float& l, float (&acc)[8], float mo, float lo,
@@ -51,7 +127,7 @@ __global__ __launch_bounds__(kAdThreads) void attn_decode_kernel(const AttnDecod
 
   int ST, n_items;
   if (SRC == kSrcSparse) {
-    build_plan([&](int u) { return unit_tokens<SRC>(a, u); }, a.units, a.target_items, sh_prefix, sh_w, &ST, &n_items);
+    build_plan<SRC>(a, sh_prefix, sh_w, &ST, &n_items);
   } else {
     ST = a.split_tokens;
     n_items = a.units * a.n_splits;
@@ -285,7 +361,7 @@ __global__ __launch_bounds__(kAdThreads) void attn_decode_combine_kernel(const A
   int b, h, i0, i1;
   if (SRC == kSrcSparse) {
     int ST, n_items;
-    build_plan([&](int u) { return unit_tokens<SRC>(a, u); }, a.units, a.target_items, sh_prefix, sh_w, &ST, &n_items);
+    build_plan<SRC>(a, sh_prefix, sh_w, &ST, &n_items);
     b = unit / a.n_ret;
     h = a.ret_heads[unit - b * a.n_ret];
     i0 = sh_prefix[unit];

@@ -4,7 +4,6 @@
 #pragma once
 
 #include "common.h"
-#include "split_plan.h"
 
 namespace rtp {
 
@@ -59,81 +58,6 @@ __device__ __forceinline__ int unit_tokens(const AttnDecodeArgs& a, int unit) {
   const int s0 = min(a.sink, n);
   const int w0 = max(a.sink, n - a.window);
   return max(s0, 0) + max(0, n - w0);
-}
-
-// Exclusive prefix sum over the block (256 threads); *total gets the block sum.
-__device__ __forceinline__ int block_excl_scan(int v, int* sh_w /*[4]*/, int* total) {
-  int incl = v;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int t = __shfl_up(incl, o);
-    if ((threadIdx.x & 63) >= o) incl += t;
-  }
-  __syncthreads();
-  if ((threadIdx.x & 63) == 63) sh_w[threadIdx.x >> 6] = incl;
-  __syncthreads();
-  int off = 0, tot = 0;
-#pragma unroll
-  for (int i = 0; i < kAdThreads / 64; ++i) {
-    if (i < (int)(threadIdx.x >> 6)) off += sh_w[i];
-    tot += sh_w[i];
-  }
-  *total = tot;
-  return off + incl - v;
-}
-
-// Every workgroup computes the same plan: split length and the exclusive item prefix per unit.
-template <class TokensOf>
-__device__ __forceinline__ void build_plan(TokensOf tokens_of, int units, int target_items, int* sh_prefix /*[kAdMaxUnits+1]*/,
-                                           int* sh_w /*[2 * waves]*/, int* split_tokens, int* n_items) {
-  const int tid = threadIdx.x;
-  int cnt[kAdMaxUnits / kAdThreads];
-  int total128 = 0, longest128 = 0;       // in blocks of 128 tokens, so the total cannot overflow int
-#pragma unroll
-  for (int i = 0; i < kAdMaxUnits / kAdThreads; ++i) {
-    const int u = tid * (kAdMaxUnits / kAdThreads) + i;
-    cnt[i] = u < units ? tokens_of(u) : 0;
-    total128 += (cnt[i] + 127) >> 7;
-    longest128 = max(longest128, (cnt[i] + 127) >> 7);
-  }
-  total128 = wave_sum(total128);
-  longest128 = wave_max_ge_m1(longest128);
-  if ((tid & 63) == 0) { sh_w[2 * (tid >> 6)] = total128; sh_w[2 * (tid >> 6) + 1] = longest128; }
-  __syncthreads();
-  total128 = longest128 = 0;
-#pragma unroll
-  for (int w = 0; w < kAdThreads / 64; ++w) {
-    total128 += sh_w[2 * w];
-    longest128 = max(longest128, sh_w[2 * w + 1]);
-  }
-  const int st = split_blocks(total128, longest128, target_items) * 128;
-  int items = 0;
-#pragma unroll
-  for (int i = 0; i < kAdMaxUnits / kAdThreads; ++i) {
-    cnt[i] = (cnt[i] + st - 1) / st;
-    items += cnt[i];
-  }
-  int tot;
-  int off = block_excl_scan(items, sh_w, &tot);
-#pragma unroll
-  for (int i = 0; i < kAdMaxUnits / kAdThreads; ++i) {
-    const int u = tid * (kAdMaxUnits / kAdThreads) + i;
-    sh_prefix[u] = off;
-    off += cnt[i];
-  }
-  if (tid == kAdThreads - 1) sh_prefix[kAdMaxUnits] = off;
-  __syncthreads();
-  *split_tokens = st;
-  *n_items = tot;
-}
-
-__device__ __forceinline__ int find_unit(const int* sh_prefix, int units, int item) {
-  int lo = 0, hi = units - 1;             // largest u with prefix[u] <= item
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (sh_prefix[mid] <= item) lo = mid; else hi = mid - 1;
-  }
-  return lo;
 }
 
 template <bool F16 = false>

@@ -25,6 +25,9 @@ namespace rtp {
 
 constexpr int kKv4MaxHeads = 128;
 
+constexpr int kMaxUnits = 1 << 20;   // (sequence, KV head) pairs of a call
+constexpr int kMaxLen = 1 << 26;   // longest context or selection: sums of the blocks of 1024 rows, or of 256 sequences, stay inside an int
+
 struct Kv4AttnArgs {
   AttnDecodeArgs d;            // (K, V, strides, seq_start, ring and table fields are not used)
   Kv4Cache c;
@@ -213,11 +216,12 @@ __device__ __forceinline__ void kv4_queries(const AttnDecodeArgs& a, int b, int 
   }
 }
 
-// Joins the four waves' states of an item through LDS and writes the partials of its heads, or, `direct`, their results.
+// Joins the waves' states of an item through LDS and writes the partials of its heads, or, `direct`, their results.
 // skip: heads (of the unit's) that the call does not serve.
-__device__ __forceinline__ void kv4_finish(const Kv4AttnArgs& a, Kv4State& st, Kv4WaveLds (&lds)[4], int item, int b, int h0, int heads,
+template <int WAVES>
+__device__ __forceinline__ void kv4_finish(const Kv4AttnArgs& a, Kv4State& st, Kv4WaveLds (&lds)[WAVES], int item, int b, int h0, int heads,
                                            bool direct, uint32_t skip) {
-  __shared__ float sh_m[4][8], sh_l[4][8];
+  __shared__ float sh_m[WAVES][8], sh_l[WAVES][8];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 15, g = lane >> 4;
   const float ninf = -__builtin_huge_valf();
   st.l = sum_rows(st.l, st.l, st.l, st.l);
@@ -235,14 +239,16 @@ __device__ __forceinline__ void kv4_finish(const Kv4AttnArgs& a, Kv4State& st, K
   }
   __syncthreads();
   float* part = a.d.part + (int64_t)item * heads * kPartStride;
-  for (int e = tid; e < heads * kHeadDim; e += kAdThreads) {
+  for (int e = tid; e < heads * kHeadDim; e += WAVES * 64) {
     const int hh = e >> 7, dim = e & 127;
     if ((skip >> hh) & 1u) continue;
-    const float M = fmaxf(fmaxf(sh_m[0][hh], sh_m[1][hh]), fmaxf(sh_m[2][hh], sh_m[3][hh]));
+    float M = sh_m[0][hh];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) M = fmaxf(M, sh_m[w][hh]);
     const float ref = M == ninf ? 0.f : M;
     float L = 0.f, A = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
       const float cw = fast_exp2(sh_m[w][hh] - ref);
       L += sh_l[w][hh] * (sh_m[w][hh] == ninf ? 1.f : cw);       // (a wave without a finite logit: its sum is 0, or NaN)
       A += lds[w].o[hh][dim] * (sh_m[w][hh] == ninf ? 1.f : cw);
@@ -265,6 +271,48 @@ __device__ __forceinline__ void kv4_clear(Kv4State& st) {
   for (int n = 0; n < 8; ++n) st.o[n] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
 }
 
+// ---- work items ------------------------------------------------------------------------------------------------------------------
+// A list of n lengths (in blocks), each worked on `times` times (the KV heads of a sequence) by items of whole rounds.
+struct Kv4Share {
+  int index, time;        // which length, which of its times
+  int j0, j1;             // the item's blocks
+  int first, count;       // the partials of (index, time)
+};
+template <int ROUND>
+__device__ __forceinline__ int whole_rounds(int blocks) { return (max(blocks, 1) + ROUND - 1) / ROUND * ROUND; }
+
+// All items of a call take about the same number of blocks, by the lengths that the device holds, so that a ragged batch keeps every
+// workgroup busy to the end.  Each wave makes the plan for itself, a lane per length: no LDS, no barrier.  The items of an index are
+// consecutive, time by time, and equal (or the last one would often be a small one).  want: an item's number, or (by_unit) the number
+// index * times + time; false: there is no such item.
+template <int ROUND, class BlocksOf>
+__device__ __forceinline__ bool kv4_share(BlocksOf blocks_of, int n, int times, int target, int want, bool by_unit, Kv4Share* s) {
+  const int lane = threadIdx.x & 63;
+  int total = 0;
+  for (int i0 = 0; i0 < n; i0 += 64) total += wave_sum(i0 + lane < n ? blocks_of(i0 + lane) : 0);
+  const int per = whole_rounds<ROUND>((int)(((int64_t)total * times + target - 1) / target));
+  int base = 0;
+  for (int i0 = 0; i0 < n; i0 += 64) {
+    const int blocks = i0 + lane < n ? blocks_of(i0 + lane) : 0;
+    const int splits = (blocks + per - 1) / per, incl = wave_incl_scan(splits * times), before = base + incl - splits * times;
+    const uint64_t mine = by_unit ? __ballot(i0 + lane == want / times) : __ballot(want >= before && want < base + incl);
+    if (mine) {
+      const int l = __ffsll((unsigned long long)mine) - 1;
+      const int sp = __builtin_amdgcn_readlane(splits, l), at = __builtin_amdgcn_readlane(before, l), len = __builtin_amdgcn_readlane(blocks, l);
+      s->index = i0 + l;
+      s->time = by_unit ? want % times : (want - at) / sp;
+      s->first = at + s->time * sp;
+      const int each = whole_rounds<ROUND>((len + sp - 1) / max(sp, 1)), split = by_unit ? 0 : want - s->first;
+      s->count = (len + each - 1) / each;
+      s->j0 = split * each;
+      s->j1 = min(len, s->j0 + each);
+      return s->j0 < s->j1;
+    }
+    base += __builtin_amdgcn_readlane(incl, 63);
+  }
+  return false;
+}
+
 // ---- every token, or sink + window --------------------------------------------------------------------------------------------
 // A unit's tokens as blocks of 16 positions (a block lies in one page): the sink's blocks, then the window's.
 struct Kv4Range {
@@ -283,79 +331,42 @@ __device__ __forceinline__ Kv4Range kv4_range(const Kv4AttnArgs& a, int b, bool 
 }
 __device__ __forceinline__ uint32_t low16(int n) { return n >= 16 ? 0xffffu : n <= 0 ? 0u : (1u << n) - 1u; }
 
-constexpr int kKv4Round = 8;           // blocks that the four waves take at a time
-constexpr int kKv4Shortest = 8;        // blocks of the shortest item (dense, 1 x 4096 tokens, 2 KV heads, both launches: 8 blocks 9.2 us,
-                                       // 16 9.8, 24 11.1)
-constexpr int kKv4Items = 1024;        // items that are resident together: 4 workgroups on each of 256 compute units
-__device__ __forceinline__ int whole_rounds(int blocks) { return (max(blocks, kKv4Shortest) + kKv4Round - 1) / kKv4Round * kKv4Round; }
+constexpr int kKv4Waves = 8;           // waves of a workgroup
+constexpr int kKv4Round = 2 * kKv4Waves;     // blocks that they take at a time; an item is whole rounds
+constexpr int kKv4Items = 256;         // items: one to a compute unit
 
-// Where an item lies: sequence and its tokens, KV head, blocks j0 .. j1 - 1, and the partials of its unit.
-struct Kv4Item {
-  int b, kvh, j0, j1;
-  int first, count;
-  Kv4Range r;
-};
-
-// Balanced: every item of the call takes the same number of blocks, by the lengths that the device holds, so that a ragged batch keeps
-// all workgroups busy to the end.  Each wave makes the plan for itself, a lane per sequence: the items of a sequence's KV heads are
-// consecutive, KV head by KV head.  want: an item's number, or (by_unit) a unit's; false: there is none.
+// The item (or unit) of a range call.  Not balanced: n_splits items to a unit, the trailing ones of a short unit empty.
 template <bool LOCAL>
-__device__ __forceinline__ bool kv4_balanced_item(const Kv4AttnArgs& a, int want, bool by_unit, Kv4Item* it) {
-  const int lane = threadIdx.x & 63;
-  int total = 0;
-  for (int b0 = 0; b0 < a.B; b0 += 64) total += wave_sum(b0 + lane < a.B ? kv4_range(a, b0 + lane, LOCAL).blocks : 0);
-  const int per = whole_rounds((int)(((int64_t)total * a.d.n_kv_heads + a.d.target_items - 1) / a.d.target_items));
-  int base = 0;
-  for (int b0 = 0; b0 < a.B; b0 += 64) {
-    const int blocks = b0 + lane < a.B ? kv4_range(a, b0 + lane, LOCAL).blocks : 0;
-    const int splits = (blocks + per - 1) / per, incl = wave_incl_scan(splits * a.d.n_kv_heads);
-    const int before = base + incl - splits * a.d.n_kv_heads;
-    const uint64_t mine = by_unit ? __ballot(b0 + lane == want / a.d.n_kv_heads) : __ballot(want >= before && want < base + incl);
-    if (mine) {
-      const int l = __ffsll((unsigned long long)mine) - 1;
-      const int sp = __builtin_amdgcn_readlane(splits, l), at = __builtin_amdgcn_readlane(before, l);
-      it->b = b0 + l;
-      it->kvh = by_unit ? want % a.d.n_kv_heads : (want - at) / sp;
-      it->first = at + it->kvh * sp;
-      it->r = kv4_range(a, it->b, LOCAL);
-      // (a unit's items are equal, or the last one would often be a small one)
-      const int each = whole_rounds((it->r.blocks + sp - 1) / max(sp, 1)), split = by_unit ? 0 : want - it->first;
-      it->count = (it->r.blocks + each - 1) / each;
-      it->j0 = split * each;
-      it->j1 = min(it->r.blocks, it->j0 + each);
-      return it->j0 < it->j1;
-    }
-    base += __builtin_amdgcn_readlane(incl, 63);
+__device__ __forceinline__ bool kv4_range_item(const Kv4AttnArgs& a, int want, bool by_unit, Kv4Share* s, Kv4Range* r) {
+  if (a.balanced) {
+    const bool there = kv4_share<kKv4Round>([&](int b) { return kv4_range(a, b, LOCAL).blocks; }, a.B, a.d.n_kv_heads, a.d.target_items, want,
+                                            by_unit, s);
+    if (there) *r = kv4_range(a, s->index, LOCAL);
+    return there;
   }
-  return false;
-}
-
-// Fixed: n_splits items to a unit, the trailing ones of a short unit empty.
-template <bool LOCAL>
-__device__ __forceinline__ bool kv4_fixed_item(const Kv4AttnArgs& a, int want, bool by_unit, Kv4Item* it) {
   const int unit = by_unit ? want : want / a.d.n_splits, split = by_unit ? 0 : want - unit * a.d.n_splits;
-  it->b = unit / a.d.n_kv_heads;
-  it->kvh = unit - it->b * a.d.n_kv_heads;
-  it->r = kv4_range(a, it->b, LOCAL);
-  const int per = whole_rounds((it->r.blocks + a.d.n_splits - 1) / a.d.n_splits);
-  it->first = unit * a.d.n_splits;
-  it->count = (it->r.blocks + per - 1) / per;
-  it->j0 = split * per;
-  it->j1 = min(it->r.blocks, it->j0 + per);
-  return it->j0 < it->j1 || (a.direct && split == 0);
+  s->index = unit / a.d.n_kv_heads;
+  s->time = unit - s->index * a.d.n_kv_heads;
+  *r = kv4_range(a, s->index, LOCAL);
+  const int per = whole_rounds<kKv4Round>((r->blocks + a.d.n_splits - 1) / a.d.n_splits);
+  s->first = unit * a.d.n_splits;
+  s->count = (r->blocks + per - 1) / per;
+  s->j0 = split * per;
+  s->j1 = min(r->blocks, s->j0 + per);
+  return s->j0 < s->j1 || (a.direct && split == 0);
 }
 
 __device__ __forceinline__ uint32_t kv4_skip(const Kv4AttnArgs& a, int kvh) { return (a.skip[kvh >> 2] >> (8 * (kvh & 3))) & 255u; }
 
 template <bool LOCAL, bool F16>
-__global__ __launch_bounds__(kAdThreads, 4) void kv4_range_kernel(const Kv4AttnArgs a) {
-  __shared__ Kv4WaveLds sh_lines[kAdThreads / 64];
-  __shared__ uint32_t sh_scales[kAdThreads / 64][64];      // two blocks: [group of four tokens][K or V][block][token]
+__global__ __launch_bounds__(kKv4Waves * 64, 2) void kv4_range_kernel(const Kv4AttnArgs a) {
+  __shared__ Kv4WaveLds sh_lines[kKv4Waves];
+  __shared__ uint32_t sh_scales[kKv4Waves][64];      // two blocks: [group of four tokens][K or V][block][token]
   const int item = blockIdx.x;
-  Kv4Item it;
-  if (!(a.balanced ? kv4_balanced_item<LOCAL>(a, item, false, &it) : kv4_fixed_item<LOCAL>(a, item, false, &it))) return;
-  const int b = it.b, kvh = it.kvh, j0 = it.j0, j1 = it.j1;
-  const Kv4Range r = it.r;
+  Kv4Share it;
+  Kv4Range r;
+  if (!kv4_range_item<LOCAL>(a, item, false, &it, &r)) return;
+  const int b = it.index, kvh = it.time, j0 = it.j0, j1 = it.j1;
   const int heads = a.d.n_q_heads / a.d.n_kv_heads, h0 = kvh * heads;
   const uint32_t skip = LOCAL ? kv4_skip(a, kvh) : 0;
   if (skip == (1u << heads) - 1u) return;
@@ -434,23 +445,26 @@ __global__ __launch_bounds__(kAdThreads, 4) void kv4_range_kernel(const Kv4AttnA
     if (valid != 0xffffffffu) clean(valid, t);
     kv4_step<F16>(t, valid, qB, a.d.scale_log2, st);
   };
-  const int step = 2 * (kAdThreads / 64);
+  const int step = 2 * kKv4Waves;
+  constexpr int kAhead = 2;                     // sets of 32 tokens in flight (3 and 4 measured the same on long contexts, 0.6 and 1.6 us more on short ones)
   int j = j0 + 2 * wave;
   if (j < j1) {
-    Kv4Lines in[2];
-    Spot p[2];
-    uint32_t sc[2], valid[2];
-    p[0] = look_up(j);
-    p[1] = look_up(j + step);
-    valid[0] = load(j, p[0], in[0], sc[0]);
-    p[0] = look_up(j + 2 * step);
-    for (; j < j1; j += 2 * step) {
-      valid[1] = load(j + step, p[1], in[1], sc[1]);
-      p[1] = look_up(j + 3 * step);
-      attend(in[0], sc[0], valid[0]);
-      valid[0] = load(j + 2 * step, p[0], in[0], sc[0]);
-      p[0] = look_up(j + 4 * step);
-      attend(in[1], sc[1], valid[1]);
+    Kv4Lines in[kAhead];
+    uint32_t sc[kAhead], valid[kAhead];
+    Spot next = look_up(j);
+#pragma unroll
+    for (int d = 0; d < kAhead - 1; ++d) {
+      valid[d] = load(j + d * step, next, in[d], sc[d]);
+      next = look_up(j + (d + 1) * step);
+    }
+    for (; j < j1; j += kAhead * step) {
+#pragma unroll
+      for (int d = 0; d < kAhead; ++d) {       // (steps beyond the item's end have no token)
+        const int e = (d + kAhead - 1) % kAhead;
+        valid[e] = load(j + (d + kAhead - 1) * step, next, in[e], sc[e]);
+        next = look_up(j + (d + kAhead) * step);
+        attend(in[d], sc[d], valid[d]);
+      }
     }
   }
   kv4_finish(a, st, sh_lines, item, b, h0, heads, a.direct != 0, skip);
@@ -502,132 +516,128 @@ __global__ __launch_bounds__(kAdThreads) void kv4_range_merge_kernel(const Kv4At
   const int heads = a.d.n_q_heads / a.d.n_kv_heads;
   const int unit = blockIdx.x / heads, hh = blockIdx.x - unit * heads;
   if (LOCAL && (kv4_skip(a, unit % a.d.n_kv_heads) >> hh) & 1u) return;
-  Kv4Item it;
-  if (a.balanced) kv4_balanced_item<LOCAL>(a, unit, true, &it);
-  else kv4_fixed_item<LOCAL>(a, unit, true, &it);
-  kv4_merge(a, heads, hh, it.b, it.kvh * heads + hh, it.first, it.first + it.count);
+  Kv4Share it = {};
+  Kv4Range r;
+  kv4_range_item<LOCAL>(a, unit, true, &it, &r);
+  kv4_merge(a, heads, hh, unit / a.d.n_kv_heads, unit % a.d.n_kv_heads * heads + hh, it.first, it.first + it.count);
 }
 
 // ---- selected tokens ------------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ int kv4_selected(const Kv4AttnArgs& a, int unit) { return min(max(a.d.sel_count[unit], 0), a.max_len); }
 
+constexpr int kSpWaves = 4;            // waves of a workgroup where rows are cut into items
+// An item (or row) of a call over selected tokens, in blocks of 64: a wave's share of a round.
+__device__ __forceinline__ bool kv4_sparse_item(const Kv4AttnArgs& a, int want, bool by_unit, Kv4Share* s) {
+  return kv4_share<kSpWaves>([&](int unit) { return (kv4_selected(a, unit) + 63) / 64; }, a.d.units, 1, a.d.target_items, want, by_unit, s);
+}
+
 // A wave takes 64 tokens at a time.  A lane looks one of them up -- its position a chunk ahead of the page, the page a chunk ahead of
 // the bytes -- and fetches its scales; the records are then loaded by eight lanes each, by the offsets that the lanes left in LDS.
-template <bool F16>
-__global__ __launch_bounds__(kAdThreads, 3) void kv4_sparse_kernel(const Kv4AttnArgs a) {
-  __shared__ int sh_prefix[kAdMaxUnits + 1];
-  __shared__ int sh_w[2 * (kAdThreads / 64)];
-  __shared__ Kv4WaveLds sh_lines[kAdThreads / 64];
-  __shared__ int64_t sh_at[kAdThreads / 64][64];          // a token's record, from the head's first byte
-  __shared__ uint32_t sh_ks[kAdThreads / 64][64];         // its four K scales
-  __shared__ __attribute__((aligned(16))) uint8_t sh_vs[kAdThreads / 64][4][64];       // V scales by block
-  int per = 0, n_items = a.d.units;
-  if (!a.direct) build_plan([&](int u) { return kv4_selected(a, u); }, a.d.units, a.d.target_items, sh_prefix, sh_w, &per, &n_items);
+// DIRECT: a workgroup of eight waves has a whole row and writes its result; else items of four waves leave partials.
+template <bool F16, bool DIRECT>
+__global__ __launch_bounds__(DIRECT ? 512 : 256, DIRECT ? 2 : 3) void kv4_sparse_kernel(const Kv4AttnArgs a) {
+  constexpr int kWaves = DIRECT ? 8 : kSpWaves, kThreads = kWaves * 64;
+  __shared__ Kv4WaveLds sh_lines[kWaves];
+  __shared__ int64_t sh_at[kWaves][64];          // a token's record, from the head's first byte
+  __shared__ uint32_t sh_ks[kWaves][64];         // its four K scales
+  __shared__ __attribute__((aligned(16))) uint8_t sh_vs[kWaves][4][64];       // V scales by block
+  const int item = blockIdx.x;
+  Kv4Share it = {item, 0, 0, kMaxLen / 64, 0, 0};
+  if (!DIRECT && !kv4_sparse_item(a, item, false, &it)) return;
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int group = a.d.n_q_heads / a.d.n_kv_heads;
-  for (int item = blockIdx.x; item < n_items; item += gridDim.x) {
-    const int unit = a.direct ? item : find_unit(sh_prefix, a.d.units, item), split = a.direct ? 0 : item - sh_prefix[unit];
-    const int b = unit / a.d.n_ret, h = a.d.ret_heads[unit - b * a.d.n_ret], kvh = h / group;
-    const int t0 = split * per, t1 = a.direct ? kv4_selected(a, unit) : min(kv4_selected(a, unit), t0 + per);
-    const int32_t* idx = a.d.sel_idx + (int64_t)unit * a.d.sel_stride;
-    const int32_t* pt = a.c.page_table + b * a.c.pt_stride;
-    const uint8_t* codes = a.c.codes + kvh * a.c.code_head_stride;
-    const uint8_t* scales = a.c.scales + kvh * a.c.scale_head_stride;
-    u32x4 qB[4];
-    kv4_queries<F16>(a.d, b, h, 1, qB);
-    Kv4State st;
-    kv4_clear(st);
+  const int unit = it.index, b = unit / a.d.n_ret, h = a.d.ret_heads[unit - b * a.d.n_ret], kvh = h / (a.d.n_q_heads / a.d.n_kv_heads);
+  const int t0 = it.j0 * 64, t1 = min(kv4_selected(a, unit), it.j1 * 64);
+  const int32_t* idx = a.d.sel_idx + (int64_t)unit * a.d.sel_stride;
+  const int32_t* pt = a.c.page_table + b * a.c.pt_stride;
+  const uint8_t* codes = a.c.codes + kvh * a.c.code_head_stride;
+  const uint8_t* scales = a.c.scales + kvh * a.c.scale_head_stride;
+  u32x4 qB[4];
+  kv4_queries<F16>(a.d, b, h, 1, qB);
+  Kv4State st;
+  kv4_clear(st);
 
-    // position of this lane's token in the chunk at `base`, and its page (-1: none)
-    auto position = [&](int base) { return base + lane < t1 ? idx[base + lane] : -1; };
-    auto page_of = [&](int pos) { return kv4_page(a.c, pt, pos); };
-    // leaves the records' offsets in LDS and asks for the scales; tokens without a page stand at the head's first record
-    auto place = [&](int pos, int page, u32x4& k4, u32x4& v4) {
-      const int slot = page < 0 ? 0 : pos & ((1 << a.c.page_shift) - 1);
-      const int64_t pg = max(page, 0);
-      wave_lds_fence();
-      sh_at[wave][lane] = pg * ((int64_t)a.c.code_page16 * 16) + (int64_t)slot * kKv4Row;
-      wave_lds_fence();
-      const u32x4* sp = reinterpret_cast<const u32x4*>(scales + pg * ((int64_t)a.c.scale_page16 * 16) + (int64_t)(slot >> 2) * kKv4Group);
-      k4 = sp[0];
-      v4 = sp[1];
-    };
-    auto load = [&](int half, Kv4Lines& in) {
+  // position of this lane's token in the chunk at `base`, and its page (-1: none)
+  auto position = [&](int base) { return base + lane < t1 ? idx[base + lane] : -1; };
+  auto page_of = [&](int pos) { return kv4_page(a.c, pt, pos); };
+  // leaves the records' offsets in LDS and asks for the scales; tokens without a page stand at the head's first record
+  auto place = [&](int pos, int page, u32x4& k4, u32x4& v4) {
+    const int slot = page < 0 ? 0 : pos & ((1 << a.c.page_shift) - 1);
+    const int64_t pg = max(page, 0);
+    wave_lds_fence();
+    sh_at[wave][lane] = pg * ((int64_t)a.c.code_page16 * 16) + (int64_t)slot * kKv4Row;
+    wave_lds_fence();
+    const u32x4* sp = reinterpret_cast<const u32x4*>(scales + pg * ((int64_t)a.c.scale_page16 * 16) + (int64_t)(slot >> 2) * kKv4Group);
+    k4 = sp[0];
+    v4 = sp[1];
+  };
+  auto load = [&](int half, Kv4Lines& in) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        in.line[q] = *reinterpret_cast<const u32x4*>(codes + sh_at[wave][32 * half + 8 * q + (lane >> 3)] + (lane & 7) * 16);
-    };
+    for (int q = 0; q < 4; ++q)
+      in.line[q] = *reinterpret_cast<const u32x4*>(codes + sh_at[wave][32 * half + 8 * q + (lane >> 3)] + (lane & 7) * 16);
+  };
 
-    int base = t0 + wave * 64;
-    if (base < t1) {
-      Kv4Lines in[2];
-      u32x4 k4, v4;
-      int pos = position(base), next_pos = position(base + kAdThreads);
-      int page = page_of(pos);
-      place(pos, page, k4, v4);
-      load(0, in[0]);
-      load(1, in[1]);
-      int next_page = page_of(next_pos), third_pos = position(base + 2 * kAdThreads);
-      for (; base < t1; base += kAdThreads) {
-        // this chunk's scales to where the tiles' lanes read them
-        const uint64_t there = __ballot(page >= 0);
-        uint32_t ks = 0, vs = 0;
-        const int sh = 8 * (pos & 3);
+  int base = t0 + wave * 64;
+  if (base < t1) {
+    Kv4Lines in[2];
+    u32x4 k4, v4;
+    int pos = position(base), next_pos = position(base + kThreads);
+    int page = page_of(pos);
+    place(pos, page, k4, v4);
+    load(0, in[0]);
+    load(1, in[1]);
+    int next_page = page_of(next_pos), third_pos = position(base + 2 * kThreads);
+    for (; base < t1; base += kThreads) {
+      // this chunk's scales to where the tiles' lanes read them
+      const uint64_t there = __ballot(page >= 0);
+      uint32_t ks = 0, vs = 0;
+      const int sh = 8 * (pos & 3);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          ks |= ((k4[q] >> sh) & 255u) << (8 * q);
-          vs |= ((v4[q] >> sh) & 255u) << (8 * q);
-        }
-        if (page < 0) vs = 0;                    // (2^-127: what it multiplies stays finite)
-        wave_lds_fence();
-        sh_ks[wave][lane] = ks;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) sh_vs[wave][q][lane] = (uint8_t)(vs >> (8 * q));
-        pos = next_pos;
-        page = next_page;
-        place(pos, page, k4, v4);
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const uint32_t valid = (uint32_t)(there >> (32 * half));
-          if (valid) {
-            Kv4Tiles t;
-            kv4_turn(in[half], sh_lines[wave], t);
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-              const int first = 32 * half + 16 * s;
-              t.ks[s] = reinterpret_cast<const uint8_t*>(&sh_ks[wave][first + c])[g];
-              t.vs[s] = *reinterpret_cast<const uint32_t*>(&sh_vs[wave][c >> 2][first + 4 * g]);
-            }
-            kv4_step<F16>(t, valid, qB, a.d.scale_log2, st);
-          }
-          load(half, in[half]);
-        }
-        next_pos = third_pos;
-        next_page = page_of(next_pos);
-        third_pos = position(base + 3 * kAdThreads);
+      for (int q = 0; q < 4; ++q) {
+        ks |= ((k4[q] >> sh) & 255u) << (8 * q);
+        vs |= ((v4[q] >> sh) & 255u) << (8 * q);
       }
+      if (page < 0) vs = 0;                    // (2^-127: what it multiplies stays finite)
+      wave_lds_fence();
+      sh_ks[wave][lane] = ks;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) sh_vs[wave][q][lane] = (uint8_t)(vs >> (8 * q));
+      pos = next_pos;
+      page = next_page;
+      place(pos, page, k4, v4);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const uint32_t valid = (uint32_t)(there >> (32 * half));
+        if (valid) {
+          Kv4Tiles t;
+          kv4_turn(in[half], sh_lines[wave], t);
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            const int first = 32 * half + 16 * s;
+            t.ks[s] = reinterpret_cast<const uint8_t*>(&sh_ks[wave][first + c])[g];
+            t.vs[s] = *reinterpret_cast<const uint32_t*>(&sh_vs[wave][c >> 2][first + 4 * g]);
+          }
+          kv4_step<F16>(t, valid, qB, a.d.scale_log2, st);
+        }
+        load(half, in[half]);
+      }
+      next_pos = third_pos;
+      next_page = page_of(next_pos);
+      third_pos = position(base + 3 * kThreads);
     }
-    kv4_finish(a, st, sh_lines, item, b, h, 1, a.direct != 0, 0);
-    __syncthreads();                             // (the joined outputs have been read: their LDS is free again)
   }
+  kv4_finish(a, st, sh_lines, item, b, h, 1, DIRECT, 0);
 }
 
 __global__ __launch_bounds__(kAdThreads) void kv4_sparse_merge_kernel(const Kv4AttnArgs a) {
-  __shared__ int sh_prefix[kAdMaxUnits + 1];
-  __shared__ int sh_w[2 * (kAdThreads / 64)];
-  int per, n_items;
-  build_plan([&](int u) { return kv4_selected(a, u); }, a.d.units, a.d.target_items, sh_prefix, sh_w, &per, &n_items);
   const int unit = blockIdx.x, b = unit / a.d.n_ret;
-  kv4_merge(a, 1, 0, b, a.d.ret_heads[unit - b * a.d.n_ret], sh_prefix[unit], unit + 1 < a.d.units ? sh_prefix[unit + 1] : n_items);
+  Kv4Share it = {};
+  kv4_sparse_item(a, unit, true, &it);
+  kv4_merge(a, 1, 0, b, a.d.ret_heads[unit - b * a.d.n_ret], it.first, it.first + it.count);
 }
 
-constexpr int64_t kMaxLen = (int64_t)1 << 30;      // (positions and counts, rounded up, stay inside an int)
 
 // ---- host -----------------------------------------------------------------------------------------------------------------------
-#ifndef RDIRECT
-#define RDIRECT 40
-#endif
 struct Kv4RangePlan {
   int32_t units, n_splits, target, grid;
   bool balanced;
@@ -642,10 +652,10 @@ static Kv4RangePlan plan_range(const rtp_layer_desc* L, bool local, int32_t B, i
     const int64_t set = ((int64_t)L->sink + 15) / 16 + ((int64_t)L->window + 15) / 16 + 1;
     if (set < blocks) blocks = set;
   }
-  const int64_t most = (blocks + kKv4Shortest - 1) / kKv4Shortest;       // items of the longest unit
+  const int64_t most = (blocks + kKv4Round - 1) / kKv4Round;             // items of the longest unit
   int64_t n = kKv4Items / p.units;
   if (n > most) n = most;
-  if (n < 1 || blocks <= RDIRECT) n = 1;
+  if (n < 1 || blocks <= 48 + p.units) n = 1;
   p.n_splits = (int32_t)n;
   p.grid = p.units * p.n_splits;
   // Lengths can differ, and a unit is more than one item: shared out by the lengths.  (Beyond 256 sequences the plan, a pass over the
@@ -662,7 +672,9 @@ static Kv4RangePlan plan_range(const rtp_layer_desc* L, bool local, int32_t B, i
 }
 
 static size_t range_ws(const rtp_layer_desc* L, bool local, int32_t B, int64_t max_ctx) {
-  if (!L || B <= 0 || max_ctx <= 0 || L->n_kv_heads <= 0 || L->n_q_heads < L->n_kv_heads) return 256;
+  if (!L || B <= 0 || max_ctx <= 0 || max_ctx > kMaxLen || L->n_kv_heads <= 0 || L->n_q_heads < L->n_kv_heads ||
+      (int64_t)B * L->n_kv_heads > kMaxUnits)
+    return 256;
   const size_t w = plan_range(L, local, B, max_ctx).ws_bytes;
   return w ? w : 256;
 }
@@ -702,13 +714,13 @@ static int32_t range_attn_kv4(const char* who, const rtp_layer_desc* layer, cons
   int32_t rc = fill_head_table(layer, &ht, who);
   if (rc != RTP_OK) return rc;
   if (B <= 0 || max_ctx <= 0 || max_ctx > kMaxLen)
-    return fail(RTP_ERR_INVALID_ARG, "%s: B must be positive, max_ctx in [1, 2^30]", who);
+    return fail(RTP_ERR_INVALID_ARG, "%s: B must be positive, max_ctx in [1, 2^26]", who);
   if (!ctx_len) return fail(RTP_ERR_INVALID_ARG, "%s: NULL ctx_len", who);
   Kv4AttnArgs a;
   rc = check_kv4_cache(who, layer, cache, max_ctx, &a.c);
   if (rc != RTP_OK) return rc;
-  if ((int64_t)B * layer->n_kv_heads > (1 << 20))
-    return fail(RTP_ERR_UNSUPPORTED, "%s: B * n_kv_heads = %lld exceeds %d", who, (long long)B * layer->n_kv_heads, 1 << 20);
+  if ((int64_t)B * layer->n_kv_heads > kMaxUnits)
+    return fail(RTP_ERR_UNSUPPORTED, "%s: B * n_kv_heads = %lld exceeds %d", who, (long long)B * layer->n_kv_heads, kMaxUnits);
   const Kv4RangePlan p = plan_range(layer, LOCAL, B, max_ctx);
   rc = check_io(who, q, out, ws, ws_bytes, p.ws_bytes);
   if (rc != RTP_OK) return rc;
@@ -727,29 +739,31 @@ static int32_t range_attn_kv4(const char* who, const rtp_layer_desc* layer, cons
     const int G = layer->n_q_heads / layer->n_kv_heads;
     for (int j = 0; j < layer->n_ret; ++j) a.skip[ht.ret_heads[j] / G / 4] |= 1u << (8 * (ht.ret_heads[j] / G % 4) + ht.ret_heads[j] % G);
   }
-  const dim3 grid((unsigned)p.grid), block(kAdThreads);
-  if (a.d.f16) RTP_LAUNCH((kv4_range_kernel<LOCAL, true>), grid, block, 0, s, a);
-  else RTP_LAUNCH((kv4_range_kernel<LOCAL, false>), grid, block, 0, s, a);
-  if (!a.direct)
-    RTP_LAUNCH(kv4_range_merge_kernel<LOCAL>, dim3((unsigned)B * layer->n_q_heads), block, 0, s, a);
+  const dim3 grid((unsigned)p.grid);
+  if (a.d.f16) RTP_LAUNCH((kv4_range_kernel<LOCAL, true>), grid, dim3(kKv4Waves * 64), 0, s, a);
+  else RTP_LAUNCH((kv4_range_kernel<LOCAL, false>), grid, dim3(kKv4Waves * 64), 0, s, a);
+  if (!a.direct) RTP_LAUNCH(kv4_range_merge_kernel<LOCAL>, dim3((unsigned)B * layer->n_q_heads), dim3(kAdThreads), 0, s, a);
   return check_launch(who);
 }
 
 struct Kv4SparsePlan {
-  int32_t target;
+  int32_t target, grid;
   bool direct;
   size_t ws_bytes;
 };
-#ifndef SDIRECT
-#define SDIRECT 640
-#endif
 static Kv4SparsePlan plan_sparse(int64_t units, int64_t max_sel) {
-  const int64_t blocks = units * ((max_sel + 127) / 128);
-  Kv4SparsePlan p;
-  p.direct = max_sel <= SDIRECT;
-  p.target = (int32_t)(blocks < 1536 ? blocks : 1536);
-  // items <= total / ceil(total / target) + units <= target + units
-  p.ws_bytes = p.direct ? 0 : align_up((size_t)(p.target + units) * kPartStride * sizeof(float), 256);
+  Kv4SparsePlan p = {};
+  // Rows of up to 1024 tokens, two rounds of eight waves, in one launch (us; 1, 8, 64, 256 rows of 640 tokens 6.6 / 7.0 / 7.2 / 9.0 against
+  // 8.5 / 8.9 / 9.2 / 15.4 in two launches, of 1024 tokens 8.3 / 8.7 / 9.0 / 13.6 against 8.5 / 8.8 / 9.2 / 21.8, 1 of 1536 10.6 against 8.5).
+  p.direct = max_sel <= 1024;
+  const int64_t most = units * ((max_sel + kSpWaves * 64 - 1) / (kSpWaves * 64));
+  // All items resident at once, three workgroups on each of 256 compute units; a row's number of items is rounded up, by a half on average.
+  // (256 rows of 8000 tokens 64.3 us, at twice the items 73.8; 200 to 30000 tokens a row 61.2 and 60.0.)
+  p.target = (int32_t)(768 - units / 2 < 256 ? 256 : 768 - units / 2);
+  int64_t grid = p.target + units;                                       // items <= total / ceil(total / target) + units
+  if (grid > most) grid = most;
+  p.grid = (int32_t)(p.direct ? units : grid);
+  p.ws_bytes = p.direct ? 0 : align_up((size_t)p.grid * kPartStride * sizeof(float), 256);
   return p;
 }
 
@@ -758,7 +772,7 @@ static Kv4SparsePlan plan_sparse(int64_t units, int64_t max_sel) {
 using namespace rtp;
 
 extern "C" size_t rtp_sparse_attn_decode_kv4_workspace_bytes(const rtp_layer_desc* layer, int32_t B, int64_t max_sel) {
-  if (!layer || B <= 0 || max_sel <= 0 || layer->n_ret <= 0) return 256;
+  if (!layer || B <= 0 || max_sel <= 0 || max_sel > kMaxLen || layer->n_ret <= 0 || (int64_t)B * layer->n_ret > kAdMaxUnits) return 256;
   const size_t w = plan_sparse((int64_t)B * layer->n_ret, max_sel).ws_bytes;
   return w ? w : 256;
 }
@@ -776,7 +790,7 @@ extern "C" int32_t rtp_sparse_attn_decode_kv4(const rtp_layer_desc* layer, const
   if (rc != RTP_OK) return rc;
   if (!sel_idx || !sel_count) return fail(RTP_ERR_INVALID_ARG, "%s: NULL sel_idx/sel_count", who);
   if (B <= 0 || max_sel <= 0 || max_sel > kMaxLen)
-    return fail(RTP_ERR_INVALID_ARG, "%s: B must be positive, max_sel in [1, 2^30]", who);
+    return fail(RTP_ERR_INVALID_ARG, "%s: B must be positive, max_sel in [1, 2^26]", who);
   if (sel_stride < max_sel) return fail(RTP_ERR_INVALID_ARG, "%s: sel_stride must be >= max_sel", who);
   const int64_t units = (int64_t)B * layer->n_ret;
   if (units > kAdMaxUnits) return fail(RTP_ERR_UNSUPPORTED, "%s: B * n_ret = %lld exceeds %d", who, (long long)units, kAdMaxUnits);
@@ -794,10 +808,15 @@ extern "C" int32_t rtp_sparse_attn_decode_kv4(const rtp_layer_desc* layer, const
   a.max_len = (int32_t)max_sel;
   a.direct = p.direct;
   hipStream_t s = (hipStream_t)stream;
-  const dim3 grid((unsigned)(p.direct ? units : p.target));
-  if (a.d.f16) RTP_LAUNCH(kv4_sparse_kernel<true>, grid, dim3(kAdThreads), 0, s, a);
-  else RTP_LAUNCH(kv4_sparse_kernel<false>, grid, dim3(kAdThreads), 0, s, a);
-  if (!p.direct) RTP_LAUNCH(kv4_sparse_merge_kernel, dim3((unsigned)units), dim3(kAdThreads), 0, s, a);
+  const dim3 grid((unsigned)p.grid);
+  if (p.direct) {
+    if (a.d.f16) RTP_LAUNCH((kv4_sparse_kernel<true, true>), grid, dim3(512), 0, s, a);
+    else RTP_LAUNCH((kv4_sparse_kernel<false, true>), grid, dim3(512), 0, s, a);
+    return check_launch(who);
+  }
+  if (a.d.f16) RTP_LAUNCH((kv4_sparse_kernel<true, false>), grid, dim3(kSpWaves * 64), 0, s, a);
+  else RTP_LAUNCH((kv4_sparse_kernel<false, false>), grid, dim3(kSpWaves * 64), 0, s, a);
+  RTP_LAUNCH(kv4_sparse_merge_kernel, dim3((unsigned)units), dim3(kAdThreads), 0, s, a);
   return check_launch(who);
 }
 

@@ -404,7 +404,7 @@ __global__ __launch_bounds__(256) void kv_pages_copy_kernel(const CopyArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int w = piece * kPieceWords + i * 64 + lane;
-      if (w < p.page16) v[i] = s[w];
+      if (w < p.page16) v[i] = __builtin_nontemporal_load(s + w);     // (983 pages of 256 KB: 77 us, 104 without, 95 with such stores too)
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {

@@ -266,6 +266,82 @@ class DecodeRun:
         return self.out.float().cpu().numpy().astype(np.float64)
 
 
+class Kv4DecodeRun(DecodeRun):
+    """A decode workload whose K and V live in a paged 4-bit cache: pages handed out and tokens appended through the library,
+    selection by the workload's own index keys, attention over the 4-bit cache.  spare_seqs: further rows of the page table, for
+    forks; spare_pages: free pages behind what the contexts take."""
+
+    def __init__(self, w: wl.DecodeWorkload, page_size: int = 64, spare_seqs: int = 0, spare_pages: int = 8):
+        super().__init__(w)
+        L, B = w.layer, self.B
+        need = [-(-n // page_size) for n in w.ctx_len]
+        self.page_size, self.n_pages = page_size, sum(need) + spare_pages
+        self.codes = torch.zeros((L.n_kv_heads, self.n_pages, page_size, 128), dtype=torch.uint8, device=DEV)
+        self.scales = torch.zeros((L.n_kv_heads, self.n_pages, page_size * 8), dtype=torch.uint8, device=DEV)
+        self.page_table = torch.empty((B + spare_seqs, max(need) + 2), dtype=torch.int32, device=DEV)
+        self.page_refs = torch.empty((self.n_pages,), dtype=torch.int32, device=DEV)
+        self.map = rtp.page_map(self.page_table, self.page_refs, page_size)
+        self.cache = rtp.kv4_cache(self.codes, self.scales, self.page_table)
+        self.pools = rtp.page_pools([self.codes, self.scales])
+        n = max(B + spare_seqs, self.n_pages)
+        self.copy_src, self.copy_dst = (torch.empty((n,), dtype=torch.int32, device=DEV) for _ in range(2))
+        self.status = torch.zeros((2,), dtype=torch.int32, device=DEV)
+        self.ws_pages = ws_alloc(rtp.rtp_kv_pages_workspace_bytes(self.map, B + spare_seqs))
+        self.ws_sparse4 = ws_alloc(rtp.rtp_sparse_attn_decode_kv4_workspace_bytes(self.desc, B, self.max_ctx))
+        self.ws_local4 = ws_alloc(rtp.rtp_local_attn_kv4_workspace_bytes(self.desc, B, self.max_ctx))
+        self.ws_dense4 = ws_alloc(rtp.rtp_dense_attn_kv4_workspace_bytes(self.desc, B, self.max_ctx))
+        rtp.rtp_kv_pages_init(self.map)
+        self.extend(range(B), [0] * B, w.ctx_len)
+        for b in range(B):                      # (the workload packs its sequences along one token axis)
+            t0, n = w.seq_start[b], w.ctx_len[b]
+            row = rtp.kv4_cache(self.codes, self.scales, self.page_table[b:b + 1])
+            rtp.rtp_kv4_append(self.desc, row, w.K[:, t0:], w.V[:, t0:], 0, 128, w.K.shape[1] * 128, i32([0]), None, 1, n)
+
+    # ---- pages ----------------------------------------------------------------------------------
+    def extend(self, seqs, old_len, new_len):
+        """Pages for sequences that grow, own copies of shared last pages among them; status holds {lacking, left}."""
+        n = len(seqs)
+        rtp.rtp_kv_pages_extend(self.map, i32(seqs), i32(old_len), i32(new_len), n, self.copy_src, self.copy_dst, self.status,
+                                self.ws_pages)
+        rtp.rtp_kv_pages_copy(self.pools, self.n_pages, self.copy_src, self.copy_dst, n)
+
+    def fork(self, src, dst, length):
+        rtp.rtp_kv_pages_fork(self.map, i32(src), i32(dst), i32(length), len(src))
+
+    def truncate(self, seqs, keep=None):
+        rtp.rtp_kv_pages_truncate(self.map, i32(seqs), None if keep is None else i32(keep), len(seqs))
+
+    def compact(self):
+        rtp.rtp_kv_pages_compact(self.map, self.copy_src, self.copy_dst, self.status, self.ws_pages)
+        rtp.rtp_kv_pages_copy(self.pools, self.n_pages, self.copy_src, self.copy_dst, self.n_pages, self.status[1:])
+
+    # ---- the step -------------------------------------------------------------------------------
+    def append(self, k_new, v_new, start, count=None):
+        """New tokens [B, T, n_kv_heads, 128] at positions start[b] (device int32)."""
+        rtp.rtp_kv4_append(self.desc, self.cache, k_new, v_new, k_new.stride(0), k_new.stride(1), k_new.stride(2), start, count,
+                           k_new.shape[0], k_new.shape[1])
+
+    def sparse_attn(self, sel_idx=None, sel_count=None, max_sel=None):
+        rtp.rtp_sparse_attn_decode_kv4(self.desc, self.w.q, self.cache, self.sel_idx if sel_idx is None else sel_idx, self.stride,
+                                       self.sel_count if sel_count is None else sel_count,
+                                       self.max_ctx if max_sel is None else max_sel, self.B, self.out, self.lse, self.ws_sparse4)
+
+    def local_attn(self, stream=None):
+        rtp.rtp_local_attn_kv4(self.desc, self.w.q, self.cache, self.ctx_len, self.B, self.max_ctx, self.out, self.lse,
+                               self.ws_local4, stream=stream)
+
+    def dense_attn(self, out=None, lse=None):
+        rtp.rtp_dense_attn_kv4(self.desc, self.w.q, self.cache, self.ctx_len, self.B, self.max_ctx,
+                               self.out if out is None else out, self.lse if lse is None else lse, self.ws_dense4)
+
+    def step(self, fused: bool = False):
+        """One decode step: index scores, top-p, attention over the 4-bit cache."""
+        self.index_score()
+        self.topp()
+        self.sparse_attn()
+        self.local_attn()
+
+
 class PrefillRun:
     """Device buffers for one prefill chunk of one sequence and the C-ABI calls on it."""
 
