@@ -574,7 +574,7 @@ __global__ __launch_bounds__(DIRECT ? 512 : 256, DIRECT ? 2 : 3) void kv4_sparse
   auto load = [&](int half, Kv4Lines& in) {
 #pragma unroll
     for (int q = 0; q < 4; ++q)
-      in.line[q] = *reinterpret_cast<const u32x4*>(codes + sh_at[wave][32 * half + 8 * q + (lane >> 3)] + (lane & 7) * 16);
+      in.line[q] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(codes + sh_at[wave][32 * half + 8 * q + (lane >> 3)] + (lane & 7) * 16));
   };
 
   int base = t0 + wave * 64;
@@ -758,7 +758,7 @@ static Kv4SparsePlan plan_sparse(int64_t units, int64_t max_sel) {
   p.direct = max_sel <= 1024;
   const int64_t most = units * ((max_sel + kSpWaves * 64 - 1) / (kSpWaves * 64));
   // All items resident at once, three workgroups on each of 256 compute units; a row's number of items is rounded up, by a half on average.
-  // (256 rows of 8000 tokens 64.3 us, at twice the items 73.8; 200 to 30000 tokens a row 61.2 and 60.0.)
+  // (256 rows of 8000 tokens 62 us, at twice the items 72; 200 to 30000 tokens a row 61 and 63.)
   p.target = (int32_t)(768 - units / 2 < 256 ? 256 : 768 - units / 2);
   int64_t grid = p.target + units;                                       // items <= total / ceil(total / target) + units
   if (grid > most) grid = most;

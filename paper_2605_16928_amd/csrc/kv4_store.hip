@@ -10,6 +10,8 @@
 // Both kernels are bound by their bytes: 512 in and 136 out per token and KV head, or the other way round.  16 lanes own a row (8 dims
 // each: one 16-byte load, one 4-byte store of codes), a block's maximum is two DPP steps over a quad, and a 16-lane group takes the
 // four positions of one scale group: eight loads in flight per lane, and whole scale words where all four positions are written.
+// The 16-bit rows that read writes go past the caches: with 32768 tokens of 8 KV heads (170 MB moved) it takes 26 us, 6.5 TB/s, with
+// ordinary stores 33; 4096 tokens are appended in 6 us.
 #include "kv4_cache.h"
 
 namespace rtp {
@@ -176,8 +178,8 @@ __global__ __launch_bounds__(kStoreThreads) void kv4_read_kernel(const Kv4StoreA
   for (int i = 0; i < 4; ++i) {
     if (s.pos0 + i < s.start || s.pos0 + i >= s.end) continue;
     const int64_t at = dst + (int64_t)(s.pos0 + i - s.start) * a.token_stride;
-    *reinterpret_cast<u32x4*>(a.k + at) = decode8<F16>(kc[i], kv4_scale(ks, i));
-    *reinterpret_cast<u32x4*>(a.v + at) = decode8<F16>(vc[i], kv4_scale(vs, i));
+    __builtin_nontemporal_store(decode8<F16>(kc[i], kv4_scale(ks, i)), reinterpret_cast<u32x4*>(a.k + at));
+    __builtin_nontemporal_store(decode8<F16>(vc[i], kv4_scale(vs, i)), reinterpret_cast<u32x4*>(a.v + at));
   }
 }
 

@@ -383,12 +383,15 @@ struct CopyArgs {
   const int32_t* count;
 };
 constexpr int kPieceWords = 256;  // a wave's piece: four 16-byte words per lane, 4 KB
+// What passes this many pieces (64 MB) streams: it is read past the caches, by two workgroups per compute unit only (983 pages of
+// 256 KB: 92 us, 5.6 TB/s; 97 with eight, 105 with ordinary loads and stores).  Less is copied by all that fit (64 such pages: 6 us, 8 by
+// two workgroups).  Stores pass the caches either way (64 pages 6.5 us without, 983 pages 105).
+constexpr int64_t kStreamPieces = 16384;
+constexpr unsigned kStreamGroups = 512;
 
-__global__ __launch_bounds__(256) void kv_pages_copy_kernel(const CopyArgs a) {
+template <bool STREAM>
+__device__ __forceinline__ void copy_pieces(const CopyArgs& a, int64_t items, int per_pair, int64_t waves) {
   const int lane = threadIdx.x & 63;
-  const int n = a.count ? min(max(*a.count, 0), a.n) : a.n;
-  const int per_pair = a.first[a.n_pools];
-  const int64_t items = (int64_t)n * per_pair, waves = (int64_t)gridDim.x * 4;
   for (int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); item < items; item += waves) {
     const int pair = (int)(item / per_pair), rest = (int)(item - (int64_t)pair * per_pair);
     const int src = a.src[pair], dst = a.dst[pair];
@@ -404,13 +407,25 @@ __global__ __launch_bounds__(256) void kv_pages_copy_kernel(const CopyArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int w = piece * kPieceWords + i * 64 + lane;
-      if (w < p.page16) v[i] = __builtin_nontemporal_load(s + w);     // (983 pages of 256 KB: 77 us, 104 without, 95 with such stores too)
+      if (w < p.page16) v[i] = STREAM ? __builtin_nontemporal_load(s + w) : s[w];
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int w = piece * kPieceWords + i * 64 + lane;
-      if (w < p.page16) d[w] = v[i];
+      if (w < p.page16) __builtin_nontemporal_store(v[i], d + w);
     }
+  }
+}
+
+__global__ __launch_bounds__(256) void kv_pages_copy_kernel(const CopyArgs a) {
+  const int n = a.count ? min(max(*a.count, 0), a.n) : a.n;
+  const int per_pair = a.first[a.n_pools];
+  const int64_t items = (int64_t)n * per_pair;
+  if (items > kStreamPieces) {
+    const unsigned groups = min(gridDim.x, kStreamGroups);
+    if (blockIdx.x < groups) copy_pieces<true>(a, items, per_pair, (int64_t)groups * 4);
+  } else {
+    copy_pieces<false>(a, items, per_pair, (int64_t)gridDim.x * 4);
   }
 }
 
