@@ -207,6 +207,22 @@ int32_t check_kv4_cache(const char* who, const rtp_layer_desc* L, const rtp_kv4_
   return RTP_OK;
 }
 
+// Rows of 128 at the multiples of three strides, nested in any order, do not overlap.
+static bool rows_apart(int64_t s0, int64_t n0, int64_t s1, int64_t n1, int64_t s2, int64_t n2) {
+  int64_t s[3] = {s0, s1, s2}, n[3] = {n0, n1, n2}, span = kHeadDim;
+  for (int round = 0; round < 3; ++round) {    // the smallest stride that is left has to pass what lies inside it
+    int i = -1;
+    for (int k = 0; k < 3; ++k)
+      if (n[k] > 1 && (i < 0 || s[k] < s[i])) i = k;
+    if (i < 0) return true;
+    if (s[i] < span) return false;
+    if (s[i] > (((int64_t)1 << 62) - span) / (n[i] - 1)) return (n[0] > 1) + (n[1] > 1) + (n[2] > 1) == 1;
+    span += s[i] * (n[i] - 1);
+    n[i] = 1;
+  }
+  return true;
+}
+
 static int32_t store_args(const char* who, const rtp_layer_desc* layer, const rtp_kv4_cache* cache, const void* k, const void* v,
                           int64_t batch_stride, int64_t token_stride, int64_t head_stride, const int32_t* start,
                           const int32_t* count, int32_t B, int32_t T, Kv4StoreArgs* a, unsigned* grid) {
@@ -262,7 +278,8 @@ extern "C" int32_t rtp_kv4_read(const rtp_layer_desc* layer, const rtp_kv4_cache
   unsigned grid = 0;
   const int32_t rc = store_args(who, layer, cache, k, v, batch_stride, token_stride, head_stride, start, count, B, T, &a, &grid);
   if (rc != RTP_OK) return rc;
-  if (token_stride < kHeadDim && T > 1) return fail(RTP_ERR_INVALID_ARG, "%s: token_stride must be >= 128", who);
+  if (!rows_apart(batch_stride, B, token_stride, T, head_stride, layer->n_kv_heads))
+    return fail(RTP_ERR_INVALID_ARG, "%s: strides let the rows that are written overlap", who);
   clear_error();
   if (layer->kv_dtype == RTP_DTYPE_FP16) RTP_LAUNCH(kv4_read_kernel<true>, dim3(grid), dim3(kStoreThreads), 0, (hipStream_t)stream, a);
   else RTP_LAUNCH(kv4_read_kernel<false>, dim3(grid), dim3(kStoreThreads), 0, (hipStream_t)stream, a);

@@ -268,3 +268,11 @@ def test_descriptors_from_tensors():
     assert (p[0].page_bytes, p[0].n_heads, p[1].page_stride, p[1].head_stride, p[1].page_bytes) == (2048, 2, 512, 256, 256) and p.n_pools == 2
     with pytest.raises(rtp.RtpError):
         rtp.page_pools([codes[:, :, :, ::2]])
+
+
+@pytest.mark.parametrize("strides", [(0, 256, 128), (2560, 0, 128), (2560, 256, 0), (2560, 128, 128), (2560, 256, 120), (2432, 256, 128),
+                                     (1280, 128, 1152), (1 << 62, 1 << 62, 128)])
+def test_read_refuses_rows_that_overlap(strides):
+    call, args = _calls()["read"]                       # 3 sequences of 10 tokens and 2 heads
+    args.update(zip(("batch_stride", "token_stride", "head_stride"), strides))
+    _refused(rtp.RTP_ERR_INVALID_ARG, call, **args)
