@@ -16,8 +16,12 @@
 // that needs the rest has p itself), and an fp16 query is split over the columns the same way.  P keeps 16 bits of mantissa thereby,
 // and one kernel serves both types.
 //
-// Work split: a unit (sequence and KV head, or sequence and retrieval head) is cut into items, an item goes to a workgroup of four
-// waves, which leaves a partial (max, sum, 128 outputs) per head for the merge launch, or the result where a unit is one item.
+// Work split: a unit (sequence and KV head, or sequence and retrieval head) is cut into items, an item goes to a workgroup of eight or
+// four waves, which leaves a partial (max, sum, 128 outputs) per head for the merge launch, or the result where a unit is one item.
+//
+// Measured: 8 contexts of 131072 tokens, 8 KV heads (1.14 GB) 181 us, 6.3 TB/s; windows of 8192 of 32 sequences (219 MB) 45 us, 4.9; 256
+// rows of 200 to 30000 selected tokens (222 MB) 56 + 4 us.  With the products left out the loads alone take 167 and 36 us for the
+// first two: some 200 vector instructions per 32 tokens are what is between.  Two rows of 100 selected tokens take 5 us, an empty launch 3.
 #include "attn_decode_shared.h"
 #include "kv4_cache.h"
 
@@ -35,6 +39,7 @@ struct Kv4AttnArgs {
   int32_t direct;              // a unit is one item and writes its result
   int32_t B;
   int32_t balanced;            // range sources: items are shared out by the lengths on the device, else n_splits to a unit
+  int32_t even;                // balanced: items of a unit where the lengths are about equal (0: by target_items like others)
   uint32_t skip[kKv4MaxHeads / 4];   // local source: byte kvh = bits of the group's heads that the call does not serve
 };
 
@@ -285,12 +290,22 @@ __device__ __forceinline__ int whole_rounds(int blocks) { return (max(blocks, 1)
 // workgroup busy to the end.  Each wave makes the plan for itself, a lane per length: no LDS, no barrier.  The items of an index are
 // consecutive, time by time, and equal (or the last one would often be a small one).  want: an item's number, or (by_unit) the number
 // index * times + time; false: there is no such item.
+// even: where it is not 0 and the lengths are about equal (the longest at most 5/4 of their mean), an index is cut into that many
+// items instead.
 template <int ROUND, class BlocksOf>
-__device__ __forceinline__ bool kv4_share(BlocksOf blocks_of, int n, int times, int target, int want, bool by_unit, Kv4Share* s) {
+__device__ __forceinline__ bool kv4_share(BlocksOf blocks_of, int n, int times, int target, int even, int want, bool by_unit, Kv4Share* s) {
   const int lane = threadIdx.x & 63;
-  int total = 0;
-  for (int i0 = 0; i0 < n; i0 += 64) total += wave_sum(i0 + lane < n ? blocks_of(i0 + lane) : 0);
-  const int per = whole_rounds<ROUND>((int)(((int64_t)total * times + target - 1) / target));
+  int total = 0, longest = 0;
+  for (int i0 = 0; i0 < n; i0 += 64) {
+    const int blocks = i0 + lane < n ? blocks_of(i0 + lane) : 0;
+    total += wave_sum(blocks);
+    longest = max(longest, blocks);
+  }
+  int per = whole_rounds<ROUND>((int)(((int64_t)total * times + target - 1) / target));
+  if (even && __ballot((int64_t)longest * n * 4 > (int64_t)total * 5) == 0ull) {
+    for (int d = 32; d > 0; d >>= 1) longest = max(longest, __shfl_xor(longest, d));
+    per = whole_rounds<ROUND>((longest + even - 1) / even);
+  }
   int base = 0;
   for (int i0 = 0; i0 < n; i0 += 64) {
     const int blocks = i0 + lane < n ? blocks_of(i0 + lane) : 0;
@@ -339,8 +354,8 @@ constexpr int kKv4Items = 256;         // items: one to a compute unit
 template <bool LOCAL>
 __device__ __forceinline__ bool kv4_range_item(const Kv4AttnArgs& a, int want, bool by_unit, Kv4Share* s, Kv4Range* r) {
   if (a.balanced) {
-    const bool there = kv4_share<kKv4Round>([&](int b) { return kv4_range(a, b, LOCAL).blocks; }, a.B, a.d.n_kv_heads, a.d.target_items, want,
-                                            by_unit, s);
+    const bool there = kv4_share<kKv4Round>([&](int b) { return kv4_range(a, b, LOCAL).blocks; }, a.B, a.d.n_kv_heads, a.d.target_items,
+                                            a.even, want, by_unit, s);
     if (there) *r = kv4_range(a, s->index, LOCAL);
     return there;
   }
@@ -467,59 +482,66 @@ __global__ __launch_bounds__(kKv4Waves * 64, 2) void kv4_range_kernel(const Kv4A
       }
     }
   }
-  kv4_finish(a, st, sh_lines, item, b, h0, heads, a.direct != 0, skip);
+  kv4_finish(a, st, sh_lines, item, b, h0, heads, a.direct || it.count == 1, skip);
 }
 
-// Merges partials i0 .. i1 - 1 of head slot hh (of `heads` in each) into the output row of query head h: 256 threads, 8 slices of 32
-// lanes with four dims each.
-__device__ __forceinline__ void kv4_merge(const Kv4AttnArgs& a, int heads, int hh, int b, int h, int i0, int i1) {
-  __shared__ float sh_m[8], sh_l[8];
-  __shared__ float sh_o[8][kHeadDim];
-  const int tid = threadIdx.x, d4 = tid & 31, slice = tid >> 5;
+// Merges the partials i0 .. i1 - 1 of the head slots hh0 .. hh0 + nh - 1 (of `heads` in each) into the output rows of the query heads
+// from h on: 32 lanes of four dims each take a slice of a head's partials, THREADS / 32 / nh slices to a head.
+template <int THREADS>
+__device__ __forceinline__ void kv4_merge(const Kv4AttnArgs& a, int heads, int hh0, int nh, int b, int h, int i0, int i1, uint32_t skip) {
+  constexpr int kGroups = THREADS / 32;
+  __shared__ float sh_m[kGroups], sh_l[kGroups];
+  __shared__ float sh_o[kGroups][kHeadDim];
+  const int tid = threadIdx.x, d4 = tid & 31, group = tid >> 5, slices = kGroups / nh;
   const float ninf = -__builtin_huge_valf();
   float M = ninf, L = 0.f;
   float4 A = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int i = i0 + slice; i < i1; i += 8) {
-    const float* p = a.d.part + ((int64_t)i * heads + hh) * kPartStride;
-    const float m = p[0], l = p[1];
-    const float4 v = *reinterpret_cast<const float4*>(p + 4 + d4 * 4);
-    const float Mn = fmaxf(M, m);
-    const float c0 = M == ninf ? 1.f : fast_exp2(M - Mn), c1 = m == ninf ? 1.f : fast_exp2(m - Mn);   // (-inf: 0, or NaN, as it is)
-    L = L * c0 + l * c1;
-    A.x = A.x * c0 + v.x * c1; A.y = A.y * c0 + v.y * c1;
-    A.z = A.z * c0 + v.z * c1; A.w = A.w * c0 + v.w * c1;
-    M = Mn;
-  }
-  if (d4 == 0) { sh_m[slice] = M; sh_l[slice] = L; }
-  *reinterpret_cast<float4*>(&sh_o[slice][d4 * 4]) = A;
-  __syncthreads();
-  if (tid < kHeadDim) {
-    float Mt = sh_m[0];
-#pragma unroll
-    for (int s = 1; s < 8; ++s) Mt = fmaxf(Mt, sh_m[s]);
-    const float ref = Mt == ninf ? 0.f : Mt;
-    float Lt = 0.f, At = 0.f;
-#pragma unroll
-    for (int s = 0; s < 8; ++s) {
-      const float cs = sh_m[s] == ninf ? 1.f : fast_exp2(sh_m[s] - ref);
-      Lt += sh_l[s] * cs;
-      At += sh_o[s][tid] * cs;
+  if (group < nh * slices) {
+    const int hh = hh0 + group / slices;
+    if (!((skip >> hh) & 1u)) {
+      for (int i = i0 + group % slices; i < i1; i += slices) {
+        const float* p = a.d.part + ((int64_t)i * heads + hh) * kPartStride;
+        const float m = p[0], l = p[1];
+        const float4 v = *reinterpret_cast<const float4*>(p + 4 + d4 * 4);
+        const float Mn = fmaxf(M, m);
+        const float c0 = M == ninf ? 1.f : fast_exp2(M - Mn), c1 = m == ninf ? 1.f : fast_exp2(m - Mn);   // (-inf: 0, or NaN, as it is)
+        L = L * c0 + l * c1;
+        A.x = A.x * c0 + v.x * c1; A.y = A.y * c0 + v.y * c1;
+        A.z = A.z * c0 + v.z * c1; A.w = A.w * c0 + v.w * c1;
+        M = Mn;
+      }
     }
-    const int64_t o = (int64_t)b * a.d.n_q_heads + h;
-    a.d.out[o * kHeadDim + tid] = out16(Lt == 0.f ? 0.f : At / Lt, a.d.f16 != 0);
-    if (a.d.lse && tid == 0) a.d.lse[o] = Lt == 0.f ? ninf : (ref + log2f(Lt)) * 0.6931471805599453f;
   }
+  if (d4 == 0) { sh_m[group] = M; sh_l[group] = L; }
+  *reinterpret_cast<float4*>(&sh_o[group][d4 * 4]) = A;
+  __syncthreads();
+  const int e = tid >> 7, dim = tid & 127;       // (THREADS / 128 heads at least nh)
+  if (e >= nh || ((skip >> (hh0 + e)) & 1u)) return;
+  float Mt = ninf;
+  for (int s = 0; s < slices; ++s) Mt = fmaxf(Mt, sh_m[e * slices + s]);
+  const float ref = Mt == ninf ? 0.f : Mt;
+  float Lt = 0.f, At = 0.f;
+  for (int s = 0; s < slices; ++s) {
+    const int w = e * slices + s;
+    const float cs = sh_m[w] == ninf ? 1.f : fast_exp2(sh_m[w] - ref);
+    Lt += sh_l[w] * cs;
+    At += sh_o[w][dim] * cs;
+  }
+  const int64_t o = (int64_t)b * a.d.n_q_heads + h + e;
+  a.d.out[o * kHeadDim + dim] = out16(Lt == 0.f ? 0.f : At / Lt, a.d.f16 != 0);
+  if (a.d.lse && dim == 0) a.d.lse[o] = Lt == 0.f ? ninf : (ref + log2f(Lt)) * 0.6931471805599453f;
 }
 
-template <bool LOCAL>
-__global__ __launch_bounds__(kAdThreads) void kv4_range_merge_kernel(const Kv4AttnArgs a) {
-  const int heads = a.d.n_q_heads / a.d.n_kv_heads;
-  const int unit = blockIdx.x / heads, hh = blockIdx.x - unit * heads;
-  if (LOCAL && (kv4_skip(a, unit % a.d.n_kv_heads) >> hh) & 1u) return;
+// grid (units, heads), or (units, 1) where a workgroup takes all heads of a unit (WIDE)
+template <bool LOCAL, bool WIDE>
+__global__ __launch_bounds__(WIDE ? 1024 : 256) void kv4_range_merge_kernel(const Kv4AttnArgs a) {
+  const int heads = a.d.n_q_heads / a.d.n_kv_heads, unit = blockIdx.x, kvh = unit % a.d.n_kv_heads, hh = WIDE ? 0 : (int)blockIdx.y;
+  const uint32_t skip = LOCAL ? kv4_skip(a, kvh) : 0;
   Kv4Share it = {};
   Kv4Range r;
   kv4_range_item<LOCAL>(a, unit, true, &it, &r);
-  kv4_merge(a, heads, hh, unit / a.d.n_kv_heads, unit % a.d.n_kv_heads * heads + hh, it.first, it.first + it.count);
+  if (it.count == 1) return;                   // (its item wrote the result)
+  kv4_merge<WIDE ? 1024 : 256>(a, heads, hh, WIDE ? heads : 1, unit / a.d.n_kv_heads, kvh * heads + hh, it.first, it.first + it.count, skip);
 }
 
 // ---- selected tokens ------------------------------------------------------------------------------------------------------------
@@ -528,7 +550,8 @@ __device__ __forceinline__ int kv4_selected(const Kv4AttnArgs& a, int unit) { re
 constexpr int kSpWaves = 4;            // waves of a workgroup where rows are cut into items
 // An item (or row) of a call over selected tokens, in blocks of 64: a wave's share of a round.
 __device__ __forceinline__ bool kv4_sparse_item(const Kv4AttnArgs& a, int want, bool by_unit, Kv4Share* s) {
-  return kv4_share<kSpWaves>([&](int unit) { return (kv4_selected(a, unit) + 63) / 64; }, a.d.units, 1, a.d.target_items, want, by_unit, s);
+  return kv4_share<kSpWaves>([&](int unit) { return (kv4_selected(a, unit) + 63) / 64; }, a.d.units, 1, a.d.target_items, 0, want,
+                             by_unit, s);
 }
 
 // A wave takes 64 tokens at a time.  A lane looks one of them up -- its position a chunk ahead of the page, the page a chunk ahead of
@@ -633,14 +656,13 @@ __global__ __launch_bounds__(kAdThreads) void kv4_sparse_merge_kernel(const Kv4A
   const int unit = blockIdx.x, b = unit / a.d.n_ret;
   Kv4Share it = {};
   kv4_sparse_item(a, unit, true, &it);
-  kv4_merge(a, 1, 0, b, a.d.ret_heads[unit - b * a.d.n_ret], it.first, it.first + it.count);
+  kv4_merge<kAdThreads>(a, 1, 0, 1, b, a.d.ret_heads[unit - b * a.d.n_ret], it.first, it.first + it.count, 0);
 }
-
 
 // ---- host -----------------------------------------------------------------------------------------------------------------------
 struct Kv4RangePlan {
-  int32_t units, n_splits, target, grid;
-  bool balanced;
+  int32_t units, n_splits, target, even, grid;
+  bool balanced, direct;
   size_t ws_bytes;
 };
 static Kv4RangePlan plan_range(const rtp_layer_desc* L, bool local, int32_t B, int64_t max_ctx) {
@@ -655,19 +677,38 @@ static Kv4RangePlan plan_range(const rtp_layer_desc* L, bool local, int32_t B, i
   const int64_t most = (blocks + kKv4Round - 1) / kKv4Round;             // items of the longest unit
   int64_t n = kKv4Items / p.units;
   if (n > most) n = most;
-  if (n < 1 || blocks <= 48 + p.units) n = 1;
+  if (n < 1) n = 1;
+  const bool many = p.units > kKv4Items / 2;
+  if (blocks <= 48 + p.units) n = 1;
   p.n_splits = (int32_t)n;
   p.grid = p.units * p.n_splits;
-  // Lengths can differ, and a unit is more than one item: shared out by the lengths.  (Beyond 256 sequences the plan, a pass over the
-  // lengths in every wave, costs more than it saves: there are at least 256 units then, of four items at most.)
-  p.balanced = n > 1 && B > 1 && B <= 256;
+  // Lengths can differ: shared out by the lengths, unless a unit in one piece is short.  (Beyond 256 sequences the plan, a pass over the
+  // lengths in every wave, costs more than it saves.  A window's units are as good as equal.)  8 KV heads, contexts up to 32768, us, every
+  // unit in one piece / shared out:   all that long   one that long, the others a sixteenth   any length
+  //   17 sequences                    157 / 116       147 / 26                                 139 /  61
+  //   32                              177 / 178       143 / 33                                 140 /  91
+  //   64                              364 / 362       152 / 47                                 249 / 192
+  //   128                             710 / 720       160 / 69                                 412 / 374
+  p.balanced = blocks > 48 + p.units && most > 1 && B > 1 && B <= 256 && !(many && local);
   if (p.balanced) {
     p.target = kKv4Items - p.units / 2;                                  // (a unit's number of items is rounded up, by a half on average)
+    if (many) {
+      p.target = p.units + 128 < 384 ? 384 : p.units + 128;
+      // equal lengths: the fewest items to a unit that come close to whole rounds of workgroups
+      float best = 0.f;
+      for (int e = 1; e <= 4; ++e) {
+        const int items = p.units * e, rounds = (items + kKv4Items - 1) / kKv4Items;
+        const float full = (float)items / ((float)rounds * kKv4Items);
+        if (full * 0.9f > best) { best = full; p.even = e; }
+      }
+    }
     int64_t grid = (int64_t)p.target + p.units;                          // items <= total / ceil(total / target) + units
+    if (grid < (int64_t)p.units * p.even) grid = (int64_t)p.units * p.even;
     if (grid > p.units * most) grid = p.units * most;
     p.grid = (int32_t)grid;
   }
-  p.ws_bytes = n == 1 ? 0 : align_up((size_t)p.grid * G * kPartStride * sizeof(float), 256);
+  p.direct = n == 1 && !p.balanced;
+  p.ws_bytes = p.direct ? 0 : align_up((size_t)p.grid * G * kPartStride * sizeof(float), 256);
   return p;
 }
 
@@ -692,6 +733,7 @@ static void fill_attn(Kv4AttnArgs& a, const rtp_layer_desc* L, const HeadTable& 
   for (uint32_t& w : a.skip) w = 0;
   a.B = 0;
   a.balanced = 0;
+  a.even = 0;
   a.d.q = (const uint16_t*)q;
   a.d.n_q_heads = L->n_q_heads;
   a.d.n_kv_heads = L->n_kv_heads;
@@ -732,9 +774,10 @@ static int32_t range_attn_kv4(const char* who, const rtp_layer_desc* layer, cons
   a.d.n_splits = p.n_splits;
   a.d.target_items = p.target;
   a.max_len = (int32_t)max_ctx;
-  a.direct = p.n_splits == 1;
+  a.direct = p.direct;
   a.B = B;
   a.balanced = p.balanced;
+  a.even = p.even;
   if (LOCAL) {
     const int G = layer->n_q_heads / layer->n_kv_heads;
     for (int j = 0; j < layer->n_ret; ++j) a.skip[ht.ret_heads[j] / G / 4] |= 1u << (8 * (ht.ret_heads[j] / G % 4) + ht.ret_heads[j] % G);
@@ -742,7 +785,12 @@ static int32_t range_attn_kv4(const char* who, const rtp_layer_desc* layer, cons
   const dim3 grid((unsigned)p.grid);
   if (a.d.f16) RTP_LAUNCH((kv4_range_kernel<LOCAL, true>), grid, dim3(kKv4Waves * 64), 0, s, a);
   else RTP_LAUNCH((kv4_range_kernel<LOCAL, false>), grid, dim3(kKv4Waves * 64), 0, s, a);
-  if (!a.direct) RTP_LAUNCH(kv4_range_merge_kernel<LOCAL>, dim3((unsigned)B * layer->n_q_heads), dim3(kAdThreads), 0, s, a);
+  if (!a.direct) {
+    // a workgroup per head, or, with units for every compute unit, one for all heads of a unit (each makes the plan)
+    const unsigned units = (unsigned)p.units, heads = (unsigned)(layer->n_q_heads / layer->n_kv_heads);
+    if (p.units > kKv4Items / 2) RTP_LAUNCH((kv4_range_merge_kernel<LOCAL, true>), dim3(units), dim3(1024), 0, s, a);
+    else RTP_LAUNCH((kv4_range_merge_kernel<LOCAL, false>), dim3(units, heads), dim3(256), 0, s, a);
+  }
   return check_launch(who);
 }
 

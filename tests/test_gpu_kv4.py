@@ -207,6 +207,30 @@ def test_long_contexts_and_wide_logits(what, n, B, size):
                 check_row(out[b, h], lse[b, h], qd[b, h], k, v, "bf16", what=f"sequence {b}, head {h}")
 
 
+@pytest.mark.parametrize("B,hkv,group,lens", [
+    (34, 4, 8, "equal"), (34, 4, 4, "one long"), (20, 8, 8, "any"), (40, 8, 1, "near"), (40, 8, 2, "any"), (256, 1, 2, "equal"),
+    (256, 1, 8, "one long"), (256, 1, 4, "empty"), (130, 8, 2, "one long"), (2, 8, 4, "one long")])
+def test_many_units_are_shared_out(B, hkv, group, lens):
+    """More (sequence, KV head) pairs than half of the compute units, with contexts that may be long: equal lengths, about equal ones,
+    one long context among short ones, any, none at all."""
+    print(f"[case] kv4 dense, {B} sequences, {hkv} KV heads of {group}, {lens}", flush=True)
+    rng = np.random.default_rng(B + group)
+    max_ctx = 16 * (B * hkv + 48) + 600
+    ctx = {"equal": [700] * B, "near": [int(x) for x in rng.integers(610, 700, B)], "any": [int(x) for x in rng.integers(0, 900, B)],
+           "one long": [max_ctx - 3 if b == B // 2 else int(x) for b, x in enumerate(rng.integers(1, 200, B))], "empty": [0] * B}[lens]
+    c = Cache(rng, hkv, ctx, 64)
+    c.table = np.pad(c.table, ((0, 0), (0, max(0, -(-max_ctx // 64) - c.table.shape[1]))), constant_values=-1)
+    c.upload()
+    q, qd = queries(rng, B, hkv * group, "bf16")
+    out, lse = _dense(_layer(hkv * group, hkv, []), q, c, ctx, max_ctx=max_ctx)
+    for b in sorted({0, 1, B // 2, B - 1} | {int(x) for x in rng.integers(0, B, 6)}):
+        for kvh in range(hkv):
+            k, v = c.rows(b, kvh, np.arange(ctx[b]))
+            for h in range(kvh * group, kvh * group + group):
+                check_row(out[b, h], lse[b, h], qd[b, h], k, v, "bf16", what=f"sequence {b}, head {h}")
+    assert np.isfinite(out).all() and (lens == "empty" or np.isfinite(lse[np.array(ctx) > 0]).all())
+
+
 def _sparse(layer, q, c, sel, max_sel=None, n_ret=1):
     B, Hq = q.shape[:2]
     counts = [len(s) for s in sel]
