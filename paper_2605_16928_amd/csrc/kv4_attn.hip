@@ -679,28 +679,32 @@ static Kv4RangePlan plan_range(const rtp_layer_desc* L, bool local, int32_t B, i
   if (n > most) n = most;
   if (n < 1) n = 1;
   const bool many = p.units > kKv4Items / 2;
+  // share of the compute units that whole rounds of workgroups keep busy, e equal items to a unit
+  auto busy = [&](int e) {
+    const int items = p.units * e, rounds = (items + kKv4Items - 1) / kKv4Items;
+    return (float)items / ((float)rounds * kKv4Items);
+  };
   if (blocks <= 48 + p.units) n = 1;
   p.n_splits = (int32_t)n;
   p.grid = p.units * p.n_splits;
   // Lengths can differ: shared out by the lengths, unless a unit in one piece is short.  (Beyond 256 sequences the plan, a pass over the
-  // lengths in every wave, costs more than it saves.  A window's units are as good as equal.)  8 KV heads, contexts up to 32768, us, every
-  // unit in one piece / shared out:   all that long   one that long, the others a sixteenth   any length
-  //   17 sequences                    157 / 116       147 / 26                                 139 /  61
-  //   32                              177 / 178       143 / 33                                 140 /  91
-  //   64                              364 / 362       152 / 47                                 249 / 192
-  //   128                             710 / 720       160 / 69                                 412 / 374
-  p.balanced = blocks > 48 + p.units && most > 1 && B > 1 && B <= 256 && !(many && local);
+  // lengths in every wave, costs more than it saves.)  8 KV heads, contexts up to 32768, us, every unit in one piece / shared out:
+  //                     all that long   one that long, the others a sixteenth   any length
+  //   17 sequences      157 / 116       147 / 26                                 139 /  61
+  //   32                177 / 178       143 / 33                                 140 /  91
+  //   64                364 / 362       152 / 47                                 249 / 192
+  //   128               710 / 720       160 / 69                                 412 / 374
+  // Windows are mostly full, i.e. equal: where units in one piece fill their rounds, they stay whole up to 12288 tokens (8192 of 32
+  // sequences 46 / 51, 40 / 32 with any length up to it; 17 sequences 44 / 38, 40 / 26; 16384 of 32 sequences 90 / 95, 73 / 53).
+  const bool whole = blocks <= 48 + p.units || (local && many && blocks <= 768 && busy(1) >= 0.9f);
+  p.balanced = !whole && most > 1 && B > 1 && B <= 256;
   if (p.balanced) {
     p.target = kKv4Items - p.units / 2;                                  // (a unit's number of items is rounded up, by a half on average)
     if (many) {
       p.target = p.units + 128 < 384 ? 384 : p.units + 128;
-      // equal lengths: the fewest items to a unit that come close to whole rounds of workgroups
-      float best = 0.f;
-      for (int e = 1; e <= 4; ++e) {
-        const int items = p.units * e, rounds = (items + kKv4Items - 1) / kKv4Items;
-        const float full = (float)items / ((float)rounds * kKv4Items);
-        if (full * 0.9f > best) { best = full; p.even = e; }
-      }
+      float best = 0.f;                                                  // equal lengths: the fewest items that come close to the best
+      for (int e = 1; e <= 4; ++e)
+        if (busy(e) * 0.9f > best) { best = busy(e); p.even = e; }
     }
     int64_t grid = (int64_t)p.target + p.units;                          // items <= total / ceil(total / target) + units
     if (grid < (int64_t)p.units * p.even) grid = (int64_t)p.units * p.even;

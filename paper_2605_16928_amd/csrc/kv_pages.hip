@@ -114,12 +114,13 @@ __device__ __forceinline__ void pg_masks(const PageMap& m, int chunk, int (&v)[k
 }
 
 // Pages that request i takes: one to copy its shared last page to, then what the new length adds.  lacks: entries that the table row has
-// no room for.
+// no room for.  first: 2 * the first entry of the table that takes one, + 1 if that is the shared page's.
 struct Request {
   int pages, lacks;
+  int64_t first;
 };
 __device__ __forceinline__ Request pg_request(const ExtendArgs& a, int i) {
-  Request r = {0, 0};
+  Request r = {0, 0, 0};
   const int seq = a.seq[i];
   if (seq < 0 || seq >= a.m.n_seqs) return r;
   const int sh = a.m.page_shift;
@@ -128,16 +129,21 @@ __device__ __forceinline__ Request pg_request(const ExtendArgs& a, int i) {
   const int64_t k0 = (from + size - 1) >> sh, k1 = (to + size - 1) >> sh;
   r.lacks = (int)max((int64_t)0, k1 - max(k0, a.m.pt_stride));
   r.pages = (int)max((int64_t)0, min(k1, a.m.pt_stride) - k0);
+  r.first = 2 * (seq * a.m.pt_stride + k0);
   if ((from & (size - 1)) && k0 <= a.m.pt_stride) {
     const int page = a.m.table[seq * a.m.pt_stride + k0 - 1];
-    if (in_pool(a.m, page) && a.m.refs[page] > 1) r.pages += 1;
+    if (in_pool(a.m, page) && a.m.refs[page] > 1) {
+      r.pages += 1;
+      r.first -= 1;
+    }
   }
   return r;
 }
 
 // Prefix sums of the requests' pages into need[0 .. n] (cut at 2^30, more than any pool has: with a total beyond the pool nobody reads
-// them); returns the entries that do not fit their rows, cut likewise.  r: request threadIdx.x (nothing, if there is none).
-__device__ __forceinline__ int pg_needs(const ExtendArgs& a, Request r, int32_t* need, uint64_t* sh) {
+// them), and into first[0 .. n - 1] (if there is one) the requests' own; returns the entries that do not fit their rows, cut likewise.
+// r: request threadIdx.x (nothing, if there is none).
+__device__ __forceinline__ int pg_needs(const ExtendArgs& a, Request r, int32_t* need, int64_t* first, uint64_t* sh) {
   constexpr uint64_t kMost = 1ull << 30;
   uint64_t base = 0, lacking = 0;
   for (int i = threadIdx.x;; ) {
@@ -147,11 +153,14 @@ __device__ __forceinline__ int pg_needs(const ExtendArgs& a, Request r, int32_t*
       pg_scan<uint64_t>((uint64_t)r.lacks, sh, &lacks);
       lacking += lacks;
     }
-    if (i < a.n) need[i] = (int32_t)min(base + off, kMost);
+    if (i < a.n) {
+      need[i] = (int32_t)min(base + off, kMost);
+      if (first) first[i] = r.first;
+    }
     base += total;
     i += kPgThreads;
     if (i - (int)threadIdx.x >= a.n) break;
-    r = i < a.n ? pg_request(a, i) : Request{0, 0};
+    r = i < a.n ? pg_request(a, i) : Request{0, 0, 0};
   }
   if (threadIdx.x == 0) need[a.n] = (int32_t)min(base, kMost);
   return (int)min(lacking, kMost);
@@ -170,7 +179,7 @@ __global__ __launch_bounds__(kPgThreads) void kv_pages_scan_kernel(const ExtendA
   a.w.before[word] = c.before[threadIdx.x];
   if (threadIdx.x == 0) a.w.count[blockIdx.x] = total;
   if (REQUESTS && blockIdx.x == 0) {
-    const int lacking = pg_needs(a, (int)threadIdx.x < a.n ? pg_request(a, threadIdx.x) : Request{0, 0}, a.w.need, sh);
+    const int lacking = pg_needs(a, (int)threadIdx.x < a.n ? pg_request(a, threadIdx.x) : Request{0, 0, 0}, a.w.need, nullptr, sh);
     if (threadIdx.x == 0) a.w.need[a.n + 1] = lacking;
   }
 }
@@ -211,16 +220,24 @@ __global__ __launch_bounds__(kPgThreads) void kv_pages_extend_kernel(const Exten
   __shared__ ChunkMasks c;
   __shared__ uint64_t sh[kPgWaves];
   __shared__ int32_t sh_need[kPgMaxSeqs + 1];
+  __shared__ int64_t sh_first[kPgMaxSeqs];     // (Request::first)
   int first = 0, total, lacking;
   if (ONE) {
     int v[kPgAhead];
     pg_counts<true>(a.m, 0, 0, v);              // (asked for before the request, a chain of loads of its own)
-    const Request r = (int)threadIdx.x < a.n ? pg_request(a, threadIdx.x) : Request{0, 0};
+    const Request r = (int)threadIdx.x < a.n ? pg_request(a, threadIdx.x) : Request{0, 0, 0};
     pg_masks<true>(a.m, 0, v, c, sh, &total);
-    lacking = pg_needs(a, r, sh_need, sh);
+    lacking = pg_needs(a, r, sh_need, sh_first, sh);
   } else {
     pg_load_chunk(a, c, sh, &first, &total);
-    for (int i = threadIdx.x; i <= a.n; i += kPgThreads) sh_need[i] = a.w.need[i];
+    for (int i = threadIdx.x; i <= a.n; i += kPgThreads) {
+      sh_need[i] = a.w.need[i];
+      if (i == a.n) break;
+      int64_t k0 = 0;                           // (what a request takes beyond its growth is its shared page)
+      const int pages = a.w.need[i + 1] - sh_need[i];
+      const int copies = pages ? pages - pg_grown(a, i, &k0) : 0;
+      sh_first[i] = pages ? 2 * (a.seq[i] * a.m.pt_stride + k0) - copies : 0;
+    }
     lacking = a.w.need[a.n + 1];
   }
   __syncthreads();
@@ -232,9 +249,7 @@ __global__ __launch_bounds__(kPgThreads) void kv_pages_extend_kernel(const Exten
       a.status[1] = total - (short_of ? 0 : need);
     }
     for (int i = threadIdx.x; i < a.n; i += kPgThreads) {      // pairs of requests that copy nothing; the others are written with their page
-      const int pages = sh_need[i + 1] - sh_need[i];
-      int64_t k0;
-      if (short_of || pages == 0 || pages <= pg_grown(a, i, &k0)) a.copy_src[i] = a.copy_dst[i] = -1;
+      if (short_of || sh_need[i + 1] == sh_need[i] || !(sh_first[i] & 1)) a.copy_src[i] = a.copy_dst[i] = -1;
     }
   }
   if (short_of) return;
@@ -251,11 +266,10 @@ __global__ __launch_bounds__(kPgThreads) void kv_pages_extend_kernel(const Exten
       const int mid = (lo + hi + 1) >> 1;
       if (sh_need[mid] <= r) lo = mid; else hi = mid - 1;
     }
-    int64_t k0;
-    const int grown = pg_grown(a, lo, &k0), j = r - sh_need[lo];
-    const int copies = sh_need[lo + 1] - sh_need[lo] - grown;   // 0 or 1
-    int32_t* entry = a.m.table + a.seq[lo] * a.m.pt_stride + k0 - copies + j;
-    if (copies && j == 0) {
+    const int64_t f = sh_first[lo];
+    const int j = r - sh_need[lo];
+    int32_t* entry = a.m.table + (f >> 1) + j;
+    if ((f & 1) && j == 0) {
       const int src = *entry;
       a.copy_src[lo] = src;
       a.copy_dst[lo] = page;

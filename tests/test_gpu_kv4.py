@@ -231,6 +231,29 @@ def test_many_units_are_shared_out(B, hkv, group, lens):
     assert np.isfinite(out).all() and (lens == "empty" or np.isfinite(lse[np.array(ctx) > 0]).all())
 
 
+@pytest.mark.parametrize("B,hkv,ret,lens", [(20, 8, [0, 3, 4, 5], "any"), (40, 8, [1, 2, 3], "equal"), (256, 1, [], "one long")])
+def test_many_windows_are_shared_out(B, hkv, ret, lens):
+    """The same for sinks and windows, where heads and whole KV heads are not the call's."""
+    print(f"[case] kv4 local, {B} sequences, {hkv} KV heads, {lens}", flush=True)
+    rng = np.random.default_rng(B)
+    hq, sink, window = 2 * hkv, 20, 16 * (B * hkv + 48) + 100 if hkv > 1 else 13000
+    ctx = {"equal": [900] * B, "any": [int(x) for x in rng.integers(0, 900, B)],
+           "one long": [window + 700 if b == 5 else int(x) for b, x in enumerate(rng.integers(1, 200, B))]}[lens]
+    max_ctx = window + 1000
+    c = Cache(rng, hkv, ctx, 64)
+    c.table = np.pad(c.table, ((0, 0), (0, max(0, -(-max_ctx // 64) - c.table.shape[1]))), constant_values=-1)
+    c.upload()
+    q, qd = queries(rng, B, hq, "bf16")
+    out, lse = _dense(_layer(hq, hkv, ret, sink=sink, window=window), q, c, ctx, max_ctx=max_ctx, what="local")
+    for b in sorted({0, 5, B - 1} | {int(x) for x in rng.integers(0, B, 6)}):
+        for h in range(hq):
+            if h in ret:
+                assert (out[b, h] == 3.0).all() and lse[b, h] == 3.0
+                continue
+            k, v = c.rows(b, h // 2, k4.local_positions(ctx[b], sink, window))
+            check_row(out[b, h], lse[b, h], qd[b, h], k, v, "bf16", what=f"sequence {b}, head {h}")
+
+
 def _sparse(layer, q, c, sel, max_sel=None, n_ret=1):
     B, Hq = q.shape[:2]
     counts = [len(s) for s in sel]
