@@ -70,6 +70,10 @@ class rtp_kv4_cache(C.Structure):
     ]
 
 
+def _int32(t) -> bool:
+    return str(t.dtype) == "torch.int32" and t.is_contiguous()
+
+
 def kv4_cache(codes, scales, page_table) -> rtp_kv4_cache:
     """Descriptor of a 4-bit cache in torch tensors: codes uint8 [n_kv_heads, n_pages, page_size, 128], scales uint8 with
     n_kv_heads and n_pages in front and page_size * 8 bytes behind them, page_table int32 [B, pages].  The first two dims of codes
@@ -77,10 +81,10 @@ def kv4_cache(codes, scales, page_table) -> rtp_kv4_cache:
     ok = codes.dim() == 4 and codes.shape[3] == 128 and min(codes.shape) > 0 and codes.element_size() == 1 \
         and scales.dim() >= 3 and scales.shape[:2] == codes.shape[:2] and scales.element_size() == 1 \
         and scales[0, 0].numel() == 8 * codes.shape[2] and codes[0, 0].is_contiguous() and scales[0, 0].is_contiguous() \
-        and page_table.dim() == 2 and page_table.element_size() == 4 and page_table.is_contiguous()
+        and page_table.dim() == 2 and _int32(page_table) and codes.device == scales.device == page_table.device
     if not ok:
         raise RtpError(RTP_ERR_INVALID_ARG, "kv4_cache: bytes in codes [heads, pages, page_size, 128] and scales [heads, pages, "
-                                            "8 * page_size], a page's own contiguous, and a contiguous int32 page_table [B, pages]")
+                                            "8 * page_size], a page's own contiguous, and a contiguous int32 page_table [B, pages], on one device")
     c = rtp_kv4_cache(codes.data_ptr(), codes.stride(1), codes.stride(0), scales.data_ptr(), scales.stride(1), scales.stride(0),
                       page_table.data_ptr(), page_table.shape[1], codes.shape[2], codes.shape[1])
     c._keepalive = (codes, scales, page_table)
@@ -99,9 +103,10 @@ class rtp_page_pool(C.Structure):
 
 def page_map(page_table, page_refs, page_size: int) -> rtp_page_map:
     """Descriptor of a page table int32 [n_seqs, pages] and reference counts int32 [n_pages], both contiguous."""
-    if page_table.dim() != 2 or page_refs.dim() != 1 or page_table.element_size() != 4 or page_refs.element_size() != 4 \
-            or not page_table.is_contiguous() or not page_refs.is_contiguous():
-        raise RtpError(RTP_ERR_INVALID_ARG, "page_map: contiguous int32 page_table [n_seqs, pages] and page_refs [n_pages] expected")
+    if page_table.dim() != 2 or page_refs.dim() != 1 or not _int32(page_table) or not _int32(page_refs) \
+            or page_table.device != page_refs.device:
+        raise RtpError(RTP_ERR_INVALID_ARG, "page_map: contiguous int32 page_table [n_seqs, pages] and page_refs [n_pages] on one "
+                                            "device expected")
     m = rtp_page_map(page_table.data_ptr(), page_table.shape[1], page_refs.data_ptr(), page_table.shape[0], page_refs.shape[0], page_size)
     m._keepalive = (page_table, page_refs)
     return m
@@ -112,11 +117,12 @@ def page_pools(pools: Sequence):
     strides (the K and V pools of the paged calls as [n_kv_heads, n_pages, page_size * 128], a 4-bit cache's codes and scales)."""
     arr = (rtp_page_pool * max(len(pools), 1))()
     for i, t in enumerate(pools):
-        if t.dim() < 3 or min(t.shape) == 0 or not t[0, 0].is_contiguous():
-            raise RtpError(RTP_ERR_INVALID_ARG, "page_pools: tensors [heads, n_pages, ...] with contiguous pages expected")
+        if t.dim() < 3 or min(t.shape) == 0 or not t[0, 0].is_contiguous() or t.device != pools[0].device:
+            raise RtpError(RTP_ERR_INVALID_ARG, "page_pools: tensors [heads, n_pages, ...] with contiguous pages on one device expected")
         e = t.element_size()
         arr[i] = rtp_page_pool(t.data_ptr(), t.stride(1) * e, t.stride(0) * e, t[0, 0].numel() * e, t.shape[0])
     arr._keepalive = list(pools)
+    arr.n_pages = min((t.shape[1] for t in pools), default=0)
     arr.n_pools = len(pools)
     return arr
 
@@ -563,5 +569,7 @@ def rtp_kv_pages_compact(map, move_src, move_dst, status, ws, stream=None):
 
 
 def rtp_kv_pages_copy(pools, n_pages, src, dst, n, count=None, stream=None):
-    """pools: what page_pools returned."""
+    """pools: what page_pools returned; n_pages: at most what its tensors have."""
+    if n_pages > pools.n_pages:
+        raise RtpError(RTP_ERR_INVALID_ARG, f"rtp_kv_pages_copy: n_pages = {n_pages}, the pools have {pools.n_pages}")
     _check(lib().rtp_kv_pages_copy(pools, pools.n_pools, n_pages, _ptr(src), _ptr(dst), n, _ptr(count), _stream(stream)))

@@ -276,3 +276,20 @@ def test_read_refuses_rows_that_overlap(strides):
     call, args = _calls()["read"]                       # 3 sequences of 10 tokens and 2 heads
     args.update(zip(("batch_stride", "token_stride", "head_stride"), strides))
     _refused(rtp.RTP_ERR_INVALID_ARG, call, **args)
+
+
+def test_descriptors_refuse_other_types_devices_and_pools_that_are_too_small():
+    import torch
+    codes, scales = torch.zeros((2, 10, 16, 128), dtype=torch.uint8), torch.zeros((2, 10, 128), dtype=torch.uint8)
+    table, refs = torch.zeros((3, 5), dtype=torch.int32), torch.zeros(10, dtype=torch.int32)
+    elsewhere = torch.zeros((3, 5), dtype=torch.int32, device="meta")
+    for make in (lambda: rtp.kv4_cache(codes, scales, table.float()), lambda: rtp.kv4_cache(codes, scales, elsewhere),
+                 lambda: rtp.kv4_cache(codes, scales.to("meta"), table), lambda: rtp.page_map(table.float(), refs, 16),
+                 lambda: rtp.page_map(table, refs.float(), 16), lambda: rtp.page_map(elsewhere, refs, 16),
+                 lambda: rtp.page_pools([codes, scales.to("meta")])):
+        with pytest.raises(rtp.RtpError):
+            make()
+    pools = rtp.page_pools([codes, scales[:, :8]])
+    assert pools.n_pages == 8
+    with pytest.raises(rtp.RtpError, match="n_pages"):
+        rtp.rtp_kv_pages_copy(pools, 9, A, A, 4)
