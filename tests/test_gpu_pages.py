@@ -215,3 +215,45 @@ def test_copy_moves_the_named_pages_only():
     rtp.rtp_kv_pages_copy(desc, n_pages, i32([12]), i32([13]), 1, i32([50]))           # (a count beyond n is cut)
     torch.cuda.synchronize()
     assert all(torch.equal(p[:, 13], w[:, 12]) for p, w in zip(pools, want))
+
+
+@pytest.mark.parametrize("n_pages", [20000, 70001])
+def test_thousands_of_requests(n_pages):
+    """More requests than threads of a workgroup, in a pool of one and of two: forks that take their own last page among sequences that
+    grow by several pages, by none, or are no sequences."""
+    print(f"[case] pages, 4000 requests, pool of {n_pages}", flush=True)
+    rng = np.random.default_rng(n_pages)
+    both = Both(4000, 6, n_pages, 16)
+    both.put(refs=(np.arange(n_pages) % 5 == 1).astype(np.int32))        # (others' pages, so that the fresh ones have gaps)
+    first = [int(x) for x in rng.integers(1, 33, 1500)]
+    both.extend(list(range(1500)), [0] * 1500, first)
+    kids = list(range(1500, 3500))
+    parents = [int(x) for x in rng.integers(0, 1500, len(kids))]
+    both.fork(parents, kids, [first[p] for p in parents])
+    old = first + [first[p] for p in parents] + [0] * 500
+    seq = rng.permutation(4000).tolist()
+    new = [old[b] + int(rng.integers(0, 45)) if b % 7 else old[b] for b in seq]
+    src, _, status = both.extend([b if i % 11 else -b - 1 for i, b in enumerate(seq)], [old[b] for b in seq], new)
+    assert status[0] == 0 and (src >= 0).sum() > 1024
+    both.compact()
+
+
+def test_copies_that_stream():
+    """More than 64 MB in one call, pieces that are not whole, two page sizes, and a list that the device's count cuts short."""
+    print("[case] page copies, large", flush=True)
+    n_pages, n = 900, 400
+    pools = [torch.randint(0, 256, (5, n_pages, 4096 * 9 + 16 * 37), dtype=torch.uint8, device=DEV),
+             torch.randint(0, 256, (n_pages, 3, 2048), dtype=torch.uint8, device=DEV).transpose(0, 1)]
+    g = torch.Generator().manual_seed(3)
+    ids = torch.randperm(n_pages, generator=g)
+    src, dst = ids[:n].to(DEV, torch.int32), ids[n:2 * n].to(DEV, torch.int32)
+    desc = rtp.page_pools(pools)
+    for count in (n - 1, 3):
+        want = [p.clone() for p in pools]
+        for w, p in zip(want, pools):
+            w[:, dst[:count].long()] = p[:, src[:count].long()]
+        rtp.rtp_kv_pages_copy(desc, n_pages, src, dst, n, i32([count]))
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, w) for p, w in zip(pools, want)), count
+        for p in pools:
+            p.copy_(p.flip(0))                         # (other bytes for the next list)
