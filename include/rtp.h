@@ -582,7 +582,7 @@ int32_t rtp_kv4_read(const rtp_layer_desc* layer, const rtp_kv4_cache* cache, co
  * stand for, exactly; products and sums are fp32, and probabilities enter the product with V with 16 bits of mantissa.  A row whose
  * set is empty writes zeros and lse = -inf; a token whose K block is NaN makes its row NaN.
  * rtp_local_attn_kv4 and rtp_dense_attn_kv4 serve any batch with B * n_kv_heads <= 2^20, rtp_sparse_attn_decode_kv4 up to 1024 rows
- * (B * n_ret <= 1024): RTP_ERR_UNSUPPORTED beyond that. */
+ * (B * n_ret <= 1024): RTP_ERR_UNSUPPORTED beyond that.  A workspace for B and max_ctx / max_sel serves every smaller call too. */
 size_t rtp_sparse_attn_decode_kv4_workspace_bytes(const rtp_layer_desc* layer, int32_t B, int64_t max_sel);
 int32_t rtp_sparse_attn_decode_kv4(const rtp_layer_desc* layer, const void* q, const rtp_kv4_cache* cache,
                                    const int32_t* sel_idx, int64_t sel_stride, const int32_t* sel_count, int64_t max_sel,

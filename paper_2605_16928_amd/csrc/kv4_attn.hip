@@ -720,8 +720,13 @@ static size_t range_ws(const rtp_layer_desc* L, bool local, int32_t B, int64_t m
   if (!L || B <= 0 || max_ctx <= 0 || max_ctx > kMaxLen || L->n_kv_heads <= 0 || L->n_q_heads < L->n_kv_heads ||
       (int64_t)B * L->n_kv_heads > kMaxUnits)
     return 256;
-  const size_t w = plan_range(L, local, B, max_ctx).ws_bytes;
-  return w ? w : 256;
+  // (what any smaller batch or context takes is enough too: fewer units may be cut into more items)
+  size_t w = 256;
+  for (int b = B < 256 ? B : 256; b > 0; --b) {
+    const size_t one = plan_range(L, local, b, max_ctx).ws_bytes;
+    if (one > w) w = one;
+  }
+  return w;
 }
 
 static int32_t check_io(const char* who, const void* q, const void* out, const void* ws, size_t ws_bytes, size_t need) {

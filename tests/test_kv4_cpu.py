@@ -293,3 +293,16 @@ def test_descriptors_refuse_other_types_devices_and_pools_that_are_too_small():
     assert pools.n_pages == 8
     with pytest.raises(rtp.RtpError, match="n_pages"):
         rtp.rtp_kv_pages_copy(pools, 9, A, A, 4)
+
+
+def test_workspaces_serve_smaller_calls():
+    """What the size functions answer does not fall when the batch, the context or the selection grows."""
+    for hq, hkv in ((8, 1), (8, 2), (32, 8), (64, 8), (16, 16)):
+        layer = rtp.layer_desc(hq, hkv, [0, 1], 4, 8192)
+        grid = [1, 2, 3, 5, 8, 15, 16, 17, 20, 25, 31, 32, 33, 40, 64, 65, 100, 128, 200, 255, 256, 257, 500, 512]
+        lens = [1, 100, 1024, 1025, 1100, 3000, 5000, 9000, 12000, 13000, 20000, 40000, 131072, 1 << 20, 1 << 26]
+        for size in (rtp.rtp_dense_attn_kv4_workspace_bytes, rtp.rtp_local_attn_kv4_workspace_bytes,
+                     rtp.rtp_sparse_attn_decode_kv4_workspace_bytes):
+            got = np.array([[size(layer, b, n) for n in lens] for b in grid])
+            assert (got % 256 == 0).all() and got.min() >= 256
+            assert (np.diff(got, axis=0) >= 0).all() and (np.diff(got, axis=1) >= 0).all(), (hq, hkv, size.__name__)
