@@ -68,6 +68,14 @@ class rtp_kv4_cache(C.Structure):
         ("scales", C.c_void_p), ("scale_page_stride", C.c_int64), ("scale_head_stride", C.c_int64),
         ("page_table", C.c_void_p), ("pt_stride", C.c_int64), ("page_size", C.c_int32), ("n_pages", C.c_int32),
     ]
+    n_heads = n_seqs = 1 << 31                      # KV heads of the pools, rows of the table: known where kv4_cache made it
+
+
+def _held(who: str, layer, cache, B: int):
+    """The C struct has no head and no row count; what a cache of tensors holds is checked here."""
+    if layer.n_kv_heads > cache.n_heads or B > cache.n_seqs:
+        raise RtpError(RTP_ERR_INVALID_ARG, f"{who}: a cache of {cache.n_heads} KV heads and {cache.n_seqs} sequences, a call over "
+                                            f"{layer.n_kv_heads} and {B}")
 
 
 def _int32(t) -> bool:
@@ -77,7 +85,8 @@ def _int32(t) -> bool:
 def kv4_cache(codes, scales, page_table) -> rtp_kv4_cache:
     """Descriptor of a 4-bit cache in torch tensors: codes uint8 [n_kv_heads, n_pages, page_size, 128], scales uint8 with
     n_kv_heads and n_pages in front and page_size * 8 bytes behind them, page_table int32 [B, pages].  The first two dims of codes
-    and scales may have any strides (a page-major pool as a transposed view)."""
+    and scales may have any strides (a page-major pool as a transposed view).  Calls over more KV heads or sequences than these
+    tensors hold are refused."""
     ok = codes.dim() == 4 and codes.shape[3] == 128 and min(codes.shape) > 0 and codes.element_size() == 1 \
         and scales.dim() >= 3 and scales.shape[:2] == codes.shape[:2] and scales.element_size() == 1 \
         and scales[0, 0].numel() == 8 * codes.shape[2] and codes[0, 0].is_contiguous() and scales[0, 0].is_contiguous() \
@@ -87,6 +96,7 @@ def kv4_cache(codes, scales, page_table) -> rtp_kv4_cache:
                                             "8 * page_size], a page's own contiguous, and a contiguous int32 page_table [B, pages], on one device")
     c = rtp_kv4_cache(codes.data_ptr(), codes.stride(1), codes.stride(0), scales.data_ptr(), scales.stride(1), scales.stride(0),
                       page_table.data_ptr(), page_table.shape[1], codes.shape[2], codes.shape[1])
+    c.n_heads, c.n_seqs = codes.shape[0], page_table.shape[0]
     c._keepalive = (codes, scales, page_table)
     return c
 
@@ -506,11 +516,13 @@ def rtp_sparsity_stats(layer, ctx_len, sel_idx, sel_stride, sel_count, lse_selec
 
 
 def rtp_kv4_append(layer, cache, k, v, batch_stride, token_stride, head_stride, start, count, B, T, stream=None):
+    _held("rtp_kv4_append", layer, cache, B)
     _check(lib().rtp_kv4_append(C.byref(layer), C.byref(cache), _ptr(k), _ptr(v), batch_stride, token_stride, head_stride,
                                 _ptr(start), _ptr(count), B, T, _stream(stream)))
 
 
 def rtp_kv4_read(layer, cache, start, count, B, T, k, v, batch_stride, token_stride, head_stride, stream=None):
+    _held("rtp_kv4_read", layer, cache, B)
     _check(lib().rtp_kv4_read(C.byref(layer), C.byref(cache), _ptr(start), _ptr(count), B, T, _ptr(k), _ptr(v), batch_stride,
                               token_stride, head_stride, _stream(stream)))
 
@@ -520,6 +532,7 @@ def rtp_sparse_attn_decode_kv4_workspace_bytes(layer, B, max_sel) -> int:
 
 
 def rtp_sparse_attn_decode_kv4(layer, q, cache, sel_idx, sel_stride, sel_count, max_sel, B, out, lse, ws, stream=None):
+    _held("rtp_sparse_attn_decode_kv4", layer, cache, B)
     _check(lib().rtp_sparse_attn_decode_kv4(C.byref(layer), _ptr(q), C.byref(cache), _ptr(sel_idx), sel_stride, _ptr(sel_count),
                                             max_sel, B, _ptr(out), _ptr(lse), _ptr(ws), _nbytes(ws), _stream(stream)))
 
@@ -529,6 +542,7 @@ def rtp_local_attn_kv4_workspace_bytes(layer, B, max_ctx) -> int:
 
 
 def rtp_local_attn_kv4(layer, q, cache, ctx_len, B, max_ctx, out, lse, ws, stream=None):
+    _held("rtp_local_attn_kv4", layer, cache, B)
     _check(lib().rtp_local_attn_kv4(C.byref(layer), _ptr(q), C.byref(cache), _ptr(ctx_len), B, max_ctx, _ptr(out), _ptr(lse),
                                     _ptr(ws), _nbytes(ws), _stream(stream)))
 
@@ -538,6 +552,7 @@ def rtp_dense_attn_kv4_workspace_bytes(layer, B, max_ctx) -> int:
 
 
 def rtp_dense_attn_kv4(layer, q, cache, ctx_len, B, max_ctx, out, lse, ws, stream=None):
+    _held("rtp_dense_attn_kv4", layer, cache, B)
     _check(lib().rtp_dense_attn_kv4(C.byref(layer), _ptr(q), C.byref(cache), _ptr(ctx_len), B, max_ctx, _ptr(out), _ptr(lse),
                                     _ptr(ws), _nbytes(ws), _stream(stream)))
 

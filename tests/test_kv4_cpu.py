@@ -306,3 +306,17 @@ def test_workspaces_serve_smaller_calls():
             got = np.array([[size(layer, b, n) for n in lens] for b in grid])
             assert (got % 256 == 0).all() and got.min() >= 256
             assert (np.diff(got, axis=0) >= 0).all() and (np.diff(got, axis=1) >= 0).all(), (hq, hkv, size.__name__)
+
+
+@pytest.mark.parametrize("name", ["append", "read", "sparse", "local", "dense"])
+def test_calls_beyond_what_the_cache_holds_are_refused(name):
+    """A pool with fewer KV heads than the layer, a page table with fewer rows than the batch: the strides alone allow both."""
+    import torch
+    codes, scales = torch.zeros((2, 10, 16, 128), dtype=torch.uint8), torch.zeros((2, 10, 128), dtype=torch.uint8)
+    cache = rtp.kv4_cache(codes, scales, torch.zeros((3, 64), dtype=torch.int32))
+    for layer, B in ((_layer(n_kv_heads=4), 3), (_layer(n_kv_heads=8), 1), (_layer(), 4), (_layer(n_kv_heads=1), 400)):
+        call, args = _calls(layer=layer, cache=cache)[name]
+        args["B"] = B
+        with pytest.raises(rtp.RtpError, match="2 KV heads and 3 sequences") as e:
+            call(**args)
+        assert e.value.code == rtp.RTP_ERR_INVALID_ARG
