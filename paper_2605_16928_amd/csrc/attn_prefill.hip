@@ -602,7 +602,7 @@ __global__ __launch_bounds__(kOrderThreads) void prefill_order_kernel(const Pref
       const uint64_t bit = __ballot((cls[k] >> b) & 1);
       same &= (cls[k] >> b) & 1 ? bit : ~bit;
     }
-    rank[k] = __popcll(same & ((1ull << lane) - 1ull));
+    rank[k] = lanes_below(same);
     if (on && rank[k] == 0) at[cls[k]][k * NW + wave] = __popcll(same);
 #pragma unroll
     for (int q = 0; q < 3; ++q) {                                  // 1/64, 1/256, 1/1024 of the context
@@ -2201,7 +2201,7 @@ __global__ __launch_bounds__(THREADS) void prefill_active_tiles_kernel(const Pre
       if (w < wave) before += n;
       base += n;
     }
-    if (on) list[before + __popcll(bal & ((1ull << lane) - 1ull))] = p;
+    if (on) list[before + lanes_below(bal)] = p;
   }
   if (tid == 0) {
     if (a.units) {

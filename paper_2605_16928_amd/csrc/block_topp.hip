@@ -256,13 +256,13 @@ __global__ __launch_bounds__(kBtThreads) void block_write_kernel(const BlockTopP
   uint64_t bits;
   chunk_kept(bins, n_here, st.thr_bin, st.flags == 1, &bits);
   if (a.mask_out && tid < kBtBlocksPerChunk && tid * kBtBlock < n_here)
-    a.mask_out[(int64_t)r * a.mask_stride + (int64_t)c * kBtBlocksPerChunk + tid] = (uint8_t)((bits >> tid) & 1ull);
+    a.mask_out[(int64_t)r * a.mask_stride + (int64_t)c * kBtBlocksPerChunk + tid] = (uint8_t)mask_bit(bits, tid);
   int32_t* out = a.sel_idx + (int64_t)r * a.sel_stride + before;
   // every block before the row's last is full, so a kept token's slot is 64 * (kept blocks before its own) + its offset
   for (int e = tid; e < n_here; e += kBtThreads) {
     const int blk = e >> 6;
-    if ((bits >> blk) & 1ull) {
-      const int kb = __popcll(bits & ((1ull << blk) - 1ull));
+    if (mask_bit(bits, blk)) {
+      const int kb = mask_below(bits, blk);
       out[kb * kBtBlock + (e & 63)] = (int32_t)(n0 + e);
     }
   }

@@ -164,6 +164,23 @@ __device__ __forceinline__ double wave_incl_scan(double x) {
 __device__ __forceinline__ int wave_last(int x) { return __builtin_amdgcn_readlane(x, 63); }
 // Wave-wide sum / maximum of non-negative-or-(-1) ints, in every lane.
 __device__ __forceinline__ int wave_sum(int x) { return wave_last(wave_incl_scan(x)); }
+// A bit of a 64-lane mask, the bits below it, and the bits below the lane's own, with a position that differs from lane to lane, in
+// 32-bit instructions.  A rank came out wrong once where a 64-bit shift took its amount from the last of the kernel's vector registers
+// (v_lshlrev_b64 by v71 of 72) and right where it lay in another.  The cause is not established; no kernel of the library takes the
+// amount of a 64-bit shift from a vector register, which tests/test_device_code.py holds them to.  (Of the half that is picked and
+// shifted the compiler would make such a shift again: the empty statement keeps the halves apart.)
+__device__ __forceinline__ bool mask_bit(uint64_t mask, int at) {
+  uint32_t lo = (uint32_t)mask, hi = (uint32_t)(mask >> 32);
+  asm("" : "+v"(lo), "+v"(hi));
+  return (((at & 32) ? hi : lo) >> (at & 31)) & 1u;
+}
+__device__ __forceinline__ int mask_below(uint64_t mask, int at) {
+  const uint32_t low = (1u << (at & 31)) - 1u;
+  return (at & 32) ? __popc((uint32_t)mask) + __popc((uint32_t)(mask >> 32) & low) : __popc((uint32_t)mask & low);
+}
+__device__ __forceinline__ int lanes_below(uint64_t mask) {
+  return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
 // max(a, b) of two values that are never NaN, as ONE vector instruction (the median of a, b and +inf).  fmaxf()
 // has to quiet signalling NaNs, which costs a canonicalising instruction for every operand the compiler cannot
 // prove quiet -- matrix-core results, cross-lane moves -- i.e. three instructions per maximum in such places.

@@ -67,16 +67,6 @@ __device__ __forceinline__ T pg_scan(T v, uint64_t* sh, T* total) {
   return off + incl - v;
 }
 
-// Bit `at` of a mask, and the bits below it, in 32-bit steps: a 64-bit shift by a vector register gave wrong results where that register was
-// the last of the kernel's (v_lshlrev_b64 by v71 of 72).
-__device__ __forceinline__ bool mask_bit(uint64_t mask, int at) {
-  return (((at & 32) ? (uint32_t)(mask >> 32) : (uint32_t)mask) >> (at & 31)) & 1u;
-}
-__device__ __forceinline__ int mask_below(uint64_t mask, int at) {
-  const uint32_t low = (1u << (at & 31)) - 1u;
-  return (at & 32) ? __popc((uint32_t)mask) + __popc((uint32_t)(mask >> 32) & low) : __popc((uint32_t)mask & low);
-}
-
 // A chunk's masks in LDS (bit i of word w = page 64 w + i of the chunk is free, or in use where FREE is false) and, for every word, the
 // set bits in front of it; *total: all of them.
 struct ChunkMasks {
@@ -260,7 +250,7 @@ __global__ __launch_bounds__(kPgThreads) void kv_pages_extend_kernel(const Exten
     const uint64_t mask = c.mask[w];
     const int before = first + c.before[w];
     if (before >= need) break;
-    const int r = before + mask_below(mask, lane);
+    const int r = before + lanes_below(mask);
     if (!mask_bit(mask, lane) || r >= need) continue;
     const int page = blockIdx.x * kPgChunk + w * 64 + lane;
     int lo = 0, hi = a.n - 1;                   // the request that rank r belongs to: the last one whose prefix is <= r
@@ -331,7 +321,7 @@ __global__ __launch_bounds__(kPgThreads) void kv_pages_moves_kernel(const Extend
   const int words = (min(a.m.n_pages - chunk0, kPgChunk) + 63) / 64;
   for (int w = threadIdx.x >> 6; w < words; w += kPgWaves) {
     const uint64_t mask = c.mask[w];
-    const int page = chunk0 + w * 64 + lane, used = first + c.before[w] + mask_below(mask, lane);
+    const int page = chunk0 + w * 64 + lane, used = first + c.before[w] + lanes_below(mask);
     const bool here = mask_bit(mask, lane);
     if (!here && page < total) a.copy_dst[page - used] = page;
     if (here && page >= total) a.copy_src[total - 1 - used] = page;
