@@ -334,12 +334,29 @@ class Kv4DecodeRun(DecodeRun):
         rtp.rtp_dense_attn_kv4(self.desc, self.w.q, self.cache, self.ctx_len, self.B, self.max_ctx,
                                self.out if out is None else out, self.lse if lse is None else lse, self.ws_dense4)
 
+    # Selection and attention are two calls over this cache.  The base class's other forms would read the workload's 16-bit K and V.
     def step(self, fused: bool = False):
         """One decode step: index scores, top-p, attention over the 4-bit cache."""
-        self.index_score()
-        self.topp()
-        self.sparse_attn()
-        self.local_attn()
+        self._two_calls(fused)
+        super().step(False)
+
+    def step_two_streams(self, side: "torch.cuda.Stream", fused: bool = False):
+        """The same step with the local heads on a second stream."""
+        self._two_calls(fused)
+        super().step_two_streams(side, False)
+
+    def _two_calls(self, fused):
+        if fused:
+            raise rtp.RtpError(rtp.RTP_ERR_UNSUPPORTED, "Kv4DecodeRun: no call selects and attends over a 4-bit cache")
+
+    @property
+    def carries_local_heads(self) -> bool:
+        return False
+
+    def _only_16_bits(self, *args, **kw):
+        raise rtp.RtpError(rtp.RTP_ERR_UNSUPPORTED, "Kv4DecodeRun: this call reads a 16-bit cache only")
+
+    select_attend = decode_attention = step_one_stream = make_ring = ring_append = local_attn_ring = _only_16_bits
 
 
 class PrefillRun:

@@ -43,6 +43,38 @@ def test_decode_step(kw, page_size):
             check_row(out[b, h], lse[b, h], q[b, h], K[kvh, t0 + pos], V[kvh, t0 + pos], L.kv_dtype, scale, f"sequence {b}, head {h}")
 
 
+def _check_heads(run, w, q, K, V, lens, what=""):
+    """Every head of the workload's sequences against 64 bits over the set it reports; K and V: rows [n_kv_heads, n, 128] per sequence."""
+    L = w.layer
+    sets, _ = run.sel_sets()
+    out, lse = run.out_f64(), run.lse.double().cpu().numpy()
+    for b in range(w.B):
+        for h in range(L.n_q_heads):
+            pos = sets[b * L.n_ret + L.ret_heads.index(h)] if h in L.ret_heads else k4.local_positions(lens[b], L.sink, L.window)
+            kvh = h // (L.n_q_heads // L.n_kv_heads)
+            check_row(out[b, h], lse[b, h], q[b, h], K[b][kvh, pos], V[b][kvh, pos], L.kv_dtype, what=f"{what}sequence {b}, head {h}")
+
+
+@pytest.mark.parametrize("form", ["two streams", "fastest"])
+def test_step_on_two_streams(form):
+    """The local heads on a second stream: the plain step's results, and both against 64 bits over the 4-bit rows (the 16-bit rows that
+    the workload also holds differ from them by far more than the bound)."""
+    print(f"[case] 4-bit decode step, {form}", flush=True)
+    w = wl.small_decode(DEV, seed=15, ctx=(700, 1531, 64, 2048), n_q_heads=8, n_kv_heads=2, ret_heads=(0, 5))
+    run = Kv4DecodeRun(w, 32)
+    side = torch.cuda.Stream()
+    K, V = ([_stored(x[:, t:t + n]) for t, n in zip(w.seq_start, w.ctx_len)] for x in (w.K, w.V))
+    for _ in range(3):
+        run.out.zero_()
+        run.lse.zero_()
+        (run.step_two_streams if form == "two streams" else run.step_fastest)(side)
+        _check_heads(run, w, w.q.double().cpu().numpy(), K, V, w.ctx_len)
+    out, lse = run.out.clone(), run.lse.clone()
+    run.step()
+    torch.cuda.synchronize()
+    assert torch.equal(out, run.out) and torch.equal(lse, run.lse)
+
+
 def test_forks_diverge_and_survive_compaction():
     """Two forks of a prompt and the prompt itself grow by tokens of their own, another sequence ends, the pool is compacted: what every
     sequence attends to stays its own, bit for bit across the move."""

@@ -320,3 +320,16 @@ def test_calls_beyond_what_the_cache_holds_are_refused(name):
         with pytest.raises(rtp.RtpError, match="2 KV heads and 3 sequences") as e:
             call(**args)
         assert e.value.code == rtp.RTP_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("form", ["select_attend", "decode_attention", "step_one_stream", "make_ring", "ring_append", "local_attn_ring",
+                                  "step", "step_two_streams", "select_then_attend"])
+def test_forms_of_a_step_that_only_read_16_bits_are_refused(form):
+    """What DecodeRun offers beside its plain step does not read the 4-bit cache behind the caller's back."""
+    from paper_2605_16928_amd.pipeline import Kv4DecodeRun
+    run = object.__new__(Kv4DecodeRun)                  # (refused before any buffer is looked at)
+    args = {"ring_append": (None, None, None), "step": (True,), "step_two_streams": (None, True), "select_then_attend": (True,)}
+    with pytest.raises(rtp.RtpError) as e:
+        getattr(run, form)(*args.get(form, ()))
+    assert e.value.code == rtp.RTP_ERR_UNSUPPORTED
+    assert run.carries_local_heads is False             # step_fastest takes two streams
