@@ -32,12 +32,13 @@ def i64(x):
 class DecodeRun:
     """Device buffers for one decode workload and the C-ABI calls on them."""
 
-    def __init__(self, w: wl.DecodeWorkload, fuse_level1: bool = True, interleaved: bool = False):
+    def __init__(self, w: wl.DecodeWorkload, fuse_level1: bool = True, interleaved: bool = False, room: int = 0):
         """fuse_level1: the score pass accumulates the selector's first histogram level (the
         configuration the benchmark times); False runs the two calls independently.
         interleaved: keep the K and V rows of a token next to each other ([Hkv, T, 2, 128], one
         512-byte piece per gathered token) instead of in two tensors; the workload's own K and V
-        are released."""
+        are released.
+        room: tokens beyond the longest context that buffers and workspaces are sized for."""
         self.w = w
         self.fuse_level1 = fuse_level1
         if interleaved:
@@ -50,7 +51,7 @@ class DecodeRun:
         self.desc = layer_desc_of(L)
         self.B, self.n_ret = w.B, L.n_ret
         self.R = self.B * self.n_ret
-        self.max_ctx = max(w.ctx_len)
+        self.max_ctx = max(w.ctx_len) + room
         self.stride = (self.max_ctx + 3) // 4 * 4
         self.seq_start, self.ctx_len = i64(w.seq_start), i32(w.ctx_len)
         self.row_len = i32([w.ctx_len[b] for b in range(self.B) for _ in range(self.n_ret)])
@@ -70,14 +71,14 @@ class DecodeRun:
         self.ws_fused = ws_alloc(rtp.rtp_select_attend_decode_workspace_bytes(self.desc, self.B, self.max_ctx))
         self.ws_local = ws_alloc(rtp.rtp_local_attn_workspace_bytes(self.desc, self.B, 1, self.max_ctx))
         self.ws_dense = ws_alloc(rtp.rtp_dense_attn_workspace_bytes(self.desc, self.B, 1, self.max_ctx))
-        self.T_tot = w.T_tot
+        self.kI, self.T_tot = w.kI, w.T_tot
 
     # ---- the five calls -------------------------------------------------------------------
     def index_score(self):
         w = self.w
         q_in = w.q_pre if w.WQ is not None else w.qI
         fuse = self.fuse_level1 and not self._level1_pending and self.R > 0
-        rtp.rtp_index_score(self.desc, q_in, w.WQ, w.kI, self.T_tot * 16, self.seq_start, self.ctx_len, None,
+        rtp.rtp_index_score(self.desc, q_in, w.WQ, self.kI, self.T_tot * 16, self.seq_start, self.ctx_len, None,
                             self.B, 1, self.max_ctx, self.scores, self.stride, self.qI_out,
                             self.ws_topp if fuse else None)
         self._level1_pending = self._level1_pending or fuse
@@ -86,21 +87,21 @@ class DecodeRun:
         """The fused score pass on its own, for timing: level 1 goes to a scratch workspace."""
         w = self.w
         q_in = w.q_pre if w.WQ is not None else w.qI
-        rtp.rtp_index_score(self.desc, q_in, w.WQ, w.kI, self.T_tot * 16, self.seq_start, self.ctx_len, None,
+        rtp.rtp_index_score(self.desc, q_in, w.WQ, self.kI, self.T_tot * 16, self.seq_start, self.ctx_len, None,
                             self.B, 1, self.max_ctx, self.scores, self.stride, self.qI_out, scratch)
 
     def index_score_plain_timing(self):
         """The score pass without the selector's histogram level, for timing."""
         w = self.w
         q_in = w.q_pre if w.WQ is not None else w.qI
-        rtp.rtp_index_score(self.desc, q_in, w.WQ, w.kI, self.T_tot * 16, self.seq_start, self.ctx_len, None,
+        rtp.rtp_index_score(self.desc, q_in, w.WQ, self.kI, self.T_tot * 16, self.seq_start, self.ctx_len, None,
                             self.B, 1, self.max_ctx, self.scores, self.stride, self.qI_out, None)
 
     def index_score_traffic_probe(self, dst):
         """The score pass's loads and stores without its arithmetic (a measurement; dst gets meaningless words)."""
         w = self.w
         q_in = w.q_pre if w.WQ is not None else w.qI
-        rtp.rtp_index_score_traffic_probe(self.desc, q_in, w.WQ, w.kI, self.T_tot * 16, self.seq_start, self.ctx_len, None,
+        rtp.rtp_index_score_traffic_probe(self.desc, q_in, w.WQ, self.kI, self.T_tot * 16, self.seq_start, self.ctx_len, None,
                                           self.B, 1, self.max_ctx, dst, self.stride)
 
     def topp(self, scores=None, p_rows=None):
@@ -269,12 +270,20 @@ class DecodeRun:
 class Kv4DecodeRun(DecodeRun):
     """A decode workload whose K and V live in a paged 4-bit cache: pages handed out and tokens appended through the library,
     selection by the workload's own index keys, attention over the 4-bit cache.  spare_seqs: further rows of the page table, for
-    forks; spare_pages: free pages behind what the contexts take."""
+    forks; spare_pages: free pages behind what the contexts may take; room: tokens that grow() may add to every context."""
 
-    def __init__(self, w: wl.DecodeWorkload, page_size: int = 64, spare_seqs: int = 0, spare_pages: int = 8):
-        super().__init__(w)
+    def __init__(self, w: wl.DecodeWorkload, page_size: int = 64, spare_seqs: int = 0, spare_pages: int = 8, room: int = 0):
+        super().__init__(w, room=room)
         L, B = w.layer, self.B
-        need = [-(-n // page_size) for n in w.ctx_len]
+        if room:                                # (index keys lie along one token axis: each sequence's with its room behind them)
+            start = [t0 + b * room for b, t0 in enumerate(w.seq_start)]
+            self.kI = torch.zeros((w.kI.shape[0], w.T_tot + B * room, w.kI.shape[2]), dtype=w.kI.dtype, device=DEV)
+            for b, n in enumerate(w.ctx_len):
+                self.kI[:, start[b]:start[b] + n] = w.kI[:, w.seq_start[b]:w.seq_start[b] + n]
+            self.seq_start, self.T_tot = i64(start), w.T_tot + B * room
+        self.len_most, self.len_limit = list(w.ctx_len), [n + room for n in w.ctx_len]    # what the host knows of the contexts
+        self._apart, self._rows = False, i32(range(B))
+        need = [-(-n // page_size) for n in self.len_limit]
         self.page_size, self.n_pages = page_size, sum(need) + spare_pages
         self.codes = torch.zeros((L.n_kv_heads, self.n_pages, page_size, 128), dtype=torch.uint8, device=DEV)
         self.scales = torch.zeros((L.n_kv_heads, self.n_pages, page_size * 8), dtype=torch.uint8, device=DEV)
@@ -298,18 +307,49 @@ class Kv4DecodeRun(DecodeRun):
             rtp.rtp_kv4_append(self.desc, row, w.K[:, t0:], w.V[:, t0:], 0, 128, w.K.shape[1] * 128, i32([0]), None, 1, n)
 
     # ---- pages ----------------------------------------------------------------------------------
+    # They know nothing of index keys: where extend() or fork() alone gave a context of the workload other tokens, step() refuses.
+    # grow() and truncate() keep pages and keys together.
     def extend(self, seqs, old_len, new_len):
         """Pages for sequences that grow, own copies of shared last pages among them; status holds {lacking, left}."""
         n = len(seqs)
-        rtp.rtp_kv_pages_extend(self.map, i32(seqs), i32(old_len), i32(new_len), n, self.copy_src, self.copy_dst, self.status,
-                                self.ws_pages)
+        self._apart = self._apart or any(b < self.B and m > self.len_most[b] for b, m in zip(seqs, new_len) if b >= 0)
+        self._extend(i32(seqs), i32(old_len), i32(new_len), n)
+
+    def _extend(self, seqs, old_len, new_len, n):
+        rtp.rtp_kv_pages_extend(self.map, seqs, old_len, new_len, n, self.copy_src, self.copy_dst, self.status, self.ws_pages)
         rtp.rtp_kv_pages_copy(self.pools, self.n_pages, self.copy_src, self.copy_dst, n)
 
     def fork(self, src, dst, length):
+        self._apart = self._apart or any(0 <= b < self.B for b in dst)
         rtp.rtp_kv_pages_fork(self.map, i32(src), i32(dst), i32(length), len(src))
 
     def truncate(self, seqs, keep=None):
+        """Releases the pages behind the first keep[i] tokens (None: all); the workload's contexts end there."""
         rtp.rtp_kv_pages_truncate(self.map, i32(seqs), None if keep is None else i32(keep), len(seqs))
+        ends = list(self.len_limit)
+        for b, k in zip(seqs, keep if keep is not None else [0] * len(seqs)):
+            if 0 <= b < self.B:
+                ends[b] = min(ends[b], max(k, 0))
+        self.len_most = [min(n, k) for n, k in zip(self.len_most, ends)]
+        self._set_len(torch.minimum(self.ctx_len, i32(ends)))
+
+    def grow(self, k_new, v_new, kI_new):
+        """T new tokens behind every context: pages, K and V [B, T, n_kv_heads, 128], index keys [n_ret, B, T, 16].  Where pages are
+        lacking (status) no context changes."""
+        T = k_new.shape[1]
+        if any(n + T > most for n, most in zip(self.len_most, self.len_limit)):
+            raise rtp.RtpError(rtp.RTP_ERR_INVALID_ARG, f"Kv4DecodeRun: no room for {T} more tokens in every context")
+        self._extend(self._rows, self.ctx_len, self.ctx_len + T, self.B)
+        added = torch.where(self.status[:1] == 0, T, 0).to(torch.int32).expand(self.B).contiguous()
+        self.append(k_new, v_new, self.ctx_len, added)          # (a last page that stayed shared is not written to)
+        rows = (self.seq_start + self.ctx_len)[:, None] + torch.arange(T, device=DEV)
+        self.kI[:, rows.flatten()] = kI_new.reshape(-1, self.B * T, 16)
+        self.len_most = [n + T for n in self.len_most]
+        self._set_len(self.ctx_len + added)
+
+    def _set_len(self, n):
+        self.ctx_len.copy_(n)
+        self.row_len.copy_(n.repeat_interleave(self.n_ret))
 
     def compact(self):
         rtp.rtp_kv_pages_compact(self.map, self.copy_src, self.copy_dst, self.status, self.ws_pages)
@@ -348,6 +388,9 @@ class Kv4DecodeRun(DecodeRun):
     def _two_calls(self, fused):
         if fused:
             raise rtp.RtpError(rtp.RTP_ERR_UNSUPPORTED, "Kv4DecodeRun: no call selects and attends over a 4-bit cache")
+        if self._apart:
+            raise rtp.RtpError(rtp.RTP_ERR_INVALID_ARG, "Kv4DecodeRun: contexts have changed by their pages alone, without index keys: "
+                                                        "grow() and truncate() change both")
 
     @property
     def carries_local_heads(self) -> bool:

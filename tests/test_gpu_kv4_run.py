@@ -1,5 +1,7 @@
 """The 4-bit cache and its pages as a server uses them together: decode steps, forks that diverge, compaction under running sequences,
 a prefill chunk behind a 4-bit context, captured steps, two streams."""
+import dataclasses
+
 import numpy as np
 import pytest
 import torch
@@ -73,6 +75,92 @@ def test_step_on_two_streams(form):
     run.step()
     torch.cuda.synchronize()
     assert torch.equal(out, run.out) and torch.equal(lse, run.lse)
+
+
+def _more(rng, w, T):
+    """T further tokens for every sequence of a workload: K and V rows, index keys near the index queries, so that they are selected."""
+    H, n_ret = w.layer.n_kv_heads, w.layer.n_ret
+    k, v = (torch.from_numpy(rng.standard_normal((w.B, T, H, 128))).to(TYPES[w.layer.kv_dtype]).to(DEV) for _ in range(2))
+    keys = 9.0 * w.qI.float().transpose(0, 1)[:, :, None] + torch.from_numpy(0.1 * rng.standard_normal((n_ret, w.B, T, 16))).to(DEV)
+    return k, v, keys.to(torch.bfloat16)
+
+
+def _grown(w, parts):
+    """The workload with `parts` ([_more] in order) behind its sequences."""
+    T, cut = sum(k.shape[1] for k, _, _ in parts), list(zip(w.seq_start, w.ctx_len))
+
+    def join(old, new):                                # old: [rows, tokens, dims], new: per sequence
+        return torch.cat([x for b, (t, n) in enumerate(cut) for x in [old[:, t:t + n]] + [m[b] for m in new]], dim=1)
+    k, v = ([p[i].permute(0, 2, 1, 3) for p in parts] for i in (0, 1))
+    return dataclasses.replace(w, ctx_len=[n + T for n in w.ctx_len], seq_start=[t + b * T for b, t in enumerate(w.seq_start)],
+                               K=join(w.K, k), V=join(w.V, v), kI=join(w.kI, [p[2].transpose(0, 1) for p in parts]))
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(n_q_heads=4, n_kv_heads=4, ret_heads=(0, 3), window=700, kv_dtype="fp16")], ids=["g4", "g1_fp16"])
+def test_steps_over_growing_contexts(kw):
+    """Tokens join every context, some over a page that a fork shares: a step selects from and attends to all of them, as a run over
+    the whole workload does; a rejected draft is cut off again; contexts changed behind the index keys' back are refused."""
+    print(f"[case] steps over growing contexts, {kw}", flush=True)
+    rng = np.random.default_rng(21)
+    w = wl.small_decode(DEV, seed=21, ctx=(700, 16, 31, 1, 2048), **kw)
+    run = Kv4DecodeRun(w, 16, spare_seqs=1, spare_pages=20, room=30)
+    run.fork([0], [5], [700])
+    parts, q, side = [], w.q.double().cpu().numpy(), torch.cuda.Stream()
+    for step, T in enumerate((1, 17, 5, 7)):
+        parts.append(_more(rng, w, T))
+        run.grow(*parts[-1])
+        assert run.status[0].item() == 0
+        run.step() if step % 2 else run.step_two_streams(side)
+        full = _grown(w, parts)
+        sets, _ = run.sel_sets()
+        whole = Kv4DecodeRun(full, 64)
+        whole.step()
+        for r, (a, b) in enumerate(zip(sets, whole.sel_sets()[0])):
+            np.testing.assert_array_equal(a, b)
+            assert a.max() >= w.ctx_len[r // w.layer.n_ret], "no new token was selected"
+        K, V = ([_stored(x[:, t:t + n]) for t, n in zip(full.seq_start, full.ctx_len)] for x in (full.K, full.V))
+        _check_heads(run, full, q, K, V, full.ctx_len, f"after {T} more, ")
+    with pytest.raises(rtp.RtpError, match="no room"):
+        run.grow(*_more(rng, w, 1))
+    # the last 7 tokens are rejected, in one sequence all of its tokens
+    run.truncate(range(5), [n + 23 for n in w.ctx_len[:3]] + [0, w.ctx_len[4] + 23])
+    kept = _grown(w, parts[:3])
+    lens = kept.ctx_len[:3] + [0] + kept.ctx_len[4:]
+    run.step()
+    _check_heads(run, kept, q, K, V, lens, "after a cut, ")
+    run.fork([0], [3], [40])
+    with pytest.raises(rtp.RtpError, match="alone"):
+        run.step()
+    run = Kv4DecodeRun(w, 16)
+    run.extend([1], [16], [17])
+    with pytest.raises(rtp.RtpError, match="alone"):
+        run.step_two_streams(side)
+
+
+def test_growth_without_pages_changes_nothing():
+    """No free page for a shared last page's copy or for a new one: no byte, no context and no result changes."""
+    print("[case] growth without pages", flush=True)
+    rng = np.random.default_rng(22)
+    w = wl.small_decode(DEV, seed=22, ctx=(30, 16), n_q_heads=8, n_kv_heads=2, ret_heads=(0, 5))
+    run = Kv4DecodeRun(w, 16, spare_seqs=2, spare_pages=0, room=20)
+    run.fork([0], [2], [20])
+    run.extend([3], [0], [64])
+    assert run.status.tolist() == [0, 0]
+    run.step()
+    state = run.codes, run.scales, run.page_table, run.page_refs, run.ctx_len, run.row_len, run.out, run.lse
+    before = [x.clone() for x in state]
+    new = _more(rng, w, 1)
+    run.grow(*new)
+    run.step()
+    assert run.status.tolist() == [2, 0]
+    assert all(torch.equal(a, b) for a, b in zip(state, before))
+    run.truncate([3])
+    run.grow(*new)
+    run.step()
+    assert run.status[0].item() == 0 and run.ctx_len.tolist() == [31, 17]
+    full = _grown(w, [new])
+    K, V = ([_stored(x[:, t:t + n]) for t, n in zip(full.seq_start, full.ctx_len)] for x in (full.K, full.V))
+    _check_heads(run, full, w.q.double().cpu().numpy(), K, V, full.ctx_len)
 
 
 def test_forks_diverge_and_survive_compaction():
