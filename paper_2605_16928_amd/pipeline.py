@@ -303,6 +303,8 @@ class Kv4DecodeRun(DecodeRun):
         self.extend(range(B), [0] * B, w.ctx_len)
         for b in range(B):                      # (the workload packs its sequences along one token axis)
             t0, n = w.seq_start[b], w.ctx_len[b]
+            if n == 0:
+                continue
             row = rtp.kv4_cache(self.codes, self.scales, self.page_table[b:b + 1])
             rtp.rtp_kv4_append(self.desc, row, w.K[:, t0:], w.V[:, t0:], 0, 128, w.K.shape[1] * 128, i32([0]), None, 1, n)
 

@@ -137,6 +137,23 @@ def test_steps_over_growing_contexts(kw):
         run.step_two_streams(side)
 
 
+def test_contexts_that_begin_empty():
+    """Sequences without a token yet, the last one of the batch among them: zeros, then their first tokens."""
+    print("[case] contexts that begin empty", flush=True)
+    rng = np.random.default_rng(23)
+    w = wl.small_decode(DEV, seed=23, ctx=(50, 0, 70, 0), n_q_heads=8, n_kv_heads=2, ret_heads=(0, 5))
+    run, q = Kv4DecodeRun(w, 16, room=8), w.q.double().cpu().numpy()
+    run.step()
+    K, V = ([_stored(x[:, t:t + n]) for t, n in zip(w.seq_start, w.ctx_len)] for x in (w.K, w.V))
+    _check_heads(run, w, q, K, V, w.ctx_len)
+    new = _more(rng, w, 3)
+    run.grow(*new)
+    run.step()
+    full = _grown(w, [new])
+    K, V = ([_stored(x[:, t:t + n]) for t, n in zip(full.seq_start, full.ctx_len)] for x in (full.K, full.V))
+    _check_heads(run, full, q, K, V, full.ctx_len)
+
+
 def test_growth_without_pages_changes_nothing():
     """No free page for a shared last page's copy or for a new one: no byte, no context and no result changes."""
     print("[case] growth without pages", flush=True)
