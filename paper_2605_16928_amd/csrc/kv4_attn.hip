@@ -773,10 +773,11 @@ static int32_t range_attn_kv4(const char* who, const rtp_layer_desc* layer, cons
   if ((int64_t)B * layer->n_kv_heads > kMaxUnits)
     return fail(RTP_ERR_UNSUPPORTED, "%s: B * n_kv_heads = %lld exceeds %d", who, (long long)B * layer->n_kv_heads, kMaxUnits);
   const Kv4RangePlan p = plan_range(layer, LOCAL, B, max_ctx);
-  rc = check_io(who, q, out, ws, ws_bytes, p.ws_bytes);
+  const bool none = LOCAL && layer->n_ret == layer->n_q_heads;    // no local head
+  rc = check_io(who, q, out, ws, ws_bytes, none ? 0 : p.ws_bytes);
   if (rc != RTP_OK) return rc;
   clear_error();
-  if (LOCAL && layer->n_ret == layer->n_q_heads) return RTP_OK;   // no local head
+  if (none) return RTP_OK;
   fill_attn(a, layer, ht, q, out, lse, ws);
   a.d.ctx_len = ctx_len;
   a.d.units = p.units;

@@ -333,3 +333,13 @@ def test_forms_of_a_step_that_only_read_16_bits_are_refused(form):
         getattr(run, form)(*args.get(form, ()))
     assert e.value.code == rtp.RTP_ERR_UNSUPPORTED
     assert run.carries_local_heads is False             # step_fastest takes two streams
+
+
+def test_nothing_to_do_asks_for_nothing():
+    """No local head, no retrieval head: no workspace either, however long the contexts are."""
+    lib, cache, vp = rtp.lib(), _cache(pt_stride=1 << 21), C.c_void_p
+    every, none = _layer(ret_heads=list(range(8)), window=1 << 20), _layer(ret_heads=[])
+    assert rtp.rtp_local_attn_kv4_workspace_bytes(every, 2, 1 << 26) > 256
+    assert lib.rtp_local_attn_kv4(C.byref(every), vp(A), C.byref(cache), vp(A), 2, 1 << 26, vp(A), None, None, 0, None) == rtp.RTP_OK
+    assert lib.rtp_sparse_attn_decode_kv4(C.byref(none), vp(A), C.byref(cache), vp(A), 1 << 20, vp(A), 1 << 20, 2, vp(A), None, None, 0,
+                                          None) == rtp.RTP_OK
