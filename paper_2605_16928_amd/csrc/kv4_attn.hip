@@ -694,8 +694,20 @@ static Kv4RangePlan plan_range(const rtp_layer_desc* L, bool local, int32_t B, i
   //   32                177 / 178       143 / 33                                 140 /  91
   //   64                364 / 362       152 / 47                                 249 / 192
   //   128               710 / 720       160 / 69                                 412 / 374
-  // Windows are mostly full, i.e. equal: where units in one piece fill their rounds, they stay whole up to 12288 tokens (8192 of 32
-  // sequences 46 / 51, 40 / 32 with any length up to it; 17 sequences 44 / 38, 40 / 26; 16384 of 32 sequences 90 / 95, 73 / 53).
+  // Windows of contexts beyond them are full, i.e. equal: where units in one piece fill their rounds (231 - 256 of them, 461 - 512, ..), they
+  // stay whole up to 12288 tokens, without the plan and the empty merge launch.  The host knows no lengths, so a ragged batch pays for it,
+  // most of all one full window among short ones.  us, in one piece / shared out (full: every window; half: every other one, the rest of any
+  // length; any: any length; one: one full, the others a sixteenth):
+  //                                          full         half         any         one
+  //   8192,  29 sequences of 8 KV heads     54 /  58     45 /  42     41 / 34     42 / 18
+  //          32 of 8                        52 /  57     45 /  52     41 / 35     42 / 18
+  //          128 of 2                       54 /  60     46 /  59     43 / 39     41 / 19
+  //          256 of 1                       54 /  62     47 /  64     44 / 43     41 / 21
+  //          58 of 8                        95 / 102     80 /  85     67 / 62     42 / 23
+  //   12000, 32 of 8                        77 /  83     64 /  72     60 / 48     59 / 22
+  //          64 of 8                       143 / 149    116 / 115     94 / 83     60 / 29
+  // Outside the bands one piece loses everywhere (17 sequences of 8, window 8192: 44 / 38 full, 40 / 26 any); longer windows win less and lose
+  // more by it (32 of 8, 16384: 90 / 95 and 73 / 53).
   const bool whole = blocks <= 48 + p.units || (local && many && blocks <= 768 && busy(1) >= 0.9f);
   p.balanced = !whole && most > 1 && B > 1 && B <= 256;
   if (p.balanced) {

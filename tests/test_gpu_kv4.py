@@ -254,6 +254,40 @@ def test_many_windows_are_shared_out(B, hkv, ret, lens):
             check_row(out[b, h], lse[b, h], qd[b, h], k, v, "bf16", what=f"sequence {b}, head {h}")
 
 
+@pytest.mark.parametrize("lens", ["full", "half", "any", "one", "empty"])
+@pytest.mark.parametrize("B,hkv,group,whole", [(29, 8, 2, True), (32, 8, 4, True), (58, 8, 1, True), (120, 2, 8, True), (20, 8, 2, False), (33, 8, 2, False)])
+def test_windows_where_whole_units_fill_their_rounds(B, hkv, group, whole, lens):
+    """Just under 256 or 512 units with windows of 8192 stay whole, one launch; other numbers of units are shared out.  All sequences read
+    one context's pages, as forks of it do."""
+    print(f"[case] kv4 local, {B} sequences, {hkv} KV heads of {group}, {lens}", flush=True)
+    rng = np.random.default_rng(B)
+    window, sink, longest = 8192, 20, 9001
+    c = Cache(rng, hkv, [longest], 64)
+    c.table = np.repeat(c.table, B, axis=0)
+    c.upload()
+    full = [int(x) for x in rng.integers(window, longest + 1, B)]
+    short = [int(x) for x in rng.integers(0, window, B)]
+    ctx = {"full": full, "half": [x for pair in zip(full, short) for x in pair][:B], "any": short,
+           "one": [longest if b == B // 3 else x % 500 for b, x in enumerate(short)], "empty": [0] * B}[lens]
+    hq, ret = hkv * group, [1, group * (hkv - 1)] + ([group * hkv - 1] if group > 1 else [])
+    layer = _layer(hq, hkv, ret, sink=sink, window=window)
+    q, qd = queries(rng, B, hq, "bf16")
+    results = []
+    names = launches(lambda: results.append(_dense(layer, q, c, ctx, max_ctx=longest, what="local")))
+    assert len(names) == (1 if whole else 2), names
+    out, lse = results[0]
+    for b in sorted({0, 1, B // 3, B - 1} | {int(x) for x in rng.integers(0, B, 3)}):
+        pos = k4.local_positions(ctx[b], sink, window)
+        for kvh in range(hkv):
+            k, v = c.rows(b, kvh, pos)
+            for h in range(kvh * group, kvh * group + group):
+                if h in ret:
+                    assert (out[b, h] == 3.0).all() and lse[b, h] == 3.0
+                else:
+                    check_row(out[b, h], lse[b, h], qd[b, h], k, v, "bf16", what=f"sequence {b}, head {h}")
+    assert np.isfinite(out).all() and (lens == "empty" or np.isfinite(lse[np.array(ctx) > 0]).all())
+
+
 def _sparse(layer, q, c, sel, max_sel=None, n_ret=1):
     B, Hq = q.shape[:2]
     counts = [len(s) for s in sel]
