@@ -542,7 +542,7 @@ int32_t rtp_local_attn_ring(const rtp_layer_desc* layer, const void* q,
  *   scales  one byte per block j at  scales + P * scale_page_stride + kvh * scale_head_stride + (r / 4) * 32 + 4 j + r % 4
  *           for K, 16 bytes further for V
  * codes, scales and all four strides (in BYTES) are multiples of 16; pages and heads may be nested either way (head-major or
- * page-major) but must not overlap.  page_size: a power of two in [16, 2^20].  A page is page_size * 128 bytes of codes and
+ * page-major) but must not overlap; the pools hold the layer's n_kv_heads heads and the table B rows, or more.  page_size: a power of two in [16, 2^20].  A page is page_size * 128 bytes of codes and
  * page_size * 8 of scales per KV head: 16-byte pieces that rtp_kv_pages_copy moves.
  *
  * An entry of page_table that is not in [0, n_pages), and a position behind pt_stride * page_size, are never followed: rtp_kv4_append
@@ -612,15 +612,19 @@ int32_t rtp_dense_attn_kv4(const rtp_layer_desc* layer, const void* q, const rtp
  *                          copy_dst[i]) says which bytes to copy before they are appended to; otherwise the pair is (-1, -1).  Fresh
  *                          pages are the lowest free ones, in the order of i (a sequence's own page before its new ones).
  *                          status: device int32 [2] = { pages that are lacking (2^29 at most), what is left of the free pages }.  If pages (or entries of a table row)
- *                          are lacking, nothing else has changed, and the pairs are all (-1, -1).  A sequence stands in the list once;
- *                          n <= 4096.
+ *                          are lacking, nothing else has changed, and the pairs are all (-1, -1): nothing may be appended then, not even
+ *                          to a last page with room, which may still be shared.  A sequence stands in the list once; n <= 4096.
+ *                          Every holder of a shared last page that grows in one call takes a page, also the last one of them: the count
+ *                          of the page that they leave falls to 0.  It is not among status's free pages, but free for the next call: the
+ *                          bytes have to be copied (rtp_kv_pages_copy on the same stream) before any other call on the map.
  *   rtp_kv_pages_fork      sequence dst_seq[i], whose row holds no page, shares the pages of the first len[i] tokens of src_seq[i].  A
  *                          source may be shared any number of times; a destination is no other's source or destination.  n <= 65535.
  *   rtp_kv_pages_truncate  sequence seq[i] keeps the pages of its first keep_len[i] tokens (keep_len NULL: none) and releases the
  *                          rest of its row, for a rejected draft or a sequence that has ended.  n <= 65535.
  *   rtp_kv_pages_compact   moves the pages in use to the front of the pool: with U pages in use, the r-th free page below U takes
  *                          the r-th page in use from the top, r = 0 .. moves - 1.  Table and counts are rewritten; the pairs are in
- *                          move_src / move_dst (int32 [n_pages], the first `moves` of each), status = { U, moves }.
+ *                          move_src / move_dst (int32 [n_pages], the first `moves` of each), status = { U, moves }.  The bytes have to
+ *                          be copied before any other call on the map and before anything reads or writes the cache by its table.
  *   rtp_kv_pages_copy      copies pages src[i] -> dst[i], i < n (and i < *count, device int32, if count is not NULL), in every
  *                          pool: page p of head h of a pool is the page_bytes bytes at base + h * head_stride + p * page_stride (bytes, multiples
  *                          of 16).  Pairs with an id outside [0, n_pages) are passed over.  No destination is another pair's source

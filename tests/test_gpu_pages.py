@@ -257,3 +257,26 @@ def test_copies_that_stream():
         assert all(torch.equal(p, w) for p, w in zip(pools, want)), count
         for p in pools:
             p.copy_(p.flip(0))                         # (other bytes for the next list)
+
+
+def test_a_page_that_all_its_holders_leave():
+    """The bytes are copied before the page is handed out again; a call whose pages are lacking leaves it shared."""
+    print("[case] pages, left by all holders", flush=True)
+    both = Both(5, 3, 6, 16)
+    pool = torch.randint(0, 256, (2, 6, 64), dtype=torch.uint8, device=DEV)
+    old = pool.clone()
+    both.extend([0], [0], [20])
+    both.fork([0, 0], [1, 2], [20, 20])
+    src, dst, status = both.extend([0, 1, 2], [20] * 3, [21] * 3)
+    rtp.rtp_kv_pages_copy(rtp.page_pools([pool]), 6, src, dst, 3)
+    assert both.refs[1].item() == 0 and status == [0, 1]
+    both.extend([3], [0], [17])
+    assert both.table[3].tolist() == [1, 5, -1]
+    pool[:, 1] = 0                                     # (its new owner writes)
+    for p in (2, 3, 4):
+        assert torch.equal(pool[:, p], old[:, 1])
+    both.truncate([3], None)
+    both.fork([0, 0], [3, 4], [20, 20])
+    before = both.table.clone(), both.refs.clone()
+    assert both.extend([0, 3, 4], [21, 20, 20], [22, 21, 21])[2] == [1, 2]
+    assert torch.equal(both.table, before[0]) and torch.equal(both.refs, before[1])

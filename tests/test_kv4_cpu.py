@@ -343,3 +343,18 @@ def test_nothing_to_do_asks_for_nothing():
     assert lib.rtp_local_attn_kv4(C.byref(every), vp(A), C.byref(cache), vp(A), 2, 1 << 26, vp(A), None, None, 0, None) == rtp.RTP_OK
     assert lib.rtp_sparse_attn_decode_kv4(C.byref(none), vp(A), C.byref(cache), vp(A), 1 << 20, vp(A), 1 << 20, 2, vp(A), None, None, 0,
                                           None) == rtp.RTP_OK
+
+
+def test_a_page_that_all_its_holders_leave():
+    """Every holder of a shared last page that grows takes a page; the one they leave is the next call's first, not this one's."""
+    m = Pages(4, 3, 6, 16)
+    assert m.extend([0], [0], [20]) == ([(-1, -1)], [0, 4])
+    m.fork([0, 0], [1, 2], [20, 20])
+    assert m.extend([0, 1, 2], [20] * 3, [21] * 3) == ([(1, 2), (1, 3), (1, 4)], [0, 1])
+    assert m.refs.tolist() == [3, 0, 1, 1, 1, 0]
+    assert m.extend([3], [0], [17]) == ([(-1, -1)], [0, 0]) and m.table[3].tolist() == [1, 5, -1]
+    # three holders and two free pages: one is lacking
+    m = Pages(4, 3, 4, 16)
+    m.extend([0], [0], [20])
+    m.fork([0, 0], [1, 2], [20, 20])
+    assert m.extend([0, 1, 2], [20] * 3, [21] * 3) == ([(-1, -1)] * 3, [1, 2])
