@@ -533,7 +533,8 @@ int32_t rtp_local_attn_ring(const rtp_layer_desc* layer, const void* q,
  * codes of sign, 2 exponent bits and 1 mantissa bit: +-{0, .5, 1, 1.5, 2, 3, 4, 6}.  rtp_kv4_append chooses, with
  * amax = max |x| of the block = (1 + M) 2^(E - 127),  s = max(2, E - 2 + [M >= 0.75]),  and rounds x 2^(127 - s) to the nearest
  * code, ties to the even one: the largest value of a block lies in [3.5, 7) steps and is off by at most half a step of the
- * codes, like every other (a bf16 maximum above 1.75 * 2^127 rounds up to 2^128 and reads as infinite).  A block that holds an
+ * codes, like every other.  (From 1.75 * 2^127 on a bf16 maximum rounds up to 2^128 and reads as infinite; from 57344 on an fp16 maximum
+ * rounds up to 65536, which the attention takes as it is and rtp_kv4_read gives back as infinite.)  A block that holds an
  * infinity or a NaN gets s = 255, and all its values read as NaN.
  *
  * Position t of sequence b lives in slot r = t % page_size of pool page P = page_table[b * pt_stride + t / page_size]:

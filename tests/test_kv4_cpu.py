@@ -345,6 +345,13 @@ def test_nothing_to_do_asks_for_nothing():
                                           None) == rtp.RTP_OK
 
 
+def test_largest_values_by_hand():
+    """Where a block's maximum rounds up beyond the 16-bit types: 57344 and 1.75 * 2^127 are halfway between 3 and 4 steps."""
+    assert _one_block([57312.0])[2] == [49152.0] and _one_block([57344.0])[2] == [65536.0] and _one_block([65504.0])[2] == [65536.0]
+    top = 2.0 ** 127
+    assert _one_block([1.7421875 * top])[2] == [1.5 * top] and _one_block([1.75 * top])[2] == [2 * top]
+
+
 def test_a_page_that_all_its_holders_leave():
     """Every holder of a shared last page that grows takes a page; the one they leave is the next call's first, not this one's."""
     m = Pages(4, 3, 6, 16)
