@@ -5,12 +5,13 @@
 // over the tokens n of the set, K and V as the values that their codes stand for.
 //
 // Bound: 136 bytes per token and KV head.  At that size the vector ALU is as near a limit as HBM is, so both products go to the matrix
-// cores, 32 tokens (two tiles of 16) per wave and step:
-//   S = K q^T    v_mfma_f32_16x16x32_bf16, A = 16 tokens: lane (token c, quarter g) holds the dims 32 g .. + 31 of its token -- one
-//                16-byte load, one scale -- as bf16, which every code times its scale is exactly.  B = the queries in 8 columns.
+// cores, 32 tokens (two tiles of 16) per wave and step.  A token's record comes from memory as one whole line, eight lanes of 16 bytes,
+// and is turned into the operands in the wave's own LDS (kv4_turn; loaded in operand order every line would be touched twice):
+//   S = K q^T    v_mfma_f32_16x16x32_bf16, A = 16 tokens: lane (token c, quarter g) has the dims 32 g .. + 31 of its token -- 16 bytes
+//                of codes, one scale -- as bf16, which every code times its scale is exactly.  B = the queries in 8 columns.
 //   O += P V     A = P, whose rows are the columns of S: lane (head c, rows g) has the tokens 4 g + i of both tiles in registers and
-//                takes them for the k positions 8 g .. + 7, so no probability changes its lane.  B = V: lane (c, g) loads the dims
-//                8 c .. + 7 (one word) of the tokens 4 g + i, and pairs of converted values are regrouped to pairs of tokens.
+//                takes them for the k positions 8 g .. + 7, so no probability changes its lane.  B = V: lane (c, g) has the dims
+//                8 c .. + 7 (one word of codes) of the tokens 4 g + i, and pairs of converted values are regrouped to pairs of tokens.
 // A GQA group has at most 8 heads, so the other 8 columns and rows are free.  They carry what 16 bits lose: P is the sum of its
 // bf16 rounding (rows 0 - 7) and the bf16 rounding of the rest (rows 8 - 15; the columns 8 - 15 of S repeat the heads, so the lane
 // that needs the rest has p itself), and an fp16 query is split over the columns the same way.  P keeps 16 bits of mantissa thereby,
@@ -19,7 +20,7 @@
 // Work split: a unit (sequence and KV head, or sequence and retrieval head) is cut into items, an item goes to a workgroup of eight or
 // four waves, which leaves a partial (max, sum, 128 outputs) per head for the merge launch, or the result where a unit is one item.
 //
-// Measured: 8 contexts of 131072 tokens, 8 KV heads (1.14 GB) 181 us, 6.3 TB/s; windows of 8192 of 32 sequences (219 MB) 45 us, 4.9; 256
+// Measured: 8 contexts of 131072 tokens, 8 KV heads (1.14 GB) 180 us, 6.3 TB/s; windows of 8192 of 32 sequences (219 MB) 45 us, 4.9; 256
 // rows of 200 to 30000 selected tokens (222 MB) 56 + 4 us.  With the products left out the loads alone take 167 and 36 us for the
 // first two: some 200 vector instructions per 32 tokens are what is between.  Two rows of 100 selected tokens take 5 us, an empty launch 3.
 #include "attn_decode_shared.h"
