@@ -7,8 +7,8 @@
 // Bound: the counts (4 bytes a page) and the table entries concerned, i.e. the launch's latency, and the bytes of the copied pages.
 // Ranks of free or used pages come from bit masks of 64 pages, a workgroup's word per thread: 65536 pages are one workgroup (one launch,
 // 256 KB of counts), larger pools leave masks and counts per workgroup in the workspace for a second launch.
-// Measured (us; an empty launch is 3): release of 64 rows 3.9, fork of 64 4.0, growth of 64 sequences with 64 copies 8.1 -- a chain: lengths,
-// table, counts, two prefix sums, entries --, moves of 4096 pages 6.3, the table rewritten 4.1, 983 pages of 256 KB copied 93, 5.5 TB/s.
+// Measured (us; an empty launch is 3): release of 64 rows 3.9, fork of 64 4.0, growth of 64 sequences with 64 copies 8.0 -- a chain: lengths,
+// table, counts, two prefix sums, entries --, moves of 4096 pages 5.0, the table rewritten 4.1, 983 pages of 256 KB copied 93, 5.5 TB/s.
 #include "common.h"
 
 namespace rtp {
