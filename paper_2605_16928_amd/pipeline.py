@@ -359,7 +359,10 @@ class Kv4DecodeRun(DecodeRun):
 
     # ---- the step -------------------------------------------------------------------------------
     def append(self, k_new, v_new, start, count=None):
-        """New tokens [B, T, n_kv_heads, 128] at positions start[b] (device int32)."""
+        """New tokens [B, T, n_kv_heads, 128], K and V alike in their strides, at positions start[b] (device int32)."""
+        if k_new.shape != v_new.shape or k_new.stride() != v_new.stride() or tuple(k_new.shape[2:]) != (self.desc.n_kv_heads, 128) \
+                or k_new.stride(3) != 1:
+            raise rtp.RtpError(rtp.RTP_ERR_INVALID_ARG, "Kv4DecodeRun: K and V [B, T, n_kv_heads, 128] of the same strides expected, rows contiguous")
         rtp.rtp_kv4_append(self.desc, self.cache, k_new, v_new, k_new.stride(0), k_new.stride(1), k_new.stride(2), start, count,
                            k_new.shape[0], k_new.shape[1])
 

@@ -365,3 +365,17 @@ def test_a_page_that_all_its_holders_leave():
     m.extend([0], [0], [20])
     m.fork([0, 0], [1, 2], [20, 20])
     assert m.extend([0, 1, 2], [20] * 3, [21] * 3) == ([(-1, -1)] * 3, [1, 2])
+
+
+def test_decode_run_refuses_rows_that_are_laid_out_differently():
+    """One set of strides goes to the library: K and V of different ones would be read from the wrong places."""
+    import torch
+    from paper_2605_16928_amd.pipeline import Kv4DecodeRun
+    run = object.__new__(Kv4DecodeRun)
+    run.desc = _layer()
+    k, fused = torch.zeros((3, 2, 2, 128)), torch.zeros((3, 2, 12, 128))
+    for bad in ((k, fused[:, :, 10:]), (k, k[:, :1]), (k.transpose(0, 1), k), (fused[:, :, 8:11], fused[:, :, 9:12]), (k[..., :64], k[..., :64]),
+                (k.expand(3, 2, 2, 128)[..., :1].expand(3, 2, 2, 128),) * 2):
+        with pytest.raises(rtp.RtpError) as e:
+            run.append(*bad, None)
+        assert e.value.code == rtp.RTP_ERR_INVALID_ARG
