@@ -338,7 +338,10 @@ class Kv4DecodeRun(DecodeRun):
     def grow(self, k_new, v_new, kI_new):
         """T new tokens behind every context: pages, K and V [B, T, n_kv_heads, 128], index keys [n_ret, B, T, 16].  Where pages are
         lacking (status) no context changes."""
+        self._same_layout(k_new, v_new)         # (all is looked at before a page is handed out)
         T = k_new.shape[1]
+        if k_new.shape[0] != self.B or tuple(kI_new.shape) != (self.n_ret, self.B, T, 16) or T < 1:
+            raise rtp.RtpError(rtp.RTP_ERR_INVALID_ARG, f"Kv4DecodeRun: tokens of {self.B} contexts and index keys [{self.n_ret}, {self.B}, T, 16] expected")
         if any(n + T > most for n, most in zip(self.len_most, self.len_limit)):
             raise rtp.RtpError(rtp.RTP_ERR_INVALID_ARG, f"Kv4DecodeRun: no room for {T} more tokens in every context")
         self._extend(self._rows, self.ctx_len, self.ctx_len + T, self.B)
@@ -360,11 +363,14 @@ class Kv4DecodeRun(DecodeRun):
     # ---- the step -------------------------------------------------------------------------------
     def append(self, k_new, v_new, start, count=None):
         """New tokens [B, T, n_kv_heads, 128], K and V alike in their strides, at positions start[b] (device int32)."""
+        self._same_layout(k_new, v_new)
+        rtp.rtp_kv4_append(self.desc, self.cache, k_new, v_new, k_new.stride(0), k_new.stride(1), k_new.stride(2), start, count,
+                           k_new.shape[0], k_new.shape[1])
+
+    def _same_layout(self, k_new, v_new):
         if k_new.shape != v_new.shape or k_new.stride() != v_new.stride() or tuple(k_new.shape[2:]) != (self.desc.n_kv_heads, 128) \
                 or k_new.stride(3) != 1:
             raise rtp.RtpError(rtp.RTP_ERR_INVALID_ARG, "Kv4DecodeRun: K and V [B, T, n_kv_heads, 128] of the same strides expected, rows contiguous")
-        rtp.rtp_kv4_append(self.desc, self.cache, k_new, v_new, k_new.stride(0), k_new.stride(1), k_new.stride(2), start, count,
-                           k_new.shape[0], k_new.shape[1])
 
     def sparse_attn(self, sel_idx=None, sel_count=None, max_sel=None):
         rtp.rtp_sparse_attn_decode_kv4(self.desc, self.w.q, self.cache, self.sel_idx if sel_idx is None else sel_idx, self.stride,

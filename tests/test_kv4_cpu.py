@@ -379,3 +379,16 @@ def test_decode_run_refuses_rows_that_are_laid_out_differently():
         with pytest.raises(rtp.RtpError) as e:
             run.append(*bad, None)
         assert e.value.code == rtp.RTP_ERR_INVALID_ARG
+
+
+def test_decode_run_refuses_growth_before_it_hands_out_pages():
+    import torch
+    from paper_2605_16928_amd.pipeline import Kv4DecodeRun
+    run = object.__new__(Kv4DecodeRun)                  # (no map, no buffers: what passed the checks would fail otherwise)
+    run.desc, run.B, run.n_ret, run.len_most, run.len_limit = _layer(), 3, 2, [5, 9, 0], [9, 13, 4]
+    k, keys = torch.zeros((3, 4, 2, 128)), torch.zeros((2, 3, 4, 16))
+    for bad in ((k[:2], k[:2], keys), (k, k, keys[:, :2]), (k, k, keys[:, :, :1]), (k, k[:, :2], keys), (k[:, :0], k[:, :0], keys[:, :, :0]),
+                (torch.zeros((3, 5, 2, 128)),) * 2 + (torch.zeros((2, 3, 5, 16)),)):
+        with pytest.raises(rtp.RtpError) as e:
+            run.grow(*bad)
+        assert e.value.code == rtp.RTP_ERR_INVALID_ARG
