@@ -656,6 +656,80 @@ int32_t rtp_kv_pages_compact(const rtp_page_map* map, int32_t* move_src, int32_t
 int32_t rtp_kv_pages_copy(const rtp_page_pool* pools, int32_t n_pools, int32_t n_pages, const int32_t* src, const int32_t* dst,
                           int32_t n, const int32_t* count, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * New tokens of a batch over a cache in pages: rotating and storing them, and the attention of all of them at once -- Sec. 3.2 in prefill
+ * (retrieval heads over every earlier token, Sec. 4.2; the other heads over sink + window) and in decode, for sequences of different
+ * lengths in one call: a chunk of a prompt, a draft to be verified, a single token each, side by side.
+ *
+ * rtp_chunk: the new tokens of B sequences, packed without padding.  Row i of q, k, v and the outputs belongs to sequence b with
+ * q_offset[b] <= i < q_offset[b + 1]; the n = q_offset[b + 1] - q_offset[b] new tokens of b (possibly none) are the last ones of its context:
+ * row q_offset[b] + t has position ctx_len[b] - n + t.  q_offset: device int32 [B + 1], ascending; ctx_len: device int32 [B], the new tokens
+ * included.  total_q >= q_offset[B], max_q >= every n and max_ctx >= every ctx_len are host bounds (they size grids and workspaces).
+ * Rows that belong to no sequence are left as they are.  B <= 65535.
+ *
+ * rtp_kv_cache: the 16-bit rows, in the layer's type.  Position t of sequence b lives in slot r = t % page_size of pool page
+ * P = page_table[b * pt_stride + t / page_size], element (kvh, c) at  K + P * page_stride + kvh * head_stride + r * row_stride + c, V alike;
+ * strides in ELEMENTS, multiples of 8, row_stride in [128, 2^24]; pages, rows and heads may be nested in any order but must not overlap.  The
+ * pools of rtp_decode_attention_paged are such a cache with page_stride = page_size * kv_row_stride.  page_size: a power of two in
+ * [16, 2^20].  An entry of page_table outside [0, n_pages) and a position behind pt_stride * page_size are never followed: rtp_kv_append
+ * drops such a token, the attention leaves it out.  Both structs are HOST memory, read during the call.
+ */
+typedef struct rtp_kv_cache {
+  void* K;
+  void* V;
+  int64_t row_stride, page_stride, head_stride;
+  const int32_t* page_table;   /* device int32 [B, pt_stride] */
+  int64_t pt_stride;
+  int32_t page_size;
+  int32_t n_pages;             /* pages of the pool */
+} rtp_kv_cache;
+typedef struct rtp_chunk {
+  const int32_t* q_offset;
+  const int32_t* ctx_len;
+  int32_t B, total_q, max_q;
+  int64_t max_ctx;
+} rtp_chunk;
+/* Rotation of the first rotary_dim values of a row (a multiple of 16, at most 128; the rest stays as it is) by the angles
+ * position * inv_freq[i], i < rotary_dim / 2: the pair (x, y) = (x_i, x_{i + rotary_dim / 2}), or (x_{2i}, x_{2i + 1}) if interleaved, becomes
+ * scale * (x cos - y sin, y cos + x sin).  inv_freq: device fp32.  The product is taken exactly and reduced in fp64 (any position is as
+ * exact as the first); cos, sin and the rotation are fp32, the result is rounded once.  scale 0 => 1. */
+typedef struct rtp_rope {
+  const float* inv_freq;
+  int32_t rotary_dim;
+  int32_t interleaved;
+  float scale;
+} rtp_rope;
+
+/* Stores the new tokens' rows, k rotated, v as it is, and gives q rotated.  q [total_q, n_q_heads, 128], k and v [total_q, n_kv_heads, 128]:
+ * tokens `stride` ELEMENTS apart (multiples of 8, at least a token's rows), 16-byte aligned -- slices of a fused projection.  q may be NULL
+ * (only K and V are stored); q_out may be q itself, with the same stride, but may not overlap q, k or v otherwise.  rope NULL: nothing is rotated, and
+ * q is only copied.  (The index keys are of the rows before rotation: rtp_index_project reads k, which is left as it is.)  A token whose
+ * position is negative is passed over, its row of q_out too.  The pages written to must belong to one sequence each.  No workspace. */
+int32_t rtp_kv_append(const rtp_layer_desc* layer, const rtp_kv_cache* cache, const rtp_chunk* chunk, const rtp_rope* rope,
+                      const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                      void* q_out, int64_t q_out_stride, void* stream);
+
+/* Causal attention of the new tokens over the cache, which holds them already: the query at position m sees the tokens n <= m
+ * (rtp_dense_attn_chunk: of every query head, or of the retrieval heads alone, as rtp_sparse_attn_prefill with p >= 1) or { n < sink } U
+ * { m - window < n <= m } (rtp_local_attn_chunk: of every other head).  q [total_q, n_q_heads, 128] with tokens q_stride elements apart; out
+ * [total_q, n_q_heads, 128] contiguous, not overlapping q; lse fp32 [total_q, n_q_heads] or NULL.  Rows of heads that the call does not serve are left as
+ * they are.  A row that sees no token writes zeros and lse = -inf; what a row does not see (NaN and infinities there too) does not
+ * change it.  The _kv4 forms read the 4-bit cache and take K and V as rtp_kv4_read gives them.
+ * A workspace for (B, total_q, max_q, max_ctx) serves every call with smaller ones. */
+#define RTP_HEADS_ALL        0
+#define RTP_HEADS_RETRIEVAL  1
+size_t rtp_dense_attn_chunk_workspace_bytes(const rtp_layer_desc* layer, int32_t B, int32_t total_q, int32_t max_q, int64_t max_ctx,
+                                            int32_t heads);
+int32_t rtp_dense_attn_chunk(const rtp_layer_desc* layer, const void* q, int64_t q_stride, const rtp_kv_cache* cache,
+                             const rtp_chunk* chunk, int32_t heads, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+int32_t rtp_dense_attn_chunk_kv4(const rtp_layer_desc* layer, const void* q, int64_t q_stride, const rtp_kv4_cache* cache,
+                                 const rtp_chunk* chunk, int32_t heads, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+size_t rtp_local_attn_chunk_workspace_bytes(const rtp_layer_desc* layer, int32_t B, int32_t total_q, int32_t max_q, int64_t max_ctx);
+int32_t rtp_local_attn_chunk(const rtp_layer_desc* layer, const void* q, int64_t q_stride, const rtp_kv_cache* cache,
+                             const rtp_chunk* chunk, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+int32_t rtp_local_attn_chunk_kv4(const rtp_layer_desc* layer, const void* q, int64_t q_stride, const rtp_kv4_cache* cache,
+                                 const rtp_chunk* chunk, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -77,6 +77,22 @@ bool strides_apart(int64_t s0, int64_t n0, int64_t s1, int64_t n1, int64_t unit)
   return s0 <= s1 ? (s1 - unit) / s0 >= n0 - 1 : (s0 - unit) / s1 >= n1 - 1;
 }
 
+// Rows of 128 at the multiples of three strides, nested in any order, do not overlap.
+bool rows_apart(int64_t s0, int64_t n0, int64_t s1, int64_t n1, int64_t s2, int64_t n2) {
+  int64_t s[3] = {s0, s1, s2}, n[3] = {n0, n1, n2}, span = kHeadDim;
+  for (int round = 0; round < 3; ++round) {    // the smallest stride that is left has to pass what lies inside it
+    int i = -1;
+    for (int k = 0; k < 3; ++k)
+      if (n[k] > 1 && (i < 0 || s[k] < s[i])) i = k;
+    if (i < 0) return true;
+    if (s[i] < span) return false;
+    if (s[i] > (((int64_t)1 << 62) - span) / (n[i] - 1)) return (n[0] > 1) + (n[1] > 1) + (n[2] > 1) == 1;
+    span += s[i] * (n[i] - 1);
+    n[i] = 1;
+  }
+  return true;
+}
+
 int32_t check_launch(const char* who) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(RTP_ERR_HIP, "%s: launch failed: %s", who, hipGetErrorString(e));

@@ -16,6 +16,7 @@
 // are adjacent in the grid so that they meet in L2; late (long) query tiles are scheduled first.
 #include "common.h"
 #include "index_project.h"
+#include "mfma_tile.h"
 #include "prefill_scan.h"
 
 #include <algorithm>
@@ -29,13 +30,6 @@ constexpr int kPfQ = 128;          // queries per workgroup
 constexpr int kPwQ = 256;          // of the wide kernel
 constexpr int kPfK = 64;           // keys per tile
 constexpr int kPfPart = kHeadDim + 4;   // floats per partial row: max, sum, 2 pad, unnormalised output[128]
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 struct PrefillArgs {
   const uint16_t* q;
@@ -134,30 +128,6 @@ constexpr int kSelRing = 4, kSelRingWide = 8;   // index-key tiles in flight per
 __device__ __forceinline__ int sel_q_of_t(float tt) {       // tt = M - s >= 0
   return (int)fminf(tt * kSelScale, (float)kSelQMax);
 }
-
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-  const f32x2 f = {a, b};
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));
-}
-// The attention tensors' element type is a template flag of the kernels (F16 = IEEE binary16, else bf16): two
-// floats rounded (nearest even) and packed, and the 32 x 32 x 16 MFMA on 16-bit operands with fp32 accumulation.
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-template <bool F16> __device__ __forceinline__ uint32_t pack16(float a, float b) {
-  if constexpr (F16) {
-    const f32x2 f = {a, b};
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, f16x2));
-  } else {
-    return pack_bf16(a, b);
-  }
-}
-template <bool F16> __device__ __forceinline__ f32x16 mfma32(const u32x4 a, const u32x4 b, const f32x16 c) {
-  if constexpr (F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-  else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
 
 // Largest of 16 matrix-core results, none NaN: medians for the first of each half (they make the compiler wait for the
 // matrix core, which it does not do for operands of an assembly statement), then three-operand maxima -- the compiler

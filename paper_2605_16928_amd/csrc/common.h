@@ -29,6 +29,8 @@ inline float softmax_scale_of(const rtp_layer_desc* L) {
 inline float index_scale_of(const rtp_layer_desc* L) { return L->index_scale != 0.f ? L->index_scale : 1.f; }
 // n0 x n1 pieces of `unit` bytes at multiples of the strides s0 and s1 do not overlap (nested either way).
 bool strides_apart(int64_t s0, int64_t n0, int64_t s1, int64_t n1, int64_t unit);
+// Rows of 128 elements at the multiples of three strides, nested in any order, do not overlap.
+bool rows_apart(int64_t s0, int64_t n0, int64_t s1, int64_t n1, int64_t s2, int64_t n2);
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 // Per-launch timing (rtp_profile_start / rtp_profile_stop): while it is on, every kernel launch of the library

@@ -45,4 +45,26 @@ __device__ __forceinline__ float kv4_scale(uint32_t word, int i) {
   return __uint_as_float(((word >> (8 * i)) & 255u) << 23);      // (one instruction: a shift with a byte select)
 }
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+// Eight codes of one block as 16-bit values (bf16: exact; fp16: one rounding where the value is none of fp16's).
+template <bool F16>
+__device__ __forceinline__ u32x4 decode8(uint32_t codes, float scale) {
+  u32x4 r;
+  if constexpr (F16) {
+    const f32x2_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 1);
+    const f32x2_t c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 3);
+    r[0] = f32_to_f16_rne(a.x) | ((uint32_t)f32_to_f16_rne(a.y) << 16);
+    r[1] = f32_to_f16_rne(b.x) | ((uint32_t)f32_to_f16_rne(b.y) << 16);
+    r[2] = f32_to_f16_rne(c.x) | ((uint32_t)f32_to_f16_rne(c.y) << 16);
+    r[3] = f32_to_f16_rne(d.x) | ((uint32_t)f32_to_f16_rne(d.y) << 16);
+  } else {
+    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0));
+    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1));
+    r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
+    r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
+  }
+  return r;
+}
+
 }  // namespace rtp

@@ -17,10 +17,8 @@
 namespace rtp {
 
 constexpr int kStoreThreads = 256;
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
-typedef float f32x2_t __attribute__((ext_vector_type(2)));
 
 struct Kv4StoreArgs {
   Kv4Cache c;
@@ -64,26 +62,6 @@ __device__ __forceinline__ uint32_t encode8(const u32x4 x, uint32_t* scale) {
     codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2_t, x3), f, 3);
   }
   return finite ? codes : 0u;
-}
-
-// Eight codes of one block as 16-bit values (bf16: exact; fp16: one rounding where the value is none of fp16's).
-template <bool F16>
-__device__ __forceinline__ u32x4 decode8(uint32_t codes, float scale) {
-  u32x4 r;
-  if constexpr (F16) {
-    const f32x2_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 1);
-    const f32x2_t c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 3);
-    r[0] = f32_to_f16_rne(a.x) | ((uint32_t)f32_to_f16_rne(a.y) << 16);
-    r[1] = f32_to_f16_rne(b.x) | ((uint32_t)f32_to_f16_rne(b.y) << 16);
-    r[2] = f32_to_f16_rne(c.x) | ((uint32_t)f32_to_f16_rne(c.y) << 16);
-    r[3] = f32_to_f16_rne(d.x) | ((uint32_t)f32_to_f16_rne(d.y) << 16);
-  } else {
-    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0));
-    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1));
-    r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
-    r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
-  }
-  return r;
 }
 
 // The group of 16 lanes -> (sequence, KV head, positions 4 * quad .. + 3); false: nothing there.
@@ -205,22 +183,6 @@ int32_t check_kv4_cache(const char* who, const rtp_layer_desc* L, const rtp_kv4_
   *out = Kv4Cache{(uint8_t*)c->codes, (uint8_t*)c->scales, c->code_head_stride, c->scale_head_stride, (uint32_t)(c->code_page_stride / 16),
                   (uint32_t)(c->scale_page_stride / 16), c->page_table, c->pt_stride, sh, c->n_pages};
   return RTP_OK;
-}
-
-// Rows of 128 at the multiples of three strides, nested in any order, do not overlap.
-static bool rows_apart(int64_t s0, int64_t n0, int64_t s1, int64_t n1, int64_t s2, int64_t n2) {
-  int64_t s[3] = {s0, s1, s2}, n[3] = {n0, n1, n2}, span = kHeadDim;
-  for (int round = 0; round < 3; ++round) {    // the smallest stride that is left has to pass what lies inside it
-    int i = -1;
-    for (int k = 0; k < 3; ++k)
-      if (n[k] > 1 && (i < 0 || s[k] < s[i])) i = k;
-    if (i < 0) return true;
-    if (s[i] < span) return false;
-    if (s[i] > (((int64_t)1 << 62) - span) / (n[i] - 1)) return (n[0] > 1) + (n[1] > 1) + (n[2] > 1) == 1;
-    span += s[i] * (n[i] - 1);
-    n[i] = 1;
-  }
-  return true;
 }
 
 static int32_t store_args(const char* who, const rtp_layer_desc* layer, const rtp_kv4_cache* cache, const void* k, const void* v,

@@ -38,9 +38,12 @@ EXPORTS = [
     "rtp_dense_attn_kv4_workspace_bytes", "rtp_dense_attn_kv4",
     "rtp_kv_pages_workspace_bytes", "rtp_kv_pages_init", "rtp_kv_pages_extend", "rtp_kv_pages_fork",
     "rtp_kv_pages_truncate", "rtp_kv_pages_compact", "rtp_kv_pages_copy",
+    "rtp_kv_append", "rtp_dense_attn_chunk_workspace_bytes", "rtp_dense_attn_chunk", "rtp_dense_attn_chunk_kv4",
+    "rtp_local_attn_chunk_workspace_bytes", "rtp_local_attn_chunk", "rtp_local_attn_chunk_kv4",
 ]
 RTP_SIDE_QUERY, RTP_SIDE_KEY = 0, 1
 RTP_DTYPE_BF16, RTP_DTYPE_FP16 = 0, 1
+RTP_HEADS_ALL, RTP_HEADS_RETRIEVAL = 0, 1
 
 
 class RtpError(RuntimeError):
@@ -99,6 +102,78 @@ def kv4_cache(codes, scales, page_table) -> rtp_kv4_cache:
     c.n_heads, c.n_seqs = codes.shape[0], page_table.shape[0]
     c._keepalive = (codes, scales, page_table)
     return c
+
+
+class rtp_kv_cache(C.Structure):
+    _fields_ = [
+        ("K", C.c_void_p), ("V", C.c_void_p), ("row_stride", C.c_int64), ("page_stride", C.c_int64), ("head_stride", C.c_int64),
+        ("page_table", C.c_void_p), ("pt_stride", C.c_int64), ("page_size", C.c_int32), ("n_pages", C.c_int32),
+    ]
+    n_heads = n_seqs = 1 << 31                      # as in rtp_kv4_cache
+
+
+class rtp_chunk(C.Structure):
+    _fields_ = [("q_offset", C.c_void_p), ("ctx_len", C.c_void_p), ("B", C.c_int32), ("total_q", C.c_int32), ("max_q", C.c_int32),
+                ("max_ctx", C.c_int64)]
+
+
+class rtp_rope(C.Structure):
+    _fields_ = [("inv_freq", C.c_void_p), ("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("scale", C.c_float)]
+
+
+def kv_cache(K, V, page_table) -> rtp_kv_cache:
+    """Descriptor of a 16-bit cache in torch tensors: K and V [n_kv_heads, n_pages, page_size, 128] of the same strides (any but the
+    last's: a pool with the pages, or the tokens, in front as a permuted view), page_table int32 [B, pages].  Calls over more KV heads or
+    sequences than these tensors hold are refused."""
+    ok = K.dim() == 4 and K.shape[3] == 128 and min(K.shape) > 0 and K.element_size() == 2 and K.stride(3) == 1 and K.dtype == V.dtype \
+        and K.shape == V.shape and K.stride() == V.stride() and page_table.dim() == 2 and _int32(page_table) \
+        and K.device == V.device == page_table.device
+    if not ok:
+        raise RtpError(RTP_ERR_INVALID_ARG, "kv_cache: 16-bit K and V [heads, pages, page_size, 128] of the same strides, rows contiguous, and a "
+                                            "contiguous int32 page_table [B, pages], on one device")
+    c = rtp_kv_cache(K.data_ptr(), V.data_ptr(), K.stride(2), K.stride(1), K.stride(0), page_table.data_ptr(), page_table.shape[1], K.shape[2],
+                     K.shape[1])
+    c.n_heads, c.n_seqs = K.shape[0], page_table.shape[0]
+    c._keepalive = (K, V, page_table)
+    return c
+
+
+def chunk_desc(q_offset, ctx_len, total_q: int, max_q: int, max_ctx: int) -> rtp_chunk:
+    """Descriptor of a batch of new tokens: q_offset int32 [B + 1], ctx_len int32 [B], and the host's bounds."""
+    if q_offset.dim() != 1 or ctx_len.dim() != 1 or not _int32(q_offset) or not _int32(ctx_len) or q_offset.shape[0] != ctx_len.shape[0] + 1 \
+            or q_offset.device != ctx_len.device:
+        raise RtpError(RTP_ERR_INVALID_ARG, "chunk_desc: contiguous int32 q_offset [B + 1] and ctx_len [B] on one device expected")
+    c = rtp_chunk(q_offset.data_ptr(), ctx_len.data_ptr(), ctx_len.shape[0], total_q, max_q, max_ctx)
+    c._keepalive = (q_offset, ctx_len)
+    return c
+
+
+def rope_desc(inv_freq, interleaved: bool = False, scale: float = 0.0) -> rtp_rope:
+    """Descriptor of a rotation: inv_freq fp32 [rotary_dim / 2]."""
+    if inv_freq.dim() != 1 or str(inv_freq.dtype) != "torch.float32" or not inv_freq.is_contiguous():
+        raise RtpError(RTP_ERR_INVALID_ARG, "rope_desc: contiguous float32 inv_freq [rotary_dim / 2] expected")
+    r = rtp_rope(inv_freq.data_ptr(), 2 * inv_freq.shape[0], 1 if interleaved else 0, scale)
+    r._keepalive = (inv_freq,)
+    return r
+
+
+def _on_one_device(who: str, descriptors, tensors):
+    """The tensors of a call, and those that its descriptors were made of, lie on the current device, whose stream takes the launches."""
+    held = [t for d in descriptors for t in getattr(d, "_keepalive", ())] + [t for t in tensors if hasattr(t, "device")]
+    if not held:
+        return
+    import torch
+    device = torch.device("cuda", torch.cuda.current_device())
+    for t in held:
+        if t.device != device:
+            raise RtpError(RTP_ERR_INVALID_ARG, f"{who}: a tensor on {t.device}, the current device is {device}")
+
+
+def _rows(who: str, t, total: int, heads: int, name: str):
+    """A tensor of packed rows [total or more, heads, 128] whose tokens are a stride apart and whose heads are not."""
+    if hasattr(t, "shape") and (t.dim() != 3 or t.shape[0] < total or tuple(t.shape[1:]) != (heads, 128) or t.element_size() != 2
+                                or (total and t.stride()[1:] != (128, 1))):
+        raise RtpError(RTP_ERR_INVALID_ARG, f"{who}: {name} of 16 bits [{total} or more, {heads}, 128] expected, a token's rows contiguous")
 
 
 class rtp_page_map(C.Structure):
@@ -243,6 +318,18 @@ def lib() -> C.CDLL:
         getattr(L, name + "_workspace_bytes").argtypes = [dp, i32, i64]
         getattr(L, name).restype = i32
         getattr(L, name).argtypes = [dp, vp, cp, vp, i32, i64, vp, vp, vp, sz, vp]
+    kp, chp, rp = C.POINTER(rtp_kv_cache), C.POINTER(rtp_chunk), C.POINTER(rtp_rope)
+    L.rtp_kv_append.restype = i32
+    L.rtp_kv_append.argtypes = [dp, kp, chp, rp, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+    L.rtp_dense_attn_chunk_workspace_bytes.restype = sz
+    L.rtp_dense_attn_chunk_workspace_bytes.argtypes = [dp, i32, i32, i32, i64, i32]
+    L.rtp_local_attn_chunk_workspace_bytes.restype = sz
+    L.rtp_local_attn_chunk_workspace_bytes.argtypes = [dp, i32, i32, i32, i64]
+    for suffix, ptr in (("", kp), ("_kv4", cp)):
+        getattr(L, "rtp_dense_attn_chunk" + suffix).restype = i32
+        getattr(L, "rtp_dense_attn_chunk" + suffix).argtypes = [dp, vp, i64, ptr, chp, i32, vp, vp, vp, sz, vp]
+        getattr(L, "rtp_local_attn_chunk" + suffix).restype = i32
+        getattr(L, "rtp_local_attn_chunk" + suffix).argtypes = [dp, vp, i64, ptr, chp, vp, vp, vp, sz, vp]
     mp = C.POINTER(rtp_page_map)
     L.rtp_kv_pages_workspace_bytes.restype = sz
     L.rtp_kv_pages_workspace_bytes.argtypes = [mp, i32]
@@ -588,3 +675,48 @@ def rtp_kv_pages_copy(pools, n_pages, src, dst, n, count=None, stream=None):
     if n_pages > pools.n_pages:
         raise RtpError(RTP_ERR_INVALID_ARG, f"rtp_kv_pages_copy: n_pages = {n_pages}, the pools have {pools.n_pages}")
     _check(lib().rtp_kv_pages_copy(pools, pools.n_pools, n_pages, _ptr(src), _ptr(dst), n, _ptr(count), _stream(stream)))
+
+
+def rtp_kv_append(layer, cache, chunk, rope, q, q_stride, k, k_stride, v, v_stride, q_out, q_out_stride, stream=None):
+    who = "rtp_kv_append"
+    _held(who, layer, cache, chunk.B)
+    _on_one_device(who, (cache, chunk, rope), (q, k, v, q_out))
+    for t, heads, name in ((q, layer.n_q_heads, "q"), (k, layer.n_kv_heads, "k"), (v, layer.n_kv_heads, "v"), (q_out, layer.n_q_heads, "q_out")):
+        _rows(who, t, chunk.total_q, heads, name)
+    _check(lib().rtp_kv_append(C.byref(layer), C.byref(cache), C.byref(chunk), None if rope is None else C.byref(rope), _ptr(q), q_stride,
+                               _ptr(k), k_stride, _ptr(v), v_stride, _ptr(q_out), q_out_stride, _stream(stream)))
+
+
+def rtp_dense_attn_chunk_workspace_bytes(layer, B, total_q, max_q, max_ctx, heads) -> int:
+    return lib().rtp_dense_attn_chunk_workspace_bytes(C.byref(layer), B, total_q, max_q, max_ctx, heads)
+
+
+def rtp_local_attn_chunk_workspace_bytes(layer, B, total_q, max_q, max_ctx) -> int:
+    return lib().rtp_local_attn_chunk_workspace_bytes(C.byref(layer), B, total_q, max_q, max_ctx)
+
+
+def _chunk_attn(who, layer, q, q_stride, cache, chunk, heads, out, lse, ws, stream):
+    _held(who, layer, cache, chunk.B)
+    _on_one_device(who, (cache, chunk), (q, out, lse, ws))
+    _rows(who, q, chunk.total_q, layer.n_q_heads, "q")
+    _rows(who, out, chunk.total_q, layer.n_q_heads, "out")
+    if hasattr(lse, "numel") and lse.numel() < chunk.total_q * layer.n_q_heads:
+        raise RtpError(RTP_ERR_INVALID_ARG, f"{who}: lse [{chunk.total_q}, {layer.n_q_heads}] expected")
+    _check(getattr(lib(), who)(C.byref(layer), _ptr(q), q_stride, C.byref(cache), C.byref(chunk), *heads, _ptr(out), _ptr(lse), _ptr(ws),
+                               _nbytes(ws), _stream(stream)))
+
+
+def rtp_dense_attn_chunk(layer, q, q_stride, cache, chunk, heads, out, lse, ws, stream=None):
+    _chunk_attn("rtp_dense_attn_chunk", layer, q, q_stride, cache, chunk, (heads,), out, lse, ws, stream)
+
+
+def rtp_dense_attn_chunk_kv4(layer, q, q_stride, cache, chunk, heads, out, lse, ws, stream=None):
+    _chunk_attn("rtp_dense_attn_chunk_kv4", layer, q, q_stride, cache, chunk, (heads,), out, lse, ws, stream)
+
+
+def rtp_local_attn_chunk(layer, q, q_stride, cache, chunk, out, lse, ws, stream=None):
+    _chunk_attn("rtp_local_attn_chunk", layer, q, q_stride, cache, chunk, (), out, lse, ws, stream)
+
+
+def rtp_local_attn_chunk_kv4(layer, q, q_stride, cache, chunk, out, lse, ws, stream=None):
+    _chunk_attn("rtp_local_attn_chunk_kv4", layer, q, q_stride, cache, chunk, (), out, lse, ws, stream)
