@@ -11,131 +11,11 @@
 //
 // A wave computes the transposed scores S^T = K Q^T of 32 keys (v_mfma_f32_32x32x16): lane (g, r) then holds 16 keys of ONE row, the softmax is
 // per lane, and the probabilities, rounded to 16 bits, are in place as the B operand of O^T = V^T P^T.
-#include "kv16_cache.h"
-#include "chunk_plan.h"
-#include "kv4_cache.h"
-#include "mfma_tile.h"
+#include "chunk_wide.h"
 
 #include <algorithm>
-#include <type_traits>
 
 namespace rtp {
-
-constexpr int kCkThreads = 512;
-constexpr int kCkWaves = kCkThreads / 64;
-constexpr int kCkK = 64;                       // keys per tile
-constexpr int kCkPart = kHeadDim + 4;          // floats per partial row: reference, sum, sum of unrounded probabilities, pad, outputs
-constexpr int kCkTileBytes = 2 * kCkK * kHeadDim * 2;
-constexpr int kCkStages = 3;
-
-struct ChunkArgs {
-  ChunkShape shape;
-  const uint16_t* q;
-  int64_t q_stride;
-  Kv16Cache c16;
-  Kv4Cache c4;
-  const int32_t* q_offset;
-  const int32_t* ctx_len;
-  int32_t n_q_heads, n_served;
-  float scale, scale_log2;
-  uint16_t* out;
-  float* lse;
-  float* part;                 // [units of cut tiles, part_rows, kCkPart]
-  int32_t part_rows;           // rows of a partial result: what a tile can have
-  int32_t* plan;               // B > 64: what chunk_plan_kernel leaves, kPlanHead ints and three lists of B + 1
-  int32_t run;                 // units in a row that go to one die
-  int32_t f16;
-};
-enum { kPlanCandidate = 0, kPlanLongest = 1, kPlanHead = 4 };
-
-// The plan of a batch of up to 64 sequences, a sequence to a lane, or of a longer one, from memory.
-struct ChunkLane {
-  int n, q0, ctx;              // new tokens, their first row, context
-  int tiles, key_tiles;
-};
-__device__ __forceinline__ ChunkLane chunk_lane(const ChunkArgs& a, int b) {
-  ChunkLane s = {0, 0, 0, 0, 1};
-  if (b < a.shape.B) {
-    const NewTokens nt = new_tokens(a.q_offset, b, a.shape.total_q, a.shape.max_q);
-    s.n = nt.n;
-    s.q0 = nt.q0;
-    s.ctx = max(a.ctx_len[b], 0);
-    s.tiles = chunk_tiles(a.shape, nt.n);
-    s.key_tiles = nt.n > 0 ? chunk_key_tiles(a.shape, nt.n, s.ctx) : 1;
-  }
-  return s;
-}
-// Lane i adds up candidate i over the sequences that the wave's lanes hold.
-__device__ __forceinline__ void chunk_add_up(const ChunkLane& s, int lanes, int longest, uint32_t magic, uint64_t* units, uint64_t* split_units) {
-  const int candidate = chunk_candidate(threadIdx.x & 63);
-  for (int k = 0; k < lanes; ++k) {
-    const int tiles = __builtin_amdgcn_readlane(s.tiles, k), kt = __builtin_amdgcn_readlane(s.key_tiles, k);
-    const int S = chunk_splits(kt, longest, candidate, magic);
-    *units += (uint64_t)tiles * (uint32_t)S;
-    *split_units += S > 1 ? (uint64_t)tiles * (uint32_t)S : 0;
-  }
-}
-// The best candidate of the lanes'.
-__device__ __forceinline__ int chunk_best(const ChunkShape& s, uint64_t work, uint64_t units, uint64_t split_units) {
-  uint32_t key = split_units > (uint64_t)s.cap ? 0xffffffffu : (chunk_cost(work, units, split_units, s.n_cu) << 6) | (threadIdx.x & 63);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) key = min(key, (uint32_t)__shfl_xor((int)key, o));
-  return chunk_candidate(key == 0xffffffffu ? 0 : (int)(key & 63u));
-}
-
-// One sequence's place in the plan.
-struct ChunkSpot {
-  int b, rel;                  // rel: unit (or row of cut sequences) inside the sequence; b = -1: there is none
-  int n, q0, ctx, splits, part0;
-};
-// The sequence of unit `at` (ROWS: of the at-th row of a sequence whose tiles are cut), found by the whole wave.
-template <bool ROWS>
-__device__ __forceinline__ ChunkSpot chunk_find(const ChunkArgs& a, int at) {
-  const ChunkShape& s = a.shape;
-  const int lane = threadIdx.x & 63;
-  ChunkSpot spot = {};
-  spot.b = -1;
-  if (s.B <= 64) {
-    const ChunkLane mine = chunk_lane(a, lane);
-    const int longest = max(wave_max_ge_m1(mine.n > 0 ? mine.key_tiles : 1), 1);
-    const uint32_t magic = chunk_magic(longest);
-    uint64_t units = 0, split_units = 0;
-    chunk_add_up(mine, s.B, longest, magic, &units, &split_units);
-    uint64_t work = (uint64_t)(uint32_t)mine.tiles * (uint32_t)mine.key_tiles;
-    work = wave_incl_scan(work);
-    work = ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(work >> 32), 63) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)work, 63);
-    const int S = chunk_splits(mine.key_tiles, longest, chunk_best(s, work, units, split_units), magic);
-    const int own = mine.tiles * S, own_rows = S > 1 ? mine.n * a.n_served : 0;
-    const int last = wave_incl_scan(ROWS ? own_rows : own);
-    const int part_last = wave_incl_scan(S > 1 ? own : 0);
-    const int b = __popcll(__ballot(last <= at));
-    if (b >= 64) return spot;
-    spot.b = b;
-    spot.rel = at - (__builtin_amdgcn_readlane(last, b) - __builtin_amdgcn_readlane(ROWS ? own_rows : own, b));
-    spot.n = __builtin_amdgcn_readlane(mine.n, b);
-    spot.q0 = __builtin_amdgcn_readlane(mine.q0, b);
-    spot.ctx = __builtin_amdgcn_readlane(mine.ctx, b);
-    spot.splits = __builtin_amdgcn_readlane(S, b);
-    spot.part0 = __builtin_amdgcn_readlane(part_last - (S > 1 ? own : 0), b);
-    return spot;
-  }
-  const int32_t* unit_first = a.plan + kPlanHead;
-  const int32_t* part_first = unit_first + s.B + 1;
-  const int32_t* row_first = part_first + s.B + 1;
-  const int32_t* list = ROWS ? row_first : unit_first;
-  if (at >= list[s.B]) return spot;
-  const int b = wave_last_at_most(list, s.B, at);
-  const ChunkLane mine = chunk_lane(a, b);
-  const int longest = a.plan[kPlanLongest];
-  spot.b = b;
-  spot.rel = at - list[b];
-  spot.n = mine.n;
-  spot.q0 = mine.q0;
-  spot.ctx = mine.ctx;
-  spot.splits = chunk_splits(mine.key_tiles, longest, a.plan[kPlanCandidate], chunk_magic(longest));
-  spot.part0 = part_first[b];
-  return spot;
-}
 
 // B > 64: the same by one workgroup, once for the launches behind it.
 constexpr int kPlanThreads = 1024;
@@ -208,283 +88,12 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(const ChunkArg
   if (tid < 3) lists[tid][s.B] = before[tid];
 }
 
-// What a row sees, as bounds: the tokens n <= hi that are below `sink` or above `lo`.
-struct RowSight {
-  int hi, lo;
-};
-
-template <bool F16, bool LOCAL, bool KV4>
+template <bool F16, bool LOCAL, bool FULL>
 __global__ __launch_bounds__(kCkThreads, 2) void chunk_attn_kernel(const ChunkArgs a) {
-  __shared__ __attribute__((aligned(16))) unsigned char smem[kCkTileBytes * kCkStages];
-  const ChunkShape& sh = a.shape;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int g = lane >> 5, r = lane & 31;
-  const float ninf = -__builtin_huge_valf();
-
-  // ---- the unit: workgroups are dealt to the eight dies in turn, `run` units in a row go to one of them ----
-  const int k8 = (int)blockIdx.x >> 3;
-  const int unit = (k8 / a.run * 8 + ((int)blockIdx.x & 7)) * a.run + k8 % a.run;
-  const ChunkSpot spot = chunk_find<false>(a, unit);
-  if (spot.b < 0) return;
-  const ChunkUnit u = chunk_unit(sh, spot.n, spot.splits, spot.rel);
-  const int nh = sh.slot_n[u.slot], tok = sh.tok[nh], kvh = sh.slot_kv[u.slot];
-  const int t0 = u.tile * tok, rows = min(tok, spot.n - t0) * nh;
-  const int pos0 = spot.ctx - spot.n + t0;                          // the first row's position; may be negative, where ctx_len says so
-  const int page_shift = KV4 ? a.c4.page_shift : a.c16.page_shift, n_pages = KV4 ? a.c4.n_pages : a.c16.n_pages;
-  const int64_t pt_stride = KV4 ? a.c4.pt_stride : a.c16.pt_stride;
-  const int32_t* const pt = (KV4 ? a.c4.page_table : a.c16.page_table) + spot.b * pt_stride;
-  const int64_t held = pt_stride << page_shift;                     // positions that the table has entries for
-  auto page_of = [&](int n) __attribute__((always_inline)) {        // 0 <= n < held
-    const int page = pt[n >> page_shift];
-    return (uint32_t)page < (uint32_t)n_pages ? page : -1;
-  };
-
-  // ---- rows ----
-  const int over = 65536 / nh + 1;                                  // row / nh by a product: exact for rows below 256, nh up to 8
-  const int row = wave * 32 + r, row_t = (row * over) >> 16;
-  const bool qok = row < rows;
-  const int head = qok ? sh.heads[sh.slot_first[u.slot] + row - row_t * nh] : 0;
-  const int64_t qi = spot.q0 + t0 + row_t;
-  u32x4 qreg[8];
-#pragma unroll
-  for (int kk = 0; kk < 8; ++kk)
-    qreg[kk] = qok ? *reinterpret_cast<const u32x4*>(a.q + qi * a.q_stride + head * kHeadDim + kk * 16 + g * 8) : (u32x4){0u, 0u, 0u, 0u};
-  const int m_lo = pos0, m_hi = pos0 + (rows - 1) / nh;             // the tile's first and last position
-  const int kend = (int)min((int64_t)max(m_hi + 1, 0), held);       // keys that some row may see
-  const int mq = pos0 + row_t;
-  const RowSight sight = {qok ? min(mq, kend - 1) : -1, LOCAL ? mq - sh.window : -1};
-  auto sees = [&](int n) __attribute__((always_inline)) { return n <= sight.hi && (!LOCAL || n < sh.sink || n > sight.lo); };
-  // the wave's rows: positions of the first and the last, -1 and less for a wave without rows
-  const int w_lo = wave * 32 < rows ? pos0 + ((wave * 32 * over) >> 16) : -1;
-  const int w_hi = wave * 32 < rows ? pos0 + ((min(wave * 32 + 31, rows - 1) * over) >> 16) : -1;
-
-  // ---- the tile's key tiles: those of the sink, then those of the band ----
-  const int all_tiles = (kend + kCkK - 1) / kCkK;
-  int sink_tiles = 0, gap = 0;
-  if (LOCAL) {
-    sink_tiles = (min(sh.sink, kend) + kCkK - 1) / kCkK;
-    const int band = sh.window > 0 ? max(m_lo - sh.window + 1, 0) / kCkK : all_tiles;
-    gap = max(band - sink_tiles, 0);
-  }
-  const int n_tiles = all_tiles - gap;
-  auto tile_n0 = [&](int it) __attribute__((always_inline)) { return (it + (it >= sink_tiles ? gap : 0)) * kCkK; };
-  const int it_lo = (int)((int64_t)n_tiles * u.split / spot.splits), it_hi = (int)((int64_t)n_tiles * (u.split + 1) / spot.splits);
-
-  // ---- staging: K rows then V rows of 256 bytes; K row n keeps 16-byte chunk c at position c ^ (n % 16), V row n 32-byte unit u
-  // at position u ^ 2 (n % 4), which spreads the operand reads below over the banks ----
-  const uint32_t lds_base = (uint32_t)(size_t)(__attribute__((address_space(3))) unsigned char*)smem;
-  const int ld_sub = lane >> 4, ld_pos = lane & 15;
-  const int ld_ck = ld_pos ^ ((4 * wave + ld_sub) & 15);
-  const int ld_cv = ((((ld_pos >> 1) ^ (2 * (ld_sub & 3))) << 1) | (ld_pos & 1));
-  const uint8_t* const Kh = KV4 ? nullptr : a.c16.K + (int64_t)kvh * a.c16.head_bytes;
-  const uint8_t* const Vh = KV4 ? nullptr : a.c16.V + (int64_t)kvh * a.c16.head_bytes;
-  // 16-bit rows go to LDS directly: four neighbouring rows (of one page) per wave and instruction.  Rows behind the last key repeat it, rows of a
-  // page that the pool does not have are the pool's first: masked all the same.
-  auto load_rows = [&](int n0, int slot, int jj) __attribute__((always_inline)) {
-    const int nb = min(n0 + 32 * jj + 4 * wave, (kend - 1) & ~3), n = min(nb + ld_sub, kend - 1);
-    const int64_t at = (int64_t)max(page_of(n), 0) * a.c16.page_bytes + (int64_t)(n & ((1 << page_shift) - 1)) * a.c16.row_bytes;
-    const uint32_t dst = lds_base + slot * kCkTileBytes + (jj * kCkWaves + wave) * 1024;
-    // (assembly, since through the compiler's intrinsic every later LDS read waits for all outstanding loads)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(Kh + at + ld_ck * 16) : "memory", "m0");
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst + kCkTileBytes / 2), "v"(Vh + at + ld_cv * 16) : "memory", "m0");
-  };
-  // A 4-bit row is 16 bytes for each of eight lanes: four blocks of K, four of V, each with its scale.
-  auto load_codes = [&](int n0, u32x4& codes, uint32_t& scale) __attribute__((always_inline)) {
-    const int n = min(n0 + 8 * wave + (lane >> 3), kend - 1), piece = lane & 7, slot = n & ((1 << page_shift) - 1);
-    const int64_t page = max(page_of(n), 0);
-    codes = *reinterpret_cast<const u32x4*>(a.c4.codes + page * a.c4.code_page16 * 16 + (int64_t)kvh * a.c4.code_head_stride + (int64_t)slot * kKv4Row + piece * 16);
-    scale = a.c4.scales[page * a.c4.scale_page16 * 16 + (int64_t)kvh * a.c4.scale_head_stride + (int64_t)(slot >> 2) * kKv4Group + piece * 4 + (slot & 3)];
-  };
-  auto put_codes = [&](int slot, const u32x4 codes, uint32_t scale) __attribute__((always_inline)) {
-    const int n = 8 * wave + (lane >> 3), piece = lane & 7, blk = piece & 3;
-    const float f = __uint_as_float(scale << 23);
-    unsigned char* const dst = smem + slot * kCkTileBytes + (piece < 4 ? 0 : kCkTileBytes / 2) + n * 256;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int ck = (4 * blk + i) ^ (n & 15), cv = ((2 * blk + (i >> 1)) ^ (2 * (n & 3))) * 2 + (i & 1);
-      *reinterpret_cast<u32x4*>(dst + (piece < 4 ? ck : cv) * 16) = decode8<F16>(codes[i], f);
-    }
-  };
-  auto loads_landed = [&]() __attribute__((always_inline)) { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); };
-
-  // ---- operand reads ----
-  const int rd_k = r * 256, rd_kx = (g ^ (r & 15)) << 4;
-  const int rd_j = lane & 15, rd_G = (lane >> 4) & 1;
-  const int rd_v = kCkTileBytes / 2 + (4 * g + (rd_j >> 2)) * 256 + 8 * (rd_j & 3);
-  const int rd_vx = (rd_G ^ (2 * (rd_j >> 2))) << 5;
-  auto read_k = [&](const unsigned char* tile, int kb, int kk) __attribute__((always_inline)) {
-    return *reinterpret_cast<const u32x4*>(tile + kb * 8192 + rd_k + ((kk << 5) ^ rd_kx));
-  };
-  // 8 keys x 1 dim of V^T: two transposing reads of 4 keys each
-  auto read_v = [&](const unsigned char* tile, int kb, int tt, int db) __attribute__((always_inline)) {
-    const unsigned char* p0 = tile + rd_v + (kb * 32 + 16 * tt) * 256 + ((db << 6) ^ rd_vx);
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(p0));
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(p0 + 8 * 256));
-    return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-  };
-
-  f32x16 O[4];
-  float mrow = ninf, lrow = 0.f, lsum_full = 0.f;
-  const float c = a.scale_log2;
-  auto mfma_S = [&](const unsigned char* tile, int kb, f32x16& S) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) S[i] = 0.f;
-#pragma unroll
-    for (int kk = 0; kk < 8; ++kk) S = mfma32<F16>(read_k(tile, kb, kk), qreg[kk], S);
-  };
-  auto mfma_PV = [&](const unsigned char* tile, int kb, const uint32_t (&P)[8]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-      for (int db = 0; db < 4; ++db)
-        O[db] = mfma32<F16>(read_v(tile, kb, tt, db), (u32x4){P[4 * tt], P[4 * tt + 1], P[4 * tt + 2], P[4 * tt + 3]}, O[db]);
-  };
-
-  // ---- running maximum, accumulators rescaled in place; the next tile's rows are on their way ----
-  auto exact_pass = [&]() __attribute__((always_inline)) {
-    f32x16 S;
-    uint32_t P[8];
-    u32x4 codes;
-    uint32_t scale = 0;
-    mrow = ninf;
-    lrow = lsum_full = 0.f;
-#pragma unroll
-    for (int db = 0; db < 4; ++db)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) O[db][i] = 0.f;
-    __syncthreads();
-    if (it_lo >= it_hi) return;
-    if constexpr (KV4) load_codes(tile_n0(it_lo), codes, scale);
-    else {
-      load_rows(tile_n0(it_lo), 0, 0);
-      load_rows(tile_n0(it_lo), 0, 1);
-    }
-    for (int it = it_lo; it < it_hi; ++it) {
-      const int buf = (it - it_lo) & 1, n0 = tile_n0(it);
-      const unsigned char* const tile = smem + buf * kCkTileBytes;
-      if constexpr (KV4) put_codes(buf, codes, scale);
-      else loads_landed();
-      __syncthreads();
-      if (it + 1 < it_hi) {
-        if constexpr (KV4) load_codes(tile_n0(it + 1), codes, scale);
-        else {
-          load_rows(tile_n0(it + 1), buf ^ 1, 0);
-          load_rows(tile_n0(it + 1), buf ^ 1, 1);
-        }
-      }
-      for (int kb = 0; kb < 2; ++kb) {
-        const int nb0 = n0 + kb * 32;
-        if (nb0 > w_hi || nb0 >= kend) continue;                     // (the same for the whole wave)
-        if (LOCAL && nb0 >= sh.sink && nb0 + 31 <= w_lo - sh.window) continue;
-        mfma_S(tile, kb, S);
-        uint32_t seen = 0;                                           // bit i: the lane's i-th key, nb0 + 8 (i / 4) + 4 g + i % 4, is seen
-#pragma unroll
-        for (int i4 = 0; i4 < 4; ++i4) {
-          const int n4 = nb0 + i4 * 8 + g * 4;
-          const bool there = n4 < kend && page_of(min(n4, kend - 1)) >= 0;       // (four neighbours share their page)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) seen |= there && sees(n4 + j) ? 1u << (i4 * 4 + j) : 0u;
-        }
-        const bool masked = __ballot(seen != 0xffffu) != 0ull;
-        float mx = ninf;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          S[i] = (seen >> i) & 1u ? S[i] : ninf;
-          mx = fmaxf(mx, S[i]);
-        }
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
-        const float mnew = fmaxf(mrow, mx), msafe = mnew == ninf ? 0.f : mnew, mc = msafe * c;
-        float lsum = 0.f, lfull = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-          const float p0 = fast_exp2(fmaf(S[i], c, -mc)), p1 = fast_exp2(fmaf(S[i + 1], c, -mc));
-          P[i >> 1] = pack16<F16>(p0, p1);
-          lfull += p0 + p1;
-          lsum += lo16<F16>(P[i >> 1]) + hi16<F16>(P[i >> 1]);
-        }
-        const float corr = fast_exp2((mrow - msafe) * c);
-        lrow = lrow * corr + lsum;
-        lsum_full = lsum_full * corr + lfull;
-#pragma unroll
-        for (int db = 0; db < 4; ++db)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) O[db][i] *= corr;
-        mrow = mnew;
-        // A key that a row does not see has probability 0, and 0 times a value that is not finite would not be 0: such a block's
-        // products are taken one by one, over the seen keys alone.
-        bool odd = false;
-        if (masked) {
-          uint32_t any = 0;
-          constexpr uint32_t kExp = F16 ? 0x7c007c00u : 0x7f807f80u, kOne = F16 ? 0x04000400u : 0x00800080u;
-#pragma unroll
-          for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-            for (int db = 0; db < 4; ++db) {
-              const u32x4 v = read_v(tile, kb, tt, db);
-#pragma unroll
-              for (int w = 0; w < 4; ++w) any |= ((v[w] & kExp) + kOne) & 0x80008000u;
-            }
-          odd = __ballot(any != 0u) != 0ull;
-        }
-        if (!odd) {
-          mfma_PV(tile, kb, P);
-        } else {
-          for (int i = 0; i < 16; ++i) {
-            float p_own = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) p_own = e == (i >> 1) ? ((i & 1) ? hi16<F16>(P[e]) : lo16<F16>(P[e])) : p_own;
-            const uint32_t seen_other = (uint32_t)__shfl_xor((int)seen, 32);
-            const float p_other = __shfl_xor(p_own, 32);
-            for (int half = 0; half < 2; ++half) {
-              const int n = kb * 32 + 8 * (i >> 2) + 4 * half + (i & 3);                    // row of the tile
-              const bool ok = ((half == g ? seen : seen_other) >> i) & 1u;
-              const float p = half == g ? p_own : p_other;
-              const unsigned char* vrow = tile + kCkTileBytes / 2 + n * 256;
-#pragma unroll
-              for (int db = 0; db < 4; ++db)
-#pragma unroll
-                for (int i4 = 0; i4 < 4; ++i4) {
-                  const int d = db * 32 + i4 * 8 + g * 4;
-                  const u32x2 w = *reinterpret_cast<const u32x2*>(vrow + ((d >> 4) ^ (2 * (n & 3))) * 32 + (d & 15) * 2);
-                  const float v[4] = {lo16<F16>(w[0]), hi16<F16>(w[0]), lo16<F16>(w[1]), hi16<F16>(w[1])};
-#pragma unroll
-                  for (int j = 0; j < 4; ++j) O[db][i4 * 4 + j] = ok ? fmaf(p, v[j], O[db][i4 * 4 + j]) : O[db][i4 * 4 + j];
-                }
-            }
-          }
-        }
-      }
-      __syncthreads();
-    }
-  };
-  exact_pass();
-
-  // ---- normalise and store, or leave the range's partial result ----
-  const float l = lrow + __shfl_xor(lrow, 32), l_full = lsum_full + __shfl_xor(lsum_full, 32);
-  if (!qok) return;
-  if (spot.splits > 1) {
-    if (row >= a.part_rows) return;
-    float* prow = a.part + ((int64_t)(spot.part0 + spot.rel) * a.part_rows + row) * kCkPart;
-    // (a sum that is not a number comes with a reference that the merge does not take for a range without keys)
-    if (g == 0) *reinterpret_cast<float4*>(prow) = make_float4(l != l && mrow == ninf ? 0.f : mrow, l, l_full, 0.f);
-#pragma unroll
-    for (int db = 0; db < 4; ++db)
-#pragma unroll
-      for (int i4 = 0; i4 < 4; ++i4)
-        *reinterpret_cast<float4*>(prow + 4 + db * 32 + i4 * 8 + g * 4) =
-            make_float4(O[db][i4 * 4], O[db][i4 * 4 + 1], O[db][i4 * 4 + 2], O[db][i4 * 4 + 3]);
-    return;
-  }
-  const bool none = l == 0.f;
-  const float inv = none ? 0.f : 1.f / l;
-  uint16_t* const orow = a.out + (qi * a.n_q_heads + head) * kHeadDim;
-#pragma unroll
-  for (int db = 0; db < 4; ++db)
-#pragma unroll
-    for (int i4 = 0; i4 < 4; ++i4)
-      *reinterpret_cast<u32x2*>(orow + db * 32 + i4 * 8 + g * 4) =
-          none ? (u32x2){0u, 0u} : (u32x2){pack16<F16>(O[db][i4 * 4] * inv, O[db][i4 * 4 + 1] * inv), pack16<F16>(O[db][i4 * 4 + 2] * inv, O[db][i4 * 4 + 3] * inv)};
-  if (a.lse && g == 0) a.lse[qi * a.n_q_heads + head] = none ? ninf : mrow * a.scale + logf(l_full);
+  __shared__ __attribute__((aligned(16))) unsigned char smem[kCkWideLds];
+  ChunkTile t;
+  if (!chunk_tile<LOCAL, false>(a, &t)) return;
+  ChunkWide<F16, LOCAL, false, FULL>(a, t, smem).run();
 }
 
 // Merges the ranges of the rows whose tiles were cut: SLICES groups of 32 lanes per row take the ranges in turn, a lane 4 of the 128 dims.
@@ -578,6 +187,9 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(const ChunkArgs a) {
     __syncthreads();
   }
 }
+
+// attn_chunk_kv4.hip
+void launch_chunk_kv4(const ChunkArgs& a, unsigned grid, bool local, bool full, hipStream_t stream);
 
 // ---- host side ----------------------------------------------------------------------------------------------------------------------
 namespace {
@@ -709,10 +321,10 @@ int32_t chunk_call(const char* who, int which, const rtp_layer_desc* layer, cons
   a.part_rows = z.part_rows;
   a.f16 = layer->kv_dtype == RTP_DTYPE_FP16;
   if (chunk->B > 64) RTP_LAUNCH(chunk_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a);
-  const bool local = a.shape.local != 0;
-#define RTP_CHUNK(F16, LOCAL, KV4)                                                                          \
-  if ((a.f16 != 0) == F16 && local == LOCAL && kv4 == KV4)                                                  \
-    RTP_LAUNCH((chunk_attn_kernel<F16, LOCAL, KV4>), dim3((unsigned)grid), dim3(kCkThreads), 0, stream, a);
+  const bool local = a.shape.local != 0, full = lse != nullptr;
+#define RTP_CHUNK(F16, LOCAL, FULL)                                                                         \
+  if ((a.f16 != 0) == F16 && local == LOCAL && full == FULL && !kv4)                                        \
+    RTP_LAUNCH((chunk_attn_kernel<F16, LOCAL, FULL>), dim3((unsigned)grid), dim3(kCkThreads), 0, stream, a);
   RTP_CHUNK(false, false, false)
   RTP_CHUNK(true, false, false)
   RTP_CHUNK(false, true, false)
@@ -722,6 +334,7 @@ int32_t chunk_call(const char* who, int which, const rtp_layer_desc* layer, cons
   RTP_CHUNK(false, true, true)
   RTP_CHUNK(true, true, true)
 #undef RTP_CHUNK
+  if (kv4) launch_chunk_kv4(a, (unsigned)grid, local, full, stream);
   if (z.cap > 0) {
     const int64_t rows = (int64_t)chunk->total_q * a.n_served;
     if (rows <= 2048) RTP_LAUNCH(chunk_merge_kernel<8>, dim3((unsigned)rows), dim3(256), 0, stream, a);

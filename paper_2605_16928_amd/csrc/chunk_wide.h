@@ -1,0 +1,497 @@
+// A query tile of up to 256 rows: eight waves of 32 rows, two per SIMD, share every staged tile of 64 keys.
+//
+// Nothing hides latency by itself at two waves per SIMD, so the loop is pipelined over blocks of 32 keys by hand: while the probabilities of a
+// block are computed on the vector ALU, the matrix pipe runs the PV product of the block before and the score product of the one behind.  For that
+// nothing may touch the accumulators in between, so there is no running maximum: every row takes its largest score in the range's first tile for a
+// reference, and a range after whose pass some row's sum or output says that this did not do (out of the middle of fp32's range, or not finite) is
+// repeated with a running maximum (wide_exact), as is one that met a page which is not there.
+//
+// K/V tiles rotate through three LDS buffers with one barrier per tile, in its middle: it publishes tile it + 1, and behind it every wave is done
+// with tile it - 1, whose buffer tile it + 2 fills.  Tiles that every row sees in full run in a loop without a branch; the others -- the first, those
+// on the diagonal and on the window's edge -- block by block, with masks.
+//
+// 16-bit rows go to LDS by direct loads.  The four rows that a wave brings per instruction lie in one page, whose place is a scalar: 64 of them, for
+// 32 tiles, are looked up at a time, a lane each, a window ahead, and taken from there with two lane reads.  4-bit rows come through registers
+// a tile ahead, 16 bytes per lane, and are turned into 16 bits on their way to LDS, between the products.
+#pragma once
+
+#include "chunk_tile.h"
+
+namespace rtp {
+
+constexpr int kCkStages = 3;
+constexpr int kCkWideLds = kCkTileBytes * kCkStages;
+
+// Sums: l of the probabilities as rounded (what the outputs are divided by), F of them before (what the log-sum is of; FULL only).
+template <bool F16, bool LOCAL, bool KV4, bool FULL>
+struct ChunkWide {
+  const ChunkArgs& a;
+  const ChunkTile& t;
+  unsigned char* const smem;
+  const int lane, wave, g, r, row;
+  const bool qok;
+  const int w_lo, w_hi;                          // positions of the wave's first and last row; w_hi < 0: the wave has none
+  const float c;
+  const ChunkReads rd;
+  const ChunkSight sight;
+  u32x4 q[8];
+  f32x16 O[4];
+  float m, l, F;
+  // staging: places of the rows that this wave brings, relative to the head's pool: piece `lane` of the window, kPieces to a tile
+  static constexpr int kPieces = KV4 ? 1 : 2, kWindow = 64 / kPieces, kRowsEach = KV4 ? 8 : 4;
+  const uint8_t* base0;                          // K, or codes
+  const uint8_t* base1;                          // V, or scales
+  uint32_t at_lo, at_hi, sc_lo, sc_hi;           // this window's (scales: 4-bit only)
+  int next_page;                                 // the next window's, as the table has it
+  uint32_t off0, off1;                           // the lane's place inside its rows
+  bool lost;
+  u32x4 codes;                                   // 4-bit: the rows on their way
+  uint32_t scale;
+
+  __device__ __forceinline__ ChunkWide(const ChunkArgs& a_, const ChunkTile& t_, unsigned char* smem_)
+      : a(a_), t(t_), smem(smem_), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), g(lane >> 5), r(lane & 31),
+        row(wave * 32 + r), qok(row < t_.rows), w_lo(wave * 32 < t_.rows ? chunk_row_pos(t_, wave * 32) : -1),
+        w_hi(wave * 32 < t_.rows ? chunk_row_pos(t_, min(wave * 32 + 31, t_.rows - 1)) : -1), c(a_.scale_log2), rd(chunk_reads()),
+        sight(chunk_sight(a_.shape, t_, row)), lost(false) {
+    const int rt = (row * t.over) >> 16;
+    const int head = qok ? a.shape.heads[t.head0 + row - rt * t.nh] : 0;
+    const uint16_t* src = a.q + (t.q0 + rt) * a.q_stride + head * kHeadDim + g * 8;
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) q[kk] = qok ? *reinterpret_cast<const u32x4*>(src + kk * 16) : (u32x4){0u, 0u, 0u, 0u};
+    if constexpr (KV4) {
+      base0 = a.c4.codes + (int64_t)t.kvh * a.c4.code_head_stride;
+      base1 = a.c4.scales + (int64_t)t.kvh * a.c4.scale_head_stride;
+      off0 = lane * 16;
+      off1 = (lane >> 5) * kKv4Group + (lane & 7) * 4 + ((lane >> 3) & 3);
+    } else {
+      base0 = a.c16.K + (int64_t)t.kvh * a.c16.head_bytes;
+      base1 = a.c16.V + (int64_t)t.kvh * a.c16.head_bytes;
+      const int sub = lane >> 4, pos = lane & 15;
+      off0 = sub * a.c16.row_bytes + (pos ^ ((4 * wave + sub) & 15)) * 16;
+      off1 = sub * a.c16.row_bytes + ((((pos >> 1) ^ (2 * sub)) << 1) | (pos & 1)) * 16;
+    }
+  }
+
+  __device__ __forceinline__ int n0_of(int it) const { return chunk_tile_n0(t, it); }
+  __device__ __forceinline__ bool any_seen(int n, int len) const { return chunk_any_seen<LOCAL>(a.shape, t, w_lo, w_hi, n, len); }
+  __device__ __forceinline__ bool all_seen(int n, int len) const { return chunk_all_seen<LOCAL>(a.shape, t, w_lo, w_hi, n, len); }
+  // A tile that every row of the workgroup sees in full (of the band: full tiles are neighbours then).
+  __device__ __forceinline__ bool full_tile(int it) const {
+    const int n = n0_of(it);
+    return n + kCkK - 1 <= t.m_lo && n + kCkK <= t.kend && (!LOCAL || n > t.m_hi - a.shape.window);
+  }
+
+  // ---- staging ----
+  // First of the rows of piece p (counted from the range's first tile) that this wave brings; past the last key and the last tile: those of the last.
+  __device__ __forceinline__ int piece_row(int p) const {
+    const int n0 = n0_of(min(t.it_lo + p / kPieces, t.it_hi - 1)) + (p % kPieces) * 32 + kRowsEach * wave;
+    return min(n0, (t.kend - 1) & ~(kRowsEach - 1));
+  }
+  __device__ __forceinline__ void look_up(int window) {
+    next_page = t.pt[piece_row(window * 64 + lane) >> (KV4 ? a.c4.page_shift : a.c16.page_shift)];
+  }
+  // (an entry that names no page is taken for the first page; the range is repeated)
+  __device__ __forceinline__ void take_window(int window) {
+    const int n = piece_row(window * 64 + lane);
+    const bool there = (uint32_t)next_page < (uint32_t)(KV4 ? a.c4.n_pages : a.c16.n_pages);
+    const uint32_t page = there ? (uint32_t)next_page : 0u;
+    const uint32_t slot = n & ((1 << (KV4 ? a.c4.page_shift : a.c16.page_shift)) - 1);
+    lost = lost || __ballot(!there) != 0ull;
+    uint64_t at;
+    if constexpr (KV4) {
+      at = (uint64_t)page * a.c4.code_page16 * 16u + (uint64_t)slot * kKv4Row;
+      const uint64_t sc = (uint64_t)page * a.c4.scale_page16 * 16u + (uint64_t)slot * (kKv4Group / 4);
+      sc_lo = (uint32_t)sc;
+      sc_hi = (uint32_t)(sc >> 32);
+    } else {
+      at = (uint64_t)page * (uint64_t)a.c16.page_bytes + (uint64_t)slot * (uint32_t)a.c16.row_bytes;
+    }
+    at_lo = (uint32_t)at;
+    at_hi = (uint32_t)(at >> 32);
+  }
+  __device__ __forceinline__ int64_t place(uint32_t lo, uint32_t hi, int p) const {
+    return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)hi, p) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)lo, p));
+  }
+  // The window of tile x (counted from the range's first) is the current one; called for every x in turn.
+  __device__ __forceinline__ void advance(int x) {
+    if (x % kWindow == 0) {
+      take_window(x / kWindow);
+      look_up(x / kWindow + 1);
+    }
+  }
+  __device__ __forceinline__ uint32_t lds_of(int slot) const {
+    return (uint32_t)(size_t)(__attribute__((address_space(3))) unsigned char*)smem + slot * kCkTileBytes;
+  }
+  // One of the four loads of tile x: K or V, first or second 32 rows.
+  __device__ __forceinline__ void load16(int x, int slot, int jj, bool v, uint32_t off) const {
+    const int64_t at = place(at_lo, at_hi, (x % kWindow) * kPieces + jj);
+    chunk_load_lds(lds_of(slot) + (v ? kCkTileBytes / 2 : 0) + (jj * kCkWaves + wave) * 1024, (v ? base1 : base0) + at, off);
+  }
+  // The lane's place where the rows behind the last key have to repeat it (they are masked, but have to be rows that somebody has written).
+  __device__ __forceinline__ uint32_t edge_off(int p, bool second) const {
+    const int left = t.kend - 1 - piece_row(p);
+    if constexpr (KV4) {
+      const int n = min(lane >> 3, left), of = lane & 7, s4 = piece_row(p) & 3;
+      (void)s4;
+      return second ? (uint32_t)((n >> 2) * kKv4Group + of * 4 + (n & 3)) : (uint32_t)(n * kKv4Row + of * 16);
+    } else {
+      const int sub = lane >> 4;
+      return (second ? off1 : off0) - (uint32_t)((sub - min(sub, left)) * a.c16.row_bytes);
+    }
+  }
+  __device__ __forceinline__ void fetch_codes(int x, bool edge) {
+    const int p = x % kWindow;
+    const uint32_t o0 = edge ? edge_off(x, false) : off0, o1 = edge ? edge_off(x, true) : off1;
+    codes = *reinterpret_cast<const u32x4*>(base0 + place(at_lo, at_hi, p) + o0);
+    scale = (base1 + place(sc_lo, sc_hi, p))[o1];
+  }
+  __device__ __forceinline__ void put_codes(int slot, int i) const {        // a quarter of the lane's values
+    const int n = 8 * wave + (lane >> 3), piece = lane & 7, blk = piece & 3;
+    const int ck = (4 * blk + i) ^ (n & 15), cv = ((2 * blk + (i >> 1)) ^ (2 * (n & 3))) * 2 + (i & 1);
+    *reinterpret_cast<u32x4*>(smem + slot * kCkTileBytes + n * 256 + (piece < 4 ? ck * 16 : kCkTileBytes / 2 + cv * 16)) =
+        decode8<F16>(codes[i], __uint_as_float(scale << 23));
+  }
+  // All of tile x, masked or not.  4-bit: the rows that have come go to LDS, tile x + 1 sets out.
+  __device__ __forceinline__ void bring(int x, int slot) {
+    if constexpr (KV4) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) put_codes(slot, i);
+      advance(x + 1);
+      fetch_codes(x + 1, true);
+    } else {
+      advance(x);
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj) {
+        load16(x, slot, jj, false, edge_off(x * kPieces + jj, false));
+        load16(x, slot, jj, true, edge_off(x * kPieces + jj, true));
+      }
+    }
+  }
+  __device__ __forceinline__ void begin() {                                 // before the first bring()
+    look_up(0);
+    if constexpr (KV4) {
+      advance(0);
+      fetch_codes(0, true);
+    }
+  }
+  __device__ __forceinline__ void landed() const {
+    if constexpr (!KV4) chunk_wait_loads<0>();
+  }
+
+  // ---- products ----
+  __device__ __forceinline__ void clear() {
+    l = F = 0.f;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) O[db][i] = 0.f;
+  }
+  __device__ __forceinline__ void scores(const unsigned char* tile, int kb, f32x16& S) const {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) S[i] = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) S = mfma32<F16>(chunk_read_k(tile + kb * 8192, rd, kk), q[kk], S);
+  }
+  __device__ __forceinline__ void pv(const unsigned char* tile, int kb, const uint32_t (&P)[8]) {
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+      for (int db = 0; db < 4; ++db)
+        O[db] = mfma32<F16>(chunk_read_v(tile + kCkTileBytes / 2 + kb * 8192, rd, tt, db), (u32x4){P[4 * tt], P[4 * tt + 1], P[4 * tt + 2], P[4 * tt + 3]}, O[db]);
+  }
+  // Adds both halves of a packed pair: what the PV product multiplies.  (Assembly, so that it stays between the products where it is written; its
+  // result may be read by another kind of instruction after three wait states only.)
+  static __device__ __forceinline__ void add_pair(float& s, uint32_t pk) {
+    if constexpr (F16) asm volatile("v_dot2c_f32_f16 %0, %1, %2" : "+v"(s) : "v"(pk), "v"(0x3c003c00u));
+    else asm volatile("v_dot2c_f32_bf16 %0, %1, %2" : "+v"(s) : "v"(pk), "v"(0x3f803f80u));
+  }
+  static __device__ __forceinline__ void settled(float& s) { asm volatile("s_nop 3" : "+v"(s)); }
+
+  float mc, l_blk, f_blk;
+  __device__ __forceinline__ void pair(int k, const f32x16& S, uint32_t (&P)[8]) {
+    const float p0 = fast_exp2(fmaf(S[2 * k], c, -mc)), p1 = fast_exp2(fmaf(S[2 * k + 1], c, -mc));
+    P[k] = pack16<F16>(p0, p1);
+    add_pair(l_blk, P[k]);
+    if constexpr (FULL) {
+      asm volatile("v_add_f32 %0, %0, %1" : "+v"(f_blk) : "v"(p0));
+      asm volatile("v_add_f32 %0, %0, %1" : "+v"(f_blk) : "v"(p1));
+    }
+  }
+  __device__ __forceinline__ void begin_block() {
+    mc = m * c;
+    l_blk = f_blk = 0.f;
+  }
+  __device__ __forceinline__ void end_block() {
+    settled(l_blk);
+    l += l_blk;
+    if constexpr (FULL) F += f_blk;
+  }
+
+  // K operands are read kAheadK products ahead, V operands kAheadV, a stream's first ones during the stream before.
+  static constexpr int kAheadK = 5, kAheadV = 4;
+  u32x4 ka_first[kAheadK], va_first[kAheadV];
+  __device__ __forceinline__ void first_k(const unsigned char* tile, int kb) {
+#pragma unroll
+    for (int kk = 0; kk < kAheadK; ++kk) ka_first[kk] = chunk_read_k(tile + kb * 8192, rd, kk);
+  }
+  __device__ __forceinline__ void first_v(const unsigned char* tile, int kb) {
+#pragma unroll
+    for (int k = 0; k < kAheadV; ++k) va_first[k] = chunk_read_v(tile + kCkTileBytes / 2 + kb * 8192, rd, k >> 2, k & 3);
+  }
+  // PV of the block before (Pin, in `tile`) beside the first half of this block's probabilities
+  __device__ __forceinline__ void pv_stream(const unsigned char* tile, int kb, const uint32_t (&Pin)[8], const f32x16& S, uint32_t (&P)[8],
+                                            const unsigned char* next_tile, int next_kb) {
+    begin_block();
+    u32x4 va[8];
+#pragma unroll
+    for (int k = 0; k < kAheadV; ++k) va[k] = va_first[k];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int tt = k >> 2, db = k & 3;
+      if (k + kAheadV < 8) va[k + kAheadV] = chunk_read_v(tile + kCkTileBytes / 2 + kb * 8192, rd, (k + kAheadV) >> 2, (k + kAheadV) & 3);
+      if (k == 8 - kAheadV) first_k(next_tile, next_kb);
+      O[db] = mfma32<F16>(va[k], (u32x4){Pin[4 * tt], Pin[4 * tt + 1], Pin[4 * tt + 2], Pin[4 * tt + 3]}, O[db]);
+      if (k & 1) pair(k / 2, S, P);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  // scores of the block behind (Snext) beside the other half
+  template <typename Work>
+  __device__ __forceinline__ void score_stream(const unsigned char* tile, int kb, f32x16& Snext, const f32x16& S, uint32_t (&P)[8], Work&& work) {
+    u32x4 ka[8];
+#pragma unroll
+    for (int kk = 0; kk < kAheadK; ++kk) ka[kk] = ka_first[kk];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) Snext[i] = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) {
+      if (kk + kAheadK < 8) ka[kk + kAheadK] = chunk_read_k(tile + kb * 8192, rd, kk + kAheadK);
+      Snext = mfma32<F16>(ka[kk], q[kk], Snext);
+      work(kk);
+      if (kk & 1) pair(4 + kk / 2, S, P);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    end_block();
+  }
+
+  // ---- the pass against fixed references; true: some row needs another ----
+  __device__ __forceinline__ bool fast_pass() {
+    const float ninf = -__builtin_huge_valf();
+    f32x16 S;
+    uint32_t P0[8], P1[8];
+    clear();
+    begin();
+    bring(0, 0);
+    bring(1, 1);
+    landed();
+    __syncthreads();
+    auto tile_at = [&](int it) __attribute__((always_inline)) { return smem + (it - t.it_lo) % kCkStages * kCkTileBytes; };
+    m = ninf;
+#pragma unroll
+    for (int kb = 1; kb >= 0; --kb) {
+      scores(smem, kb, S);
+      float mx = S[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, S[i]);
+      m = fmaxf(m, fmaxf(mx, __shfl_xor(mx, 32)));
+    }
+    // At the start of half hf of tile it: S holds the scores of that block if the wave has a row that sees one of its keys; if `pend`, the
+    // probabilities of the block before wait in P1 (hf = 0, V in the tile before) or P0; tiles it and it + 1 are in LDS.
+    bool pend = false;
+    int it = t.it_lo;
+    auto half = [&](auto hf_tag) __attribute__((always_inline)) {
+      constexpr int hf = decltype(hf_tag)::value;
+      const int nb0 = n0_of(it) + hf * 32;
+      const uint32_t (&Pin)[8] = hf == 0 ? P1 : P0;
+      uint32_t (&Pout)[8] = hf == 0 ? P0 : P1;
+      if (pend) pv(tile_at(hf == 0 ? it - 1 : it), 1 - hf, Pin);
+      pend = any_seen(nb0, 32);
+      if (pend) {
+        if (!all_seen(nb0, 32)) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) S[i] = chunk_sees<LOCAL>(a.shape, sight, nb0 + 8 * (i >> 2) + 4 * g + (i & 3)) ? S[i] : ninf;
+        }
+        begin_block();
+#pragma unroll
+        for (int k = 0; k < 8; ++k) pair(k, S, Pout);
+        end_block();
+      }
+      if (hf == 0) {
+        if (any_seen(nb0 + 32, 32)) scores(tile_at(it), 1, S);
+        landed();
+        __syncthreads();
+      } else {
+        bring(it - t.it_lo + 2, (it - t.it_lo + 2) % kCkStages);            // (behind the last tile: once more into a buffer that nobody reads)
+        if (it + 1 < t.it_hi && any_seen(n0_of(it + 1), 32)) scores(tile_at(it + 1), 0, S);
+      }
+    };
+    auto edge_tile = [&]() __attribute__((always_inline)) {
+      half(std::integral_constant<int, 0>{});
+      half(std::integral_constant<int, 1>{});
+      ++it;
+    };
+    // a tile for the loop without masks: seen in full, and so are the rows that it sends for
+    constexpr int kSends = KV4 ? 3 : 2;
+    auto steady = [&]() __attribute__((always_inline)) {
+      return it < t.it_hi && full_tile(it) && (it + kSends >= t.it_hi || n0_of(it + kSends) + kCkK <= t.kend);
+    };
+    do edge_tile();
+    while (it < t.it_hi && !steady());
+    int x = it - t.it_lo;
+    if (it >= t.it_hi) {
+    } else if (w_hi >= 0) {
+      if (!pend) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) P1[k] = 0u;
+      }
+      pend = true;
+      f32x16 S1;
+      do {
+        advance(x + kSends);
+        first_v(tile_at(it - 1), 1);
+        do {
+          pv_stream(tile_at(it - 1), 1, P1, S, P0, tile_at(it), 1);
+          score_stream(tile_at(it), 1, S1, S, P0, [](int) __attribute__((always_inline)) {});
+          first_v(tile_at(it), 0);
+          landed();
+          __syncthreads();
+          pv_stream(tile_at(it), 0, P0, S1, P1, tile_at(it + 1), 0);
+          const int slot = (x + 2) % kCkStages;
+          score_stream(tile_at(it + 1), 0, S, S1, P1, [&](int kk) __attribute__((always_inline)) {
+            if constexpr (KV4) {
+              if (kk < 4) put_codes(slot, kk);
+              if (kk == 4) fetch_codes(x + 3, false);
+            } else {
+              if (kk < 4) load16(x + 2, slot, kk >> 1, kk & 1, (kk & 1) ? off1 : off0);
+            }
+          });
+          first_v(tile_at(it), 1);
+          ++it;
+          ++x;
+        } while (steady() && (x + kSends) % kWindow != 0);
+      } while (steady());
+    } else {
+      do {
+        advance(x + kSends);
+        landed();
+        __syncthreads();
+        const int slot = (x + 2) % kCkStages;
+        if constexpr (KV4) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) put_codes(slot, i);
+          fetch_codes(x + 3, false);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) load16(x + 2, slot, k >> 1, k & 1, (k & 1) ? off1 : off0);
+        }
+        ++it;
+        ++x;
+      } while (steady());
+    }
+    while (it < t.it_hi) edge_tile();
+    if (pend) pv(tile_at(t.it_hi - 1), 1, P1);
+    landed();
+    // Was every reference within reach?  A row that sees a key of the range has a sum in the middle of fp32's range (fp16: nothing above 65504 is
+    // finite; where the largest probability is below 2^-6 most of the mass may be in subnormals), and outputs are finite.
+    const float sum = l + __shfl_xor(l, 32);
+    float z = 0.f;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) z = fmaf(O[db][i], 0.f, z);
+    bool bad = lost || !(z == 0.f) || !(sum < 0x1p100f);
+    if (qok && sight.hi >= 0 && !(sum > (F16 ? 0x1p-6f : 0x1p-60f))) {
+      // does the row see a key of the range?  Of the sink's tiles ...
+      const int first = n0_of(t.it_lo), end = min(n0_of(t.it_hi - 1) + kCkK, t.kend), band = t.it_lo < t.sink_tiles ? n0_of(t.sink_tiles) : first;
+      bool sees = !LOCAL && first <= sight.hi;
+      if (LOCAL) sees = first <= min(min(a.shape.sink - 1, sight.hi), end - 1) || max(max(first, sight.lo + 1), t.gap > 0 ? band : 0) <= min(end - 1, sight.hi);
+      bad = bad || sees;
+    }
+    return __syncthreads_or(bad ? 1 : 0) != 0;
+  }
+
+  // ---- running maximum, accumulators rescaled in place ----
+  __device__ __forceinline__ void exact_pass() {
+    const float ninf = -__builtin_huge_valf();
+    f32x16 S;
+    uint32_t P[8];
+    clear();
+    m = ninf;
+    __syncthreads();
+    begin();
+    if constexpr (!KV4) bring(0, 0);
+#pragma unroll 1
+    for (int it = t.it_lo; it < t.it_hi; ++it) {
+      const int x = it - t.it_lo;
+      const unsigned char* const tile = smem + (x & 1) * kCkTileBytes;
+      if constexpr (KV4) bring(x, x & 1);
+      landed();
+      __syncthreads();
+      if constexpr (!KV4) bring(x + 1, (x + 1) & 1);
+#pragma unroll 1
+      for (int kb = 0; kb < 2; ++kb) {
+        const int nb0 = n0_of(it) + kb * 32;
+        if (!any_seen(nb0, 32)) continue;                                   // (the same for the whole wave)
+        scores(tile, kb, S);
+        uint32_t seen = 0;                                                  // bit i: the lane's i-th key
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) {
+          const int n4 = nb0 + i4 * 8 + g * 4;
+          const bool there = n4 < t.kend && chunk_page<KV4>(a, t, min(n4, t.kend - 1)) >= 0;      // (four neighbours share their page)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) seen |= there && chunk_sees<LOCAL>(a.shape, sight, n4 + j) ? 1u << (i4 * 4 + j) : 0u;
+        }
+        float mx = ninf;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          S[i] = (seen >> i) & 1u ? S[i] : ninf;
+          mx = fmaxf(mx, S[i]);
+        }
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float m_new = fmaxf(m, mx), ref = m_new == ninf ? 0.f : m_new, corr = fast_exp2((m - ref) * c);
+        float sum = 0.f, full = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) {
+          const float p0 = fast_exp2(fmaf(S[i], c, -ref * c)), p1 = fast_exp2(fmaf(S[i + 1], c, -ref * c));
+          P[i >> 1] = pack16<F16>(p0, p1);
+          full += p0 + p1;
+          sum += lo16<F16>(P[i >> 1]) + hi16<F16>(P[i >> 1]);
+        }
+        l = l * corr + sum;
+        F = F * corr + full;
+#pragma unroll
+        for (int db = 0; db < 4; ++db)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) O[db][i] *= corr;
+        m = m_new;
+        const unsigned char* const v_rows = tile + kCkTileBytes / 2 + kb * 8192;
+        uint32_t odd = 0;
+        if (__ballot(seen != 0xffffu) != 0ull) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) odd |= chunk_not_finite<F16>(chunk_read_v(v_rows, rd, k >> 2, k & 3));
+        }
+        if (__ballot(odd != 0u) == 0ull) pv(tile, kb, P);
+        else chunk_pv_seen<F16>(v_rows, seen, P, O);
+      }
+      __syncthreads();
+    }
+  }
+
+  __device__ __forceinline__ void run() {
+    m = -__builtin_huge_valf();
+    clear();
+    if (t.it_lo < t.it_hi && fast_pass()) exact_pass();
+    const float sum = l + __shfl_xor(l, 32), full = F + __shfl_xor(F, 32);
+    if (!qok) return;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) {
+        const float o[4] = {O[db][i4 * 4], O[db][i4 * 4 + 1], O[db][i4 * 4 + 2], O[db][i4 * 4 + 3]};
+        const int dim = db * 32 + i4 * 8 + g * 4;
+        chunk_store4<F16>(a, t, row, dim, m, sum, full, o);
+      }
+  }
+};
+
+}  // namespace rtp
