@@ -11,7 +11,7 @@
 //
 // A wave computes the transposed scores S^T = K Q^T of 32 keys (v_mfma_f32_32x32x16): lane (g, r) then holds 16 keys of ONE row, the softmax is
 // per lane, and the probabilities, rounded to 16 bits, are in place as the B operand of O^T = V^T P^T.
-#include "chunk_wide.h"
+#include "chunk_narrow.h"
 
 #include <algorithm>
 
@@ -90,10 +90,8 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(const ChunkArg
 
 template <bool F16, bool LOCAL, bool FULL>
 __global__ __launch_bounds__(kCkThreads, 2) void chunk_attn_kernel(const ChunkArgs a) {
-  __shared__ __attribute__((aligned(16))) unsigned char smem[kCkWideLds];
-  ChunkTile t;
-  if (!chunk_tile<LOCAL, false>(a, &t)) return;
-  ChunkWide<F16, LOCAL, false, FULL>(a, t, smem).run();
+  __shared__ __attribute__((aligned(16))) unsigned char smem[kCkLds];
+  chunk_unit_attend<F16, LOCAL, false, FULL>(a, smem);
 }
 
 // Merges the ranges of the rows whose tiles were cut: SLICES groups of 32 lanes per row take the ranges in turn, a lane 4 of the 128 dims.

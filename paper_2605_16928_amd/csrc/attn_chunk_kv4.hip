@@ -1,14 +1,12 @@
 // The attention of attn_chunk.hip with the 4-bit cache as the source of K and V.
-#include "chunk_wide.h"
+#include "chunk_narrow.h"
 
 namespace rtp {
 
 template <bool F16, bool LOCAL, bool FULL>
 __global__ __launch_bounds__(kCkThreads, 2) void chunk_attn_kv4_kernel(const ChunkArgs a) {
-  __shared__ __attribute__((aligned(16))) unsigned char smem[kCkWideLds];
-  ChunkTile t;
-  if (!chunk_tile<LOCAL, true>(a, &t)) return;
-  ChunkWide<F16, LOCAL, true, FULL>(a, t, smem).run();
+  __shared__ __attribute__((aligned(16))) unsigned char smem[kCkLds];
+  chunk_unit_attend<F16, LOCAL, true, FULL>(a, smem);
 }
 
 void launch_chunk_kv4(const ChunkArgs& a, unsigned grid, bool local, bool full, hipStream_t stream) {

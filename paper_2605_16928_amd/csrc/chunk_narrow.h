@@ -1,0 +1,398 @@
+// A query tile of up to 32 rows -- single tokens, drafts, the ends of chunks: bound by the bytes of K and V.  All rows fit one wave, so the eight
+// waves of the workgroup take blocks of 32 keys in turn, each on its own: no barrier until the waves' results are joined in LDS.
+//
+// 16-bit rows: a wave owns 16 KiB, K and V of one block.  The next K sets out when the scores have been computed, the next V behind the PV product;
+// eight waves at different places keep 64 to 128 KiB of a compute unit's loads in flight, without a second buffer.
+// 4-bit rows: a block is 4 KiB and 256 bytes of scales, two blocks ahead in registers, loaded as whole lines and put in operand order by way of the
+// wave's LDS:  K: lane (g, r) takes the dims 64 g .. + 63 of token r, and the queries lie alike, so that a word of codes is one product's operand;
+// V: lane (g, r) takes the dims 4 r .. + 3 (two bytes) of its 16 tokens, so that accumulator db holds the dims 4 rho + db.
+//
+// The running reference follows a row's maximum only when it is left behind by more than 2^8.  Probabilities enter the product in two parts, their
+// rounding to 16 bits and the rounding of the rest: the matrix cores have the time, and an output is then as exact as its own rounding.
+#pragma once
+
+#include "chunk_wide.h"
+
+namespace rtp {
+
+constexpr int kCkNarrowRows = 32;
+constexpr int kCkBlockBytes = 2 * 32 * kHeadDim * 2;                        // K and V of 32 keys; 32 rows of 128 outputs
+constexpr int kCkNarrowLds = kCkWaves * kCkBlockBytes + kCkWaves * kCkNarrowRows * 2 * 4;
+constexpr int kCkLds = kCkNarrowLds > kCkWideLds ? kCkNarrowLds : kCkWideLds;
+
+// LDS words that only the own wave writes and reads.
+__device__ __forceinline__ void chunk_wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+template <bool F16, bool LOCAL, bool KV4>
+struct ChunkNarrow {
+  const ChunkArgs& a;
+  const ChunkTile& t;
+  unsigned char* const smem;
+  unsigned char* const mine;                     // the wave's own LDS
+  const int lane, wave, g, r;
+  const float c;
+  const ChunkReads rd;
+  const ChunkSight sight;
+  const int n_blocks;                            // of this wave: block k starts at key n0(k)
+  u32x4 q[8];
+  f32x16 O[4];
+  float m, l;
+  const uint8_t* base0;
+  const uint8_t* base1;
+  uint32_t at_lo, at_hi, sc_lo, sc_hi;           // places of half blocks (16 keys lie in one page), two per block, 32 blocks
+  int next_page, window;
+  bool lost;
+
+  __device__ __forceinline__ ChunkNarrow(const ChunkArgs& a_, const ChunkTile& t_, unsigned char* smem_)
+      : a(a_), t(t_), smem(smem_), mine(smem_ + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kCkBlockBytes), lane(threadIdx.x & 63),
+        wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), g(lane >> 5), r(lane & 31), c(a_.scale_log2), rd(chunk_reads()),
+        sight(chunk_sight(a_.shape, t_, lane & 31)), n_blocks((2 * (t_.it_hi - t_.it_lo) - wave + kCkWaves - 1) / kCkWaves), window(-2), lost(false) {
+    const bool qok = r < t.rows;
+    const int rt = (r * t.over) >> 16;
+    const int head = qok ? a.shape.heads[t.head0 + r - rt * t.nh] : 0;
+    const uint16_t* src = a.q + (t.q0 + rt) * a.q_stride + head * kHeadDim + g * (KV4 ? 64 : 8);
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) q[kk] = qok ? *reinterpret_cast<const u32x4*>(src + kk * (KV4 ? 8 : 16)) : (u32x4){0u, 0u, 0u, 0u};
+    if constexpr (KV4) {
+      base0 = a.c4.codes + (int64_t)t.kvh * a.c4.code_head_stride;
+      base1 = a.c4.scales + (int64_t)t.kvh * a.c4.scale_head_stride;
+    } else {
+      base0 = a.c16.K + (int64_t)t.kvh * a.c16.head_bytes;
+      base1 = a.c16.V + (int64_t)t.kvh * a.c16.head_bytes;
+    }
+    m = -__builtin_huge_valf();
+    l = 0.f;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) O[db][i] = 0.f;
+  }
+
+  // First key of the wave's block k.
+  __device__ __forceinline__ int n0(int k) const {
+    const int j = wave + k * kCkWaves;
+    return chunk_tile_n0(t, t.it_lo + (j >> 1)) + (j & 1) * 32;
+  }
+  __device__ __forceinline__ int next_seen(int k) const {
+    while (k < n_blocks && !chunk_any_seen<LOCAL>(a.shape, t, t.m_lo, t.m_hi, n0(k), 32)) ++k;
+    return k;
+  }
+  // First key of half h of block k, or, where that lies behind the last key, of the 16 that hold it.
+  __device__ __forceinline__ int half_n0(int k, int h) const { return min(n0(min(k, n_blocks - 1)) + 16 * h, (t.kend - 1) & ~15); }
+  __device__ __forceinline__ void look_up(int w) {
+    next_page = t.pt[half_n0(w * 32 + (lane >> 1), lane & 1) >> (KV4 ? a.c4.page_shift : a.c16.page_shift)];
+  }
+  __device__ __forceinline__ void advance(int k) {
+    const int w = k >> 5;
+    if (w == window) return;
+    if (w != window + 1) look_up(w);
+    const int n = half_n0(w * 32 + (lane >> 1), lane & 1);
+    const bool there = (uint32_t)next_page < (uint32_t)(KV4 ? a.c4.n_pages : a.c16.n_pages);
+    const uint32_t page = there ? (uint32_t)next_page : 0u, slot = n & ((1 << (KV4 ? a.c4.page_shift : a.c16.page_shift)) - 1);
+    lost = lost || __ballot(!there) != 0ull;
+    uint64_t at;
+    if constexpr (KV4) {
+      at = (uint64_t)page * a.c4.code_page16 * 16u + (uint64_t)slot * kKv4Row;
+      const uint64_t sc = (uint64_t)page * a.c4.scale_page16 * 16u + (uint64_t)slot * (kKv4Group / 4);
+      sc_lo = (uint32_t)sc;
+      sc_hi = (uint32_t)(sc >> 32);
+    } else {
+      at = (uint64_t)page * (uint64_t)a.c16.page_bytes + (uint64_t)slot * (uint32_t)a.c16.row_bytes;
+    }
+    at_lo = (uint32_t)at;
+    at_hi = (uint32_t)(at >> 32);
+    window = w;
+    look_up(w + 1);
+  }
+  __device__ __forceinline__ int64_t place(uint32_t lo, uint32_t hi, int k, int h) const {
+    const int p = (k & 31) * 2 + h;
+    return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)hi, p) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)lo, p));
+  }
+  // Keys of half h behind its first that are there.
+  __device__ __forceinline__ int left(int k, int h) const { return t.kend - 1 - half_n0(k, h); }
+
+  // ---- 16-bit rows: eight loads of four rows for K, eight for V ----
+  __device__ __forceinline__ void send(int k, bool v) {
+    const uint32_t lds = (uint32_t)(size_t)(__attribute__((address_space(3))) unsigned char*)mine + (v ? kCkBlockBytes / 2 : 0);
+    const int sub = lane >> 4, pos = lane & 15;
+    const bool edge = n0(k) + 32 > t.kend;
+    const uint8_t* const base = v ? base1 : base0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int rel = 4 * (i & 3) + sub;                                    // row in its half
+      const int chunk = v ? (((pos >> 1) ^ (2 * sub)) << 1) | (pos & 1) : pos ^ rel;
+      const int at = edge ? min(rel, left(k, i >> 2)) : rel;
+      chunk_load_lds(lds + i * 1024, base + place(at_lo, at_hi, k, i >> 2), (uint32_t)(at * a.c16.row_bytes + chunk * 16));
+    }
+  }
+  static __device__ __forceinline__ void reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+  // ---- 4-bit rows ----
+  struct Codes {
+    u32x4 line[4];                               // token 8 i + lane / 8, 16 bytes of its 128
+    uint32_t scales;                             // word lane % 8 of the scales of tokens 4 (lane / 8) .. + 3
+  };
+  __device__ __forceinline__ void fetch(int k, Codes& x) {
+    const bool edge = n0(k) + 32 > t.kend;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      int rel = 8 * (i & 1) + (lane >> 3);
+      if (edge) rel = min(rel, left(k, i >> 1));
+      x.line[i] = *reinterpret_cast<const u32x4*>(base0 + place(at_lo, at_hi, k, i >> 1) + rel * kKv4Row + (lane & 7) * 16);
+    }
+    const int64_t s0 = place(sc_lo, sc_hi, k, 0), s1 = place(sc_lo, sc_hi, k, 1);
+    int group = (lane >> 3) & 3;
+    uint32_t keep = 0xffffffffu;
+    if (edge) {                                                             // (scales that nobody has written stay out: V times 0 has to be 0)
+      const int have = left(k, g);
+      group = min(group, have >> 2);
+      if (group == have >> 2) keep >>= 24 - 8 * (have & 3);
+    }
+    x.scales = *reinterpret_cast<const uint32_t*>(base1 + (g ? s1 : s0) + group * kKv4Group + (lane & 7) * 4) & keep;
+  }
+  static __device__ __forceinline__ int line_at(int token, int piece) { return token * 128 + (piece ^ ((token >> 1) & 7)) * 16; }
+  static constexpr int kScalesAt = 32 * kKv4Row;
+  __device__ __forceinline__ void turn(const Codes& x) const {
+    chunk_wave_fence();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<u32x4*>(mine + line_at(8 * i + (lane >> 3), lane & 7)) = x.line[i];
+    *reinterpret_cast<uint32_t*>(mine + kScalesAt + lane * 4) = x.scales;
+    chunk_wave_fence();
+  }
+  __device__ __forceinline__ void scores4(f32x16& S) const {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) S[i] = 0.f;
+#pragma unroll
+    for (int w4 = 0; w4 < 2; ++w4) {
+      const u32x4 w = *reinterpret_cast<const u32x4*>(mine + line_at(r, 2 * g + w4));
+      const float f = __uint_as_float((uint32_t)mine[kScalesAt + (r >> 2) * kKv4Group + (2 * g + w4) * 4 + (r & 3)] << 23);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) S = mfma32<F16>(decode8<F16>(w[i], f), q[4 * w4 + i], S);
+    }
+  }
+  // V^T of 16 keys (tt), the lane's dims 4 r + db
+  __device__ __forceinline__ void values4(int tt, u32x4 (&v)[4]) const {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int i4 = 2 * tt + e;
+      const uint32_t sc = *reinterpret_cast<const uint32_t*>(mine + kScalesAt + (2 * i4 + g) * kKv4Group + 16 + (r >> 3) * 4);
+#pragma unroll
+      for (int j = 0; j < 4; j += 2) {
+        const int n = 8 * i4 + 4 * g + j;
+        const uint32_t x = *reinterpret_cast<const uint16_t*>(mine + line_at(n, 4 + (r >> 3)) + (r & 7) * 2);
+        const uint32_t y = *reinterpret_cast<const uint16_t*>(mine + line_at(n + 1, 4 + (r >> 3)) + (r & 7) * 2);
+        const float fx = kv4_scale(sc, j), fy = kv4_scale(sc, j + 1);
+        const int w = 2 * e + (j >> 1);
+        if constexpr (F16) {
+          const f32x2_t x0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x, fx, 0), x1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x, fx, 1);
+          const f32x2_t y0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(y, fy, 0), y1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(y, fy, 1);
+          v[0][w] = pack16<true>(x0.x, y0.x);
+          v[1][w] = pack16<true>(x0.y, y0.y);
+          v[2][w] = pack16<true>(x1.x, y1.x);
+          v[3][w] = pack16<true>(x1.y, y1.y);
+        } else {
+          const uint32_t x0 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, fx, 0));
+          const uint32_t x1 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, fx, 1));
+          const uint32_t y0 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(y, fy, 0));
+          const uint32_t y1 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(y, fy, 1));
+          v[0][w] = __builtin_amdgcn_perm(y0, x0, 0x05040100u);
+          v[1][w] = __builtin_amdgcn_perm(y0, x0, 0x07060302u);
+          v[2][w] = __builtin_amdgcn_perm(y1, x1, 0x05040100u);
+          v[3][w] = __builtin_amdgcn_perm(y1, x1, 0x07060302u);
+        }
+      }
+    }
+  }
+
+  // ---- a block's probabilities, as their rounding P and the rounding of the rest R ----
+  __device__ __forceinline__ void softmax(int n, f32x16& S, uint32_t (&P)[8], uint32_t (&R)[8]) {
+    const float ninf = -__builtin_huge_valf();
+    if (!chunk_all_seen<LOCAL>(a.shape, t, t.m_lo, t.m_hi, n, 32) || t.rows < kCkNarrowRows) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) S[i] = chunk_sees<LOCAL>(a.shape, sight, n + 8 * (i >> 2) + 4 * g + (i & 3)) ? S[i] : ninf;
+    }
+    float mx = fmaxf(S[0], S[1]);
+#pragma unroll
+    for (int i = 2; i < 16; ++i) mx = fmaxf(mx, S[i]);
+    if (__ballot((mx - m) * c > 8.f || (m == ninf && mx > ninf)) != 0ull) {
+      const float m_new = fmaxf(m, fmaxf(mx, __shfl_xor(mx, 32)));
+      const float corr = m_new == ninf ? 1.f : fast_exp2((m - m_new) * c);
+      m = m_new;
+      l *= corr;
+#pragma unroll
+      for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) O[db][i] *= corr;
+    }
+    const float mc = m == ninf ? 0.f : m * c;
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      const float p0 = fast_exp2(fmaf(S[i], c, -mc)), p1 = fast_exp2(fmaf(S[i + 1], c, -mc));
+      l += p0 + p1;
+      P[i >> 1] = pack16<F16>(p0, p1);
+      R[i >> 1] = pack16<F16>(p0 - lo16<F16>(P[i >> 1]), p1 - hi16<F16>(P[i >> 1]));
+    }
+  }
+  __device__ __forceinline__ void pv(const u32x4 (&v)[4], int tt, const uint32_t (&P)[8], const uint32_t (&R)[8]) {
+#pragma unroll
+    for (int db = 0; db < 4; ++db) {
+      O[db] = mfma32<F16>(v[db], (u32x4){P[4 * tt], P[4 * tt + 1], P[4 * tt + 2], P[4 * tt + 3]}, O[db]);
+      O[db] = mfma32<F16>(v[db], (u32x4){R[4 * tt], R[4 * tt + 1], R[4 * tt + 2], R[4 * tt + 3]}, O[db]);
+    }
+  }
+
+  __device__ __forceinline__ void pass16() {
+    f32x16 S;
+    uint32_t P[8], R[8];
+    int k = next_seen(0);
+    if (k < n_blocks) {
+      advance(k);
+      send(k, false);
+      send(k, true);
+    }
+    while (k < n_blocks) {
+      const int next = next_seen(k + 1);
+      const bool more = next < n_blocks;
+      if (more) advance(next);
+      chunk_wait_loads<8>();                                                // K, in front of V's eight
+#pragma unroll
+      for (int i = 0; i < 16; ++i) S[i] = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk) S = mfma32<F16>(chunk_read_k(mine, rd, kk), q[kk], S);
+      reads_done();
+      if (more) send(next, false);
+      softmax(n0(k), S, P, R);
+      if (more) chunk_wait_loads<8>();
+      else chunk_wait_loads<0>();
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        u32x4 v[4];
+#pragma unroll
+        for (int db = 0; db < 4; ++db) v[db] = chunk_read_v(mine + kCkBlockBytes / 2, rd, tt, db);
+        pv(v, tt, P, R);
+      }
+      reads_done();
+      if (more) send(next, true);
+      k = next;
+    }
+  }
+  __device__ __forceinline__ void pass4() {
+    Codes x[2];
+    int at[2];
+    at[0] = next_seen(0);
+    at[1] = next_seen(at[0] + 1);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      if (at[u] < n_blocks) {
+        advance(at[u]);
+        fetch(at[u], x[u]);
+      }
+    auto step = [&](Codes& y, int& k, int behind) __attribute__((always_inline)) {      // behind: the block that is on its way behind this one
+      f32x16 S;
+      uint32_t P[8], R[8];
+      turn(y);
+      const int n = n0(k);
+      k = next_seen(behind + 1);
+      if (k < n_blocks) {
+        advance(k);
+        fetch(k, y);
+      }
+      scores4(S);
+      softmax(n, S, P, R);
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        u32x4 v[4];
+        values4(tt, v);
+        pv(v, tt, P, R);
+      }
+    };
+    while (at[0] < n_blocks) {
+      step(x[0], at[0], at[1]);
+      if (at[1] >= n_blocks) break;
+      step(x[1], at[1], at[0]);
+    }
+  }
+
+  // true: a page was not there, or a value not finite, and the range has to be taken one key at a time
+  __device__ __forceinline__ bool run() {
+    if (n_blocks > 0) {
+      if constexpr (KV4) pass4();
+      else pass16();
+    }
+    float z = 0.f;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) z = fmaf(O[db][i], 0.f, z);
+    l += __shfl_xor(l, 32);
+    if (__syncthreads_or(lost || !(z == 0.f) || !(l < 0x1p120f) ? 1 : 0) != 0) return true;
+    // ---- the waves' results, joined: rows of 32 groups of four outputs, group d of row r at d ^ r ----
+    float* const sh_m = reinterpret_cast<float*>(smem + kCkWaves * kCkBlockBytes);
+    float* const sh_l = sh_m + kCkWaves * kCkNarrowRows;
+    if (g == 0) {
+      sh_m[wave * kCkNarrowRows + r] = m;
+      sh_l[wave * kCkNarrowRows + r] = l;
+    }
+    if (r < t.rows) {
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        int d;                                                              // group of four dims
+        float4 o;
+        if constexpr (KV4) {
+          d = (k >> 2) * 8 + g * 4 + (k & 3);
+          o = make_float4(O[0][k], O[1][k], O[2][k], O[3][k]);
+        } else {
+          const int db = k >> 2, i4 = k & 3;
+          d = db * 8 + i4 * 2 + g;
+          o = make_float4(O[db][i4 * 4], O[db][i4 * 4 + 1], O[db][i4 * 4 + 2], O[db][i4 * 4 + 3]);
+        }
+        *reinterpret_cast<float4*>(mine + r * 512 + ((d ^ r) & 31) * 16) = o;
+      }
+    }
+    __syncthreads();
+    const int row = threadIdx.x >> 4;
+    if (row >= t.rows) return false;
+    const float ninf = -__builtin_huge_valf();
+    float M = ninf, L = 0.f;
+#pragma unroll
+    for (int w = 0; w < kCkWaves; ++w) M = fmaxf(M, sh_m[w * kCkNarrowRows + row]);
+    float o[2][4] = {};
+    if (M != ninf) {
+#pragma unroll
+      for (int w = 0; w < kCkWaves; ++w) {
+        const float cw = fast_exp2((sh_m[w * kCkNarrowRows + row] - M) * c);
+        L += sh_l[w * kCkNarrowRows + row] * cw;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int d = (threadIdx.x & 15) + 16 * e;
+          const float4 v = *reinterpret_cast<const float4*>(smem + w * kCkBlockBytes + row * 512 + ((d ^ row) & 31) * 16);
+          o[e][0] = fmaf(v.x, cw, o[e][0]);
+          o[e][1] = fmaf(v.y, cw, o[e][1]);
+          o[e][2] = fmaf(v.z, cw, o[e][2]);
+          o[e][3] = fmaf(v.w, cw, o[e][3]);
+        }
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) chunk_store4<F16>(a, t, row, 4 * ((threadIdx.x & 15) + 16 * e), M, L, L, o[e]);
+    return false;
+  }
+};
+
+// A workgroup's unit, either way.
+template <bool F16, bool LOCAL, bool KV4, bool FULL>
+__device__ __forceinline__ void chunk_unit_attend(const ChunkArgs& a, unsigned char* smem) {
+  ChunkTile t;
+  if (!chunk_tile<LOCAL, KV4>(a, &t)) return;
+  bool exact = false;
+  if (t.rows <= kCkNarrowRows) {
+    exact = ChunkNarrow<F16, LOCAL, KV4>(a, t, smem).run();
+    if (!exact) return;
+  }
+  ChunkWide<F16, LOCAL, KV4, FULL>(a, t, smem).run(exact);
+}
+
+}  // namespace rtp

@@ -298,7 +298,8 @@ __device__ __forceinline__ void chunk_pv_seen(const unsigned char* v_rows, uint3
 // 16 bytes per lane from global memory to LDS, 1 KiB per wave.  (Assembly, since through the compiler's intrinsic every later LDS read waits for
 // all outstanding loads; whoever reads the rows waits for them itself.)
 __device__ __forceinline__ void chunk_load_lds(uint32_t dst, const uint8_t* base, uint32_t offset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(offset), "s"(base) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(dst)), "v"(offset),
+               "s"(uniform64((int64_t)(uintptr_t)base)) : "memory", "m0");
 }
 template <int N>
 __device__ __forceinline__ void chunk_wait_loads() {          // all but the last N of the wave's loads have landed

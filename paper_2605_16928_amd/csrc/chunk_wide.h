@@ -477,10 +477,11 @@ struct ChunkWide {
     }
   }
 
-  __device__ __forceinline__ void run() {
+  // exact: a first pass has been made, and does not do
+  __device__ __forceinline__ void run(bool exact) {
     m = -__builtin_huge_valf();
     clear();
-    if (t.it_lo < t.it_hi && fast_pass()) exact_pass();
+    if (t.it_lo < t.it_hi && (exact || fast_pass())) exact_pass();
     const float sum = l + __shfl_xor(l, 32), full = F + __shfl_xor(F, 32);
     if (!qok) return;
 #pragma unroll
