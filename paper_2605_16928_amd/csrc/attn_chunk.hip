@@ -20,8 +20,10 @@ namespace rtp {
 // B > 64: the same by one workgroup, once for the launches behind it.
 constexpr int kPlanThreads = 1024;
 __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(const ChunkArgs a) {
+  fetch_arguments<ChunkArgs>();
   constexpr int NW = kPlanThreads / 64;
-  __shared__ uint64_t sh_units[NW][64], sh_split[NW][64], sh_work[NW];
+  __shared__ ChunkSums sh_sums[NW][64];
+  __shared__ float sh_work[NW];
   __shared__ int sh_longest[NW], sh_candidate, sh_sum[3][NW];
   const ChunkShape& s = a.shape;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -34,25 +36,27 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(const ChunkArg
   __syncthreads();
   for (int w = 0; w < NW; ++w) longest = max(longest, sh_longest[w]);
   const uint32_t magic = chunk_magic(longest);
-  uint64_t units = 0, split_units = 0, work = 0;
+  ChunkSums sums = {};
+  float work = 0.f;
   for (int b0 = wave * 64; b0 < s.B; b0 += kPlanThreads) {
     const ChunkLane mine = chunk_lane(a, b0 + lane);
-    chunk_add_up(mine, min(64, s.B - b0), longest, magic, &units, &split_units);
-    work += (uint64_t)(uint32_t)mine.tiles * (uint32_t)mine.key_tiles;
+    chunk_add_up(s, mine, min(64, s.B - b0), longest, magic, &sums);
+    work += (float)mine.tiles * (float)mine.key_tiles;
   }
-  work = wave_incl_scan(work);
-  sh_units[wave][lane] = units;
-  sh_split[wave][lane] = split_units;
-  if (lane == 63) sh_work[wave] = work;
+  work = wave_sum_f32(work);
+  sh_sums[wave][lane] = sums;
+  if (lane == 0) sh_work[wave] = work;
   __syncthreads();
   if (wave == 0) {
-    units = split_units = work = 0;
+    sums = ChunkSums{};
+    work = 0.f;
     for (int w = 0; w < NW; ++w) {
-      units += sh_units[w][lane];
-      split_units += sh_split[w][lane];
+      sums.units += sh_sums[w][lane].units;
+      sums.cut_units += sh_sums[w][lane].cut_units;
+      sums.cut_rows += sh_sums[w][lane].cut_rows;
       work += sh_work[w];
     }
-    const int best = chunk_best(s, work, units, split_units);
+    const int best = s.cap > 0 ? chunk_best(s, longest, work, sums) : 1;
     if (lane == 0) {
       sh_candidate = best;
       a.plan[kPlanCandidate] = best;
@@ -65,7 +69,7 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(const ChunkArg
   for (int b0 = 0; b0 < s.B; b0 += kPlanThreads) {
     const ChunkLane mine = chunk_lane(a, b0 + tid);
     const int S = chunk_splits(mine.key_tiles, longest, sh_candidate, magic), own = mine.tiles * S;
-    const int add[3] = {own, S > 1 ? own : 0, S > 1 ? mine.n * a.n_served : 0};
+    const int add[3] = {own, S > 1 ? own : 0, S > 1 ? mine.n * a.shape.n_served : 0};
     int last[3];
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
@@ -88,30 +92,37 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(const ChunkArg
   if (tid < 3) lists[tid][s.B] = before[tid];
 }
 
-template <bool F16, bool LOCAL, bool FULL>
-__global__ __launch_bounds__(kCkThreads, 2) void chunk_attn_kernel(const ChunkArgs a) {
-  __shared__ __attribute__((aligned(16))) unsigned char smem[kCkLds];
-  chunk_unit_attend<F16, LOCAL, false, FULL>(a, smem);
+RTP_CHUNK_KERNELS(chunk_attn_kernel, chunk_again_kernel, chunk_narrow_kernel, false)
+
+static void launch_chunk_16(const ChunkArgs& a, unsigned grid, bool narrow, hipStream_t stream) {
+  RTP_CHUNK_LAUNCH(chunk_attn_kernel, chunk_again_kernel, chunk_narrow_kernel, false, false)
+  RTP_CHUNK_LAUNCH(chunk_attn_kernel, chunk_again_kernel, chunk_narrow_kernel, true, false)
+  RTP_CHUNK_LAUNCH(chunk_attn_kernel, chunk_again_kernel, chunk_narrow_kernel, false, true)
+  RTP_CHUNK_LAUNCH(chunk_attn_kernel, chunk_again_kernel, chunk_narrow_kernel, true, true)
 }
+// attn_chunk_kv4.hip
+void launch_chunk_kv4(const ChunkArgs& a, unsigned grid, bool narrow, hipStream_t stream);
 
 // Merges the ranges of the rows whose tiles were cut: SLICES groups of 32 lanes per row take the ranges in turn, a lane 4 of the 128 dims.
 template <int SLICES>
 __global__ __launch_bounds__(256) void chunk_merge_kernel(const ChunkArgs a) {
+  fetch_arguments<ChunkArgs>();
   __shared__ float sh_h[8][3];
   __shared__ __attribute__((aligned(16))) float sh_acc[8][kHeadDim];
   constexpr int kRows = 8 / SLICES;
   const ChunkShape& sh = a.shape;
   const int tid = threadIdx.x, d4 = tid & 31, grp = tid >> 5, slice = grp % SLICES;
   const float ninf = -__builtin_huge_valf();
+  const ChunkPlan plan = chunk_plan(a);
   for (int at0 = blockIdx.x * kRows;; at0 += (int)gridDim.x * kRows) {
-    const ChunkSpot spot = chunk_find<true>(a, at0);                 // (the rows of a workgroup: those of one sequence, or the next ones' too)
+    const ChunkSpot spot = chunk_find<true>(a, plan, at0);                 // (the rows of a workgroup: those of one sequence, or the next ones' too)
     if (spot.b < 0) return;
     // row -> (token, served head)
     const int at = at0 + grp / SLICES;
     ChunkSpot mine = spot;
-    if (spot.rel + kRows > spot.n * a.n_served) {                     // (the same for the whole workgroup)
+    if (spot.rel + kRows > spot.n * a.shape.n_served) {                     // (the same for the whole workgroup)
       for (int k = 0; k < kRows; ++k) {
-        const ChunkSpot other = chunk_find<true>(a, at0 + k);
+        const ChunkSpot other = chunk_find<true>(a, plan, at0 + k);
         if (grp / SLICES == k) mine = other;
       }
     } else {
@@ -122,16 +133,11 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(const ChunkArgs a) {
     float4 A = make_float4(0.f, 0.f, 0.f, 0.f);
     int64_t o = 0;
     if (have) {
-      const int t = mine.rel / a.n_served, hs = mine.rel - t * a.n_served;
-      int slot = 0;
-      while (hs >= sh.slot_first[slot] + sh.slot_n[slot]) ++slot;
-      const int nh = sh.slot_n[slot], tile = t / sh.tok[nh];
-      const int row = (t - tile * sh.tok[nh]) * nh + hs - sh.slot_first[slot];
-      int step;
-      const int first = chunk_unit_of(sh, mine.n, mine.splits, slot, tile, &step);
-      o = (int64_t)(mine.q0 + t) * a.n_q_heads + sh.heads[hs];
-      const float* p = a.part + ((int64_t)(mine.part0 + first) * a.part_rows + row) * kCkPart;
-      const int64_t pstep = (int64_t)step * a.part_rows * kCkPart;
+      const int t = mine.rel / sh.n_served;
+      const ChunkRow x = chunk_row(sh, mine.n, mine.splits, t, mine.rel - t * sh.n_served);
+      o = (int64_t)(mine.q0 + t) * a.n_q_heads + x.head;
+      const float* p = a.part + ((int64_t)(mine.part0 + x.unit) * a.part_rows + x.row) * kCkPart;
+      const int64_t pstep = (int64_t)x.step * a.part_rows * kCkPart;
       for (int s0 = slice; s0 < mine.splits; s0 += 4 * SLICES) {
         float4 h[4], v[4];
 #pragma unroll
@@ -186,9 +192,6 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(const ChunkArgs a) {
   }
 }
 
-// attn_chunk_kv4.hip
-void launch_chunk_kv4(const ChunkArgs& a, unsigned grid, bool local, bool full, hipStream_t stream);
-
 // ---- host side ----------------------------------------------------------------------------------------------------------------------
 namespace {
 int compute_units() {
@@ -203,49 +206,53 @@ int compute_units() {
 
 enum { kServeAll = 0, kServeRet = 1, kServeLocal = 2 };
 
-// The heads that a call serves, by KV head.
-void serve(const rtp_layer_desc* L, const HeadTable& ht, int which, ChunkShape* s, int32_t* n_served) {
-  const int group = L->n_q_heads / L->n_kv_heads;
-  int n = 0;
-  for (int kv = 0; kv < L->n_kv_heads; ++kv) {
-    const int first = n;
-    for (int h = kv * group; h < (kv + 1) * group; ++h)
-      if (which == kServeAll || (ht.is_ret[h] != 0) == (which == kServeRet)) s->heads[n++] = (uint8_t)h;
-    if (n == first) continue;
-    s->slot_kv[s->n_slots] = (uint8_t)kv;
-    s->slot_first[s->n_slots] = (uint8_t)first;
-    s->slot_n[s->n_slots] = (uint8_t)(n - first);
-    ++s->cnt[n - first];
-    ++s->n_slots;
-  }
-  for (int k = 1; k <= 8; ++k) s->tok[k] = (uint16_t)(kChunkRows / k);
-  *n_served = n;
+// The heads that a call serves, and which tokens they see.
+void serve(const rtp_layer_desc* L, const HeadTable& ht, int which, ChunkShape* s) {
+  s->group = L->n_q_heads / L->n_kv_heads;
+  s->n_kv = L->n_kv_heads;
+  for (int h = 0; h < L->n_q_heads; ++h)
+    if (which == kServeAll || (ht.is_ret[h] != 0) == (which == kServeRet)) {
+      s->served[h >> 5] |= 1u << (h & 31);
+      ++s->n_served;
+    }
+  for (int kv = 0; kv < s->n_kv; ++kv)
+    if (const int n = chunk_bits(chunk_members(*s, kv))) ++s->count[8 - chunk_shift(n)];
+  for (int kv = 0; kv < s->n_kv; ++kv) s->widest = std::max(s->widest, chunk_bits(chunk_members(*s, kv)));
+  s->local = which == kServeLocal;
+  s->sink = L->sink;
+  s->window = L->window;
 }
+
+constexpr int kUncutKeys = 1024;
 
 struct ChunkSizes {
   int64_t tiles;               // query tiles that the bounds allow
   int64_t cap;                 // units of cut tiles
   int32_t part_rows;
-  size_t plan_bytes, part_bytes;
-  size_t total() const { return plan_bytes + part_bytes; }
+  bool narrow;                 // no tile has more than 32 rows
+  int64_t run;                 // units in a row on one die
+  size_t plan_bytes, again_bytes, part_bytes;
+  size_t total() const { return plan_bytes + again_bytes + part_bytes; }
 };
 ChunkSizes chunk_sizes(const ChunkShape& s, int32_t B, int64_t total_q, int64_t max_q, int64_t max_ctx) {
   ChunkSizes z = {};
-  int widest = 1;
   max_q = std::max<int64_t>(1, std::min(max_q, total_q));
-  for (int h = 1; h <= 8; ++h) {
-    if (!s.cnt[h]) continue;
-    widest = h;
+  for (int k = 0; k < 4; ++k) {
     // a sequence of n tokens has ceil(n / tok) tiles: at most n of them, at most one more than its share
-    const int64_t per_seq = (max_q + s.tok[h] - 1) / s.tok[h];
-    z.tiles += s.cnt[h] * std::min(std::min(total_q, total_q / s.tok[h] + B), per_seq * B);
+    const int64_t tok = kChunkRows >> k, per_seq = (max_q + tok - 1) / tok;
+    z.tiles += s.count[k] * std::min(std::min(total_q, total_q / tok + B), per_seq * B);
   }
-  // ranges of two key tiles and more, about two units to a compute unit
+  const int widest = std::max(s.widest, 1);
+  z.narrow = max_q * widest <= kCkNarrowRows;
+  // ranges of two key tiles and more, at most four per compute unit; contexts that a workgroup goes through in the time of a merge launch are not cut
   int64_t keys = max_ctx;
   if (s.local) keys = std::min<int64_t>(keys, (int64_t)s.sink + s.window + 64);
-  const int64_t ranges = std::max<int64_t>(1, std::min<int64_t>((keys + 2 * kCkK - 1) / (2 * kCkK), 289));
+  const int64_t ranges = keys <= kUncutKeys ? 1 : std::min<int64_t>((keys + 2 * kCkK - 1) / (2 * kCkK), 289);
   z.cap = ranges > 1 ? std::min<int64_t>(z.tiles * ranges, 4 * (int64_t)compute_units()) : 0;
   z.part_rows = (int32_t)std::min<int64_t>(kChunkRows, max_q * widest);
+  // (a run: the tiles of one sequence, about)
+  for (z.run = 1; z.run < 32 && z.run * 2 <= (max_q + kChunkRows / 8 - 1) / (kChunkRows / 8);) z.run *= 2;
+  z.again_bytes = z.narrow ? 0 : align_up((size_t)(z.tiles + z.cap + 8 * 32) * sizeof(int32_t), 256);
   z.plan_bytes = B > 64 ? align_up((size_t)(kPlanHead + 3 * ((int64_t)B + 1)) * sizeof(int32_t), 256) : 0;
   z.part_bytes = align_up((size_t)z.cap * z.part_rows * kCkPart * sizeof(float), 256);
   return z;
@@ -257,11 +264,7 @@ size_t chunk_workspace(const rtp_layer_desc* layer, int which, int32_t B, int32_
       max_ctx <= 0 || max_ctx > ((int64_t)1 << 30))
     return 256;
   ChunkShape s = {};
-  int32_t served = 0;
-  serve(layer, ht, which, &s, &served);
-  s.local = which == kServeLocal;
-  s.sink = layer->sink;
-  s.window = layer->window;
+  serve(layer, ht, which, &s);
   return std::max<size_t>(256, chunk_sizes(s, B, total_q, max_q, max_ctx).total());
 }
 
@@ -283,28 +286,22 @@ int32_t chunk_call(const char* who, int which, const rtp_layer_desc* layer, cons
     return fail(RTP_ERR_INVALID_ARG, "%s: q_stride must be a multiple of 8 elements that holds a token's rows", who);
   if (chunk->total_q > 0 && rows_overlap(q, q_stride, width, out, width, width, chunk->total_q))
     return fail(RTP_ERR_INVALID_ARG, "%s: out overlaps q", who);
-  serve(layer, ht, which, &a.shape, &a.n_served);
-  a.shape.local = which == kServeLocal;
-  a.shape.sink = layer->sink;
-  a.shape.window = layer->window;
-  if (a.n_served == 0 || chunk->total_q == 0) {
+  serve(layer, ht, which, &a.shape);
+  if (a.shape.n_served == 0 || chunk->total_q == 0) {
     clear_error();
     return RTP_OK;
   }
   const ChunkSizes z = chunk_sizes(a.shape, chunk->B, chunk->total_q, chunk->max_q, chunk->max_ctx);
   if (z.total() > 0 && (!ws || ((uintptr_t)ws & 255) || ws_bytes < z.total()))
     return fail(RTP_ERR_WORKSPACE, "%s: workspace of %zu bytes, 256-byte aligned, needed", who, z.total());
-  const int64_t run = std::min<int64_t>(32, (std::min(chunk->max_q, chunk->total_q) + kChunkRows / 8 - 1) / (kChunkRows / 8));
-  a.run = 1;
-  while (a.run * 2 <= run) a.run *= 2;
-  const int64_t deal = 8 * (int64_t)a.run, grid = (z.tiles + z.cap + deal - 1) / deal * deal;
+  const int64_t grid = (z.tiles + z.cap + 8 * z.run - 1) / (8 * z.run) * (8 * z.run);
   if (grid > 0x7fffffff / kCkThreads) return fail(RTP_ERR_UNSUPPORTED, "%s: too many query tiles for one call", who);
   clear_error();
   a.shape.B = chunk->B;
   a.shape.total_q = chunk->total_q;
   a.shape.max_q = chunk->max_q;
   a.shape.cap = (int32_t)z.cap;
-  a.shape.n_cu = compute_units();
+  a.shape.places = (float)(compute_units() * (z.narrow ? 2 : 1));
   a.q = (const uint16_t*)q;
   a.q_stride = q_stride;
   a.q_offset = chunk->q_offset;
@@ -315,28 +312,18 @@ int32_t chunk_call(const char* who, int which, const rtp_layer_desc* layer, cons
   a.out = (uint16_t*)out;
   a.lse = lse;
   a.plan = (int32_t*)ws;
-  a.part = (float*)((uint8_t*)ws + z.plan_bytes);
+  a.again = (int32_t*)((uint8_t*)ws + z.plan_bytes);
+  a.part = (float*)((uint8_t*)ws + z.plan_bytes + z.again_bytes);
+  while ((1 << a.run_shift) < z.run) ++a.run_shift;
   a.part_rows = z.part_rows;
   a.f16 = layer->kv_dtype == RTP_DTYPE_FP16;
   if (chunk->B > 64) RTP_LAUNCH(chunk_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a);
-  const bool local = a.shape.local != 0, full = lse != nullptr;
-#define RTP_CHUNK(F16, LOCAL, FULL)                                                                         \
-  if ((a.f16 != 0) == F16 && local == LOCAL && full == FULL && !kv4)                                        \
-    RTP_LAUNCH((chunk_attn_kernel<F16, LOCAL, FULL>), dim3((unsigned)grid), dim3(kCkThreads), 0, stream, a);
-  RTP_CHUNK(false, false, false)
-  RTP_CHUNK(true, false, false)
-  RTP_CHUNK(false, true, false)
-  RTP_CHUNK(true, true, false)
-  RTP_CHUNK(false, false, true)
-  RTP_CHUNK(true, false, true)
-  RTP_CHUNK(false, true, true)
-  RTP_CHUNK(true, true, true)
-#undef RTP_CHUNK
-  if (kv4) launch_chunk_kv4(a, (unsigned)grid, local, full, stream);
+  if (kv4) launch_chunk_kv4(a, (unsigned)grid, z.narrow, stream);
+  else launch_chunk_16(a, (unsigned)grid, z.narrow, stream);
   if (z.cap > 0) {
-    const int64_t rows = (int64_t)chunk->total_q * a.n_served;
-    if (rows <= 2048) RTP_LAUNCH(chunk_merge_kernel<8>, dim3((unsigned)rows), dim3(256), 0, stream, a);
-    else RTP_LAUNCH(chunk_merge_kernel<2>, dim3((unsigned)std::min<int64_t>((rows + 3) / 4, 8192)), dim3(256), 0, stream, a);
+    const int64_t rows = (int64_t)chunk->total_q * a.shape.n_served;
+    if (rows <= 2048) RTP_LAUNCH(chunk_merge_kernel<8>, dim3((unsigned)std::min<int64_t>(rows, 1024)), dim3(256), 0, stream, a);
+    else RTP_LAUNCH(chunk_merge_kernel<2>, dim3((unsigned)std::min<int64_t>((rows + 3) / 4, 1024)), dim3(256), 0, stream, a);
   }
   return check_launch(who);
 }

@@ -1,5 +1,5 @@
-// A query tile of up to 32 rows -- single tokens, drafts, the ends of chunks: bound by the bytes of K and V.  All rows fit one wave, so the eight
-// waves of the workgroup take blocks of 32 keys in turn, each on its own: no barrier until the waves' results are joined in LDS.
+// A query tile of up to 32 rows -- single tokens, drafts, the ends of chunks: bound by the bytes of K and V.  All rows fit one wave, so the waves of
+// the workgroup take blocks of 32 keys in turn, each on its own: no barrier until their results are joined in LDS.
 //
 // 16-bit rows: a wave owns 16 KiB, K and V of one block.  The next K sets out when the scores have been computed, the next V behind the PV product;
 // eight waves at different places keep 64 to 128 KiB of a compute unit's loads in flight, without a second buffer.
@@ -9,6 +9,9 @@
 //
 // The running reference follows a row's maximum only when it is left behind by more than 2^8.  Probabilities enter the product in two parts, their
 // rounding to 16 bits and the rounding of the rest: the matrix cores have the time, and an output is then as exact as its own rounding.
+//
+// Where a page was not there or a result is not finite, the tile is taken again with care: keys are masked by their pages too, and what a row does
+// not see does not reach it, whatever it holds.
 #pragma once
 
 #include "chunk_wide.h"
@@ -17,8 +20,8 @@ namespace rtp {
 
 constexpr int kCkNarrowRows = 32;
 constexpr int kCkBlockBytes = 2 * 32 * kHeadDim * 2;                        // K and V of 32 keys; 32 rows of 128 outputs
-constexpr int kCkNarrowLds = kCkWaves * kCkBlockBytes + kCkWaves * kCkNarrowRows * 2 * 4;
-constexpr int kCkLds = kCkNarrowLds > kCkWideLds ? kCkNarrowLds : kCkWideLds;
+constexpr int chunk_narrow_lds(int waves) { return waves * (kCkBlockBytes + kCkNarrowRows * 2 * 4); }
+constexpr int kCkLds = chunk_narrow_lds(kCkWaves) > kCkWideLds ? chunk_narrow_lds(kCkWaves) : kCkWideLds;
 
 // LDS words that only the own wave writes and reads.
 __device__ __forceinline__ void chunk_wave_fence() {
@@ -26,7 +29,7 @@ __device__ __forceinline__ void chunk_wave_fence() {
   __builtin_amdgcn_wave_barrier();
 }
 
-template <bool F16, bool LOCAL, bool KV4>
+template <bool F16, bool LOCAL, bool KV4, int NW, bool CARE>
 struct ChunkNarrow {
   const ChunkArgs& a;
   const ChunkTile& t;
@@ -49,13 +52,11 @@ struct ChunkNarrow {
   __device__ __forceinline__ ChunkNarrow(const ChunkArgs& a_, const ChunkTile& t_, unsigned char* smem_)
       : a(a_), t(t_), smem(smem_), mine(smem_ + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kCkBlockBytes), lane(threadIdx.x & 63),
         wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), g(lane >> 5), r(lane & 31), c(a_.scale_log2), rd(chunk_reads()),
-        sight(chunk_sight(a_.shape, t_, lane & 31)), n_blocks((2 * (t_.it_hi - t_.it_lo) - wave + kCkWaves - 1) / kCkWaves), window(-2), lost(false) {
-    const bool qok = r < t.rows;
-    const int rt = (r * t.over) >> 16;
-    const int head = qok ? a.shape.heads[t.head0 + r - rt * t.nh] : 0;
-    const uint16_t* src = a.q + (t.q0 + rt) * a.q_stride + head * kHeadDim + g * (KV4 ? 64 : 8);
+        sight(chunk_sight(a_.shape, t_, lane & 31)), n_blocks((2 * (t_.it_hi - t_.it_lo) - wave + NW - 1) / NW), window(-2), lost(false) {
+    const int row_c = min(r, t.rows - 1), rt = (row_c * t.over) >> 16;
+    const uint16_t* src = a.q + (t.q0 + rt) * a.q_stride + chunk_head(a, t, row_c, rt) * kHeadDim + g * (KV4 ? 64 : 8);
 #pragma unroll
-    for (int kk = 0; kk < 8; ++kk) q[kk] = qok ? *reinterpret_cast<const u32x4*>(src + kk * (KV4 ? 8 : 16)) : (u32x4){0u, 0u, 0u, 0u};
+    for (int kk = 0; kk < 8; ++kk) q[kk] = *reinterpret_cast<const u32x4*>(src + kk * (KV4 ? 8 : 16));
     if constexpr (KV4) {
       base0 = a.c4.codes + (int64_t)t.kvh * a.c4.code_head_stride;
       base1 = a.c4.scales + (int64_t)t.kvh * a.c4.scale_head_stride;
@@ -73,7 +74,7 @@ struct ChunkNarrow {
 
   // First key of the wave's block k.
   __device__ __forceinline__ int n0(int k) const {
-    const int j = wave + k * kCkWaves;
+    const int j = wave + k * NW;
     return chunk_tile_n0(t, t.it_lo + (j >> 1)) + (j & 1) * 32;
   }
   __device__ __forceinline__ int next_seen(int k) const {
@@ -118,14 +119,21 @@ struct ChunkNarrow {
   __device__ __forceinline__ void send(int k, bool v) {
     const uint32_t lds = (uint32_t)(size_t)(__attribute__((address_space(3))) unsigned char*)mine + (v ? kCkBlockBytes / 2 : 0);
     const int sub = lane >> 4, pos = lane & 15;
-    const bool edge = n0(k) + 32 > t.kend;
     const uint8_t* const base = v ? base1 : base0;
+    const int64_t half[2] = {place(at_lo, at_hi, k, 0), place(at_lo, at_hi, k, 1)};
+    if (n0(k) + 32 <= t.kend) {
+      const uint32_t off = sub * a.c16.row_bytes;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int rel = 4 * (i & 3) + sub;                                    // row in its half
-      const int chunk = v ? (((pos >> 1) ^ (2 * sub)) << 1) | (pos & 1) : pos ^ rel;
-      const int at = edge ? min(rel, left(k, i >> 2)) : rel;
-      chunk_load_lds(lds + i * 1024, base + place(at_lo, at_hi, k, i >> 2), (uint32_t)(at * a.c16.row_bytes + chunk * 16));
+      for (int i = 0; i < 8; ++i) {                                         // row 4 (i % 4) + sub of its half
+        const int chunk = v ? (((pos >> 1) ^ (2 * sub)) << 1) | (pos & 1) : pos ^ sub ^ (4 * (i & 3));
+        chunk_load_lds(lds + i * 1024, base + half[i >> 2] + (i & 3) * 4 * a.c16.row_bytes, off + chunk * 16);
+      }
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < 8; ++i) {
+        const int rel = 4 * (i & 3) + sub, chunk = v ? (((pos >> 1) ^ (2 * sub)) << 1) | (pos & 1) : pos ^ rel;
+        chunk_load_lds(lds + i * 1024, base + (i < 4 ? half[0] : half[1]), (uint32_t)(min(rel, left(k, i >> 2)) * a.c16.row_bytes + chunk * 16));
+      }
     }
   }
   static __device__ __forceinline__ void reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
@@ -184,7 +192,11 @@ struct ChunkNarrow {
         const int n = 8 * i4 + 4 * g + j;
         const uint32_t x = *reinterpret_cast<const uint16_t*>(mine + line_at(n, 4 + (r >> 3)) + (r & 7) * 2);
         const uint32_t y = *reinterpret_cast<const uint16_t*>(mine + line_at(n + 1, 4 + (r >> 3)) + (r & 7) * 2);
-        const float fx = kv4_scale(sc, j), fy = kv4_scale(sc, j + 1);
+        float fx = kv4_scale(sc, j), fy = kv4_scale(sc, j + 1);
+        if constexpr (CARE) {                                               // (not_numbers() has the blocks that are none)
+          fx = fx < __builtin_huge_valf() ? fx : 0.f;
+          fy = fy < __builtin_huge_valf() ? fy : 0.f;
+        }
         const int w = 2 * e + (j >> 1);
         if constexpr (F16) {
           const f32x2_t x0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x, fx, 0), x1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x, fx, 1);
@@ -207,12 +219,33 @@ struct ChunkNarrow {
     }
   }
 
-  // ---- a block's probabilities, as their rounding P and the rounding of the rest R ----
-  __device__ __forceinline__ void softmax(int n, f32x16& S, uint32_t (&P)[8], uint32_t (&R)[8]) {
-    const float ninf = -__builtin_huge_valf();
-    if (!chunk_all_seen<LOCAL>(a.shape, t, t.m_lo, t.m_hi, n, 32) || t.rows < kCkNarrowRows) {
+  // Rows that see a token whose V has a block that is not a number have none there either.
+  __device__ __forceinline__ void not_numbers(uint32_t seen) {
+    uint32_t hit = 0;                                                       // bit: block of 32 dims
 #pragma unroll
-      for (int i = 0; i < 16; ++i) S[i] = chunk_sees<LOCAL>(a.shape, sight, n + 8 * (i >> 2) + 4 * g + (i & 3)) ? S[i] : ninf;
+    for (int i = 0; i < 16; ++i) {
+      const unsigned char* sc = mine + kScalesAt + (2 * (i >> 2) + g) * kKv4Group + 16 + (i & 3);
+#pragma unroll
+      for (int blk = 0; blk < 4; ++blk) hit |= ((seen >> i) & 1u) && sc[blk * 4] == 255 ? 1u << blk : 0u;
+    }
+    hit |= (uint32_t)__shfl_xor((int)hit, 32);
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+#pragma unroll
+      for (int db = 0; db < 4; ++db) O[db][i] = (hit >> (i >> 2)) & 1u ? __builtin_nanf("") : O[db][i];
+  }
+
+  // ---- a block's probabilities, as their rounding P and the rounding of the rest R ----
+  // CARE: seen = bit i, the row sees the lane's i-th key, whose page is there.
+  __device__ __forceinline__ void softmax(int n, f32x16& S, uint32_t (&P)[8], uint32_t (&R)[8], uint32_t& seen) {
+    const float ninf = -__builtin_huge_valf();
+    seen = 0xffffu;
+    if constexpr (CARE) {
+      seen = chunk_seen<LOCAL, KV4>(a, t, sight, n + 4 * g);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) S[i] = (seen >> i) & 1u ? S[i] : ninf;
+    } else if (!chunk_all_seen<LOCAL>(a.shape, t, t.m_lo, t.m_hi, n, 32) || t.rows < kCkNarrowRows) {
+      chunk_mask<LOCAL>(sight, n + 4 * g, S);
     }
     float mx = fmaxf(S[0], S[1]);
 #pragma unroll
@@ -246,7 +279,7 @@ struct ChunkNarrow {
 
   __device__ __forceinline__ void pass16() {
     f32x16 S;
-    uint32_t P[8], R[8];
+    uint32_t P[8], R[8], seen;
     int k = next_seen(0);
     if (k < n_blocks) {
       advance(k);
@@ -264,11 +297,22 @@ struct ChunkNarrow {
       for (int kk = 0; kk < 8; ++kk) S = mfma32<F16>(chunk_read_k(mine, rd, kk), q[kk], S);
       reads_done();
       if (more) send(next, false);
-      softmax(n0(k), S, P, R);
+      softmax(n0(k), S, P, R, seen);
       if (more) chunk_wait_loads<8>();
       else chunk_wait_loads<0>();
+      bool odd = false;
+      if constexpr (CARE) {
+        uint32_t any = 0;
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
+        for (int e = 0; e < 8; ++e) any |= chunk_not_finite<F16>(chunk_read_v(mine + kCkBlockBytes / 2, rd, e >> 2, e & 3));
+        odd = __ballot(any != 0u) != 0ull;
+        if (odd) {
+          chunk_pv_seen<F16>(mine + kCkBlockBytes / 2, seen, P, O);
+          chunk_pv_seen<F16>(mine + kCkBlockBytes / 2, seen, R, O);
+        }
+      }
+#pragma unroll
+      for (int tt = 0; tt < 2 && !odd; ++tt) {
         u32x4 v[4];
 #pragma unroll
         for (int db = 0; db < 4; ++db) v[db] = chunk_read_v(mine + kCkBlockBytes / 2, rd, tt, db);
@@ -292,7 +336,7 @@ struct ChunkNarrow {
       }
     auto step = [&](Codes& y, int& k, int behind) __attribute__((always_inline)) {      // behind: the block that is on its way behind this one
       f32x16 S;
-      uint32_t P[8], R[8];
+      uint32_t P[8], R[8], seen;
       turn(y);
       const int n = n0(k);
       k = next_seen(behind + 1);
@@ -301,13 +345,14 @@ struct ChunkNarrow {
         fetch(k, y);
       }
       scores4(S);
-      softmax(n, S, P, R);
+      softmax(n, S, P, R, seen);
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
         u32x4 v[4];
         values4(tt, v);
         pv(v, tt, P, R);
       }
+      if constexpr (CARE) not_numbers(seen);
     };
     while (at[0] < n_blocks) {
       step(x[0], at[0], at[1]);
@@ -316,7 +361,7 @@ struct ChunkNarrow {
     }
   }
 
-  // true: a page was not there, or a value not finite, and the range has to be taken one key at a time
+  // true: a page was not there or a result is not finite (never with CARE)
   __device__ __forceinline__ bool run() {
     if (n_blocks > 0) {
       if constexpr (KV4) pass4();
@@ -328,10 +373,11 @@ struct ChunkNarrow {
 #pragma unroll
       for (int i = 0; i < 16; ++i) z = fmaf(O[db][i], 0.f, z);
     l += __shfl_xor(l, 32);
-    if (__syncthreads_or(lost || !(z == 0.f) || !(l < 0x1p120f) ? 1 : 0) != 0) return true;
+    if constexpr (CARE) __syncthreads();
+    else if (__syncthreads_or(lost || !(z == 0.f) || !(l < 0x1p120f) ? 1 : 0) != 0) return true;
     // ---- the waves' results, joined: rows of 32 groups of four outputs, group d of row r at d ^ r ----
-    float* const sh_m = reinterpret_cast<float*>(smem + kCkWaves * kCkBlockBytes);
-    float* const sh_l = sh_m + kCkWaves * kCkNarrowRows;
+    float* const sh_m = reinterpret_cast<float*>(smem + NW * kCkBlockBytes);
+    float* const sh_l = sh_m + NW * kCkNarrowRows;
     if (g == 0) {
       sh_m[wave * kCkNarrowRows + r] = m;
       sh_l[wave * kCkNarrowRows + r] = l;
@@ -353,21 +399,23 @@ struct ChunkNarrow {
       }
     }
     __syncthreads();
-    const int row = threadIdx.x >> 4;
+    constexpr int kLanes = NW * 64 / kCkNarrowRows, kEach = kHeadDim / 4 / kLanes;       // threads per row, groups of four outputs per thread
+    const int row = threadIdx.x / kLanes, d0 = threadIdx.x % kLanes;
     if (row >= t.rows) return false;
     const float ninf = -__builtin_huge_valf();
     float M = ninf, L = 0.f;
 #pragma unroll
-    for (int w = 0; w < kCkWaves; ++w) M = fmaxf(M, sh_m[w * kCkNarrowRows + row]);
-    float o[2][4] = {};
-    if (M != ninf) {
+    for (int w = 0; w < NW; ++w) M = fmaxf(M, sh_m[w * kCkNarrowRows + row]);
+    float o[kEach][4] = {};
+    {
+      // (a wave without a finite logit: its sum is 0, or not a number)
 #pragma unroll
-      for (int w = 0; w < kCkWaves; ++w) {
-        const float cw = fast_exp2((sh_m[w * kCkNarrowRows + row] - M) * c);
+      for (int w = 0; w < NW; ++w) {
+        const float m_w = sh_m[w * kCkNarrowRows + row], cw = m_w == ninf ? 1.f : fast_exp2((m_w - M) * c);
         L += sh_l[w * kCkNarrowRows + row] * cw;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int d = (threadIdx.x & 15) + 16 * e;
+        for (int e = 0; e < kEach; ++e) {
+          const int d = d0 + kLanes * e;
           const float4 v = *reinterpret_cast<const float4*>(smem + w * kCkBlockBytes + row * 512 + ((d ^ row) & 31) * 16);
           o[e][0] = fmaf(v.x, cw, o[e][0]);
           o[e][1] = fmaf(v.y, cw, o[e][1]);
@@ -377,22 +425,72 @@ struct ChunkNarrow {
       }
     }
 #pragma unroll
-    for (int e = 0; e < 2; ++e) chunk_store4<F16>(a, t, row, 4 * ((threadIdx.x & 15) + 16 * e), M, L, L, o[e]);
+    for (int e = 0; e < kEach; ++e) chunk_store4<F16>(a, t, row, 4 * (d0 + kLanes * e), M, L, L, o[e]);
     return false;
   }
 };
 
-// A workgroup's unit, either way.
-template <bool F16, bool LOCAL, bool KV4, bool FULL>
-__device__ __forceinline__ void chunk_unit_attend(const ChunkArgs& a, unsigned char* smem) {
-  ChunkTile t;
-  if (!chunk_tile<LOCAL, KV4>(a, &t)) return;
-  bool exact = false;
-  if (t.rows <= kCkNarrowRows) {
-    exact = ChunkNarrow<F16, LOCAL, KV4>(a, t, smem).run();
-    if (!exact) return;
+// The kernels.  ANY: tiles of any size; what has to be taken again is noted by workgroup, for AGAIN.  NARROW: where the host knows that no tile has
+// more than 32 rows; takes its tiles again itself.
+#define RTP_CHUNK_KERNELS(ANY, AGAIN, NARROW, KV4)                                                                      \
+  template <bool F16, bool LOCAL, bool FULL>                                                                            \
+  __global__ __launch_bounds__(kCkThreads, 2) void ANY(const ChunkArgs a) {                                             \
+    fetch_arguments<ChunkArgs>();                                                                                       \
+    __shared__ __attribute__((aligned(16))) unsigned char smem[kCkLds];                                                 \
+    ChunkTile t;                                                                                                        \
+    bool again = false;                                                                                                 \
+    if (chunk_tile<LOCAL, KV4>(a, blockIdx.x, &t)) {                                                                    \
+      if (t.rows <= kCkNarrowRows) {                                                                                    \
+        again = ChunkNarrow<F16, LOCAL, KV4, kCkWaves, false>(a, t, smem).run();                                        \
+      } else {                                                                                                          \
+        ChunkWide<F16, LOCAL, KV4, FULL> w(a, t, smem);                                                                 \
+        w.m = -__builtin_huge_valf();                                                                                   \
+        w.clear();                                                                                                      \
+        again = t.it_lo < t.it_hi && w.fast_pass();                                                                     \
+        if (!again) w.store();                                                                                          \
+      }                                                                                                                 \
+    }                                                                                                                   \
+    if (threadIdx.x == 0) a.again[blockIdx.x] = again ? 1 : 0;                                                          \
+  }                                                                                                                     \
+  template <bool F16, bool LOCAL>                                                                                       \
+  __global__ __launch_bounds__(kCkThreads, 2) void AGAIN(const ChunkArgs a, int n) {                                    \
+    fetch_arguments<ChunkArgs>();                                                                                       \
+    __shared__ __attribute__((aligned(16))) unsigned char smem[kCkLds];                                                 \
+    for (int first = blockIdx.x, i = first; i < n; i += gridDim.x) {                                                    \
+      if ((i - first) / (int)gridDim.x % kCkThreads == 0) {             /* this workgroup's next flags, one to a thread */ \
+        const int64_t at = i + (int64_t)threadIdx.x * gridDim.x;                                                        \
+        if (!__syncthreads_or(at < n ? a.again[at] : 0)) {                                                              \
+          i += (kCkThreads - 1) * gridDim.x;                                                                            \
+          continue;                                                                                                     \
+        }                                                                                                               \
+      }                                                                                                                 \
+      ChunkTile t;                                                                                                      \
+      if (a.again[i] == 0 || !chunk_tile<LOCAL, KV4>(a, i, &t)) continue;                                               \
+      __syncthreads();                                                                                                  \
+      ChunkWide<F16, LOCAL, KV4, true> w(a, t, smem);                                                                   \
+      w.exact_pass();                                                                                                   \
+      w.store();                                                                                                        \
+    }                                                                                                                   \
+  }                                                                                                                     \
+  template <bool F16, bool LOCAL>                                                                                       \
+  __global__ __launch_bounds__(kCkSmallWaves * 64, 2) void NARROW(const ChunkArgs a) {                                  \
+    fetch_arguments<ChunkArgs>();                                                                                       \
+    __shared__ __attribute__((aligned(16))) unsigned char smem[chunk_narrow_lds(kCkSmallWaves)];                        \
+    ChunkTile t;                                                                                                        \
+    if (!chunk_tile<LOCAL, KV4>(a, blockIdx.x, &t)) return;                                                             \
+    if (ChunkNarrow<F16, LOCAL, KV4, kCkSmallWaves, false>(a, t, smem).run())                                           \
+      ChunkNarrow<F16, LOCAL, KV4, kCkSmallWaves, true>(a, t, smem).run();                                              \
   }
-  ChunkWide<F16, LOCAL, KV4, FULL>(a, t, smem).run(exact);
-}
+// Launches those that a call's flags name.
+#define RTP_CHUNK_LAUNCH(ANY, AGAIN, NARROW, F16_, LOCAL_)                                                              \
+  if ((a.f16 != 0) == F16_ && (a.shape.local != 0) == LOCAL_) {                                                         \
+    if (narrow) {                                                                                                       \
+      RTP_LAUNCH((NARROW<F16_, LOCAL_>), dim3(grid), dim3(kCkSmallWaves * 64), 0, stream, a);                           \
+    } else {                                                                                                            \
+      if (a.lse) RTP_LAUNCH((ANY<F16_, LOCAL_, true>), dim3(grid), dim3(kCkThreads), 0, stream, a);                     \
+      else RTP_LAUNCH((ANY<F16_, LOCAL_, false>), dim3(grid), dim3(kCkThreads), 0, stream, a);                          \
+      RTP_LAUNCH((AGAIN<F16_, LOCAL_>), dim3(grid < 256 ? grid : 256), dim3(kCkThreads), 0, stream, a, (int)grid);      \
+    }                                                                                                                   \
+  }
 
 }  // namespace rtp

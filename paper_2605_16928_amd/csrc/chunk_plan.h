@@ -1,12 +1,14 @@
 // How the attention of a batch of new tokens (attn_chunk.hip) is cut into units of work, from the lengths that only the device knows.
 // Apart from the kernels so that it also compiles for the host.
 //
-// A KV head with n served query heads takes floor(256 / n) tokens per query tile; a tile's rows are (token, head) pairs, the heads of a token
-// side by side.  A tile's keys are cut into as many ranges as its sequence has splits; a unit is one range of one tile.  A sequence's units are
+// A KV head with h served query heads takes 256, 128, 64 or 32 tokens per query tile, the most whose rows are 256 or fewer; a tile's rows are
+// (token, head) pairs, the heads of a token side by side.  A tile's keys are cut into as many ranges as its sequence has splits; a unit is one range of one tile.  A sequence's units are
 // numbered (KV head, range, tile from the last to the first): those that read the same keys are neighbours.
 //
 // One number, the candidate, fixes all splits: sequence b has ceil(candidate * key tiles of b / key tiles of the longest), so that the
 // ranges of all sequences are about equally long.
+//
+// What a kernel knows of the heads fits a few scalars: tables among a kernel's arguments lie in memory that takes microseconds to reach.
 #pragma once
 
 #include <math.h>
@@ -15,37 +17,53 @@
 namespace rtp {
 
 constexpr int kChunkRows = 256;          // rows of a query tile
-constexpr int kChunkMaxHeads = 128;
 constexpr int kChunkMostKeyTiles = 1 << 22;
 constexpr int kChunkCandidates = 64;
-// What a unit costs beside its key tiles, in key tiles: its way to the first product; its partial results, written and merged.
-constexpr int kChunkUnitCost = 3, kChunkPartCost = 2;
+// What a unit costs beside its key tiles, in key tiles: its way to the first product and from the last; a launch's, that results are merged; and
+// the rows of partial results, written and read, that take as long as a key tile per place (two passes over 528 bytes, 32 KiB a tile).
+constexpr int kChunkUnitCost = 3, kChunkMergeCost = 4, kChunkRowsPerTile = 31;
 
 struct ChunkShape {
   int32_t B, total_q, max_q;
-  int32_t n_slots;                       // KV heads with served query heads
+  int32_t group, n_kv;                   // query heads per KV head (1, 2, 4 or 8), KV heads
   int32_t local, sink, window;
   int32_t cap;                           // most units of tiles that are cut into ranges
-  int32_t n_cu;
-  uint16_t tok[9];                       // tokens per tile with n heads per KV head
-  uint16_t cnt[9];                       // KV heads with n heads
-  uint8_t slot_kv[kChunkMaxHeads], slot_n[kChunkMaxHeads], slot_first[kChunkMaxHeads];   // a slot's KV head, number of heads, first of them
-  uint8_t heads[kChunkMaxHeads];         // served query heads, ascending
+  float places;                          // workgroups that run at the same time
+  int32_t n_served, widest;              // served query heads; the most of one KV head
+  uint32_t served[4];                    // bit h: query head h is one of them
+  int32_t count[4];                      // KV heads with 1, 2, 3 or 4, and 5 to 8 of them
 };
 
 __host__ __device__ __forceinline__ int chunk_min(int a, int b) { return a < b ? a : b; }
 __host__ __device__ __forceinline__ int chunk_max(int a, int b) { return a > b ? a : b; }
-__host__ __device__ __forceinline__ int chunk_div_up(int a, int b) { return (int)(((uint32_t)a + (uint32_t)b - 1u) / (uint32_t)b); }
+
+// Tokens per query tile of a KV head with h served heads, as a power of two, and its query tiles for n new tokens.
+__host__ __device__ __forceinline__ int chunk_shift(int h) { return h > 1 ? __builtin_clz((unsigned)(h - 1)) - 24 : 8; }
+__host__ __device__ __forceinline__ int chunk_query_tiles(int n, int shift) { return (n + (1 << shift) - 1) >> shift; }
+// The served heads of a KV head, as bits, and how many they are.
+__host__ __device__ __forceinline__ uint32_t chunk_members(const ChunkShape& s, int kv) {
+  const int at = kv * s.group;
+  const uint32_t w01 = (at & 32) ? s.served[1] : s.served[0], w23 = (at & 32) ? s.served[3] : s.served[2];
+  return (((at & 64) ? w23 : w01) >> (at & 31)) & ((1u << s.group) - 1u);
+}
+__host__ __device__ __forceinline__ int chunk_bits(uint32_t m) { return __builtin_popcount(m); }
+// The place of the k-th set bit.
+__host__ __device__ __forceinline__ int chunk_nth(uint32_t m, int k) {
+  int at = 0;
+#pragma unroll
+  for (int b = 0; b < 8; ++b) {
+    at = ((m >> b) & 1u) && k == 0 ? b : at;
+    k -= (int)((m >> b) & 1u);
+  }
+  return at;
+}
 
 // Splits of the longest sequence that candidate i (0 .. 63) stands for: 1 .. 32, then 40, 48 .. 288.
 __host__ __device__ __forceinline__ int chunk_candidate(int i) { return i < 32 ? i + 1 : 32 + 8 * (i - 31); }
 
 // Query tiles of a sequence with n new tokens, over all KV heads.
 __host__ __device__ __forceinline__ int chunk_tiles(const ChunkShape& s, int n) {
-  int t = 0;
-  for (int h = 1; h <= 8; ++h)
-    if (s.cnt[h]) t += s.cnt[h] * chunk_div_up(n, s.tok[h]);
-  return t;
+  return s.count[0] * chunk_query_tiles(n, 8) + s.count[1] * chunk_query_tiles(n, 7) + s.count[2] * chunk_query_tiles(n, 6) + s.count[3] * chunk_query_tiles(n, 5);
 }
 // 64-key tiles that one of its query tiles reads (a middling one).
 __host__ __device__ __forceinline__ int chunk_key_tiles(const ChunkShape& s, int n, int ctx) {
@@ -54,48 +72,91 @@ __host__ __device__ __forceinline__ int chunk_key_tiles(const ChunkShape& s, int
     const int64_t band = (int64_t)s.sink + s.window + chunk_min(n, 64);
     if (band < keys) keys = (int)band;
   }
-  return chunk_max(1, chunk_min(chunk_div_up(keys, 64), kChunkMostKeyTiles));
+  return chunk_max(1, chunk_min((int)(((uint32_t)keys + 63u) >> 6), kChunkMostKeyTiles));
 }
-// (whole numbers only: every launch of a call comes to the same splits)
+// (Every launch of a call has to come to the same splits: whole numbers, single multiply-adds, and sums in the same order.  And it is code that
+// every workgroup goes through once, from memory: no wide division, no wide sums.)
 __host__ __device__ __forceinline__ uint32_t chunk_magic(int longest) { return 0xffffffffu / (uint32_t)longest; }
 __host__ __device__ __forceinline__ int chunk_splits(int key_tiles, int longest, int candidate, uint32_t magic) {
   const uint32_t x = (uint32_t)key_tiles * (uint32_t)candidate + (uint32_t)longest - 1u;      // at most 2^22 * 289
   return chunk_max(1, (int)(((uint64_t)x * magic) >> 32));
 }
-// What a candidate costs: rounds of units over the compute units, each as long as the mean one.
-__host__ __device__ __forceinline__ float chunk_float(uint64_t x) {      // (in halves: no shift by a count of leading zeros)
-  return fmaf((float)(uint32_t)(x >> 32), 4294967296.f, (float)(uint32_t)x);
+struct ChunkSums {
+  float units, cut_units, cut_rows;      // units; those of cut tiles; rows of partial results
+};
+__host__ __device__ __forceinline__ void chunk_sum(ChunkSums* sums, float tiles, float rows, int splits) {
+  const float S = (float)splits, cut = splits > 1 ? S : 0.f;
+  sums->units = fmaf(tiles, S, sums->units);
+  sums->cut_units = fmaf(tiles, cut, sums->cut_units);
+  sums->cut_rows = fmaf(rows, cut, sums->cut_rows);
 }
-__host__ __device__ __forceinline__ uint32_t chunk_cost(uint64_t work, uint64_t units, uint64_t split_units, int n_cu) {
-  if (units > (1u << 26)) return 0x3ffffffu;
-  const uint32_t u = units > 0 ? (uint32_t)units : 1u;
-  const float length = chunk_float(work) / (float)u;
-  const uint32_t rounds = (u + (uint32_t)n_cu - 1u) / (uint32_t)n_cu;
-  const uint64_t each = (length < 67108864.f ? (uint32_t)length : 67108864u) + 1u + kChunkUnitCost + (split_units ? kChunkPartCost : 0);
-  const uint64_t cost = rounds * each;
-  return cost < 0x3ffffffu ? (uint32_t)cost : 0x3ffffffu;
+// What a candidate costs: rounds of units over the places for workgroups, each as long as the mean one, and what the longest sequence's units are
+// longer than that: all of it where every unit has a place at once, half of it (the last round's) otherwise; and its partial results.
+__host__ __device__ __forceinline__ float chunk_over(float x, float y) {      // x / y to a few steps
+#ifdef __HIP_DEVICE_COMPILE__
+  return x * __builtin_amdgcn_rcpf(y);
+#else
+  return x / y;
+#endif
+}
+__host__ __device__ __forceinline__ float chunk_cost(float work, const ChunkSums& sums, int longest, int candidate, float places) {
+  const float mean = ceilf(chunk_over(work, sums.units)), most = ceilf(chunk_over((float)longest, (float)candidate));
+  const float rounds = ceilf(chunk_over(sums.units, places) - 0.001f);
+  float cost = rounds * (mean + (float)kChunkUnitCost);
+  cost = fmaf(most > mean ? most - mean : 0.f, rounds > 1.f ? 0.5f : 1.f, cost);
+  cost = fmaf(sums.cut_rows, chunk_over(1.f / kChunkRowsPerTile, places), cost);
+  return sums.cut_units > 0.f ? cost + (float)kChunkMergeCost : cost;
+}
+// The range of n key tiles that split k of S has: [first, first of k + 1).
+__host__ __device__ __forceinline__ void chunk_range(int n, int k, int S, int* lo, int* hi) {
+  const int each = (int)((uint32_t)n / (uint32_t)S), more = n - each * S;
+  *lo = k * each + chunk_min(k, more);
+  *hi = *lo + each + (k < more ? 1 : 0);
 }
 
 struct ChunkUnit {
-  int slot, split, tile;
+  int kv, split, tile;
+  int heads, first;                      // the KV head's served heads, and how many the KV heads before it have
 };
 // Unit r of a sequence with n new tokens and S splits.
 __host__ __device__ __forceinline__ ChunkUnit chunk_unit(const ChunkShape& s, int n, int S, int r) {
-  int slot = 0, tiles = 1;
-  for (; slot < s.n_slots; ++slot) {
-    tiles = chunk_div_up(n, s.tok[s.slot_n[slot]]);
+  ChunkUnit u = {0, 0, 0, 1, 0};
+  int tiles = 1;
+  for (; u.kv < s.n_kv; ++u.kv) {
+    u.heads = chunk_bits(chunk_members(s, u.kv));
+    if (u.heads == 0) continue;
+    tiles = chunk_query_tiles(n, chunk_shift(u.heads));
     if (r < tiles * S) break;
     r -= tiles * S;
+    u.first += u.heads;
   }
-  const int split = (int)((uint32_t)r / (uint32_t)tiles);
-  return ChunkUnit{slot, split, tiles - 1 - (r - split * tiles)};
+  u.split = (int)((uint32_t)r / (uint32_t)tiles);
+  u.tile = tiles - 1 - (r - u.split * tiles);
+  return u;
 }
-// The other way round: the number of (slot, range 0, tile) and the step from range to range.
-__host__ __device__ __forceinline__ int chunk_unit_of(const ChunkShape& s, int n, int S, int slot, int tile, int* step) {
-  int r = 0;
-  for (int k = 0; k < slot; ++k) r += chunk_div_up(n, s.tok[s.slot_n[k]]) * S;
-  *step = chunk_div_up(n, s.tok[s.slot_n[slot]]);
-  return r + *step - 1 - tile;
+// Where the partial results of served head `served` of token t lie: the number of range 0's unit, the step from range to range, the row in the unit.
+struct ChunkRow {
+  int kv, head, unit, step, row;
+};
+__host__ __device__ __forceinline__ ChunkRow chunk_row(const ChunkShape& s, int n, int S, int t, int served) {
+  ChunkRow x = {0, 0, 0, 1, 0};
+  for (; x.kv < s.n_kv; ++x.kv) {
+    const uint32_t m = chunk_members(s, x.kv);
+    const int h = chunk_bits(m);
+    if (h == 0) continue;
+    const int shift = chunk_shift(h);
+    x.step = chunk_query_tiles(n, shift);
+    if (served < h) {
+      const int tile = t >> shift;
+      x.head = x.kv * s.group + chunk_nth(m, served);
+      x.unit += x.step - 1 - tile;
+      x.row = (t - (tile << shift)) * h + served;
+      break;
+    }
+    x.unit += x.step * S;
+    served -= h;
+  }
+  return x;
 }
 
 }  // namespace rtp

@@ -11,33 +11,36 @@
 
 namespace rtp {
 
-constexpr int kCkThreads = 512;
-constexpr int kCkWaves = kCkThreads / 64;
+constexpr int kCkWaves = 8;                     // of the workgroups that take wide tiles
+constexpr int kCkThreads = kCkWaves * 64;
+constexpr int kCkSmallWaves = 4;                // of those that take narrow ones alone, two to a compute unit
 constexpr int kCkK = 64;                       // keys per tile
 constexpr int kCkPart = kHeadDim + 4;          // floats per partial row: reference, sum, sum of unrounded probabilities, pad, outputs
 constexpr int kCkTileBytes = 2 * kCkK * kHeadDim * 2;
 
 struct ChunkArgs {
   ChunkShape shape;
+  int32_t n_q_heads, f16;
+  float scale, scale_log2;
   const uint16_t* q;
   int64_t q_stride;
-  Kv16Cache c16;
-  Kv4Cache c4;
   const int32_t* q_offset;
   const int32_t* ctx_len;
-  int32_t n_q_heads, n_served;
-  float scale, scale_log2;
   uint16_t* out;
   float* lse;
   float* part;                 // [units of cut tiles, part_rows, kCkPart]
   int32_t part_rows;           // rows of a partial result: what a tile can have
+  int32_t run_shift;           // 2^run_shift units in a row go to one die
   int32_t* plan;               // B > 64: what chunk_plan_kernel leaves, kPlanHead ints and three lists of B + 1
-  int32_t run;                 // units in a row that go to one die
-  int32_t f16;
+  int32_t* again;              // [workgroups]: 1 = its unit has to be taken again
+  Kv16Cache c16;
+  Kv4Cache c4;
 };
 enum { kPlanCandidate = 0, kPlanLongest = 1, kPlanHead = 4 };
 
-// The plan of a batch of up to 64 sequences, a sequence to a lane, or of a longer one, from memory.
+__device__ __forceinline__ int64_t uniform64(int64_t x) {
+  return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x));
+}
 struct ChunkLane {
   int n, q0, ctx;              // new tokens, their first row, context
   int tiles, key_tiles;
@@ -55,21 +58,57 @@ __device__ __forceinline__ ChunkLane chunk_lane(const ChunkArgs& a, int b) {
   return s;
 }
 // Lane i adds up candidate i over the sequences that the wave's lanes hold.
-__device__ __forceinline__ void chunk_add_up(const ChunkLane& s, int lanes, int longest, uint32_t magic, uint64_t* units, uint64_t* split_units) {
+__device__ __forceinline__ void chunk_add_up(const ChunkShape& shape, const ChunkLane& s, int lanes, int longest, uint32_t magic, ChunkSums* sums) {
   const int candidate = chunk_candidate(threadIdx.x & 63);
-  for (int k = 0; k < lanes; ++k) {
-    const int tiles = __builtin_amdgcn_readlane(s.tiles, k), kt = __builtin_amdgcn_readlane(s.key_tiles, k);
-    const int S = chunk_splits(kt, longest, candidate, magic);
-    *units += (uint64_t)tiles * (uint32_t)S;
-    *split_units += S > 1 ? (uint64_t)tiles * (uint32_t)S : 0;
-  }
+  const int tiles = __float_as_int((float)s.tiles), rows = __float_as_int((float)(s.n * shape.n_served));
+#pragma unroll 1
+  for (int k = 0; k < lanes; ++k)
+    chunk_sum(sums, __int_as_float(__builtin_amdgcn_readlane(tiles, k)), __int_as_float(__builtin_amdgcn_readlane(rows, k)),
+              chunk_splits(__builtin_amdgcn_readlane(s.key_tiles, k), longest, candidate, magic));
 }
-// The best candidate of the lanes'.
-__device__ __forceinline__ int chunk_best(const ChunkShape& s, uint64_t work, uint64_t units, uint64_t split_units) {
-  uint32_t key = split_units > (uint64_t)s.cap ? 0xffffffffu : (chunk_cost(work, units, split_units, s.n_cu) << 6) | (threadIdx.x & 63);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) key = min(key, (uint32_t)__shfl_xor((int)key, o));
-  return chunk_candidate(key == 0xffffffffu ? 0 : (int)(key & 63u));
+// The best candidate of the lanes': the least cost, to within 2^-17.
+__device__ __forceinline__ int chunk_best(const ChunkShape& s, int longest, float work, const ChunkSums& sums) {
+  const float cost = chunk_cost(work, sums, longest, chunk_candidate(threadIdx.x & 63), s.places);
+  const bool fits = sums.cut_units <= (float)s.cap && cost < __builtin_huge_valf();
+  int key = fits ? -(int)((__float_as_uint(cost) & ~63u) | (threadIdx.x & 63)) : -0x7fffffff;         // (negative: the largest is wanted)
+#define RTP_STEP(CTRL, MASK) key = max(key, __builtin_amdgcn_update_dpp(-0x7fffffff, key, CTRL, MASK, 0xf, false));
+  RTP_WAVE_SCAN_STEPS(RTP_STEP)
+#undef RTP_STEP
+  key = -wave_last(key);
+  return chunk_candidate(key == 0x7fffffff ? 0 : key & 63);
+}
+__device__ __forceinline__ float wave_sum_f32(float x) {
+#define RTP_STEP(CTRL, MASK) x += __int_as_float(dpp_or_zero<CTRL, MASK>(__float_as_int(x)));
+  RTP_WAVE_SCAN_STEPS(RTP_STEP)
+#undef RTP_STEP
+  return __int_as_float(wave_last(__float_as_int(x)));
+}
+
+// The plan as a wave has it: of up to 64 sequences one to a lane (scans inclusive), of more in memory.
+struct ChunkPlan {
+  ChunkLane seq;
+  int splits, units, unit_last, part_last, row_last;
+};
+__device__ __forceinline__ ChunkPlan chunk_plan(const ChunkArgs& a) {
+  const ChunkShape& s = a.shape;
+  ChunkPlan p = {};
+  if (__builtin_expect(s.B > 64, 0)) return p;
+  p.seq = chunk_lane(a, threadIdx.x & 63);
+  const int longest = max(wave_max_ge_m1(p.seq.n > 0 ? p.seq.key_tiles : 1), 1);
+  const uint32_t magic = chunk_magic(longest);
+  int candidate = 1;
+  if (s.cap > 0) {
+    ChunkSums sums = {};
+    chunk_add_up(s, p.seq, s.B, longest, magic, &sums);
+    const float work = wave_sum_f32((float)p.seq.tiles * (float)p.seq.key_tiles);
+    candidate = chunk_best(s, longest, work, sums);
+  }
+  p.splits = chunk_splits(p.seq.key_tiles, longest, candidate, magic);
+  p.units = p.seq.tiles * p.splits;
+  p.unit_last = wave_incl_scan(p.units);
+  p.part_last = wave_incl_scan(p.splits > 1 ? p.units : 0);
+  p.row_last = wave_incl_scan(p.splits > 1 ? p.seq.n * s.n_served : 0);
+  return p;
 }
 
 // One sequence's place in the plan.
@@ -79,33 +118,21 @@ struct ChunkSpot {
 };
 // The sequence of unit `at` (ROWS: of the at-th row of a sequence whose tiles are cut), found by the whole wave.
 template <bool ROWS>
-__device__ __forceinline__ ChunkSpot chunk_find(const ChunkArgs& a, int at) {
+__device__ __forceinline__ ChunkSpot chunk_find(const ChunkArgs& a, const ChunkPlan& p, int at) {
   const ChunkShape& s = a.shape;
-  const int lane = threadIdx.x & 63;
   ChunkSpot spot = {};
   spot.b = -1;
-  if (s.B <= 64) {
-    const ChunkLane mine = chunk_lane(a, lane);
-    const int longest = max(wave_max_ge_m1(mine.n > 0 ? mine.key_tiles : 1), 1);
-    const uint32_t magic = chunk_magic(longest);
-    uint64_t units = 0, split_units = 0;
-    chunk_add_up(mine, s.B, longest, magic, &units, &split_units);
-    uint64_t work = (uint64_t)(uint32_t)mine.tiles * (uint32_t)mine.key_tiles;
-    work = wave_incl_scan(work);
-    work = ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(work >> 32), 63) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)work, 63);
-    const int S = chunk_splits(mine.key_tiles, longest, chunk_best(s, work, units, split_units), magic);
-    const int own = mine.tiles * S, own_rows = S > 1 ? mine.n * a.n_served : 0;
-    const int last = wave_incl_scan(ROWS ? own_rows : own);
-    const int part_last = wave_incl_scan(S > 1 ? own : 0);
+  if (__builtin_expect(s.B <= 64, 1)) {
+    const int last = ROWS ? p.row_last : p.unit_last, own = ROWS ? (p.splits > 1 ? p.seq.n * s.n_served : 0) : p.units;
     const int b = __popcll(__ballot(last <= at));
     if (b >= 64) return spot;
     spot.b = b;
-    spot.rel = at - (__builtin_amdgcn_readlane(last, b) - __builtin_amdgcn_readlane(ROWS ? own_rows : own, b));
-    spot.n = __builtin_amdgcn_readlane(mine.n, b);
-    spot.q0 = __builtin_amdgcn_readlane(mine.q0, b);
-    spot.ctx = __builtin_amdgcn_readlane(mine.ctx, b);
-    spot.splits = __builtin_amdgcn_readlane(S, b);
-    spot.part0 = __builtin_amdgcn_readlane(part_last - (S > 1 ? own : 0), b);
+    spot.rel = at - __builtin_amdgcn_readlane(last - own, b);
+    spot.n = __builtin_amdgcn_readlane(p.seq.n, b);
+    spot.q0 = __builtin_amdgcn_readlane(p.seq.q0, b);
+    spot.ctx = __builtin_amdgcn_readlane(p.seq.ctx, b);
+    spot.splits = __builtin_amdgcn_readlane(p.splits, b);
+    spot.part0 = __builtin_amdgcn_readlane(p.part_last - (p.splits > 1 ? p.units : 0), b);
     return spot;
   }
   const int32_t* unit_first = a.plan + kPlanHead;
@@ -129,7 +156,7 @@ __device__ __forceinline__ ChunkSpot chunk_find(const ChunkArgs& a, int at) {
 // A workgroup's unit: a query tile of one KV head, and the range of its key tiles [it_lo, it_hi).
 struct ChunkTile {
   int nh, over;                // heads per token; row / nh = row * over >> 16 (exact for rows below 256, nh up to 8)
-  int kvh, head0;              // KV head; its first served head's place in ChunkShape::heads
+  int kvh, members;            // KV head; its served heads, as bits
   int rows;                    // (token, head) pairs of the tile
   int64_t q0;                  // its first token's row of q
   int m_lo, m_hi;              // its first and last position; may be negative, where ctx_len says so
@@ -141,31 +168,36 @@ struct ChunkTile {
 };
 
 __device__ __forceinline__ int chunk_tile_n0(const ChunkTile& t, int it) { return (it + (it >= t.sink_tiles ? t.gap : 0)) * kCkK; }
+__device__ __forceinline__ int chunk_row_factor(int h) { return (int)(65536.f * __builtin_amdgcn_rcpf((float)h)) + 1; }     // 65536 / h + 1
+// Query head of a row, whose token is the rt-th.
+__device__ __forceinline__ int chunk_head(const ChunkArgs& a, const ChunkTile& t, int row, int rt) {
+  const int k = row - rt * t.nh;
+  return t.kvh * a.shape.group + (t.nh == a.shape.group ? k : chunk_nth((uint32_t)t.members, k));
+}
 __device__ __forceinline__ int chunk_row_pos(const ChunkTile& t, int row) { return t.m_lo + ((row * t.over) >> 16); }
 
-__device__ __forceinline__ int64_t uniform64(int64_t x) {
-  return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x));
-}
-// The workgroup's unit (false: there is none).  Workgroups are dealt to the eight dies in turn; `run` units in a row go to one die.
+// A workgroup's unit (false: there is none).  Workgroups are dealt to the eight dies in turn; 2^run_shift units in a row go to one die.
 template <bool LOCAL, bool KV4>
-__device__ __forceinline__ bool chunk_tile(const ChunkArgs& a, ChunkTile* t) {
+__device__ __forceinline__ bool chunk_tile(const ChunkArgs& a, int workgroup, ChunkTile* t) {
   const ChunkShape& s = a.shape;
-  const int k8 = (int)blockIdx.x >> 3;
-  const ChunkSpot spot = chunk_find<false>(a, (k8 / a.run * 8 + ((int)blockIdx.x & 7)) * a.run + k8 % a.run);
+  const int k8 = workgroup >> 3, in_run = k8 & ((1 << a.run_shift) - 1);
+  const ChunkSpot spot = chunk_find<false>(a, chunk_plan(a), ((((k8 >> a.run_shift) * 8 + (workgroup & 7)) << a.run_shift) + in_run));
   if (spot.b < 0) return false;
   const ChunkUnit u = chunk_unit(s, spot.n, spot.splits, spot.rel);
-  t->nh = s.slot_n[u.slot];
-  t->over = 65536 / t->nh + 1;
-  t->kvh = s.slot_kv[u.slot];
-  t->head0 = s.slot_first[u.slot];
-  const int t0 = u.tile * s.tok[t->nh], tokens = min((int)s.tok[t->nh], spot.n - t0);
+  t->nh = u.heads;
+  t->over = chunk_row_factor(u.heads);
+  t->kvh = u.kv;
+  t->members = (int)chunk_members(s, u.kv);
+  const int shift_q = chunk_shift(u.heads), t0 = u.tile << shift_q, tokens = min(1 << shift_q, spot.n - t0);
   t->rows = tokens * t->nh;
   t->q0 = spot.q0 + t0;
   t->m_lo = spot.ctx - spot.n + t0;
   t->m_hi = t->m_lo + tokens - 1;
   const int64_t pt_stride = KV4 ? a.c4.pt_stride : a.c16.pt_stride;
   t->pt = (KV4 ? a.c4.page_table : a.c16.page_table) + spot.b * pt_stride;
-  t->kend = (int)min((int64_t)max(t->m_hi + 1, 0), pt_stride << (KV4 ? a.c4.page_shift : a.c16.page_shift));
+  const int shift = KV4 ? a.c4.page_shift : a.c16.page_shift;          // (kend: not behind the table, in 32 bits)
+  t->kend = max(t->m_hi + 1, 0);
+  if (pt_stride <= 0x7fffffff >> shift) t->kend = min(t->kend, (int)pt_stride << shift);
   const int all = (t->kend + kCkK - 1) / kCkK;
   t->sink_tiles = t->gap = 0;
   if (LOCAL) {
@@ -173,12 +205,11 @@ __device__ __forceinline__ bool chunk_tile(const ChunkArgs& a, ChunkTile* t) {
     t->gap = max((s.window > 0 ? max(t->m_lo - s.window + 1, 0) / kCkK : all) - t->sink_tiles, 0);
   }
   const int n_tiles = all - t->gap;
-  t->it_lo = (int)((int64_t)n_tiles * u.split / spot.splits);
-  t->it_hi = (int)((int64_t)n_tiles * (u.split + 1) / spot.splits);
+  chunk_range(n_tiles, u.split, spot.splits, &t->it_lo, &t->it_hi);
   t->splits = spot.splits;
   t->part = spot.part0 + spot.rel;
   // (the same in every lane, which the compiler does not see everywhere)
-  int* const whole[] = {&t->nh, &t->over, &t->kvh, &t->head0, &t->rows, &t->m_lo, &t->m_hi, &t->kend, &t->sink_tiles, &t->gap, &t->it_lo, &t->it_hi,
+  int* const whole[] = {&t->nh, &t->over, &t->kvh, &t->members, &t->rows, &t->m_lo, &t->m_hi, &t->kend, &t->sink_tiles, &t->gap, &t->it_lo, &t->it_hi,
                         &t->splits, &t->part};
 #pragma unroll
   for (int* w : whole) *w = __builtin_amdgcn_readfirstlane(*w);
@@ -187,17 +218,42 @@ __device__ __forceinline__ bool chunk_tile(const ChunkArgs& a, ChunkTile* t) {
   return true;
 }
 
+template <bool KV4>
+__device__ __forceinline__ int chunk_page(const ChunkArgs& a, const ChunkTile& t, int n) {       // 0 <= n < kend; -1: a page that is not there
+  const int page = t.pt[n >> (KV4 ? a.c4.page_shift : a.c16.page_shift)];
+  return (uint32_t)page < (uint32_t)(KV4 ? a.c4.n_pages : a.c16.n_pages) ? page : -1;
+}
+
 // What one row sees: the tokens n <= hi that are below the sink or above lo.
 struct ChunkSight {
-  int hi, lo;
+  int hi, lo, sink;
 };
 __device__ __forceinline__ ChunkSight chunk_sight(const ChunkShape& s, const ChunkTile& t, int row) {
   const int m = chunk_row_pos(t, row);
-  return ChunkSight{row < t.rows ? min(m, t.kend - 1) : -1, m - s.window};
+  return ChunkSight{row < t.rows ? min(m, t.kend - 1) : -1, m - s.window, s.sink};
 }
+// Bit i: the row sees key n + 8 (i / 4) + i % 4, the lane's i-th of a block if n is the block's first plus 4 g.
 template <bool LOCAL>
-__device__ __forceinline__ bool chunk_sees(const ChunkShape& s, const ChunkSight& e, int n) {
-  return n <= e.hi && (!LOCAL || n < s.sink || n > e.lo);
+__device__ __forceinline__ bool chunk_sees(const ChunkSight& e, int off) { return off <= e.hi && (!LOCAL || off < e.sink || off > e.lo); }
+template <bool LOCAL>
+__device__ __forceinline__ void chunk_mask(const ChunkSight& sight, int n, f32x16& S) {
+  const ChunkSight e = {sight.hi - n, sight.lo - n, sight.sink - n};
+#pragma unroll
+  for (int i = 0; i < 16; ++i) S[i] = chunk_sees<LOCAL>(e, 8 * (i >> 2) + (i & 3)) ? S[i] : -__builtin_huge_valf();
+}
+// The same as bits, of keys whose pages are there.
+template <bool LOCAL, bool KV4>
+__device__ __forceinline__ uint32_t chunk_seen(const ChunkArgs& a, const ChunkTile& t, const ChunkSight& sight, int n) {
+  const ChunkSight e = {sight.hi - n, sight.lo - n, sight.sink - n};
+  uint32_t seen = 0;
+#pragma unroll
+  for (int i4 = 0; i4 < 4; ++i4) {
+    const int n4 = n + i4 * 8;                                              // (four neighbours share their page)
+    const bool there = n4 < t.kend && chunk_page<KV4>(a, t, min(n4, t.kend - 1)) >= 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) seen |= there && chunk_sees<LOCAL>(e, i4 * 8 + j) ? 1u << (i4 * 4 + j) : 0u;
+  }
+  return seen;
 }
 // Rows at the positions [lo, hi] (hi < 0: no rows) and keys [n, n + len): does some row see one of them; does some row not see all of them.
 template <bool LOCAL>
@@ -208,12 +264,6 @@ template <bool LOCAL>
 __device__ __forceinline__ bool chunk_all_seen(const ChunkShape& s, const ChunkTile& t, int lo, int hi, int n, int len) {
   return n + len - 1 <= lo && n + len <= t.kend && (!LOCAL || n + len <= s.sink || n > hi - s.window);
 }
-template <bool KV4>
-__device__ __forceinline__ int chunk_page(const ChunkArgs& a, const ChunkTile& t, int n) {       // 0 <= n < kend; -1: a page that is not there
-  const int page = t.pt[n >> (KV4 ? a.c4.page_shift : a.c16.page_shift)];
-  return (uint32_t)page < (uint32_t)(KV4 ? a.c4.n_pages : a.c16.n_pages) ? page : -1;
-}
-
 // The reference that goes with a sum: none for a range without keys; a sum that is not a number has one that the merge does not take for that.
 __device__ __forceinline__ float chunk_reference(float m, float l) {
   const float ninf = -__builtin_huge_valf();
@@ -231,7 +281,7 @@ __device__ __forceinline__ void chunk_store4(const ChunkArgs& a, const ChunkTile
     return;
   }
   const int rt = (row * t.over) >> 16;
-  const int64_t at = (t.q0 + rt) * a.n_q_heads + a.shape.heads[t.head0 + row - rt * t.nh];
+  const int64_t at = (t.q0 + rt) * a.n_q_heads + chunk_head(a, t, row, rt);
   const bool none = l == 0.f;
   const float inv = none ? 0.f : 1.f / l;
   *reinterpret_cast<u32x2*>(a.out + at * kHeadDim + dim) =
@@ -272,25 +322,24 @@ template <bool F16>
 __device__ __forceinline__ void chunk_pv_seen(const unsigned char* v_rows, uint32_t seen, const uint32_t (&P)[8], f32x16 (&O)[4]) {
   const int g = (threadIdx.x & 63) >> 5;
   const uint32_t seen_other = (uint32_t)__shfl_xor((int)seen, 32);
-  for (int i = 0; i < 16; ++i) {
-    float p_own = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) p_own = e == (i >> 1) ? ((i & 1) ? hi16<F16>(P[e]) : lo16<F16>(P[e])) : p_own;
-    const float p_other = __shfl_xor(p_own, 32);
-    for (int half = 0; half < 2; ++half) {
-      const int n = 8 * (i >> 2) + 4 * half + (i & 3);
+  for (int db = 0; db < 4; ++db) {
+#pragma unroll 1
+    for (int k = 0; k < 32; ++k) {                                         // key 8 (i / 4) + 4 half + i % 4
+      const int i = k >> 1, half = k & 1, n = 8 * (i >> 2) + 4 * half + (i & 3);
+      uint32_t w = P[0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) w = e == (i >> 1) ? P[e] : w;
+      const float p_own = (i & 1) ? hi16<F16>(w) : lo16<F16>(w), p_other = __shfl_xor(p_own, 32), p = half == g ? p_own : p_other;
       const bool ok = ((half == g ? seen : seen_other) >> i) & 1u;
-      const float p = half == g ? p_own : p_other;
 #pragma unroll
-      for (int db = 0; db < 4; ++db)
+      for (int i4 = 0; i4 < 4; ++i4) {
+        const int d = db * 32 + i4 * 8 + g * 4;
+        const u32x2 v = *reinterpret_cast<const u32x2*>(v_rows + n * 256 + ((d >> 4) ^ (2 * (n & 3))) * 32 + (d & 15) * 2);
+        const float x[4] = {lo16<F16>(v[0]), hi16<F16>(v[0]), lo16<F16>(v[1]), hi16<F16>(v[1])};
 #pragma unroll
-        for (int i4 = 0; i4 < 4; ++i4) {
-          const int d = db * 32 + i4 * 8 + g * 4;
-          const u32x2 w = *reinterpret_cast<const u32x2*>(v_rows + n * 256 + ((d >> 4) ^ (2 * (n & 3))) * 32 + (d & 15) * 2);
-          const float v[4] = {lo16<F16>(w[0]), hi16<F16>(w[0]), lo16<F16>(w[1]), hi16<F16>(w[1])};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) O[db][i4 * 4 + j] = ok ? fmaf(p, v[j], O[db][i4 * 4 + j]) : O[db][i4 * 4 + j];
-        }
+        for (int j = 0; j < 4; ++j) O[db][i4 * 4 + j] = ok ? fmaf(p, x[j], O[db][i4 * 4 + j]) : O[db][i4 * 4 + j];
+      }
     }
   }
 }

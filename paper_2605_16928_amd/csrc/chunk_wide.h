@@ -3,12 +3,12 @@
 // Nothing hides latency by itself at two waves per SIMD, so the loop is pipelined over blocks of 32 keys by hand: while the probabilities of a
 // block are computed on the vector ALU, the matrix pipe runs the PV product of the block before and the score product of the one behind.  For that
 // nothing may touch the accumulators in between, so there is no running maximum: every row takes its largest score in the range's first tile for a
-// reference, and a range after whose pass some row's sum or output says that this did not do (out of the middle of fp32's range, or not finite) is
-// repeated with a running maximum (wide_exact), as is one that met a page which is not there.
+// reference, and a range after whose pass some row's sum or output says that this did not do (out of the middle of fp32's range, or not finite), or
+// which met a page that is not there, is left to a launch that goes through such ranges with a running maximum (exact_pass).
 //
-// K/V tiles rotate through three LDS buffers with one barrier per tile, in its middle: it publishes tile it + 1, and behind it every wave is done
-// with tile it - 1, whose buffer tile it + 2 fills.  Tiles that every row sees in full run in a loop without a branch; the others -- the first, those
-// on the diagonal and on the window's edge -- block by block, with masks.
+// K/V tiles rotate through three LDS buffers with one barrier per tile, in its middle: it publishes tile x + 1, and behind it every wave is done
+// with tile x - 1, whose buffer tile x + 2 fills.  Tiles that every row sees in full run in a loop without a branch; the others -- the first, those
+// on the window's edge and on the diagonal -- block by block, with masks.
 //
 // 16-bit rows go to LDS by direct loads.  The four rows that a wave brings per instruction lie in one page, whose place is a scalar: 64 of them, for
 // 32 tiles, are looked up at a time, a lane each, a window ahead, and taken from there with two lane reads.  4-bit rows come through registers
@@ -52,12 +52,12 @@ struct ChunkWide {
       : a(a_), t(t_), smem(smem_), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), g(lane >> 5), r(lane & 31),
         row(wave * 32 + r), qok(row < t_.rows), w_lo(wave * 32 < t_.rows ? chunk_row_pos(t_, wave * 32) : -1),
         w_hi(wave * 32 < t_.rows ? chunk_row_pos(t_, min(wave * 32 + 31, t_.rows - 1)) : -1), c(a_.scale_log2), rd(chunk_reads()),
-        sight(chunk_sight(a_.shape, t_, row)), lost(false) {
-    const int rt = (row * t.over) >> 16;
-    const int head = qok ? a.shape.heads[t.head0 + row - rt * t.nh] : 0;
-    const uint16_t* src = a.q + (t.q0 + rt) * a.q_stride + head * kHeadDim + g * 8;
+        sight(chunk_sight(a_.shape, t_, row)), lost(false), n_tiles(t_.it_hi - t_.it_lo), n_full(0), n_moved(0) {
+    // (rows behind the tile's last repeat it)
+    const int row_c = min(row, t.rows - 1), rt = (row_c * t.over) >> 16;
+    const uint16_t* src = a.q + (t.q0 + rt) * a.q_stride + chunk_head(a, t, row_c, rt) * kHeadDim + g * 8;
 #pragma unroll
-    for (int kk = 0; kk < 8; ++kk) q[kk] = qok ? *reinterpret_cast<const u32x4*>(src + kk * 16) : (u32x4){0u, 0u, 0u, 0u};
+    for (int kk = 0; kk < 8; ++kk) q[kk] = *reinterpret_cast<const u32x4*>(src + kk * 16);
     if constexpr (KV4) {
       base0 = a.c4.codes + (int64_t)t.kvh * a.c4.code_head_stride;
       base1 = a.c4.scales + (int64_t)t.kvh * a.c4.scale_head_stride;
@@ -72,19 +72,28 @@ struct ChunkWide {
     }
   }
 
-  __device__ __forceinline__ int n0_of(int it) const { return chunk_tile_n0(t, it); }
+  // The x-th tile of the pass: the range's tiles in order, but that those between its first and the first one that every row sees in full come
+  // behind the full ones: so these are neighbours, and the loop over them has one tile in front of it.
+  int n_tiles, n_full, n_moved;
+  __device__ __forceinline__ int n0_of(int x) const {
+    const int y = n_moved > 0 && x >= 1 && x <= n_full + n_moved ? (x <= n_full ? x + n_moved : x - n_full) : x;
+    return chunk_tile_n0(t, t.it_lo + y);
+  }
+  __device__ __forceinline__ void arrange() {
+    int lo = t.it_lo, hi = min(t.it_hi, min(t.m_lo + 1, t.kend) / kCkK - t.gap);                // (m_lo >= 0 where there are full tiles)
+    if (LOCAL) lo = max(max(lo, t.sink_tiles), (max(t.m_hi - a.shape.window + 1, 0) + kCkK - 1) / kCkK - t.gap);
+    lo = max(lo, t.it_lo + 1);
+    if (lo < hi) {
+      n_moved = lo - t.it_lo - 1;
+      n_full = hi - lo;
+    }
+  }
   __device__ __forceinline__ bool any_seen(int n, int len) const { return chunk_any_seen<LOCAL>(a.shape, t, w_lo, w_hi, n, len); }
   __device__ __forceinline__ bool all_seen(int n, int len) const { return chunk_all_seen<LOCAL>(a.shape, t, w_lo, w_hi, n, len); }
-  // A tile that every row of the workgroup sees in full (of the band: full tiles are neighbours then).
-  __device__ __forceinline__ bool full_tile(int it) const {
-    const int n = n0_of(it);
-    return n + kCkK - 1 <= t.m_lo && n + kCkK <= t.kend && (!LOCAL || n > t.m_hi - a.shape.window);
-  }
-
   // ---- staging ----
-  // First of the rows of piece p (counted from the range's first tile) that this wave brings; past the last key and the last tile: those of the last.
+  // First of the rows of piece p (counted from the pass's first tile) that this wave brings; past the last key and the last tile: those of the last.
   __device__ __forceinline__ int piece_row(int p) const {
-    const int n0 = n0_of(min(t.it_lo + p / kPieces, t.it_hi - 1)) + (p % kPieces) * 32 + kRowsEach * wave;
+    const int n0 = n0_of(min(p / kPieces, n_tiles - 1)) + (p % kPieces) * 32 + kRowsEach * wave;
     return min(n0, (t.kend - 1) & ~(kRowsEach - 1));
   }
   __device__ __forceinline__ void look_up(int window) {
@@ -112,7 +121,7 @@ struct ChunkWide {
   __device__ __forceinline__ int64_t place(uint32_t lo, uint32_t hi, int p) const {
     return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)hi, p) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)lo, p));
   }
-  // The window of tile x (counted from the range's first) is the current one; called for every x in turn.
+  // The window of tile x is the current one; called for every x in turn.
   __device__ __forceinline__ void advance(int x) {
     if (x % kWindow == 0) {
       take_window(x / kWindow);
@@ -280,65 +289,68 @@ struct ChunkWide {
     f32x16 S;
     uint32_t P0[8], P1[8];
     clear();
+    arrange();
     begin();
     bring(0, 0);
     bring(1, 1);
     landed();
     __syncthreads();
-    auto tile_at = [&](int it) __attribute__((always_inline)) { return smem + (it - t.it_lo) % kCkStages * kCkTileBytes; };
+    auto tile_at = [&](int y) __attribute__((always_inline)) { return smem + y % kCkStages * kCkTileBytes; };
+    // (of what the row sees there, if it does see anything)
+    float any = ninf;
     m = ninf;
 #pragma unroll
     for (int kb = 1; kb >= 0; --kb) {
       scores(smem, kb, S);
-      float mx = S[0];
+      const int nb0 = n0_of(0) + kb * 32;
 #pragma unroll
-      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, S[i]);
-      m = fmaxf(m, fmaxf(mx, __shfl_xor(mx, 32)));
+      for (int i = 0; i < 16; ++i) any = fmaxf(any, S[i]);
+      if (!all_seen(nb0, 32)) chunk_mask<LOCAL>(sight, nb0 + 4 * g, S);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) m = fmaxf(m, S[i]);
     }
-    // At the start of half hf of tile it: S holds the scores of that block if the wave has a row that sees one of its keys; if `pend`, the
-    // probabilities of the block before wait in P1 (hf = 0, V in the tile before) or P0; tiles it and it + 1 are in LDS.
+    m = fmaxf(m, __shfl_xor(m, 32));
+    any = fmaxf(any, __shfl_xor(any, 32));
+    m = m > ninf ? m : any;
+    // At the start of half hf of tile x: S holds the scores of that block if the wave has a row that sees one of its keys; if `pend`, the
+    // probabilities of the block before wait in P1 (hf = 0, V in the tile before) or P0; tiles x and x + 1 are in LDS.
     bool pend = false;
-    int it = t.it_lo;
+    int x = 0;
     auto half = [&](auto hf_tag) __attribute__((always_inline)) {
       constexpr int hf = decltype(hf_tag)::value;
-      const int nb0 = n0_of(it) + hf * 32;
+      const int nb0 = n0_of(x) + hf * 32;
       const uint32_t (&Pin)[8] = hf == 0 ? P1 : P0;
       uint32_t (&Pout)[8] = hf == 0 ? P0 : P1;
-      if (pend) pv(tile_at(hf == 0 ? it - 1 : it), 1 - hf, Pin);
+      if (pend) pv(tile_at(hf == 0 ? x - 1 : x), 1 - hf, Pin);
       pend = any_seen(nb0, 32);
       if (pend) {
-        if (!all_seen(nb0, 32)) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) S[i] = chunk_sees<LOCAL>(a.shape, sight, nb0 + 8 * (i >> 2) + 4 * g + (i & 3)) ? S[i] : ninf;
-        }
+        if (!all_seen(nb0, 32)) chunk_mask<LOCAL>(sight, nb0 + 4 * g, S);
         begin_block();
 #pragma unroll
         for (int k = 0; k < 8; ++k) pair(k, S, Pout);
         end_block();
       }
       if (hf == 0) {
-        if (any_seen(nb0 + 32, 32)) scores(tile_at(it), 1, S);
+        if (any_seen(nb0 + 32, 32)) scores(tile_at(x), 1, S);
         landed();
         __syncthreads();
       } else {
-        bring(it - t.it_lo + 2, (it - t.it_lo + 2) % kCkStages);            // (behind the last tile: once more into a buffer that nobody reads)
-        if (it + 1 < t.it_hi && any_seen(n0_of(it + 1), 32)) scores(tile_at(it + 1), 0, S);
+        bring(x + 2, (x + 2) % kCkStages);                                 // (behind the last tile: once more into a buffer that nobody reads)
+        if (x + 1 < n_tiles && any_seen(n0_of(x + 1), 32)) scores(tile_at(x + 1), 0, S);
       }
     };
     auto edge_tile = [&]() __attribute__((always_inline)) {
       half(std::integral_constant<int, 0>{});
       half(std::integral_constant<int, 1>{});
-      ++it;
+      ++x;
     };
-    // a tile for the loop without masks: seen in full, and so are the rows that it sends for
+    // the loop without masks: full tiles, while the rows that it sends for are all there
     constexpr int kSends = KV4 ? 3 : 2;
     auto steady = [&]() __attribute__((always_inline)) {
-      return it < t.it_hi && full_tile(it) && (it + kSends >= t.it_hi || n0_of(it + kSends) + kCkK <= t.kend);
+      return x <= n_full && (x + kSends >= n_tiles || n0_of(x + kSends) + kCkK <= t.kend);
     };
-    do edge_tile();
-    while (it < t.it_hi && !steady());
-    int x = it - t.it_lo;
-    if (it >= t.it_hi) {
+    edge_tile();
+    if (!steady()) {
     } else if (w_hi >= 0) {
       if (!pend) {
 #pragma unroll
@@ -348,16 +360,16 @@ struct ChunkWide {
       f32x16 S1;
       do {
         advance(x + kSends);
-        first_v(tile_at(it - 1), 1);
+        first_v(tile_at(x - 1), 1);
         do {
-          pv_stream(tile_at(it - 1), 1, P1, S, P0, tile_at(it), 1);
-          score_stream(tile_at(it), 1, S1, S, P0, [](int) __attribute__((always_inline)) {});
-          first_v(tile_at(it), 0);
+          pv_stream(tile_at(x - 1), 1, P1, S, P0, tile_at(x), 1);
+          score_stream(tile_at(x), 1, S1, S, P0, [](int) __attribute__((always_inline)) {});
+          first_v(tile_at(x), 0);
           landed();
           __syncthreads();
-          pv_stream(tile_at(it), 0, P0, S1, P1, tile_at(it + 1), 0);
+          pv_stream(tile_at(x), 0, P0, S1, P1, tile_at(x + 1), 0);
           const int slot = (x + 2) % kCkStages;
-          score_stream(tile_at(it + 1), 0, S, S1, P1, [&](int kk) __attribute__((always_inline)) {
+          score_stream(tile_at(x + 1), 0, S, S1, P1, [&](int kk) __attribute__((always_inline)) {
             if constexpr (KV4) {
               if (kk < 4) put_codes(slot, kk);
               if (kk == 4) fetch_codes(x + 3, false);
@@ -365,8 +377,7 @@ struct ChunkWide {
               if (kk < 4) load16(x + 2, slot, kk >> 1, kk & 1, (kk & 1) ? off1 : off0);
             }
           });
-          first_v(tile_at(it), 1);
-          ++it;
+          first_v(tile_at(x), 1);
           ++x;
         } while (steady() && (x + kSends) % kWindow != 0);
       } while (steady());
@@ -384,12 +395,11 @@ struct ChunkWide {
 #pragma unroll
           for (int k = 0; k < 4; ++k) load16(x + 2, slot, k >> 1, k & 1, (k & 1) ? off1 : off0);
         }
-        ++it;
         ++x;
       } while (steady());
     }
-    while (it < t.it_hi) edge_tile();
-    if (pend) pv(tile_at(t.it_hi - 1), 1, P1);
+    while (x < n_tiles) edge_tile();
+    if (pend) pv(tile_at(n_tiles - 1), 1, P1);
     landed();
     // Was every reference within reach?  A row that sees a key of the range has a sum in the middle of fp32's range (fp16: nothing above 65504 is
     // finite; where the largest probability is below 2^-6 most of the mass may be in subnormals), and outputs are finite.
@@ -402,7 +412,8 @@ struct ChunkWide {
     bool bad = lost || !(z == 0.f) || !(sum < 0x1p100f);
     if (qok && sight.hi >= 0 && !(sum > (F16 ? 0x1p-6f : 0x1p-60f))) {
       // does the row see a key of the range?  Of the sink's tiles ...
-      const int first = n0_of(t.it_lo), end = min(n0_of(t.it_hi - 1) + kCkK, t.kend), band = t.it_lo < t.sink_tiles ? n0_of(t.sink_tiles) : first;
+      const int first = chunk_tile_n0(t, t.it_lo), end = min(chunk_tile_n0(t, t.it_hi - 1) + kCkK, t.kend);
+      const int band = t.it_lo < t.sink_tiles ? chunk_tile_n0(t, t.sink_tiles) : first;
       bool sees = !LOCAL && first <= sight.hi;
       if (LOCAL) sees = first <= min(min(a.shape.sink - 1, sight.hi), end - 1) || max(max(first, sight.lo + 1), t.gap > 0 ? band : 0) <= min(end - 1, sight.hi);
       bad = bad || sees;
@@ -410,7 +421,7 @@ struct ChunkWide {
     return __syncthreads_or(bad ? 1 : 0) != 0;
   }
 
-  // ---- running maximum, accumulators rescaled in place ----
+  // ---- running maximum, accumulators rescaled in place, keys masked by their pages too (apart from the pass above: its registers are its own) ----
   __device__ __forceinline__ void exact_pass() {
     const float ninf = -__builtin_huge_valf();
     f32x16 S;
@@ -421,8 +432,7 @@ struct ChunkWide {
     begin();
     if constexpr (!KV4) bring(0, 0);
 #pragma unroll 1
-    for (int it = t.it_lo; it < t.it_hi; ++it) {
-      const int x = it - t.it_lo;
+    for (int x = 0; x < n_tiles; ++x) {
       const unsigned char* const tile = smem + (x & 1) * kCkTileBytes;
       if constexpr (KV4) bring(x, x & 1);
       landed();
@@ -430,17 +440,10 @@ struct ChunkWide {
       if constexpr (!KV4) bring(x + 1, (x + 1) & 1);
 #pragma unroll 1
       for (int kb = 0; kb < 2; ++kb) {
-        const int nb0 = n0_of(it) + kb * 32;
+        const int nb0 = n0_of(x) + kb * 32;
         if (!any_seen(nb0, 32)) continue;                                   // (the same for the whole wave)
         scores(tile, kb, S);
-        uint32_t seen = 0;                                                  // bit i: the lane's i-th key
-#pragma unroll
-        for (int i4 = 0; i4 < 4; ++i4) {
-          const int n4 = nb0 + i4 * 8 + g * 4;
-          const bool there = n4 < t.kend && chunk_page<KV4>(a, t, min(n4, t.kend - 1)) >= 0;      // (four neighbours share their page)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) seen |= there && chunk_sees<LOCAL>(a.shape, sight, n4 + j) ? 1u << (i4 * 4 + j) : 0u;
-        }
+        const uint32_t seen = chunk_seen<LOCAL, KV4>(a, t, sight, nb0 + 4 * g);
         float mx = ninf;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -477,11 +480,7 @@ struct ChunkWide {
     }
   }
 
-  // exact: a first pass has been made, and does not do
-  __device__ __forceinline__ void run(bool exact) {
-    m = -__builtin_huge_valf();
-    clear();
-    if (t.it_lo < t.it_hi && (exact || fast_pass())) exact_pass();
+  __device__ __forceinline__ void store() {
     const float sum = l + __shfl_xor(l, 32), full = F + __shfl_xor(F, 32);
     if (!qok) return;
 #pragma unroll

@@ -125,6 +125,20 @@ __device__ __forceinline__ float pair_sum(float x) {
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// A kernel's arguments lie in memory that every compute unit fetches anew, at some microseconds a round trip; the compiler loads a field where it is
+// first used, one round trip after the other.  At a kernel's entry: one word of every cache line of them, all at once.
+template <typename Args>
+__device__ __forceinline__ void fetch_arguments() {
+  const __attribute__((address_space(4))) uint32_t* k = (const __attribute__((address_space(4))) uint32_t*)__builtin_amdgcn_kernarg_segment_ptr();
+  constexpr int n = (sizeof(Args) + 63) / 64;
+  static_assert(n <= 16, "one word of each of sixteen lines");
+#define RTP_ARG_WORD(I) k[16 * ((I) < n ? (I) : n - 1)]
+  asm volatile("" ::"s"(RTP_ARG_WORD(0)), "s"(RTP_ARG_WORD(1)), "s"(RTP_ARG_WORD(2)), "s"(RTP_ARG_WORD(3)), "s"(RTP_ARG_WORD(4)), "s"(RTP_ARG_WORD(5)),
+               "s"(RTP_ARG_WORD(6)), "s"(RTP_ARG_WORD(7)), "s"(RTP_ARG_WORD(8)), "s"(RTP_ARG_WORD(9)), "s"(RTP_ARG_WORD(10)), "s"(RTP_ARG_WORD(11)),
+               "s"(RTP_ARG_WORD(12)), "s"(RTP_ARG_WORD(13)), "s"(RTP_ARG_WORD(14)), "s"(RTP_ARG_WORD(15)));
+#undef RTP_ARG_WORD
+}
+
 // ---- wave-wide inclusive prefix sums on the DPP data path ------------------------------------------
 // Four shifts inside the 16-lane rows, then lane 15 of rows 0 and 2 into rows 1 and 3 (row_bcast:15) and
 // lane 31 into the upper half (row_bcast:31): six dependent vector-ALU steps, where a shuffle-based scan

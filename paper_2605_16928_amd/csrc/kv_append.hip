@@ -36,6 +36,7 @@ struct AppendArgs {
 
 template <bool F16>
 __global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(const AppendArgs a) {
+  fetch_arguments<AppendArgs>();
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t slot_w = (int64_t)blockIdx.x * (kAppendThreads / 64) + wave;
   const int64_t i64 = slot_w / a.waves;

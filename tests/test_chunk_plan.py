@@ -11,42 +11,40 @@ CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
 SOURCE = """
 #include "chunk_plan.h"
 using namespace rtp;
-static ChunkShape shape(const int* slot_n, int n_slots, int local, int sink, int window, int cap, int n_cu) {
+static ChunkShape shape(const int* members, int n_kv, int group, int local, int sink, int window, int cap, int places) {
   ChunkShape s = {};
-  int first = 0;
-  for (int k = 0; k < n_slots; ++k) {
-    s.slot_n[k] = slot_n[k];
-    s.slot_first[k] = first;
-    first += slot_n[k];
-    ++s.cnt[slot_n[k]];
+  s.group = group; s.n_kv = n_kv; s.local = local; s.sink = sink; s.window = window; s.cap = cap; s.places = (float)places;
+  for (int k = 0; k < n_kv; ++k) {
+    s.served[k * group / 32] |= (uint32_t)members[k] << (k * group % 32);
+    const int n = chunk_bits(members[k]);
+    s.n_served += n;
+    if (n) ++s.count[8 - chunk_shift(n)];
   }
-  for (int k = 1; k <= 8; ++k) s.tok[k] = kChunkRows / k;
-  s.n_slots = n_slots; s.local = local; s.sink = sink; s.window = window; s.cap = cap; s.n_cu = n_cu;
   return s;
 }
+extern "C" void range_of(int n, int k, int S, int* out) { chunk_range(n, k, S, out, out + 1); }
+extern "C" int tiles_of(int n, int h) { return chunk_query_tiles(n, chunk_shift(h)); }
+extern "C" int tokens_of(int h) { return 1 << chunk_shift(h); }
 // The splits of every sequence; returns the units of cut tiles.
-extern "C" long plan(const int* slot_n, int n_slots, int local, int sink, int window, int cap, int n_cu, int B, const int* n, const int* ctx,
+extern "C" long plan(const int* members, int n_kv, int group, int local, int sink, int window, int cap, int places, int B, const int* n, const int* ctx,
                      int* splits, int* tiles) {
-  const ChunkShape s = shape(slot_n, n_slots, local, sink, window, cap, n_cu);
+  const ChunkShape s = shape(members, n_kv, group, local, sink, window, cap, places);
   int longest = 1;
-  uint64_t work = 0;
+  float work = 0;
   for (int b = 0; b < B; ++b) {
     tiles[b] = chunk_tiles(s, n[b]);
     const int kt = n[b] > 0 ? chunk_key_tiles(s, n[b], ctx[b]) : 1;
     if (n[b] > 0) longest = chunk_max(longest, kt);
-    work += (uint64_t)tiles[b] * kt;
+    work += (float)tiles[b] * (float)kt;
   }
   const uint32_t magic = chunk_magic(longest);
-  uint32_t best = 0xffffffffu;
+  float best = INFINITY;
   int candidate = 1;
   for (int i = 0; i < kChunkCandidates; ++i) {
-    uint64_t units = 0, cut = 0;
-    for (int b = 0; b < B; ++b) {
-      const int S = chunk_splits(n[b] > 0 ? chunk_key_tiles(s, n[b], ctx[b]) : 1, longest, chunk_candidate(i), magic);
-      units += (uint64_t)tiles[b] * S;
-      cut += S > 1 ? (uint64_t)tiles[b] * S : 0;
-    }
-    const uint32_t cost = cut > (uint64_t)cap ? 0xffffffffu : chunk_cost(work, units, cut, n_cu);
+    ChunkSums sums = {};
+    for (int b = 0; b < B; ++b)
+      chunk_sum(&sums, tiles[b], n[b] * s.n_served, chunk_splits(n[b] > 0 ? chunk_key_tiles(s, n[b], ctx[b]) : 1, longest, chunk_candidate(i), magic));
+    const float cost = sums.cut_units > (float)cap ? INFINITY : chunk_cost(work, sums, longest, chunk_candidate(i), (float)places);
     if (cost < best) { best = cost; candidate = chunk_candidate(i); }
   }
   long cut = 0;
@@ -56,12 +54,15 @@ extern "C" long plan(const int* slot_n, int n_slots, int local, int sink, int wi
   }
   return cut;
 }
-extern "C" void unit(const int* slot_n, int n_slots, int n, int S, int r, int* out) {
-  const ChunkShape s = shape(slot_n, n_slots, 0, 0, 0, 0, 1);
+extern "C" void unit(const int* members, int n_kv, int group, int n, int S, int r, int* out) {
+  const ChunkShape s = shape(members, n_kv, group, 0, 0, 0, 0, 1);
   const ChunkUnit u = chunk_unit(s, n, S, r);
-  int step;
-  const int first = chunk_unit_of(s, n, S, u.slot, u.tile, &step);
-  out[0] = u.slot; out[1] = u.split; out[2] = u.tile; out[3] = first + u.split * step;
+  out[0] = u.kv; out[1] = u.split; out[2] = u.tile; out[3] = u.heads; out[4] = u.first;
+}
+extern "C" void row(const int* members, int n_kv, int group, int n, int S, int t, int served, int* out) {
+  const ChunkShape s = shape(members, n_kv, group, 0, 0, 0, 0, 1);
+  const ChunkRow x = chunk_row(s, n, S, t, served);
+  out[0] = x.kv; out[1] = x.head; out[2] = x.unit; out[3] = x.step; out[4] = x.row;
 }
 """
 
@@ -84,22 +85,48 @@ def ints(x):
     return (C.c_int * max(len(x), 1))(*x)
 
 
-@pytest.mark.parametrize("slots", [[1], [4] * 8, [3, 4, 3, 4], [8], [1] * 16, [7, 5, 6, 2]])
+TOKENS = [0, 256, 128, 64, 64, 32, 32, 32, 32]          # per tile, by the number of served heads
+MEMBERS = [([1], 1), ([15] * 8, 4), ([7, 15, 0, 13], 4), ([255], 8), ([1] * 16, 1), ([127, 31, 62, 3], 8), ([0, 2, 0, 1], 2)]
+
+
+@pytest.mark.parametrize("members,group", MEMBERS)
 @pytest.mark.parametrize("n,S", [(1, 1), (1, 7), (31, 2), (32, 3), (33, 1), (300, 5), (5000, 1)])
-def test_every_unit_once(lib, slots, n, S):
-    tiles = [-(-n // (256 // k)) for k in slots]
-    seen, out = set(), (C.c_int * 4)()
+def test_every_unit_and_every_row_once(lib, members, group, n, S):
+    heads = [bin(m).count("1") for m in members]
+    tiles = [-(-n // TOKENS[h]) if h else 0 for h in heads]
+    units, out = {}, (C.c_int * 5)()
     for r in range(sum(tiles) * S):
-        lib.unit(ints(slots), len(slots), n, S, r, out)
-        slot, split, tile, back = out
-        assert 0 <= slot < len(slots) and 0 <= split < S and 0 <= tile < tiles[slot] and back == r
-        seen.add((slot, split, tile))
-    assert len(seen) == sum(tiles) * S
+        lib.unit(ints(members), len(members), group, n, S, r, out)
+        kv, split, tile, h, first = out
+        assert 0 <= split < S and 0 <= tile < tiles[kv] and h == heads[kv] and first == sum(heads[:kv])
+        units[r] = (kv, split, tile)
+    assert len(set(units.values())) == sum(tiles) * S
+    seen = set()
+    for t in list(range(min(n, 90))) + [n - 1]:
+        for served in range(sum(heads)):
+            lib.row(ints(members), len(members), group, n, S, t, served, out)
+            kv, head, unit, step, row = out
+            tok = TOKENS[heads[kv]]
+            at = [k for k in range(8) if members[kv] >> k & 1][served - sum(heads[:kv])]
+            assert head == kv * group + at and row == t % tok * heads[kv] + served - sum(heads[:kv])
+            assert [units[unit + s * step] for s in range(S)] == [(kv, s, t // tok) for s in range(S)]
+            seen.add((kv, t // tok, row))
+    assert len(seen) == len(set(list(range(min(n, 90))) + [n - 1])) * sum(heads)
 
 
-def _plan(lib, slots, new, ctx, local=0, sink=4, window=64, cap=1024, n_cu=256):
+@pytest.mark.parametrize("h", range(1, 9))
+def test_tiles(lib, h):
+    tok = TOKENS[h]
+    assert lib.tokens_of(h) == tok and h * tok <= 256 < 2 * h * tok
+    rng = random.Random(h)
+    for n in list(range(2000)) + [rng.randint(0, 1 << 24) for _ in range(5000)] + [(1 << 24) - k for k in range(600)] + [(1 << 24) // tok * tok + k for k in (-1, 0, 1)]:
+        assert lib.tiles_of(n, h) == -(-n // tok)
+
+
+def _plan(lib, heads, new, ctx, local=0, sink=4, window=64, cap=1024, places=256):
     splits, tiles = ints([0] * len(new)), ints([0] * len(new))
-    cut = lib.plan(ints(slots), len(slots), local, sink, window, cap, n_cu, len(new), ints(new), ints(ctx), splits, tiles)
+    members = [(1 << h) - 1 for h in heads]
+    cut = lib.plan(ints(members), len(heads), 8, local, sink, window, cap, places, len(new), ints(new), ints(ctx), splits, tiles)
     return cut, list(splits)[:len(new)], list(tiles)[:len(new)]
 
 
@@ -114,7 +141,7 @@ def test_cut_units_stay_inside_the_workspace(lib):
         cut, splits, tiles = _plan(lib, slots, new, ctx, rng.randint(0, 1), cap=cap)
         assert 0 <= cut <= cap and min(splits) >= 1 and max(splits) <= 289
         # the share of the workgroups' numbers that the host counts on
-        most = sum(-(-n // (256 // k)) for n in new for k in slots)
+        most = sum(-(-n // TOKENS[k]) for n in new for k in slots)
         assert sum(tiles) == most
 
 
@@ -132,3 +159,14 @@ def test_few_rows_fill_the_chip(lib):
 def test_splits_follow_the_lengths(lib):
     _, splits, _ = _plan(lib, [4] * 2, [1] * 4, [100000, 50000, 1000, 10])
     assert splits[0] >= splits[1] >= splits[2] >= splits[3] == 1 and abs(splits[0] - 2 * splits[1]) <= 2
+
+
+def test_ranges_are_neighbours_and_alike(lib):
+    rng, out = random.Random(2), (C.c_int * 2)()
+    for n, S in [(0, 1), (0, 7), (3, 7), (7, 7), (8, 7), (1 << 24, 289)] + [(rng.randint(0, 5000), rng.randint(1, 289)) for _ in range(300)]:
+        at = 0
+        for k in range(S):
+            lib.range_of(n, k, S, out)
+            assert out[0] == at and n // S <= out[1] - out[0] <= n // S + 1
+            at = out[1]
+        assert at == n
