@@ -11,7 +11,7 @@
 //
 // A wave computes the transposed scores S^T = K Q^T of 32 keys (v_mfma_f32_32x32x16): lane (g, r) then holds 16 keys of ONE row, the softmax is
 // per lane, and the probabilities, rounded to 16 bits, are in place as the B operand of O^T = V^T P^T.
-#include "chunk_narrow.h"
+#include "chunk_kernels.h"
 
 #include <algorithm>
 
@@ -54,6 +54,7 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(const ChunkArg
       sums.units += sh_sums[w][lane].units;
       sums.cut_units += sh_sums[w][lane].cut_units;
       sums.cut_rows += sh_sums[w][lane].cut_rows;
+      sums.most = fmaxf(sums.most, sh_sums[w][lane].most);
       work += sh_work[w];
     }
     const int best = s.cap > 0 ? chunk_best(s, longest, work, sums) : 1;
@@ -94,14 +95,16 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(const ChunkArg
 
 RTP_CHUNK_KERNELS(chunk_attn_kernel, chunk_again_kernel, chunk_narrow_kernel, false)
 
-static void launch_chunk_16(const ChunkArgs& a, unsigned grid, bool narrow, hipStream_t stream) {
+// rows: the most that a tile can have.
+static void launch_chunk_16(const ChunkArgs& a, unsigned grid, int rows, hipStream_t stream) {
+  const bool narrow = rows <= kCkNarrowRows;
   RTP_CHUNK_LAUNCH(chunk_attn_kernel, chunk_again_kernel, chunk_narrow_kernel, false, false)
   RTP_CHUNK_LAUNCH(chunk_attn_kernel, chunk_again_kernel, chunk_narrow_kernel, true, false)
   RTP_CHUNK_LAUNCH(chunk_attn_kernel, chunk_again_kernel, chunk_narrow_kernel, false, true)
   RTP_CHUNK_LAUNCH(chunk_attn_kernel, chunk_again_kernel, chunk_narrow_kernel, true, true)
 }
 // attn_chunk_kv4.hip
-void launch_chunk_kv4(const ChunkArgs& a, unsigned grid, bool narrow, hipStream_t stream);
+void launch_chunk_kv4(const ChunkArgs& a, unsigned grid, int rows, hipStream_t stream);
 
 // Merges the ranges of the rows whose tiles were cut: SLICES groups of 32 lanes per row take the ranges in turn, a lane 4 of the 128 dims.
 template <int SLICES>
@@ -301,7 +304,7 @@ int32_t chunk_call(const char* who, int which, const rtp_layer_desc* layer, cons
   a.shape.total_q = chunk->total_q;
   a.shape.max_q = chunk->max_q;
   a.shape.cap = (int32_t)z.cap;
-  a.shape.places = (float)(compute_units() * (z.narrow ? 2 : 1));
+  a.shape.places = (float)(compute_units() * (kv4 && z.part_rows <= kCkSlimRows ? 4 : z.narrow ? 2 : 1));
   a.q = (const uint16_t*)q;
   a.q_stride = q_stride;
   a.q_offset = chunk->q_offset;
@@ -318,8 +321,8 @@ int32_t chunk_call(const char* who, int which, const rtp_layer_desc* layer, cons
   a.part_rows = z.part_rows;
   a.f16 = layer->kv_dtype == RTP_DTYPE_FP16;
   if (chunk->B > 64) RTP_LAUNCH(chunk_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a);
-  if (kv4) launch_chunk_kv4(a, (unsigned)grid, z.narrow, stream);
-  else launch_chunk_16(a, (unsigned)grid, z.narrow, stream);
+  if (kv4) launch_chunk_kv4(a, (unsigned)grid, z.part_rows, stream);
+  else launch_chunk_16(a, (unsigned)grid, z.part_rows, stream);
   if (z.cap > 0) {
     const int64_t rows = (int64_t)chunk->total_q * a.shape.n_served;
     if (rows <= 2048) RTP_LAUNCH(chunk_merge_kernel<8>, dim3((unsigned)std::min<int64_t>(rows, 1024)), dim3(256), 0, stream, a);

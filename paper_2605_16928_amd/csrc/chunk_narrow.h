@@ -29,34 +29,22 @@ __device__ __forceinline__ void chunk_wave_fence() {
   __builtin_amdgcn_wave_barrier();
 }
 
-template <bool F16, bool LOCAL, bool KV4, int NW, bool CARE>
-struct ChunkNarrow {
+// The blocks of 32 keys that a wave takes, and where their rows lie: block k of wave w is block w + NW k of the range.
+template <bool LOCAL, bool KV4, int NW>
+struct ChunkBlocks {
   const ChunkArgs& a;
   const ChunkTile& t;
-  unsigned char* const smem;
-  unsigned char* const mine;                     // the wave's own LDS
-  const int lane, wave, g, r;
-  const float c;
-  const ChunkReads rd;
-  const ChunkSight sight;
-  const int n_blocks;                            // of this wave: block k starts at key n0(k)
-  u32x4 q[8];
-  f32x16 O[4];
-  float m, l;
-  const uint8_t* base0;
+  const int lane, wave, g;
+  const int count;
+  const uint8_t* base0;                          // K or codes, V or scales, of the KV head
   const uint8_t* base1;
-  uint32_t at_lo, at_hi, sc_lo, sc_hi;           // places of half blocks (16 keys lie in one page), two per block, 32 blocks
+  uint32_t at_lo, at_hi, sc_lo, sc_hi;           // places of half blocks (16 keys lie in one page), two per block, of 32 blocks
   int next_page, window;
-  bool lost;
+  bool lost;                                     // a page was not there; the first was taken for it
 
-  __device__ __forceinline__ ChunkNarrow(const ChunkArgs& a_, const ChunkTile& t_, unsigned char* smem_)
-      : a(a_), t(t_), smem(smem_), mine(smem_ + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kCkBlockBytes), lane(threadIdx.x & 63),
-        wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), g(lane >> 5), r(lane & 31), c(a_.scale_log2), rd(chunk_reads()),
-        sight(chunk_sight(a_.shape, t_, lane & 31)), n_blocks((2 * (t_.it_hi - t_.it_lo) - wave + NW - 1) / NW), window(-2), lost(false) {
-    const int row_c = min(r, t.rows - 1), rt = (row_c * t.over) >> 16;
-    const uint16_t* src = a.q + (t.q0 + rt) * a.q_stride + chunk_head(a, t, row_c, rt) * kHeadDim + g * (KV4 ? 64 : 8);
-#pragma unroll
-    for (int kk = 0; kk < 8; ++kk) q[kk] = *reinterpret_cast<const u32x4*>(src + kk * (KV4 ? 8 : 16));
+  __device__ __forceinline__ ChunkBlocks(const ChunkArgs& a_, const ChunkTile& t_)
+      : a(a_), t(t_), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), g(lane >> 5),
+        count((2 * (t_.it_hi - t_.it_lo) - wave + NW - 1) / NW), window(-2), lost(false) {
     if constexpr (KV4) {
       base0 = a.c4.codes + (int64_t)t.kvh * a.c4.code_head_stride;
       base1 = a.c4.scales + (int64_t)t.kvh * a.c4.scale_head_stride;
@@ -64,12 +52,6 @@ struct ChunkNarrow {
       base0 = a.c16.K + (int64_t)t.kvh * a.c16.head_bytes;
       base1 = a.c16.V + (int64_t)t.kvh * a.c16.head_bytes;
     }
-    m = -__builtin_huge_valf();
-    l = 0.f;
-#pragma unroll
-    for (int db = 0; db < 4; ++db)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) O[db][i] = 0.f;
   }
 
   // First key of the wave's block k.
@@ -78,11 +60,11 @@ struct ChunkNarrow {
     return chunk_tile_n0(t, t.it_lo + (j >> 1)) + (j & 1) * 32;
   }
   __device__ __forceinline__ int next_seen(int k) const {
-    while (k < n_blocks && !chunk_any_seen<LOCAL>(a.shape, t, t.m_lo, t.m_hi, n0(k), 32)) ++k;
+    while (k < count && !chunk_any_seen<LOCAL>(a.shape, t, t.m_lo, t.m_hi, n0(k), 32)) ++k;
     return k;
   }
   // First key of half h of block k, or, where that lies behind the last key, of the 16 that hold it.
-  __device__ __forceinline__ int half_n0(int k, int h) const { return min(n0(min(k, n_blocks - 1)) + 16 * h, (t.kend - 1) & ~15); }
+  __device__ __forceinline__ int half_n0(int k, int h) const { return min(n0(min(k, count - 1)) + 16 * h, (t.kend - 1) & ~15); }
   __device__ __forceinline__ void look_up(int w) {
     next_page = t.pt[half_n0(w * 32 + (lane >> 1), lane & 1) >> (KV4 ? a.c4.page_shift : a.c16.page_shift)];
   }
@@ -115,30 +97,7 @@ struct ChunkNarrow {
   // Keys of half h behind its first that are there.
   __device__ __forceinline__ int left(int k, int h) const { return t.kend - 1 - half_n0(k, h); }
 
-  // ---- 16-bit rows: eight loads of four rows for K, eight for V ----
-  __device__ __forceinline__ void send(int k, bool v) {
-    const uint32_t lds = (uint32_t)(size_t)(__attribute__((address_space(3))) unsigned char*)mine + (v ? kCkBlockBytes / 2 : 0);
-    const int sub = lane >> 4, pos = lane & 15;
-    const uint8_t* const base = v ? base1 : base0;
-    const int64_t half[2] = {place(at_lo, at_hi, k, 0), place(at_lo, at_hi, k, 1)};
-    if (n0(k) + 32 <= t.kend) {
-      const uint32_t off = sub * a.c16.row_bytes;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {                                         // row 4 (i % 4) + sub of its half
-        const int chunk = v ? (((pos >> 1) ^ (2 * sub)) << 1) | (pos & 1) : pos ^ sub ^ (4 * (i & 3));
-        chunk_load_lds(lds + i * 1024, base + half[i >> 2] + (i & 3) * 4 * a.c16.row_bytes, off + chunk * 16);
-      }
-    } else {
-#pragma unroll 1
-      for (int i = 0; i < 8; ++i) {
-        const int rel = 4 * (i & 3) + sub, chunk = v ? (((pos >> 1) ^ (2 * sub)) << 1) | (pos & 1) : pos ^ rel;
-        chunk_load_lds(lds + i * 1024, base + (i < 4 ? half[0] : half[1]), (uint32_t)(min(rel, left(k, i >> 2)) * a.c16.row_bytes + chunk * 16));
-      }
-    }
-  }
-  static __device__ __forceinline__ void reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
-
-  // ---- 4-bit rows ----
+  // ---- 4-bit records and their scales, as they come from memory ----
   struct Codes {
     u32x4 line[4];                               // token 8 i + lane / 8, 16 bytes of its 128
     uint32_t scales;                             // word lane % 8 of the scales of tokens 4 (lane / 8) .. + 3
@@ -161,22 +120,82 @@ struct ChunkNarrow {
     }
     x.scales = *reinterpret_cast<const uint32_t*>(base1 + (g ? s1 : s0) + group * kKv4Group + (lane & 7) * 4) & keep;
   }
-  static __device__ __forceinline__ int line_at(int token, int piece) { return token * 128 + (piece ^ ((token >> 1) & 7)) * 16; }
-  static constexpr int kScalesAt = 32 * kKv4Row;
-  __device__ __forceinline__ void turn(const Codes& x) const {
-    chunk_wave_fence();
+};
+
+// A record (K in the pieces 0 .. 3 of 16 bytes, V in the rest) and the scales of a wave's 32 tokens in its LDS.
+__device__ __forceinline__ int chunk_record_at(int token, int piece) { return token * 128 + (piece ^ ((token >> 1) & 7)) * 16; }
+constexpr int kCkScalesAt = 32 * kKv4Row;
+template <typename Codes>
+__device__ __forceinline__ void chunk_put_records(unsigned char* mine, const Codes& x) {
+  const int lane = threadIdx.x & 63;
+  chunk_wave_fence();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) *reinterpret_cast<u32x4*>(mine + line_at(8 * i + (lane >> 3), lane & 7)) = x.line[i];
-    *reinterpret_cast<uint32_t*>(mine + kScalesAt + lane * 4) = x.scales;
-    chunk_wave_fence();
+  for (int i = 0; i < 4; ++i) *reinterpret_cast<u32x4*>(mine + chunk_record_at(8 * i + (lane >> 3), lane & 7)) = x.line[i];
+  *reinterpret_cast<uint32_t*>(mine + kCkScalesAt + lane * 4) = x.scales;
+  chunk_wave_fence();
+}
+
+template <bool F16, bool LOCAL, bool KV4, int NW, bool CARE>
+struct ChunkNarrow {
+  const ChunkArgs& a;
+  const ChunkTile& t;
+  unsigned char* const smem;
+  unsigned char* const mine;                     // the wave's own LDS
+  const int lane, wave, g, r;
+  const float c;
+  const ChunkReads rd;
+  const ChunkSight sight;
+  ChunkBlocks<LOCAL, KV4, NW> blocks;
+  u32x4 q[8];
+  f32x16 O[4];
+  float m, l;
+
+  __device__ __forceinline__ ChunkNarrow(const ChunkArgs& a_, const ChunkTile& t_, unsigned char* smem_)
+      : a(a_), t(t_), smem(smem_), mine(smem_ + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kCkBlockBytes), lane(threadIdx.x & 63),
+        wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), g(lane >> 5), r(lane & 31), c(a_.scale_log2), rd(chunk_reads()),
+        sight(chunk_sight(a_.shape, t_, lane & 31)), blocks(a_, t_) {
+    const int row_c = min(r, t.rows - 1), rt = (row_c * t.over) >> 16;
+    const uint16_t* src = a.q + (t.q0 + rt) * a.q_stride + chunk_head(a, t, row_c, rt) * kHeadDim + g * (KV4 ? 64 : 8);
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) q[kk] = *reinterpret_cast<const u32x4*>(src + kk * (KV4 ? 8 : 16));
+    m = -__builtin_huge_valf();
+    l = 0.f;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) O[db][i] = 0.f;
   }
+
+  // ---- 16-bit rows: eight loads of four rows for K, eight for V ----
+  __device__ __forceinline__ void send(int k, bool v) {
+    const uint32_t lds = (uint32_t)(size_t)(__attribute__((address_space(3))) unsigned char*)mine + (v ? kCkBlockBytes / 2 : 0);
+    const int sub = lane >> 4, pos = lane & 15;
+    const uint8_t* const base = v ? blocks.base1 : blocks.base0;
+    const int64_t half[2] = {blocks.place(blocks.at_lo, blocks.at_hi, k, 0), blocks.place(blocks.at_lo, blocks.at_hi, k, 1)};
+    if (blocks.n0(k) + 32 <= t.kend) {
+      const uint32_t off = sub * a.c16.row_bytes;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {                                         // row 4 (i % 4) + sub of its half
+        const int chunk = v ? (((pos >> 1) ^ (2 * sub)) << 1) | (pos & 1) : pos ^ sub ^ (4 * (i & 3));
+        chunk_load_lds(lds + i * 1024, base + half[i >> 2] + (i & 3) * 4 * a.c16.row_bytes, off + chunk * 16);
+      }
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < 8; ++i) {
+        const int rel = 4 * (i & 3) + sub, chunk = v ? (((pos >> 1) ^ (2 * sub)) << 1) | (pos & 1) : pos ^ rel;
+        chunk_load_lds(lds + i * 1024, base + (i < 4 ? half[0] : half[1]), (uint32_t)(min(rel, blocks.left(k, i >> 2)) * a.c16.row_bytes + chunk * 16));
+      }
+    }
+  }
+  static __device__ __forceinline__ void reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
   __device__ __forceinline__ void scores4(f32x16& S) const {
 #pragma unroll
     for (int i = 0; i < 16; ++i) S[i] = 0.f;
 #pragma unroll
     for (int w4 = 0; w4 < 2; ++w4) {
-      const u32x4 w = *reinterpret_cast<const u32x4*>(mine + line_at(r, 2 * g + w4));
-      const float f = __uint_as_float((uint32_t)mine[kScalesAt + (r >> 2) * kKv4Group + (2 * g + w4) * 4 + (r & 3)] << 23);
+      const u32x4 w = *reinterpret_cast<const u32x4*>(mine + chunk_record_at(r, 2 * g + w4));
+      const float f = __uint_as_float((uint32_t)mine[kCkScalesAt + (r >> 2) * kKv4Group + (2 * g + w4) * 4 + (r & 3)] << 23);
 #pragma unroll
       for (int i = 0; i < 4; ++i) S = mfma32<F16>(decode8<F16>(w[i], f), q[4 * w4 + i], S);
     }
@@ -186,12 +205,12 @@ struct ChunkNarrow {
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const int i4 = 2 * tt + e;
-      const uint32_t sc = *reinterpret_cast<const uint32_t*>(mine + kScalesAt + (2 * i4 + g) * kKv4Group + 16 + (r >> 3) * 4);
+      const uint32_t sc = *reinterpret_cast<const uint32_t*>(mine + kCkScalesAt + (2 * i4 + g) * kKv4Group + 16 + (r >> 3) * 4);
 #pragma unroll
       for (int j = 0; j < 4; j += 2) {
         const int n = 8 * i4 + 4 * g + j;
-        const uint32_t x = *reinterpret_cast<const uint16_t*>(mine + line_at(n, 4 + (r >> 3)) + (r & 7) * 2);
-        const uint32_t y = *reinterpret_cast<const uint16_t*>(mine + line_at(n + 1, 4 + (r >> 3)) + (r & 7) * 2);
+        const uint32_t x = *reinterpret_cast<const uint16_t*>(mine + chunk_record_at(n, 4 + (r >> 3)) + (r & 7) * 2);
+        const uint32_t y = *reinterpret_cast<const uint16_t*>(mine + chunk_record_at(n + 1, 4 + (r >> 3)) + (r & 7) * 2);
         float fx = kv4_scale(sc, j), fy = kv4_scale(sc, j + 1);
         if constexpr (CARE) {                                               // (not_numbers() has the blocks that are none)
           fx = fx < __builtin_huge_valf() ? fx : 0.f;
@@ -224,7 +243,7 @@ struct ChunkNarrow {
     uint32_t hit = 0;                                                       // bit: block of 32 dims
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const unsigned char* sc = mine + kScalesAt + (2 * (i >> 2) + g) * kKv4Group + 16 + (i & 3);
+      const unsigned char* sc = mine + kCkScalesAt + (2 * (i >> 2) + g) * kKv4Group + 16 + (i & 3);
 #pragma unroll
       for (int blk = 0; blk < 4; ++blk) hit |= ((seen >> i) & 1u) && sc[blk * 4] == 255 ? 1u << blk : 0u;
     }
@@ -280,16 +299,16 @@ struct ChunkNarrow {
   __device__ __forceinline__ void pass16() {
     f32x16 S;
     uint32_t P[8], R[8], seen;
-    int k = next_seen(0);
-    if (k < n_blocks) {
-      advance(k);
+    int k = blocks.next_seen(0);
+    if (k < blocks.count) {
+      blocks.advance(k);
       send(k, false);
       send(k, true);
     }
-    while (k < n_blocks) {
-      const int next = next_seen(k + 1);
-      const bool more = next < n_blocks;
-      if (more) advance(next);
+    while (k < blocks.count) {
+      const int next = blocks.next_seen(k + 1);
+      const bool more = next < blocks.count;
+      if (more) blocks.advance(next);
       chunk_wait_loads<8>();                                                // K, in front of V's eight
 #pragma unroll
       for (int i = 0; i < 16; ++i) S[i] = 0.f;
@@ -297,7 +316,7 @@ struct ChunkNarrow {
       for (int kk = 0; kk < 8; ++kk) S = mfma32<F16>(chunk_read_k(mine, rd, kk), q[kk], S);
       reads_done();
       if (more) send(next, false);
-      softmax(n0(k), S, P, R, seen);
+      softmax(blocks.n0(k), S, P, R, seen);
       if (more) chunk_wait_loads<8>();
       else chunk_wait_loads<0>();
       bool odd = false;
@@ -324,25 +343,25 @@ struct ChunkNarrow {
     }
   }
   __device__ __forceinline__ void pass4() {
-    Codes x[2];
+    typename ChunkBlocks<LOCAL, KV4, NW>::Codes x[2];
     int at[2];
-    at[0] = next_seen(0);
-    at[1] = next_seen(at[0] + 1);
+    at[0] = blocks.next_seen(0);
+    at[1] = blocks.next_seen(at[0] + 1);
 #pragma unroll
     for (int u = 0; u < 2; ++u)
-      if (at[u] < n_blocks) {
-        advance(at[u]);
-        fetch(at[u], x[u]);
+      if (at[u] < blocks.count) {
+        blocks.advance(at[u]);
+        blocks.fetch(at[u], x[u]);
       }
-    auto step = [&](Codes& y, int& k, int behind) __attribute__((always_inline)) {      // behind: the block that is on its way behind this one
+    auto step = [&](typename ChunkBlocks<LOCAL, KV4, NW>::Codes& y, int& k, int behind) __attribute__((always_inline)) {      // behind: the block that is on its way behind this one
       f32x16 S;
       uint32_t P[8], R[8], seen;
-      turn(y);
-      const int n = n0(k);
-      k = next_seen(behind + 1);
-      if (k < n_blocks) {
-        advance(k);
-        fetch(k, y);
+      chunk_put_records(mine, y);
+      const int n = blocks.n0(k);
+      k = blocks.next_seen(behind + 1);
+      if (k < blocks.count) {
+        blocks.advance(k);
+        blocks.fetch(k, y);
       }
       scores4(S);
       softmax(n, S, P, R, seen);
@@ -354,16 +373,16 @@ struct ChunkNarrow {
       }
       if constexpr (CARE) not_numbers(seen);
     };
-    while (at[0] < n_blocks) {
+    while (at[0] < blocks.count) {
       step(x[0], at[0], at[1]);
-      if (at[1] >= n_blocks) break;
+      if (at[1] >= blocks.count) break;
       step(x[1], at[1], at[0]);
     }
   }
 
   // true: a page was not there or a result is not finite (never with CARE)
   __device__ __forceinline__ bool run() {
-    if (n_blocks > 0) {
+    if (blocks.count > 0) {
       if constexpr (KV4) pass4();
       else pass16();
     }
@@ -374,7 +393,7 @@ struct ChunkNarrow {
       for (int i = 0; i < 16; ++i) z = fmaf(O[db][i], 0.f, z);
     l += __shfl_xor(l, 32);
     if constexpr (CARE) __syncthreads();
-    else if (__syncthreads_or(lost || !(z == 0.f) || !(l < 0x1p120f) ? 1 : 0) != 0) return true;
+    else if (__syncthreads_or(blocks.lost || !(z == 0.f) || !(l < 0x1p120f) ? 1 : 0) != 0) return true;
     // ---- the waves' results, joined: rows of 32 groups of four outputs, group d of row r at d ^ r ----
     float* const sh_m = reinterpret_cast<float*>(smem + NW * kCkBlockBytes);
     float* const sh_l = sh_m + NW * kCkNarrowRows;
@@ -429,68 +448,5 @@ struct ChunkNarrow {
     return false;
   }
 };
-
-// The kernels.  ANY: tiles of any size; what has to be taken again is noted by workgroup, for AGAIN.  NARROW: where the host knows that no tile has
-// more than 32 rows; takes its tiles again itself.
-#define RTP_CHUNK_KERNELS(ANY, AGAIN, NARROW, KV4)                                                                      \
-  template <bool F16, bool LOCAL, bool FULL>                                                                            \
-  __global__ __launch_bounds__(kCkThreads, 2) void ANY(const ChunkArgs a) {                                             \
-    fetch_arguments<ChunkArgs>();                                                                                       \
-    __shared__ __attribute__((aligned(16))) unsigned char smem[kCkLds];                                                 \
-    ChunkTile t;                                                                                                        \
-    bool again = false;                                                                                                 \
-    if (chunk_tile<LOCAL, KV4>(a, blockIdx.x, &t)) {                                                                    \
-      if (t.rows <= kCkNarrowRows) {                                                                                    \
-        again = ChunkNarrow<F16, LOCAL, KV4, kCkWaves, false>(a, t, smem).run();                                        \
-      } else {                                                                                                          \
-        ChunkWide<F16, LOCAL, KV4, FULL> w(a, t, smem);                                                                 \
-        w.m = -__builtin_huge_valf();                                                                                   \
-        w.clear();                                                                                                      \
-        again = t.it_lo < t.it_hi && w.fast_pass();                                                                     \
-        if (!again) w.store();                                                                                          \
-      }                                                                                                                 \
-    }                                                                                                                   \
-    if (threadIdx.x == 0) a.again[blockIdx.x] = again ? 1 : 0;                                                          \
-  }                                                                                                                     \
-  template <bool F16, bool LOCAL>                                                                                       \
-  __global__ __launch_bounds__(kCkThreads, 2) void AGAIN(const ChunkArgs a, int n) {                                    \
-    fetch_arguments<ChunkArgs>();                                                                                       \
-    __shared__ __attribute__((aligned(16))) unsigned char smem[kCkLds];                                                 \
-    for (int first = blockIdx.x, i = first; i < n; i += gridDim.x) {                                                    \
-      if ((i - first) / (int)gridDim.x % kCkThreads == 0) {             /* this workgroup's next flags, one to a thread */ \
-        const int64_t at = i + (int64_t)threadIdx.x * gridDim.x;                                                        \
-        if (!__syncthreads_or(at < n ? a.again[at] : 0)) {                                                              \
-          i += (kCkThreads - 1) * gridDim.x;                                                                            \
-          continue;                                                                                                     \
-        }                                                                                                               \
-      }                                                                                                                 \
-      ChunkTile t;                                                                                                      \
-      if (a.again[i] == 0 || !chunk_tile<LOCAL, KV4>(a, i, &t)) continue;                                               \
-      __syncthreads();                                                                                                  \
-      ChunkWide<F16, LOCAL, KV4, true> w(a, t, smem);                                                                   \
-      w.exact_pass();                                                                                                   \
-      w.store();                                                                                                        \
-    }                                                                                                                   \
-  }                                                                                                                     \
-  template <bool F16, bool LOCAL>                                                                                       \
-  __global__ __launch_bounds__(kCkSmallWaves * 64, 2) void NARROW(const ChunkArgs a) {                                  \
-    fetch_arguments<ChunkArgs>();                                                                                       \
-    __shared__ __attribute__((aligned(16))) unsigned char smem[chunk_narrow_lds(kCkSmallWaves)];                        \
-    ChunkTile t;                                                                                                        \
-    if (!chunk_tile<LOCAL, KV4>(a, blockIdx.x, &t)) return;                                                             \
-    if (ChunkNarrow<F16, LOCAL, KV4, kCkSmallWaves, false>(a, t, smem).run())                                           \
-      ChunkNarrow<F16, LOCAL, KV4, kCkSmallWaves, true>(a, t, smem).run();                                              \
-  }
-// Launches those that a call's flags name.
-#define RTP_CHUNK_LAUNCH(ANY, AGAIN, NARROW, F16_, LOCAL_)                                                              \
-  if ((a.f16 != 0) == F16_ && (a.shape.local != 0) == LOCAL_) {                                                         \
-    if (narrow) {                                                                                                       \
-      RTP_LAUNCH((NARROW<F16_, LOCAL_>), dim3(grid), dim3(kCkSmallWaves * 64), 0, stream, a);                           \
-    } else {                                                                                                            \
-      if (a.lse) RTP_LAUNCH((ANY<F16_, LOCAL_, true>), dim3(grid), dim3(kCkThreads), 0, stream, a);                     \
-      else RTP_LAUNCH((ANY<F16_, LOCAL_, false>), dim3(grid), dim3(kCkThreads), 0, stream, a);                          \
-      RTP_LAUNCH((AGAIN<F16_, LOCAL_>), dim3(grid < 256 ? grid : 256), dim3(kCkThreads), 0, stream, a, (int)grid);      \
-    }                                                                                                                   \
-  }
 
 }  // namespace rtp

@@ -83,15 +83,8 @@ __host__ __device__ __forceinline__ int chunk_splits(int key_tiles, int longest,
 }
 struct ChunkSums {
   float units, cut_units, cut_rows;      // units; those of cut tiles; rows of partial results
+  float most;                            // what the units of one sequence take by themselves, at the most
 };
-__host__ __device__ __forceinline__ void chunk_sum(ChunkSums* sums, float tiles, float rows, int splits) {
-  const float S = (float)splits, cut = splits > 1 ? S : 0.f;
-  sums->units = fmaf(tiles, S, sums->units);
-  sums->cut_units = fmaf(tiles, cut, sums->cut_units);
-  sums->cut_rows = fmaf(rows, cut, sums->cut_rows);
-}
-// What a candidate costs: rounds of units over the places for workgroups, each as long as the mean one, and what the longest sequence's units are
-// longer than that: all of it where every unit has a place at once, half of it (the last round's) otherwise; and its partial results.
 __host__ __device__ __forceinline__ float chunk_over(float x, float y) {      // x / y to a few steps
 #ifdef __HIP_DEVICE_COMPILE__
   return x * __builtin_amdgcn_rcpf(y);
@@ -99,11 +92,22 @@ __host__ __device__ __forceinline__ float chunk_over(float x, float y) {      //
   return x / y;
 #endif
 }
+__host__ __device__ __forceinline__ void chunk_sum(ChunkSums* sums, float tiles, float rows, float key_tiles, int splits, float per_place) {
+  const float S = (float)splits, cut = splits > 1 ? S : 0.f;
+  sums->most = fmaxf(sums->most, ceilf(tiles * S * per_place - 0.001f) * (ceilf(chunk_over(key_tiles, S)) + (float)kChunkUnitCost));
+  sums->units = fmaf(tiles, S, sums->units);
+  sums->cut_units = fmaf(tiles, cut, sums->cut_units);
+  sums->cut_rows = fmaf(rows, cut, sums->cut_rows);
+}
+// What a candidate costs.  Units that are alike go in rounds over the places for workgroups; what the longest sequence's are longer than the mean
+// comes on top, all of it where every unit has a place at once, half of it otherwise.  Units that differ fill up the places as they come, but for half
+// of the longest at the end.  A sequence's own units, which are alike, take whole rounds in any case.  And the partial results.
 __host__ __device__ __forceinline__ float chunk_cost(float work, const ChunkSums& sums, int longest, int candidate, float places) {
   const float mean = ceilf(chunk_over(work, sums.units)), most = ceilf(chunk_over((float)longest, (float)candidate));
   const float rounds = ceilf(chunk_over(sums.units, places) - 0.001f);
-  float cost = rounds * (mean + (float)kChunkUnitCost);
-  cost = fmaf(most > mean ? most - mean : 0.f, rounds > 1.f ? 0.5f : 1.f, cost);
+  const float alike = fmaf(most > mean ? most - mean : 0.f, rounds > 1.f ? 0.5f : 1.f, rounds * (mean + (float)kChunkUnitCost));
+  const float mixed = fmaf(0.5f, most, chunk_over(fmaf(sums.units, (float)kChunkUnitCost, work), places));
+  float cost = fmaxf(rounds > 1.f ? fminf(alike, mixed) : alike, sums.most);
   cost = fmaf(sums.cut_rows, chunk_over(1.f / kChunkRowsPerTile, places), cost);
   return sums.cut_units > 0.f ? cost + (float)kChunkMergeCost : cost;
 }

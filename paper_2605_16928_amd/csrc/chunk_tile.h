@@ -61,10 +61,13 @@ __device__ __forceinline__ ChunkLane chunk_lane(const ChunkArgs& a, int b) {
 __device__ __forceinline__ void chunk_add_up(const ChunkShape& shape, const ChunkLane& s, int lanes, int longest, uint32_t magic, ChunkSums* sums) {
   const int candidate = chunk_candidate(threadIdx.x & 63);
   const int tiles = __float_as_int((float)s.tiles), rows = __float_as_int((float)(s.n * shape.n_served));
+  const float per_place = chunk_over(1.f, shape.places);
 #pragma unroll 1
-  for (int k = 0; k < lanes; ++k)
-    chunk_sum(sums, __int_as_float(__builtin_amdgcn_readlane(tiles, k)), __int_as_float(__builtin_amdgcn_readlane(rows, k)),
-              chunk_splits(__builtin_amdgcn_readlane(s.key_tiles, k), longest, candidate, magic));
+  for (int k = 0; k < lanes; ++k) {
+    const int kt = __builtin_amdgcn_readlane(s.key_tiles, k);
+    chunk_sum(sums, __int_as_float(__builtin_amdgcn_readlane(tiles, k)), __int_as_float(__builtin_amdgcn_readlane(rows, k)), (float)kt,
+              chunk_splits(kt, longest, candidate, magic), per_place);
+  }
 }
 // The best candidate of the lanes': the least cost, to within 2^-17.
 __device__ __forceinline__ int chunk_best(const ChunkShape& s, int longest, float work, const ChunkSums& sums) {

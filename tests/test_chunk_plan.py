@@ -42,8 +42,10 @@ extern "C" long plan(const int* members, int n_kv, int group, int local, int sin
   int candidate = 1;
   for (int i = 0; i < kChunkCandidates; ++i) {
     ChunkSums sums = {};
-    for (int b = 0; b < B; ++b)
-      chunk_sum(&sums, tiles[b], n[b] * s.n_served, chunk_splits(n[b] > 0 ? chunk_key_tiles(s, n[b], ctx[b]) : 1, longest, chunk_candidate(i), magic));
+    for (int b = 0; b < B; ++b) {
+      const int kt = n[b] > 0 ? chunk_key_tiles(s, n[b], ctx[b]) : 1;
+      chunk_sum(&sums, tiles[b], n[b] * s.n_served, kt, chunk_splits(kt, longest, chunk_candidate(i), magic), 1.f / places);
+    }
     const float cost = sums.cut_units > (float)cap ? INFINITY : chunk_cost(work, sums, longest, chunk_candidate(i), (float)places);
     if (cost < best) { best = cost; candidate = chunk_candidate(i); }
   }
