@@ -70,7 +70,7 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(const ChunkArg
   for (int b0 = 0; b0 < s.B; b0 += kPlanThreads) {
     const ChunkLane mine = chunk_lane(a, b0 + tid);
     const int S = chunk_splits(mine.key_tiles, longest, sh_candidate, magic), own = mine.tiles * S;
-    const int add[3] = {own, S > 1 ? own : 0, S > 1 ? mine.n * a.shape.n_served : 0};
+    const int add[3] = {own, S > 1 ? own : 0, mine.tiles};
     int last[3];
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
@@ -106,92 +106,83 @@ static void launch_chunk_16(const ChunkArgs& a, unsigned grid, int rows, hipStre
 // attn_chunk_kv4.hip
 void launch_chunk_kv4(const ChunkArgs& a, unsigned grid, int rows, hipStream_t stream);
 
-// Merges the ranges of the rows whose tiles were cut: SLICES groups of 32 lanes per row take the ranges in turn, a lane 4 of the 128 dims.
+// Merges the ranges of the tiles that were cut (blockIdx.x: tile; blockIdx.y takes its rows in turn): SLICES groups of 32 lanes per row take the ranges
+// in turn, four at a time, a lane 4 of the 128 dims.
 template <int SLICES>
-__global__ __launch_bounds__(256) void chunk_merge_kernel(const ChunkArgs a) {
-  fetch_arguments<ChunkArgs>();
+__global__ __launch_bounds__(256) void chunk_merge_kernel(const ChunkMerge* merge, const float* part, int part_rows, float scale, float scale_log2,
+                                                          int group, int n_q_heads, int f16, uint16_t* out, float* lse) {
   __shared__ float sh_h[8][3];
   __shared__ __attribute__((aligned(16))) float sh_acc[8][kHeadDim];
   constexpr int kRows = 8 / SLICES;
-  const ChunkShape& sh = a.shape;
   const int tid = threadIdx.x, d4 = tid & 31, grp = tid >> 5, slice = grp % SLICES;
   const float ninf = -__builtin_huge_valf();
-  const ChunkPlan plan = chunk_plan(a);
-  for (int at0 = blockIdx.x * kRows;; at0 += (int)gridDim.x * kRows) {
-    const ChunkSpot spot = chunk_find<true>(a, plan, at0);                 // (the rows of a workgroup: those of one sequence, or the next ones' too)
-    if (spot.b < 0) return;
-    // row -> (token, served head)
-    const int at = at0 + grp / SLICES;
-    ChunkSpot mine = spot;
-    if (spot.rel + kRows > spot.n * a.shape.n_served) {                     // (the same for the whole workgroup)
-      for (int k = 0; k < kRows; ++k) {
-        const ChunkSpot other = chunk_find<true>(a, plan, at0 + k);
-        if (grp / SLICES == k) mine = other;
-      }
-    } else {
-      mine.rel += at - at0;
-    }
-    const bool have = mine.b >= 0;
+  const ChunkMerge t = merge[blockIdx.x];
+  const int rows = min(t.rows, part_rows);
+  const int64_t step = (int64_t)t.step * part_rows * kCkPart;
+  for (int row0 = blockIdx.y * kRows; row0 < rows; row0 += gridDim.y * kRows) {
+    const int row = row0 + grp / SLICES;
     float M = ninf, L = 0.f, F = 0.f;
     float4 A = make_float4(0.f, 0.f, 0.f, 0.f);
-    int64_t o = 0;
-    if (have) {
-      const int t = mine.rel / sh.n_served;
-      const ChunkRow x = chunk_row(sh, mine.n, mine.splits, t, mine.rel - t * sh.n_served);
-      o = (int64_t)(mine.q0 + t) * a.n_q_heads + x.head;
-      const float* p = a.part + ((int64_t)(mine.part0 + x.unit) * a.part_rows + x.row) * kCkPart;
-      const int64_t pstep = (int64_t)x.step * a.part_rows * kCkPart;
-      for (int s0 = slice; s0 < mine.splits; s0 += 4 * SLICES) {
-        float4 h[4], v[4];
+    const float* p = part + ((int64_t)t.part * part_rows + row) * kCkPart;
+    for (int s0 = slice; row < rows && s0 < t.splits; s0 += 4 * SLICES) {
+      float4 h[4], v[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int s = s0 + k * SLICES;
-          h[k] = make_float4(ninf, 0.f, 0.f, 0.f);
-          v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (s < mine.splits) {
-            h[k] = *reinterpret_cast<const float4*>(p + s * pstep);
-            v[k] = *reinterpret_cast<const float4*>(p + s * pstep + 4 + d4 * 4);
-          }
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float Mn = fmaxf(M, h[k].x);
-          if (Mn == ninf) continue;
-          const float c0 = fast_exp2((M - Mn) * a.scale_log2), c1 = fast_exp2((h[k].x - Mn) * a.scale_log2);
-          L = L * c0 + h[k].y * c1;
-          F = F * c0 + h[k].z * c1;
-          A.x = A.x * c0 + v[k].x * c1; A.y = A.y * c0 + v[k].y * c1;
-          A.z = A.z * c0 + v[k].z * c1; A.w = A.w * c0 + v[k].w * c1;
-          M = Mn;
+      for (int k = 0; k < 4; ++k) {
+        const int s = s0 + k * SLICES;
+        h[k] = make_float4(ninf, 0.f, 0.f, 0.f);
+        v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (s < t.splits) {
+          h[k] = *reinterpret_cast<const float4*>(p + s * step);
+          v[k] = *reinterpret_cast<const float4*>(p + s * step + 4 + d4 * 4);
         }
       }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float Mn = fmaxf(M, h[k].x);
+        if (Mn == ninf) continue;
+        const float c0 = fast_exp2((M - Mn) * scale_log2), c1 = fast_exp2((h[k].x - Mn) * scale_log2);
+        L = L * c0 + h[k].y * c1;
+        F = F * c0 + h[k].z * c1;
+        A.x = A.x * c0 + v[k].x * c1; A.y = A.y * c0 + v[k].y * c1;
+        A.z = A.z * c0 + v[k].z * c1; A.w = A.w * c0 + v[k].w * c1;
+        M = Mn;
+      }
     }
-    if (d4 == 0) { sh_h[grp][0] = M; sh_h[grp][1] = L; sh_h[grp][2] = F; }
-    *reinterpret_cast<float4*>(&sh_acc[grp][d4 * 4]) = A;
-    __syncthreads();
-    if (slice == 0 && have) {
+    if constexpr (SLICES > 1) {
+      if (d4 == 0) { sh_h[grp][0] = M; sh_h[grp][1] = L; sh_h[grp][2] = F; }
+      *reinterpret_cast<float4*>(&sh_acc[grp][d4 * 4]) = A;
+      __syncthreads();
       float Mt = ninf, Lt = 0.f, Ft = 0.f;
       float4 At = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (slice == 0) {
 #pragma unroll
-      for (int k = 0; k < SLICES; ++k) Mt = fmaxf(Mt, sh_h[grp + k][0]);
-      if (Mt != ninf) {
+        for (int k = 0; k < SLICES; ++k) Mt = fmaxf(Mt, sh_h[grp + k][0]);
+        if (Mt != ninf) {
 #pragma unroll
-        for (int k = 0; k < SLICES; ++k) {
-          const float cw = fast_exp2((sh_h[grp + k][0] - Mt) * a.scale_log2);
-          const float4 v = *reinterpret_cast<const float4*>(&sh_acc[grp + k][d4 * 4]);
-          Lt += sh_h[grp + k][1] * cw;
-          Ft += sh_h[grp + k][2] * cw;
-          At.x += v.x * cw; At.y += v.y * cw; At.z += v.z * cw; At.w += v.w * cw;
+          for (int k = 0; k < SLICES; ++k) {
+            const float cw = fast_exp2((sh_h[grp + k][0] - Mt) * scale_log2);
+            const float4 v = *reinterpret_cast<const float4*>(&sh_acc[grp + k][d4 * 4]);
+            Lt += sh_h[grp + k][1] * cw;
+            Ft += sh_h[grp + k][2] * cw;
+            At.x += v.x * cw; At.y += v.y * cw; At.z += v.z * cw; At.w += v.w * cw;
+          }
         }
       }
-      const bool none = Lt == 0.f;
-      const float inv = none ? 0.f : 1.f / Lt;
-      const u32x2 w = a.f16 ? (u32x2){pack16<true>(At.x * inv, At.y * inv), pack16<true>(At.z * inv, At.w * inv)}
-                            : (u32x2){pack16<false>(At.x * inv, At.y * inv), pack16<false>(At.z * inv, At.w * inv)};
-      *reinterpret_cast<u32x2*>(a.out + o * kHeadDim + d4 * 4) = none ? (u32x2){0u, 0u} : w;
-      if (a.lse && d4 == 0) a.lse[o] = none ? ninf : Mt * a.scale + logf(Ft);
+      __syncthreads();
+      M = Mt;
+      L = Lt;
+      F = Ft;
+      A = At;
     }
-    __syncthreads();
+    if (slice != 0 || row >= rows) continue;
+    const int rt = (row * chunk_row_factor(t.heads)) >> 16, k = row - rt * t.heads;
+    const int64_t o = (int64_t)(t.q0 + rt) * n_q_heads + t.kvh * group + (t.heads == group ? k : chunk_nth((uint32_t)t.members, k));
+    const bool none = L == 0.f;
+    const float inv = none ? 0.f : 1.f / L;
+    const u32x2 w = f16 ? (u32x2){pack16<true>(A.x * inv, A.y * inv), pack16<true>(A.z * inv, A.w * inv)}
+                        : (u32x2){pack16<false>(A.x * inv, A.y * inv), pack16<false>(A.z * inv, A.w * inv)};
+    *reinterpret_cast<u32x2*>(out + o * kHeadDim + d4 * 4) = none ? (u32x2){0u, 0u} : w;
+    if (lse && d4 == 0) lse[o] = none ? ninf : M * scale + logf(F);
   }
 }
 
@@ -234,8 +225,8 @@ struct ChunkSizes {
   int32_t part_rows;
   bool narrow;                 // no tile has more than 32 rows
   int64_t run;                 // units in a row on one die
-  size_t plan_bytes, again_bytes, part_bytes;
-  size_t total() const { return plan_bytes + again_bytes + part_bytes; }
+  size_t plan_bytes, again_bytes, merge_bytes, part_bytes;
+  size_t total() const { return plan_bytes + again_bytes + merge_bytes + part_bytes; }
 };
 ChunkSizes chunk_sizes(const ChunkShape& s, int32_t B, int64_t total_q, int64_t max_q, int64_t max_ctx) {
   ChunkSizes z = {};
@@ -257,6 +248,7 @@ ChunkSizes chunk_sizes(const ChunkShape& s, int32_t B, int64_t total_q, int64_t 
   for (z.run = 1; z.run < 32 && z.run * 2 <= (max_q + kChunkRows / 8 - 1) / (kChunkRows / 8);) z.run *= 2;
   z.again_bytes = z.narrow ? 0 : align_up((size_t)(z.tiles + z.cap + 8 * 32) * sizeof(int32_t), 256);
   z.plan_bytes = B > 64 ? align_up((size_t)(kPlanHead + 3 * ((int64_t)B + 1)) * sizeof(int32_t), 256) : 0;
+  z.merge_bytes = z.cap > 0 ? align_up((size_t)z.tiles * sizeof(ChunkMerge), 256) : 0;
   z.part_bytes = align_up((size_t)z.cap * z.part_rows * kCkPart * sizeof(float), 256);
   return z;
 }
@@ -304,7 +296,7 @@ int32_t chunk_call(const char* who, int which, const rtp_layer_desc* layer, cons
   a.shape.total_q = chunk->total_q;
   a.shape.max_q = chunk->max_q;
   a.shape.cap = (int32_t)z.cap;
-  a.shape.places = (float)(compute_units() * (kv4 && z.part_rows <= kCkSlimRows ? 4 : z.narrow ? 2 : 1));
+  a.shape.places = (float)(compute_units() * (kv4 && z.part_rows <= kCkSlimRows ? 3 : z.narrow ? 2 : 1));
   a.q = (const uint16_t*)q;
   a.q_stride = q_stride;
   a.q_offset = chunk->q_offset;
@@ -316,7 +308,9 @@ int32_t chunk_call(const char* who, int which, const rtp_layer_desc* layer, cons
   a.lse = lse;
   a.plan = (int32_t*)ws;
   a.again = (int32_t*)((uint8_t*)ws + z.plan_bytes);
-  a.part = (float*)((uint8_t*)ws + z.plan_bytes + z.again_bytes);
+  a.merge = z.cap > 0 ? (ChunkMerge*)((uint8_t*)ws + z.plan_bytes + z.again_bytes) : nullptr;
+  a.n_merge = (int32_t)z.tiles;
+  a.part = (float*)((uint8_t*)ws + z.plan_bytes + z.again_bytes + z.merge_bytes);
   while ((1 << a.run_shift) < z.run) ++a.run_shift;
   a.part_rows = z.part_rows;
   a.f16 = layer->kv_dtype == RTP_DTYPE_FP16;
@@ -324,9 +318,17 @@ int32_t chunk_call(const char* who, int which, const rtp_layer_desc* layer, cons
   if (kv4) launch_chunk_kv4(a, (unsigned)grid, z.part_rows, stream);
   else launch_chunk_16(a, (unsigned)grid, z.part_rows, stream);
   if (z.cap > 0) {
-    const int64_t rows = (int64_t)chunk->total_q * a.shape.n_served;
-    if (rows <= 2048) RTP_LAUNCH(chunk_merge_kernel<8>, dim3((unsigned)std::min<int64_t>(rows, 1024)), dim3(256), 0, stream, a);
-    else RTP_LAUNCH(chunk_merge_kernel<2>, dim3((unsigned)std::min<int64_t>((rows + 3) / 4, 1024)), dim3(256), 0, stream, a);
+    // eight slices of the ranges where there are few rows (and many ranges, then), none where there are many; about 4096 workgroups at the most
+    const int slices = (int64_t)chunk->total_q * a.shape.n_served <= 2048 ? 8 : z.part_rows <= 64 ? 2 : 1;
+    const int64_t each = (z.part_rows * slices + 7) / 8, rows = std::max<int64_t>(1, std::min<int64_t>(each, 4096 / z.tiles));
+    const dim3 grid((unsigned)z.tiles, (unsigned)rows), block(256);
+#define RTP_CHUNK_MERGE(SLICES)                                                                                                      \
+  RTP_LAUNCH(chunk_merge_kernel<SLICES>, grid, block, 0, stream, a.merge, a.part, a.part_rows, a.scale, a.scale_log2, a.shape.group, \
+             a.n_q_heads, a.f16, a.out, a.lse)
+    if (slices == 8) RTP_CHUNK_MERGE(8);
+    else if (slices == 2) RTP_CHUNK_MERGE(2);
+    else RTP_CHUNK_MERGE(1);
+#undef RTP_CHUNK_MERGE
   }
   return check_launch(who);
 }

@@ -7,7 +7,7 @@ RTP_CHUNK_KERNELS(chunk_attn_kv4_kernel, chunk_again_kv4_kernel, chunk_narrow_kv
 
 // No tile has more than 16 rows.
 template <bool F16, bool LOCAL>
-__global__ __launch_bounds__(kCkSmallWaves * 64, 4) void chunk_slim_kv4_kernel(const ChunkArgs a) {
+__global__ __launch_bounds__(kCkSmallWaves * 64, 3) void chunk_slim_kv4_kernel(const ChunkArgs a) {
   fetch_arguments<ChunkArgs>();
   __shared__ __attribute__((aligned(16))) unsigned char smem[chunk_slim_lds(kCkSmallWaves)];
   ChunkTile t;

@@ -44,7 +44,7 @@ struct ChunkBlocks {
 
   __device__ __forceinline__ ChunkBlocks(const ChunkArgs& a_, const ChunkTile& t_)
       : a(a_), t(t_), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), g(lane >> 5),
-        count((2 * (t_.it_hi - t_.it_lo) - wave + NW - 1) / NW), window(-2), lost(false) {
+        count((blocks_of(t_) - wave + NW - 1) / NW), window(-2), lost(false) {
     if constexpr (KV4) {
       base0 = a.c4.codes + (int64_t)t.kvh * a.c4.code_head_stride;
       base1 = a.c4.scales + (int64_t)t.kvh * a.c4.scale_head_stride;
@@ -54,12 +54,19 @@ struct ChunkBlocks {
     }
   }
 
+  // (without a band every block up to the last key is seen by some row)
+  static __device__ __forceinline__ int blocks_of(const ChunkTile& t) {
+    const int all = 2 * (t.it_hi - t.it_lo);
+    return LOCAL ? all : min(all, ((t.kend + 31) >> 5) - 2 * t.it_lo);
+  }
   // First key of the wave's block k.
   __device__ __forceinline__ int n0(int k) const {
     const int j = wave + k * NW;
+    if (!LOCAL) return t.it_lo * kCkK + j * 32;
     return chunk_tile_n0(t, t.it_lo + (j >> 1)) + (j & 1) * 32;
   }
   __device__ __forceinline__ int next_seen(int k) const {
+    if (!LOCAL) return k;
     while (k < count && !chunk_any_seen<LOCAL>(a.shape, t, t.m_lo, t.m_hi, n0(k), 32)) ++k;
     return k;
   }

@@ -119,48 +119,24 @@ __host__ __device__ __forceinline__ void chunk_range(int n, int k, int S, int* l
 }
 
 struct ChunkUnit {
-  int kv, split, tile;
-  int heads, first;                      // the KV head's served heads, and how many the KV heads before it have
+  int kv, heads;                         // KV head, its served heads
+  int split, tile;
+  int tiles, before;                     // query tiles of this KV head, and of those before it
 };
-// Unit r of a sequence with n new tokens and S splits.
+// Unit r of a sequence with n new tokens and S splits.  Its tile is the (before + tiles - 1 - tile)-th of the sequence.
 __host__ __device__ __forceinline__ ChunkUnit chunk_unit(const ChunkShape& s, int n, int S, int r) {
-  ChunkUnit u = {0, 0, 0, 1, 0};
-  int tiles = 1;
+  ChunkUnit u = {0, 1, 0, 0, 1, 0};
   for (; u.kv < s.n_kv; ++u.kv) {
     u.heads = chunk_bits(chunk_members(s, u.kv));
     if (u.heads == 0) continue;
-    tiles = chunk_query_tiles(n, chunk_shift(u.heads));
-    if (r < tiles * S) break;
-    r -= tiles * S;
-    u.first += u.heads;
+    u.tiles = chunk_query_tiles(n, chunk_shift(u.heads));
+    if (r < u.tiles * S) break;
+    r -= u.tiles * S;
+    u.before += u.tiles;
   }
-  u.split = (int)((uint32_t)r / (uint32_t)tiles);
-  u.tile = tiles - 1 - (r - u.split * tiles);
+  u.split = (int)((uint32_t)r / (uint32_t)u.tiles);
+  u.tile = u.tiles - 1 - (r - u.split * u.tiles);
   return u;
-}
-// Where the partial results of served head `served` of token t lie: the number of range 0's unit, the step from range to range, the row in the unit.
-struct ChunkRow {
-  int kv, head, unit, step, row;
-};
-__host__ __device__ __forceinline__ ChunkRow chunk_row(const ChunkShape& s, int n, int S, int t, int served) {
-  ChunkRow x = {0, 0, 0, 1, 0};
-  for (; x.kv < s.n_kv; ++x.kv) {
-    const uint32_t m = chunk_members(s, x.kv);
-    const int h = chunk_bits(m);
-    if (h == 0) continue;
-    const int shift = chunk_shift(h);
-    x.step = chunk_query_tiles(n, shift);
-    if (served < h) {
-      const int tile = t >> shift;
-      x.head = x.kv * s.group + chunk_nth(m, served);
-      x.unit += x.step - 1 - tile;
-      x.row = (t - (tile << shift)) * h + served;
-      break;
-    }
-    x.unit += x.step * S;
-    served -= h;
-  }
-  return x;
 }
 
 }  // namespace rtp

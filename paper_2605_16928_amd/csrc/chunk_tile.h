@@ -31,10 +31,17 @@ struct ChunkArgs {
   float* part;                 // [units of cut tiles, part_rows, kCkPart]
   int32_t part_rows;           // rows of a partial result: what a tile can have
   int32_t run_shift;           // 2^run_shift units in a row go to one die
+  struct ChunkMerge* merge;    // [n_merge]: the tiles, for the merge launch (NULL: nothing is cut)
+  int32_t n_merge;
   int32_t* plan;               // B > 64: what chunk_plan_kernel leaves, kPlanHead ints and three lists of B + 1
   int32_t* again;              // [workgroups]: 1 = its unit has to be taken again
   Kv16Cache c16;
   Kv4Cache c4;
+};
+// A query tile as the merge launch needs it; rows = 0: its results are complete.
+struct ChunkMerge {
+  int32_t rows, splits, part, step;      // ranges: partial results part, part + step ...
+  int32_t heads, members, kvh, q0;
 };
 enum { kPlanCandidate = 0, kPlanLongest = 1, kPlanHead = 4 };
 
@@ -90,7 +97,7 @@ __device__ __forceinline__ float wave_sum_f32(float x) {
 // The plan as a wave has it: of up to 64 sequences one to a lane (scans inclusive), of more in memory.
 struct ChunkPlan {
   ChunkLane seq;
-  int splits, units, unit_last, part_last, row_last;
+  int splits, units, unit_last, part_last, tile_last;
 };
 __device__ __forceinline__ ChunkPlan chunk_plan(const ChunkArgs& a) {
   const ChunkShape& s = a.shape;
@@ -110,49 +117,56 @@ __device__ __forceinline__ ChunkPlan chunk_plan(const ChunkArgs& a) {
   p.units = p.seq.tiles * p.splits;
   p.unit_last = wave_incl_scan(p.units);
   p.part_last = wave_incl_scan(p.splits > 1 ? p.units : 0);
-  p.row_last = wave_incl_scan(p.splits > 1 ? p.seq.n * s.n_served : 0);
+  p.tile_last = wave_incl_scan(p.seq.tiles);
   return p;
 }
 
-// One sequence's place in the plan.
+// A unit's sequence: the unit's number in it, what it has, and the numbers of its first partial result and its first tile.  b = -1: the unit is `rel`
+// behind the last one, and there are `tile0` tiles.
 struct ChunkSpot {
-  int b, rel;                  // rel: unit (or row of cut sequences) inside the sequence; b = -1: there is none
-  int n, q0, ctx, splits, part0;
+  int b, rel, n, q0, ctx, splits, part0, tile0;
 };
-// The sequence of unit `at` (ROWS: of the at-th row of a sequence whose tiles are cut), found by the whole wave.
-template <bool ROWS>
-__device__ __forceinline__ ChunkSpot chunk_find(const ChunkArgs& a, const ChunkPlan& p, int at) {
+__device__ __forceinline__ ChunkSpot chunk_find(const ChunkArgs& a, int at) {
   const ChunkShape& s = a.shape;
   ChunkSpot spot = {};
   spot.b = -1;
   if (__builtin_expect(s.B <= 64, 1)) {
-    const int last = ROWS ? p.row_last : p.unit_last, own = ROWS ? (p.splits > 1 ? p.seq.n * s.n_served : 0) : p.units;
-    const int b = __popcll(__ballot(last <= at));
-    if (b >= 64) return spot;
+    const ChunkPlan p = chunk_plan(a);
+    const int b = __popcll(__ballot(p.unit_last <= at));
+    if (b >= 64) {
+      spot.rel = at - wave_last(p.unit_last);
+      spot.tile0 = wave_last(p.tile_last);
+      return spot;
+    }
     spot.b = b;
-    spot.rel = at - __builtin_amdgcn_readlane(last - own, b);
+    spot.rel = at - __builtin_amdgcn_readlane(p.unit_last - p.units, b);
     spot.n = __builtin_amdgcn_readlane(p.seq.n, b);
     spot.q0 = __builtin_amdgcn_readlane(p.seq.q0, b);
     spot.ctx = __builtin_amdgcn_readlane(p.seq.ctx, b);
     spot.splits = __builtin_amdgcn_readlane(p.splits, b);
     spot.part0 = __builtin_amdgcn_readlane(p.part_last - (p.splits > 1 ? p.units : 0), b);
+    spot.tile0 = __builtin_amdgcn_readlane(p.tile_last - p.seq.tiles, b);
     return spot;
   }
   const int32_t* unit_first = a.plan + kPlanHead;
   const int32_t* part_first = unit_first + s.B + 1;
-  const int32_t* row_first = part_first + s.B + 1;
-  const int32_t* list = ROWS ? row_first : unit_first;
-  if (at >= list[s.B]) return spot;
-  const int b = wave_last_at_most(list, s.B, at);
+  const int32_t* tile_first = part_first + s.B + 1;
+  if (at >= unit_first[s.B]) {
+    spot.rel = at - unit_first[s.B];
+    spot.tile0 = tile_first[s.B];
+    return spot;
+  }
+  const int b = wave_last_at_most(unit_first, s.B, at);
   const ChunkLane mine = chunk_lane(a, b);
   const int longest = a.plan[kPlanLongest];
   spot.b = b;
-  spot.rel = at - list[b];
+  spot.rel = at - unit_first[b];
   spot.n = mine.n;
   spot.q0 = mine.q0;
   spot.ctx = mine.ctx;
   spot.splits = chunk_splits(mine.key_tiles, longest, a.plan[kPlanCandidate], chunk_magic(longest));
   spot.part0 = part_first[b];
+  spot.tile0 = tile_first[b];
   return spot;
 }
 
@@ -184,8 +198,12 @@ template <bool LOCAL, bool KV4>
 __device__ __forceinline__ bool chunk_tile(const ChunkArgs& a, int workgroup, ChunkTile* t) {
   const ChunkShape& s = a.shape;
   const int k8 = workgroup >> 3, in_run = k8 & ((1 << a.run_shift) - 1);
-  const ChunkSpot spot = chunk_find<false>(a, chunk_plan(a), ((((k8 >> a.run_shift) * 8 + (workgroup & 7)) << a.run_shift) + in_run));
-  if (spot.b < 0) return false;
+  const ChunkSpot spot = chunk_find(a, ((((k8 >> a.run_shift) * 8 + (workgroup & 7)) << a.run_shift) + in_run));
+  if (spot.b < 0) {
+    // (there are as many workgroups without a unit as there may be tiles that are not there)
+    if (a.merge && threadIdx.x == 0 && spot.tile0 + spot.rel < a.n_merge) a.merge[spot.tile0 + spot.rel].rows = 0;
+    return false;
+  }
   const ChunkUnit u = chunk_unit(s, spot.n, spot.splits, spot.rel);
   t->nh = u.heads;
   t->over = chunk_row_factor(u.heads);
@@ -211,6 +229,9 @@ __device__ __forceinline__ bool chunk_tile(const ChunkArgs& a, int workgroup, Ch
   chunk_range(n_tiles, u.split, spot.splits, &t->it_lo, &t->it_hi);
   t->splits = spot.splits;
   t->part = spot.part0 + spot.rel;
+  if (a.merge && u.split == 0 && threadIdx.x == 0)
+    a.merge[spot.tile0 + u.before + u.tiles - 1 - u.tile] =
+        ChunkMerge{spot.splits > 1 ? t->rows : 0, spot.splits, t->part, u.tiles, u.heads, t->members, u.kv, (int)t->q0};
   // (the same in every lane, which the compiler does not see everywhere)
   int* const whole[] = {&t->nh, &t->over, &t->kvh, &t->members, &t->rows, &t->m_lo, &t->m_hi, &t->kend, &t->sink_tiles, &t->gap, &t->it_lo, &t->it_hi,
                         &t->splits, &t->part};

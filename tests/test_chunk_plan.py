@@ -59,12 +59,7 @@ extern "C" long plan(const int* members, int n_kv, int group, int local, int sin
 extern "C" void unit(const int* members, int n_kv, int group, int n, int S, int r, int* out) {
   const ChunkShape s = shape(members, n_kv, group, 0, 0, 0, 0, 1);
   const ChunkUnit u = chunk_unit(s, n, S, r);
-  out[0] = u.kv; out[1] = u.split; out[2] = u.tile; out[3] = u.heads; out[4] = u.first;
-}
-extern "C" void row(const int* members, int n_kv, int group, int n, int S, int t, int served, int* out) {
-  const ChunkShape s = shape(members, n_kv, group, 0, 0, 0, 0, 1);
-  const ChunkRow x = chunk_row(s, n, S, t, served);
-  out[0] = x.kv; out[1] = x.head; out[2] = x.unit; out[3] = x.step; out[4] = x.row;
+  out[0] = u.kv; out[1] = u.split; out[2] = u.tile; out[3] = u.heads; out[4] = u.tiles; out[5] = u.before;
 }
 """
 
@@ -93,27 +88,21 @@ MEMBERS = [([1], 1), ([15] * 8, 4), ([7, 15, 0, 13], 4), ([255], 8), ([1] * 16, 
 
 @pytest.mark.parametrize("members,group", MEMBERS)
 @pytest.mark.parametrize("n,S", [(1, 1), (1, 7), (31, 2), (32, 3), (33, 1), (300, 5), (5000, 1)])
-def test_every_unit_and_every_row_once(lib, members, group, n, S):
+def test_every_unit_once(lib, members, group, n, S):
     heads = [bin(m).count("1") for m in members]
     tiles = [-(-n // TOKENS[h]) if h else 0 for h in heads]
-    units, out = {}, (C.c_int * 5)()
+    units, numbers, out = [], set(), (C.c_int * 6)()
     for r in range(sum(tiles) * S):
         lib.unit(ints(members), len(members), group, n, S, r, out)
-        kv, split, tile, h, first = out
-        assert 0 <= split < S and 0 <= tile < tiles[kv] and h == heads[kv] and first == sum(heads[:kv])
-        units[r] = (kv, split, tile)
-    assert len(set(units.values())) == sum(tiles) * S
-    seen = set()
-    for t in list(range(min(n, 90))) + [n - 1]:
-        for served in range(sum(heads)):
-            lib.row(ints(members), len(members), group, n, S, t, served, out)
-            kv, head, unit, step, row = out
-            tok = TOKENS[heads[kv]]
-            at = [k for k in range(8) if members[kv] >> k & 1][served - sum(heads[:kv])]
-            assert head == kv * group + at and row == t % tok * heads[kv] + served - sum(heads[:kv])
-            assert [units[unit + s * step] for s in range(S)] == [(kv, s, t // tok) for s in range(S)]
-            seen.add((kv, t // tok, row))
-    assert len(seen) == len(set(list(range(min(n, 90))) + [n - 1])) * sum(heads)
+        kv, split, tile, h, mine, before = out
+        assert 0 <= split < S and 0 <= tile < tiles[kv] and h == heads[kv] and mine == tiles[kv] and before == sum(tiles[:kv])
+        units.append((kv, split, tile))
+        if split == 0:                                  # the ranges of a tile are `tiles` units apart; every tile has a number of its own
+            numbers.add(before + mine - 1 - tile)
+    assert len(set(units)) == sum(tiles) * S and numbers == set(range(sum(tiles)))
+    for r, (kv, split, tile) in enumerate(units):
+        if split == 0:
+            assert [units[r + s * tiles[kv]] for s in range(S)] == [(kv, s, tile) for s in range(S)]
 
 
 @pytest.mark.parametrize("h", range(1, 9))
