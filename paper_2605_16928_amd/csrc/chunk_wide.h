@@ -295,7 +295,16 @@ struct ChunkWide {
     bring(1, 1);
     landed();
     __syncthreads();
-    auto tile_at = [&](int y) __attribute__((always_inline)) { return smem + y % kCkStages * kCkTileBytes; };
+    // the buffers of tile x - 1, which tile x + 2 goes to, of tile x and of tile x + 1
+    static_assert(kCkStages == 3, "they go round");
+    int slot_before = 2, slot_here = 0, slot_next = 1;
+    auto tile_of = [&](int slot) __attribute__((always_inline)) { return smem + slot * kCkTileBytes; };
+    auto go_round = [&]() __attribute__((always_inline)) {
+      const int freed = slot_before;
+      slot_before = slot_here;
+      slot_here = slot_next;
+      slot_next = freed;
+    };
     // (of what the row sees there, if it does see anything)
     float any = ninf;
     m = ninf;
@@ -321,7 +330,7 @@ struct ChunkWide {
       const int nb0 = n0_of(x) + hf * 32;
       const uint32_t (&Pin)[8] = hf == 0 ? P1 : P0;
       uint32_t (&Pout)[8] = hf == 0 ? P0 : P1;
-      if (pend) pv(tile_at(hf == 0 ? x - 1 : x), 1 - hf, Pin);
+      if (pend) pv(tile_of(hf == 0 ? slot_before : slot_here), 1 - hf, Pin);
       pend = any_seen(nb0, 32);
       if (pend) {
         if (!all_seen(nb0, 32)) chunk_mask<LOCAL>(sight, nb0 + 4 * g, S);
@@ -331,26 +340,26 @@ struct ChunkWide {
         end_block();
       }
       if (hf == 0) {
-        if (any_seen(nb0 + 32, 32)) scores(tile_at(x), 1, S);
+        if (any_seen(nb0 + 32, 32)) scores(tile_of(slot_here), 1, S);
         landed();
         __syncthreads();
       } else {
-        bring(x + 2, (x + 2) % kCkStages);                                 // (behind the last tile: once more into a buffer that nobody reads)
-        if (x + 1 < n_tiles && any_seen(n0_of(x + 1), 32)) scores(tile_at(x + 1), 0, S);
+        bring(x + 2, slot_before);                                         // (behind the last tile: once more into a buffer that nobody reads)
+        if (x + 1 < n_tiles && any_seen(n0_of(x + 1), 32)) scores(tile_of(slot_next), 0, S);
       }
     };
     auto edge_tile = [&]() __attribute__((always_inline)) {
       half(std::integral_constant<int, 0>{});
       half(std::integral_constant<int, 1>{});
       ++x;
+      go_round();
     };
-    // the loop without masks: full tiles, while the rows that it sends for are all there
+    // The loop without masks: full tiles, while the rows that it sends for are all there (the last tile may be a part of one).
     constexpr int kSends = KV4 ? 3 : 2;
-    auto steady = [&]() __attribute__((always_inline)) {
-      return x <= n_full && (x + kSends >= n_tiles || n0_of(x + kSends) + kCkK <= t.kend);
-    };
+    const bool part = chunk_tile_n0(t, t.it_hi - 1) + kCkK > t.kend;
+    const int x_stop = min(n_full + 1, part ? n_tiles - 1 - kSends : n_tiles);
     edge_tile();
-    if (!steady()) {
+    if (x >= x_stop) {
     } else if (w_hi >= 0) {
       if (!pend) {
 #pragma unroll
@@ -360,46 +369,47 @@ struct ChunkWide {
       f32x16 S1;
       do {
         advance(x + kSends);
-        first_v(tile_at(x - 1), 1);
+        const int x_end = min(x_stop, (x + kSends) / kWindow * kWindow + kWindow - kSends);      // (as far as the window reaches)
+        first_v(tile_of(slot_before), 1);
         do {
-          pv_stream(tile_at(x - 1), 1, P1, S, P0, tile_at(x), 1);
-          score_stream(tile_at(x), 1, S1, S, P0, [](int) __attribute__((always_inline)) {});
-          first_v(tile_at(x), 0);
+          pv_stream(tile_of(slot_before), 1, P1, S, P0, tile_of(slot_here), 1);
+          score_stream(tile_of(slot_here), 1, S1, S, P0, [](int) __attribute__((always_inline)) {});
+          first_v(tile_of(slot_here), 0);
           landed();
           __syncthreads();
-          pv_stream(tile_at(x), 0, P0, S1, P1, tile_at(x + 1), 0);
-          const int slot = (x + 2) % kCkStages;
-          score_stream(tile_at(x + 1), 0, S, S1, P1, [&](int kk) __attribute__((always_inline)) {
+          pv_stream(tile_of(slot_here), 0, P0, S1, P1, tile_of(slot_next), 0);
+          score_stream(tile_of(slot_next), 0, S, S1, P1, [&](int kk) __attribute__((always_inline)) {
             if constexpr (KV4) {
-              if (kk < 4) put_codes(slot, kk);
+              if (kk < 4) put_codes(slot_before, kk);
               if (kk == 4) fetch_codes(x + 3, false);
             } else {
-              if (kk < 4) load16(x + 2, slot, kk >> 1, kk & 1, (kk & 1) ? off1 : off0);
+              if (kk < 4) load16(x + 2, slot_before, kk >> 1, kk & 1, (kk & 1) ? off1 : off0);
             }
           });
-          first_v(tile_at(x), 1);
+          first_v(tile_of(slot_here), 1);
           ++x;
-        } while (steady() && (x + kSends) % kWindow != 0);
-      } while (steady());
+          go_round();
+        } while (x < x_end);
+      } while (x < x_stop);
     } else {
       do {
         advance(x + kSends);
         landed();
         __syncthreads();
-        const int slot = (x + 2) % kCkStages;
         if constexpr (KV4) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) put_codes(slot, i);
+          for (int i = 0; i < 4; ++i) put_codes(slot_before, i);
           fetch_codes(x + 3, false);
         } else {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) load16(x + 2, slot, k >> 1, k & 1, (k & 1) ? off1 : off0);
+          for (int k = 0; k < 4; ++k) load16(x + 2, slot_before, k >> 1, k & 1, (k & 1) ? off1 : off0);
         }
         ++x;
-      } while (steady());
+        go_round();
+      } while (x < x_stop);
     }
     while (x < n_tiles) edge_tile();
-    if (pend) pv(tile_at(n_tiles - 1), 1, P1);
+    if (pend) pv(tile_of(slot_before), 1, P1);
     landed();
     // Was every reference within reach?  A row that sees a key of the range has a sum in the middle of fp32's range (fp16: nothing above 65504 is
     // finite; where the largest probability is below 2^-6 most of the mass may be in subnormals), and outputs are finite.

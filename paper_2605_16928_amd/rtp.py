@@ -72,6 +72,7 @@ class rtp_kv4_cache(C.Structure):
         ("page_table", C.c_void_p), ("pt_stride", C.c_int64), ("page_size", C.c_int32), ("n_pages", C.c_int32),
     ]
     n_heads = n_seqs = 1 << 31                      # KV heads of the pools, rows of the table: known where kv4_cache made it
+    _device = None                                  # and of which device
 
 
 def _held(who: str, layer, cache, B: int):
@@ -100,7 +101,7 @@ def kv4_cache(codes, scales, page_table) -> rtp_kv4_cache:
     c = rtp_kv4_cache(codes.data_ptr(), codes.stride(1), codes.stride(0), scales.data_ptr(), scales.stride(1), scales.stride(0),
                       page_table.data_ptr(), page_table.shape[1], codes.shape[2], codes.shape[1])
     c.n_heads, c.n_seqs = codes.shape[0], page_table.shape[0]
-    c._keepalive = (codes, scales, page_table)
+    c._keepalive, c._device = (codes, scales, page_table), codes.get_device()
     return c
 
 
@@ -110,15 +111,18 @@ class rtp_kv_cache(C.Structure):
         ("page_table", C.c_void_p), ("pt_stride", C.c_int64), ("page_size", C.c_int32), ("n_pages", C.c_int32),
     ]
     n_heads = n_seqs = 1 << 31                      # as in rtp_kv4_cache
+    _device = None
 
 
 class rtp_chunk(C.Structure):
     _fields_ = [("q_offset", C.c_void_p), ("ctx_len", C.c_void_p), ("B", C.c_int32), ("total_q", C.c_int32), ("max_q", C.c_int32),
                 ("max_ctx", C.c_int64)]
+    _device = None
 
 
 class rtp_rope(C.Structure):
     _fields_ = [("inv_freq", C.c_void_p), ("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("scale", C.c_float)]
+    _device = None
 
 
 def kv_cache(K, V, page_table) -> rtp_kv_cache:
@@ -134,7 +138,7 @@ def kv_cache(K, V, page_table) -> rtp_kv_cache:
     c = rtp_kv_cache(K.data_ptr(), V.data_ptr(), K.stride(2), K.stride(1), K.stride(0), page_table.data_ptr(), page_table.shape[1], K.shape[2],
                      K.shape[1])
     c.n_heads, c.n_seqs = K.shape[0], page_table.shape[0]
-    c._keepalive = (K, V, page_table)
+    c._keepalive, c._device = (K, V, page_table), K.get_device()
     return c
 
 
@@ -144,7 +148,7 @@ def chunk_desc(q_offset, ctx_len, total_q: int, max_q: int, max_ctx: int) -> rtp
             or q_offset.device != ctx_len.device:
         raise RtpError(RTP_ERR_INVALID_ARG, "chunk_desc: contiguous int32 q_offset [B + 1] and ctx_len [B] on one device expected")
     c = rtp_chunk(q_offset.data_ptr(), ctx_len.data_ptr(), ctx_len.shape[0], total_q, max_q, max_ctx)
-    c._keepalive = (q_offset, ctx_len)
+    c._keepalive, c._device = (q_offset, ctx_len), q_offset.get_device()
     return c
 
 
@@ -153,27 +157,29 @@ def rope_desc(inv_freq, interleaved: bool = False, scale: float = 0.0) -> rtp_ro
     if inv_freq.dim() != 1 or str(inv_freq.dtype) != "torch.float32" or not inv_freq.is_contiguous():
         raise RtpError(RTP_ERR_INVALID_ARG, "rope_desc: contiguous float32 inv_freq [rotary_dim / 2] expected")
     r = rtp_rope(inv_freq.data_ptr(), 2 * inv_freq.shape[0], 1 if interleaved else 0, scale)
-    r._keepalive = (inv_freq,)
+    r._keepalive, r._device = (inv_freq,), inv_freq.get_device()
     return r
 
 
 def _on_one_device(who: str, descriptors, tensors):
-    """The tensors of a call, and those that its descriptors were made of, lie on the current device, whose stream takes the launches."""
-    held = [t for d in descriptors for t in getattr(d, "_keepalive", ())] + [t for t in tensors if hasattr(t, "device")]
-    if not held:
-        return
-    import torch
-    device = torch.device("cuda", torch.cuda.current_device())
-    for t in held:
-        if t.device != device:
-            raise RtpError(RTP_ERR_INVALID_ARG, f"{who}: a tensor on {t.device}, the current device is {device}")
+    """The tensors of a call, and those that its descriptors were made of, lie on the current device, whose stream takes the launches.
+    (Integers, not device objects: a call of one short kernel is bound by its host time.)"""
+    at = [d._device for d in descriptors if d is not None and d._device is not None]
+    at += [t.get_device() for t in tensors if hasattr(t, "get_device")]
+    if at:
+        import torch
+        current = torch.cuda.current_device()
+        if min(at) != current or max(at) != current:
+            raise RtpError(RTP_ERR_INVALID_ARG, f"{who}: tensors on devices {sorted(set(at))}, the current one is {current}")
 
 
 def _rows(who: str, t, total: int, heads: int, name: str):
     """A tensor of packed rows [total or more, heads, 128] whose tokens are a stride apart and whose heads are not."""
-    if hasattr(t, "shape") and (t.dim() != 3 or t.shape[0] < total or tuple(t.shape[1:]) != (heads, 128) or t.element_size() != 2
-                                or (total and t.stride()[1:] != (128, 1))):
-        raise RtpError(RTP_ERR_INVALID_ARG, f"{who}: {name} of 16 bits [{total} or more, {heads}, 128] expected, a token's rows contiguous")
+    if hasattr(t, "stride"):
+        n = t.shape
+        if len(n) != 3 or n[0] < total or n[1] != heads or n[2] != 128 or t.element_size() != 2 \
+                or (total and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != 128))):
+            raise RtpError(RTP_ERR_INVALID_ARG, f"{who}: {name} of 16 bits [{total} or more, {heads}, 128] expected, a token's rows contiguous")
 
 
 class rtp_page_map(C.Structure):
