@@ -95,8 +95,8 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(const ChunkArg
 
 RTP_CHUNK_KERNELS(chunk_attn_kernel, chunk_again_kernel, chunk_narrow_kernel, false)
 
-// rows: the most that a tile can have.
-static void launch_chunk_16(const ChunkArgs& a, unsigned grid, int rows, hipStream_t stream) {
+// rows: the most that a tile can have; few: no more units than compute units.
+static void launch_chunk_16(const ChunkArgs& a, unsigned grid, int rows, bool few, hipStream_t stream) {
   const bool narrow = rows <= kCkNarrowRows;
   RTP_CHUNK_LAUNCH(chunk_attn_kernel, chunk_again_kernel, chunk_narrow_kernel, false, false)
   RTP_CHUNK_LAUNCH(chunk_attn_kernel, chunk_again_kernel, chunk_narrow_kernel, true, false)
@@ -104,7 +104,7 @@ static void launch_chunk_16(const ChunkArgs& a, unsigned grid, int rows, hipStre
   RTP_CHUNK_LAUNCH(chunk_attn_kernel, chunk_again_kernel, chunk_narrow_kernel, true, true)
 }
 // attn_chunk_kv4.hip
-void launch_chunk_kv4(const ChunkArgs& a, unsigned grid, int rows, hipStream_t stream);
+void launch_chunk_kv4(const ChunkArgs& a, unsigned grid, int rows, bool few, hipStream_t stream);
 
 // Merges the ranges of the tiles that were cut (blockIdx.x: tile; blockIdx.y takes its rows in turn): SLICES groups of 32 lanes per row take the ranges
 // in turn, four at a time, a lane 4 of the 128 dims.
@@ -217,7 +217,9 @@ void serve(const rtp_layer_desc* L, const HeadTable& ht, int which, ChunkShape* 
   s->window = L->window;
 }
 
-constexpr int kUncutKeys = 1024;
+// Contexts up to here are not cut: a workgroup is through with them by the time that the results of ranges would be merged.  One call, whole and cut:
+// one token of 32 heads over 8 KV heads, 500 keys 10.9 and 11.2 us, 1000 keys 13.9 and 11.2; 512 tokens, 500 keys 25.9 and 27.6, 2000 keys 62 and 45.
+constexpr int kUncutKeys = 512;
 
 struct ChunkSizes {
   int64_t tiles;               // query tiles that the bounds allow
@@ -238,7 +240,7 @@ ChunkSizes chunk_sizes(const ChunkShape& s, int32_t B, int64_t total_q, int64_t 
   }
   const int widest = std::max(s.widest, 1);
   z.narrow = max_q * widest <= kCkNarrowRows;
-  // ranges of two key tiles and more, at most four per compute unit; contexts that a workgroup goes through in the time of a merge launch are not cut
+  // ranges of two key tiles and more, at most four per compute unit
   int64_t keys = max_ctx;
   if (s.local) keys = std::min<int64_t>(keys, (int64_t)s.sink + s.window + 64);
   const int64_t ranges = keys <= kUncutKeys ? 1 : std::min<int64_t>((keys + 2 * kCkK - 1) / (2 * kCkK), 289);
@@ -315,8 +317,9 @@ int32_t chunk_call(const char* who, int which, const rtp_layer_desc* layer, cons
   a.part_rows = z.part_rows;
   a.f16 = layer->kv_dtype == RTP_DTYPE_FP16;
   if (chunk->B > 64) RTP_LAUNCH(chunk_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a);
-  if (kv4) launch_chunk_kv4(a, (unsigned)grid, z.part_rows, stream);
-  else launch_chunk_16(a, (unsigned)grid, z.part_rows, stream);
+  const bool few = z.tiles + z.cap <= compute_units();
+  if (kv4) launch_chunk_kv4(a, (unsigned)grid, z.part_rows, few, stream);
+  else launch_chunk_16(a, (unsigned)grid, z.part_rows, few, stream);
   if (z.cap > 0) {
     // eight slices of the ranges where there are few rows (and many ranges, then), none where there are many; about 4096 workgroups at the most
     const int slices = (int64_t)chunk->total_q * a.shape.n_served <= 2048 ? 8 : z.part_rows <= 64 ? 2 : 1;

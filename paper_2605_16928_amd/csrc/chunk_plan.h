@@ -74,7 +74,8 @@ __host__ __device__ __forceinline__ int chunk_key_tiles(const ChunkShape& s, int
   }
   return chunk_max(1, chunk_min((int)(((uint32_t)keys + 63u) >> 6), kChunkMostKeyTiles));
 }
-// (Every launch of a call has to come to the same splits: whole numbers, single multiply-adds, and sums in the same order.  And it is code that
+// (Every launch of a call has to come to the same splits: whole numbers, multiply-adds where they are
+// written and nowhere else, and sums in the same order.  And it is code that
 // every workgroup goes through once, from memory: no wide division, no wide sums.)
 __host__ __device__ __forceinline__ uint32_t chunk_magic(int longest) { return 0xffffffffu / (uint32_t)longest; }
 __host__ __device__ __forceinline__ int chunk_splits(int key_tiles, int longest, int candidate, uint32_t magic) {
@@ -93,6 +94,7 @@ __host__ __device__ __forceinline__ float chunk_over(float x, float y) {      //
 #endif
 }
 __host__ __device__ __forceinline__ void chunk_sum(ChunkSums* sums, float tiles, float rows, float key_tiles, int splits, float per_place) {
+#pragma clang fp contract(off)
   const float S = (float)splits, cut = splits > 1 ? S : 0.f;
   sums->most = fmaxf(sums->most, ceilf(tiles * S * per_place - 0.001f) * (ceilf(chunk_over(key_tiles, S)) + (float)kChunkUnitCost));
   sums->units = fmaf(tiles, S, sums->units);
@@ -103,6 +105,7 @@ __host__ __device__ __forceinline__ void chunk_sum(ChunkSums* sums, float tiles,
 // comes on top, all of it where every unit has a place at once, half of it otherwise.  Units that differ fill up the places as they come, but for half
 // of the longest at the end.  A sequence's own units, which are alike, take whole rounds in any case.  And the partial results.
 __host__ __device__ __forceinline__ float chunk_cost(float work, const ChunkSums& sums, int longest, int candidate, float places) {
+#pragma clang fp contract(off)
   const float mean = ceilf(chunk_over(work, sums.units)), most = ceilf(chunk_over((float)longest, (float)candidate));
   const float rounds = ceilf(chunk_over(sums.units, places) - 0.001f);
   const float alike = fmaf(most > mean ? most - mean : 0.f, rounds > 1.f ? 0.5f : 1.f, rounds * (mean + (float)kChunkUnitCost));
