@@ -221,11 +221,17 @@ void serve(const rtp_layer_desc* L, const HeadTable& ht, int which, ChunkShape* 
 // one token of 32 heads over 8 KV heads, 500 keys 10.9 and 11.2 us, 1000 keys 13.9 and 11.2; 512 tokens, 500 keys 25.9 and 27.6, 2000 keys 62 and 45.
 constexpr int kUncutKeys = 512;
 
+// Up to this many rows of a KV head to a sequence, its tiles have 32 rows, whose waves need not wait for each other; two that read the same keys are
+// neighbours on a die and share its L2.  8 contexts of 8000, 64 over 8 heads, 8 new tokens (64 rows) 53 us and 61 as one tile, 12 tokens 90 and 64;
+// 30000 in 4 bits, 8 tokens 143 and 166, 16 tokens 260 and 185.
+constexpr int kFineRows = 64;
+
 struct ChunkSizes {
   int64_t tiles;               // query tiles that the bounds allow
   int64_t cap;                 // units of cut tiles
   int32_t part_rows;
   bool narrow;                 // no tile has more than 32 rows
+  int32_t fine;
   int64_t run;                 // units in a row on one die
   size_t plan_bytes, again_bytes, merge_bytes, part_bytes;
   size_t total() const { return plan_bytes + again_bytes + merge_bytes + part_bytes; }
@@ -233,26 +239,34 @@ struct ChunkSizes {
 ChunkSizes chunk_sizes(const ChunkShape& s, int32_t B, int64_t total_q, int64_t max_q, int64_t max_ctx) {
   ChunkSizes z = {};
   max_q = std::max<int64_t>(1, std::min(max_q, total_q));
+  const int widest = std::max(s.widest, 1);
+  z.narrow = max_q * widest <= kFineRows;
+  z.fine = z.narrow ? 3 : 0;
+  const int rows = kChunkRows >> z.fine;
   for (int k = 0; k < 4; ++k) {
     // a sequence of n tokens has ceil(n / tok) tiles: at most n of them, at most one more than its share
-    const int64_t tok = kChunkRows >> k, per_seq = (max_q + tok - 1) / tok;
+    const int64_t tok = rows >> k, per_seq = (max_q + tok - 1) / tok;
     z.tiles += s.count[k] * std::min(std::min(total_q, total_q / tok + B), per_seq * B);
   }
-  const int widest = std::max(s.widest, 1);
-  z.narrow = max_q * widest <= kCkNarrowRows;
   // ranges of two key tiles and more, at most four per compute unit
   int64_t keys = max_ctx;
   if (s.local) keys = std::min<int64_t>(keys, (int64_t)s.sink + s.window + 64);
   const int64_t ranges = keys <= kUncutKeys ? 1 : std::min<int64_t>((keys + 2 * kCkK - 1) / (2 * kCkK), 289);
   z.cap = ranges > 1 ? std::min<int64_t>(z.tiles * ranges, 4 * (int64_t)compute_units()) : 0;
-  z.part_rows = (int32_t)std::min<int64_t>(kChunkRows, max_q * widest);
+  z.part_rows = (int32_t)std::min<int64_t>(rows, max_q * widest);
   // (a run: the tiles of one sequence, about)
-  for (z.run = 1; z.run < 32 && z.run * 2 <= (max_q + kChunkRows / 8 - 1) / (kChunkRows / 8);) z.run *= 2;
+  for (z.run = 1; z.run < 32 && z.run * 2 <= (max_q + rows / 8 - 1) / (rows / 8);) z.run *= 2;
   z.again_bytes = z.narrow ? 0 : align_up((size_t)(z.tiles + z.cap + 8 * 32) * sizeof(int32_t), 256);
   z.plan_bytes = B > 64 ? align_up((size_t)(kPlanHead + 3 * ((int64_t)B + 1)) * sizeof(int32_t), 256) : 0;
   z.merge_bytes = z.cap > 0 ? align_up((size_t)z.tiles * sizeof(ChunkMerge), 256) : 0;
   z.part_bytes = align_up((size_t)z.cap * z.part_rows * kCkPart * sizeof(float), 256);
   return z;
+}
+
+// What a call needs, and every one with smaller bounds: finer tiles among them.
+size_t chunk_bytes(const ChunkShape& s, int32_t B, int64_t total_q, int64_t max_q, int64_t max_ctx) {
+  const size_t bytes = std::max<size_t>(256, chunk_sizes(s, B, total_q, max_q, max_ctx).total());
+  return std::max(bytes, chunk_sizes(s, B, total_q, std::min<int64_t>(max_q, kFineRows / std::max(s.widest, 1)), max_ctx).total());
 }
 
 size_t chunk_workspace(const rtp_layer_desc* layer, int which, int32_t B, int32_t total_q, int32_t max_q, int64_t max_ctx) {
@@ -262,7 +276,7 @@ size_t chunk_workspace(const rtp_layer_desc* layer, int which, int32_t B, int32_
     return 256;
   ChunkShape s = {};
   serve(layer, ht, which, &s);
-  return std::max<size_t>(256, chunk_sizes(s, B, total_q, max_q, max_ctx).total());
+  return chunk_bytes(s, B, total_q, max_q, max_ctx);
 }
 
 int32_t chunk_call(const char* who, int which, const rtp_layer_desc* layer, const void* q, int64_t q_stride, const rtp_kv_cache* c16,
@@ -289,14 +303,16 @@ int32_t chunk_call(const char* who, int which, const rtp_layer_desc* layer, cons
     return RTP_OK;
   }
   const ChunkSizes z = chunk_sizes(a.shape, chunk->B, chunk->total_q, chunk->max_q, chunk->max_ctx);
-  if (z.total() > 0 && (!ws || ((uintptr_t)ws & 255) || ws_bytes < z.total()))
-    return fail(RTP_ERR_WORKSPACE, "%s: workspace of %zu bytes, 256-byte aligned, needed", who, z.total());
+  const size_t bytes = chunk_bytes(a.shape, chunk->B, chunk->total_q, chunk->max_q, chunk->max_ctx);
+  if (!ws || ((uintptr_t)ws & 255) || ws_bytes < bytes)
+    return fail(RTP_ERR_WORKSPACE, "%s: workspace of %zu bytes, 256-byte aligned, needed", who, bytes);
   const int64_t grid = (z.tiles + z.cap + 8 * z.run - 1) / (8 * z.run) * (8 * z.run);
   if (grid > 0x7fffffff / kCkThreads) return fail(RTP_ERR_UNSUPPORTED, "%s: too many query tiles for one call", who);
   clear_error();
   a.shape.B = chunk->B;
   a.shape.total_q = chunk->total_q;
   a.shape.max_q = chunk->max_q;
+  a.shape.fine = z.fine;
   a.shape.cap = (int32_t)z.cap;
   a.shape.places = (float)(compute_units() * (kv4 && z.part_rows <= kCkSlimRows ? 3 : z.narrow ? 2 : 1));
   a.q = (const uint16_t*)q;

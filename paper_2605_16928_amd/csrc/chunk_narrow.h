@@ -160,7 +160,7 @@ struct ChunkNarrow {
   __device__ __forceinline__ ChunkNarrow(const ChunkArgs& a_, const ChunkTile& t_, unsigned char* smem_)
       : a(a_), t(t_), smem(smem_), mine(smem_ + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kCkBlockBytes), lane(threadIdx.x & 63),
         wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), g(lane >> 5), r(lane & 31), c(a_.scale_log2), rd(chunk_reads()),
-        sight(chunk_sight(a_.shape, t_, lane & 31)), blocks(a_, t_) {
+        sight(chunk_sight(a_.shape, t_, min(lane & 31, t_.rows - 1))), blocks(a_, t_) {
     const int row_c = min(r, t.rows - 1), rt = (row_c * t.over) >> 16;
     const uint16_t* src = a.q + (t.q0 + rt) * a.q_stride + chunk_head(a, t, row_c, rt) * kHeadDim + g * (KV4 ? 64 : 8);
 #pragma unroll
@@ -270,7 +270,7 @@ struct ChunkNarrow {
       seen = chunk_seen<LOCAL, KV4>(a, t, sight, n + 4 * g);
 #pragma unroll
       for (int i = 0; i < 16; ++i) S[i] = (seen >> i) & 1u ? S[i] : ninf;
-    } else if (!chunk_all_seen<LOCAL>(a.shape, t, t.m_lo, t.m_hi, n, 32) || t.rows < kCkNarrowRows) {
+    } else if (!chunk_all_seen<LOCAL>(a.shape, t, t.m_lo, t.m_hi, n, 32)) {
       chunk_mask<LOCAL>(sight, n + 4 * g, S);
     }
     float mx = fmaxf(S[0], S[1]);

@@ -2,7 +2,7 @@
 // Apart from the kernels so that it also compiles for the host.
 //
 // A KV head with h served query heads takes 256, 128, 64 or 32 tokens per query tile, the most whose rows are 256 or fewer; a tile's rows are
-// (token, head) pairs, the heads of a token side by side.  A tile's keys are cut into as many ranges as its sequence has splits; a unit is one range of one tile.  A sequence's units are
+// (token, head) pairs, the heads of a token side by side.  Where all sequences have few rows (`fine`), an eighth of that.  A tile's keys are cut into as many ranges as its sequence has splits; a unit is one range of one tile.  A sequence's units are
 // numbered (KV head, range, tile from the last to the first): those that read the same keys are neighbours.
 //
 // One number, the candidate, fixes all splits: sequence b has ceil(candidate * key tiles of b / key tiles of the longest), so that the
@@ -25,6 +25,7 @@ constexpr int kChunkUnitCost = 3, kChunkMergeCost = 4, kChunkRowsPerTile = 31;
 
 struct ChunkShape {
   int32_t B, total_q, max_q;
+  int32_t fine;                          // a query tile's tokens are halved so often
   int32_t group, n_kv;                   // query heads per KV head (1, 2, 4 or 8), KV heads
   int32_t local, sink, window;
   int32_t cap;                           // most units of tiles that are cut into ranges
@@ -63,7 +64,9 @@ __host__ __device__ __forceinline__ int chunk_candidate(int i) { return i < 32 ?
 
 // Query tiles of a sequence with n new tokens, over all KV heads.
 __host__ __device__ __forceinline__ int chunk_tiles(const ChunkShape& s, int n) {
-  return s.count[0] * chunk_query_tiles(n, 8) + s.count[1] * chunk_query_tiles(n, 7) + s.count[2] * chunk_query_tiles(n, 6) + s.count[3] * chunk_query_tiles(n, 5);
+  const int shift = 8 - s.fine;
+  return s.count[0] * chunk_query_tiles(n, shift) + s.count[1] * chunk_query_tiles(n, shift - 1) + s.count[2] * chunk_query_tiles(n, shift - 2) +
+         s.count[3] * chunk_query_tiles(n, shift - 3);
 }
 // 64-key tiles that one of its query tiles reads (a middling one).
 __host__ __device__ __forceinline__ int chunk_key_tiles(const ChunkShape& s, int n, int ctx) {
@@ -132,7 +135,7 @@ __host__ __device__ __forceinline__ ChunkUnit chunk_unit(const ChunkShape& s, in
   for (; u.kv < s.n_kv; ++u.kv) {
     u.heads = chunk_bits(chunk_members(s, u.kv));
     if (u.heads == 0) continue;
-    u.tiles = chunk_query_tiles(n, chunk_shift(u.heads));
+    u.tiles = chunk_query_tiles(n, chunk_shift(u.heads) - s.fine);
     if (r < u.tiles * S) break;
     r -= u.tiles * S;
     u.before += u.tiles;

@@ -39,7 +39,7 @@ struct ChunkSlim {
 
   __device__ __forceinline__ ChunkSlim(const ChunkArgs& a_, const ChunkTile& t_, unsigned char* smem_)
       : a(a_), t(t_), smem(smem_), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), g(lane >> 4), c(lane & 15),
-        mine(smem_ + wave * kCkSlimWave), scale(a_.scale_log2), sight(chunk_sight(a_.shape, t_, lane & 15)), blocks(a_, t_) {
+        mine(smem_ + wave * kCkSlimWave), scale(a_.scale_log2), sight(chunk_sight(a_.shape, t_, min(lane & 15, t_.rows - 1))), blocks(a_, t_) {
     const int row_c = min(c, t.rows - 1), rt = (row_c * t.over) >> 16;
     const uint16_t* src = a.q + (t.q0 + rt) * a.q_stride + chunk_head(a, t, row_c, rt) * kHeadDim + g * 32;
 #pragma unroll
@@ -71,7 +71,7 @@ struct ChunkSlim {
     }
     // ---- what the row does not see; the reference ----
     uint32_t seen = 0xffu;                                                  // bit 4 s + i: key n0 + 16 s + 4 g + i
-    if (CARE || !chunk_all_seen<LOCAL>(a.shape, t, t.m_lo, t.m_hi, n0, 32) || t.rows < kCkSlimRows) {
+    if (CARE || !chunk_all_seen<LOCAL>(a.shape, t, t.m_lo, t.m_hi, n0, 32)) {
       seen = 0;
 #pragma unroll
       for (int s = 0; s < 2; ++s) {

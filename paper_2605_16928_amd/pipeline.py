@@ -385,6 +385,24 @@ class Kv4DecodeRun(DecodeRun):
         rtp.rtp_dense_attn_kv4(self.desc, self.w.q, self.cache, self.ctx_len, self.B, self.max_ctx,
                                self.out if out is None else out, self.lse if lse is None else lse, self.ws_dense4)
 
+    def draft_attn(self, q, out=None, lse=None):
+        """Attention of the last T tokens of every context (a draft that grow() added), q [B, T, n_q_heads, 128], as a verification
+        needs it: the retrieval heads over every token up to their own, the others over the sink and the window."""
+        L, B = self.w.layer, self.B
+        if q.dim() != 4 or q.shape[0] != B or q.shape[1] < 1 or not q.is_contiguous():
+            raise rtp.RtpError(rtp.RTP_ERR_INVALID_ARG, f"Kv4DecodeRun: contiguous queries of {B} contexts expected")
+        T, q = q.shape[1], q.reshape(-1, *q.shape[2:])
+        out = torch.zeros_like(q) if out is None else out
+        lse = torch.zeros(q.shape[:2], dtype=torch.float32, device=DEV) if lse is None else lse
+        chunk = rtp.chunk_desc(torch.arange(0, B * T + 1, T, dtype=torch.int32, device=DEV), self.ctx_len, B * T, T, self.max_ctx)
+        if L.n_ret:
+            ws = ws_alloc(rtp.rtp_dense_attn_chunk_workspace_bytes(self.desc, B, B * T, T, self.max_ctx, rtp.RTP_HEADS_RETRIEVAL))
+            rtp.rtp_dense_attn_chunk_kv4(self.desc, q, q.stride(0), self.cache, chunk, rtp.RTP_HEADS_RETRIEVAL, out, lse, ws)
+        if L.n_ret < L.n_q_heads:
+            ws = ws_alloc(rtp.rtp_local_attn_chunk_workspace_bytes(self.desc, B, B * T, T, self.max_ctx))
+            rtp.rtp_local_attn_chunk_kv4(self.desc, q, q.stride(0), self.cache, chunk, out, lse, ws)
+        return out.view(B, T, *out.shape[1:]), lse.view(B, T, -1)
+
     # Selection and attention are two calls over this cache.  The base class's other forms would read the workload's 16-bit K and V.
     def step(self, fused: bool = False):
         """One decode step: index scores, top-p, attention over the 4-bit cache."""
@@ -457,3 +475,75 @@ class PrefillRun:
     def tile_stats(self):
         """(64-key tiles visited, tiles of plain causal attention) of the last sparse_prefill call with p < 1."""
         return rtp.rtp_sparse_attn_prefill_tile_stats(self.desc, self.w.T, self.w.chunk_start, self.ws)
+
+
+class ServeRun:
+    """One layer's attention in a server of `seqs` places: every step takes the new tokens of all places, packed -- a prompt's chunk beside
+    drafts and single tokens, none where a place waits --, hands out pages of a 16-bit cache, rotates the rows and appends them, and attends:
+    the retrieval heads over every token, the others over the sink and the window.  The host knows the lengths, so that a step that
+    lacks pages or room is refused before anything changes."""
+
+    def __init__(self, layer: wl.Layer, seqs: int, n_pages: int, page_size: int = 64, max_ctx: int = 32768, max_tokens: int = 4096,
+                 inv_freq=None, interleaved: bool = False):
+        """max_tokens: new tokens of a step, of all places together.  inv_freq: the rotation's frequencies (fp32, on the device); None: the
+        rows are stored as they come."""
+        H, dtype = layer.n_kv_heads, torch.float16 if layer.kv_dtype == "fp16" else torch.bfloat16
+        self.layer, self.desc, self.B = layer, layer_desc_of(layer), seqs
+        self.page_size, self.n_pages, self.max_ctx, self.max_tokens = page_size, n_pages, max_ctx, max_tokens
+        self.K, self.V = (torch.zeros((H, n_pages, page_size, 128), dtype=dtype, device=DEV) for _ in range(2))
+        self.page_table = torch.empty((seqs, -(-max_ctx // page_size)), dtype=torch.int32, device=DEV)
+        self.page_refs = torch.empty((n_pages,), dtype=torch.int32, device=DEV)
+        self.map = rtp.page_map(self.page_table, self.page_refs, page_size)
+        self.cache = rtp.kv_cache(self.K, self.V, self.page_table)
+        self.rope = None if inv_freq is None else rtp.rope_desc(inv_freq, interleaved)
+        self.q = torch.empty((max_tokens, layer.n_q_heads, 128), dtype=dtype, device=DEV)
+        self.out, self.lse = torch.zeros_like(self.q), torch.zeros((max_tokens, layer.n_q_heads), dtype=torch.float32, device=DEV)
+        self.copy_src, self.copy_dst = (torch.empty((max(seqs, n_pages),), dtype=torch.int32, device=DEV) for _ in range(2))
+        self.status = torch.zeros((2,), dtype=torch.int32, device=DEV)
+        self.ws_pages = ws_alloc(rtp.rtp_kv_pages_workspace_bytes(self.map, seqs))
+        self.ws_dense = ws_alloc(rtp.rtp_dense_attn_chunk_workspace_bytes(self.desc, seqs, max_tokens, max_tokens, max_ctx, rtp.RTP_HEADS_RETRIEVAL))
+        self.ws_local = ws_alloc(rtp.rtp_local_attn_chunk_workspace_bytes(self.desc, seqs, max_tokens, max_tokens, max_ctx))
+        self.ctx_len = [0] * seqs
+        rtp.rtp_kv_pages_init(self.map)
+
+    def _refuse(self, why):
+        raise rtp.RtpError(rtp.RTP_ERR_INVALID_ARG, f"ServeRun: {why}")
+
+    def pages(self, n):
+        return -(-n // self.page_size)
+
+    def step(self, q, k, v, new):
+        """new[b] tokens behind every place's context: rows q [total, n_q_heads, 128], k and v [total, n_kv_heads, 128] before rotation, packed in
+        the places' order; a token's rows contiguous, tokens a stride apart (slices of a fused projection).  (out, lse) of the new tokens,
+        until the next step."""
+        total, grown = sum(new), [n + c for n, c in zip(new, self.ctx_len)]
+        if len(new) != self.B or min(new) < 0 or total > self.max_tokens:
+            self._refuse(f"{self.B} counts of at most {self.max_tokens} tokens together expected")
+        if any(x.dim() != 3 or x.shape[0] != total for x in (q, k, v)):
+            self._refuse(f"rows of {total} tokens expected")
+        if max(grown) > self.max_ctx or sum(map(self.pages, grown)) > self.n_pages:
+            self._refuse("no room for these tokens")
+        if total == 0:
+            return self.out[:0], self.lse[:0]
+        at = [b for b in range(self.B) if new[b]]
+        rtp.rtp_kv_pages_extend(self.map, i32(at), i32([self.ctx_len[b] for b in at]), i32([grown[b] for b in at]), len(at), self.copy_src,
+                                self.copy_dst, self.status, self.ws_pages)     # (no page is shared: there is nothing to copy)
+        off = [0]
+        for n in new:
+            off.append(off[-1] + n)
+        chunk = rtp.chunk_desc(i32(off), i32(grown), total, max(new), max(grown))
+        rtp.rtp_kv_append(self.desc, self.cache, chunk, self.rope, q, q.stride(0), k, k.stride(0), v, v.stride(0), self.q, self.q.stride(0))
+        if self.layer.n_ret:
+            rtp.rtp_dense_attn_chunk(self.desc, self.q, self.q.stride(0), self.cache, chunk, rtp.RTP_HEADS_RETRIEVAL, self.out, self.lse, self.ws_dense)
+        if self.layer.n_ret < self.layer.n_q_heads:
+            rtp.rtp_local_attn_chunk(self.desc, self.q, self.q.stride(0), self.cache, chunk, self.out, self.lse, self.ws_local)
+        self.ctx_len = grown
+        return self.out[:total], self.lse[:total]
+
+    def truncate(self, keep):
+        """Every place keeps its first keep[b] tokens: the rejected ones of a draft go, or a conversation that has ended (0)."""
+        if len(keep) != self.B or min(keep) < 0:
+            self._refuse(f"{self.B} lengths expected")
+        keep = [min(n, k) for n, k in zip(self.ctx_len, keep)]
+        rtp.rtp_kv_pages_truncate(self.map, i32(range(self.B)), i32(keep), self.B)
+        self.ctx_len = keep
