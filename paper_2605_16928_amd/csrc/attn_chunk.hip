@@ -210,7 +210,7 @@ void serve(const rtp_layer_desc* L, const HeadTable& ht, int which, ChunkShape* 
       ++s->n_served;
     }
   for (int kv = 0; kv < s->n_kv; ++kv)
-    if (const int n = chunk_bits(chunk_members(*s, kv))) ++s->count[8 - chunk_shift(n)];
+    if (const int n = chunk_bits(chunk_members(*s, kv))) ++s->count[n - 1];
   for (int kv = 0; kv < s->n_kv; ++kv) s->widest = std::max(s->widest, chunk_bits(chunk_members(*s, kv)));
   s->local = which == kServeLocal;
   s->sink = L->sink;
@@ -243,9 +243,9 @@ ChunkSizes chunk_sizes(const ChunkShape& s, int32_t B, int64_t total_q, int64_t 
   z.narrow = max_q * widest <= kFineRows;
   z.fine = z.narrow ? 3 : 0;
   const int rows = kChunkRows >> z.fine;
-  for (int k = 0; k < 4; ++k) {
+  for (int k = 0; k < 8; ++k) {
     // a sequence of n tokens has ceil(n / tok) tiles: at most n of them, at most one more than its share
-    const int64_t tok = rows >> k, per_seq = (max_q + tok - 1) / tok;
+    const int64_t tok = rows / (k + 1), per_seq = (max_q + tok - 1) / tok;
     z.tiles += s.count[k] * std::min(std::min(total_q, total_q / tok + B), per_seq * B);
   }
   // ranges of two key tiles and more, at most four per compute unit
@@ -313,6 +313,7 @@ int32_t chunk_call(const char* who, int which, const rtp_layer_desc* layer, cons
   a.shape.total_q = chunk->total_q;
   a.shape.max_q = chunk->max_q;
   a.shape.fine = z.fine;
+  for (int h = 1; h <= 8; ++h) a.shape.per_tile[h - 1] = chunk_inverse(chunk_tokens(z.fine, h));
   a.shape.cap = (int32_t)z.cap;
   a.shape.places = (float)(compute_units() * (kv4 && z.part_rows <= kCkSlimRows ? 3 : z.narrow ? 2 : 1));
   a.q = (const uint16_t*)q;

@@ -1,9 +1,9 @@
 // How the attention of a batch of new tokens (attn_chunk.hip) is cut into units of work, from the lengths that only the device knows.
 // Apart from the kernels so that it also compiles for the host.
 //
-// A KV head with h served query heads takes 256, 128, 64 or 32 tokens per query tile, the most whose rows are 256 or fewer; a tile's rows are
-// (token, head) pairs, the heads of a token side by side.  Where all sequences have few rows (`fine`), an eighth of that.  A tile's keys are cut into as many ranges as its sequence has splits; a unit is one range of one tile.  A sequence's units are
-// numbered (KV head, range, tile from the last to the first): those that read the same keys are neighbours.
+// A KV head with h served query heads takes 256 / h tokens per query tile (an eighth of the rows where all sequences have few: `fine`); a tile's rows
+// are (token, head) pairs, the heads of a token side by side.  A tile's keys are cut into as many ranges as its sequence has splits; a unit is one
+// range of one tile.  A sequence's units are numbered (KV head, range, tile from the last to the first): those that read the same keys are neighbours.
 //
 // One number, the candidate, fixes all splits: sequence b has ceil(candidate * key tiles of b / key tiles of the longest), so that the
 // ranges of all sequences are about equally long.
@@ -25,22 +25,27 @@ constexpr int kChunkUnitCost = 3, kChunkMergeCost = 4, kChunkRowsPerTile = 31;
 
 struct ChunkShape {
   int32_t B, total_q, max_q;
-  int32_t fine;                          // a query tile's tokens are halved so often
+  int32_t fine;                          // a query tile's rows are halved so often
   int32_t group, n_kv;                   // query heads per KV head (1, 2, 4 or 8), KV heads
   int32_t local, sink, window;
   int32_t cap;                           // most units of tiles that are cut into ranges
   float places;                          // workgroups that run at the same time
   int32_t n_served, widest;              // served query heads; the most of one KV head
   uint32_t served[4];                    // bit h: query head h is one of them
-  int32_t count[4];                      // KV heads with 1, 2, 3 or 4, and 5 to 8 of them
+  int32_t count[8];                      // KV heads with 1 .. 8 of them
+  uint32_t per_tile[8];                  // 2^32 / tokens per tile of such a head, as chunk_inverse has it
 };
 
 __host__ __device__ __forceinline__ int chunk_min(int a, int b) { return a < b ? a : b; }
 __host__ __device__ __forceinline__ int chunk_max(int a, int b) { return a > b ? a : b; }
 
-// Tokens per query tile of a KV head with h served heads, as a power of two, and its query tiles for n new tokens.
-__host__ __device__ __forceinline__ int chunk_shift(int h) { return h > 1 ? __builtin_clz((unsigned)(h - 1)) - 24 : 8; }
-__host__ __device__ __forceinline__ int chunk_query_tiles(int n, int shift) { return (n + (1 << shift) - 1) >> shift; }
+// Tokens per query tile of a KV head with h served heads, and the number that multiplies in place of a division by them: n tokens, 1 .. 2^24, have
+// floor((n - 1) inverse / 2^32) + 1 tiles (the excess of the inverse, less than 1, times n - 1 stays below 2^32 / tokens).
+__host__ __device__ __forceinline__ int chunk_tokens(int fine, int h) { return (kChunkRows >> fine) / h; }
+__host__ __device__ __forceinline__ uint32_t chunk_inverse(int tokens) { return 0xffffffffu / (uint32_t)tokens + 1u; }
+__host__ __device__ __forceinline__ int chunk_query_tiles(int n, uint32_t inverse) {
+  return n > 0 ? (int)(((uint64_t)(uint32_t)(n - 1) * inverse) >> 32) + 1 : 0;
+}
 // The served heads of a KV head, as bits, and how many they are.
 __host__ __device__ __forceinline__ uint32_t chunk_members(const ChunkShape& s, int kv) {
   const int at = kv * s.group;
@@ -64,9 +69,10 @@ __host__ __device__ __forceinline__ int chunk_candidate(int i) { return i < 32 ?
 
 // Query tiles of a sequence with n new tokens, over all KV heads.
 __host__ __device__ __forceinline__ int chunk_tiles(const ChunkShape& s, int n) {
-  const int shift = 8 - s.fine;
-  return s.count[0] * chunk_query_tiles(n, shift) + s.count[1] * chunk_query_tiles(n, shift - 1) + s.count[2] * chunk_query_tiles(n, shift - 2) +
-         s.count[3] * chunk_query_tiles(n, shift - 3);
+  int tiles = 0;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) tiles += s.count[k] * ((int)(((uint64_t)(uint32_t)(n - 1) * s.per_tile[k]) >> 32) + 1);
+  return n > 0 ? tiles : 0;
 }
 // 64-key tiles that one of its query tiles reads (a middling one).
 __host__ __device__ __forceinline__ int chunk_key_tiles(const ChunkShape& s, int n, int ctx) {
@@ -135,7 +141,10 @@ __host__ __device__ __forceinline__ ChunkUnit chunk_unit(const ChunkShape& s, in
   for (; u.kv < s.n_kv; ++u.kv) {
     u.heads = chunk_bits(chunk_members(s, u.kv));
     if (u.heads == 0) continue;
-    u.tiles = chunk_query_tiles(n, chunk_shift(u.heads) - s.fine);
+    uint32_t inverse = s.per_tile[0];                                     // (scalars: nothing is looked up in memory)
+#pragma unroll
+    for (int k = 1; k < 8; ++k) inverse = u.heads == k + 1 ? s.per_tile[k] : inverse;
+    u.tiles = chunk_query_tiles(n, inverse);
     if (r < u.tiles * S) break;
     r -= u.tiles * S;
     u.before += u.tiles;

@@ -209,7 +209,7 @@ __device__ __forceinline__ bool chunk_tile(const ChunkArgs& a, int workgroup, Ch
   t->over = chunk_row_factor(u.heads);
   t->kvh = u.kv;
   t->members = (int)chunk_members(s, u.kv);
-  const int shift_q = chunk_shift(u.heads) - s.fine, t0 = u.tile << shift_q, tokens = min(1 << shift_q, spot.n - t0);
+  const int most = ((kChunkRows >> s.fine) * t->over) >> 16, t0 = u.tile * most, tokens = min(most, spot.n - t0);
   t->rows = tokens * t->nh;
   t->q0 = spot.q0 + t0;
   t->m_lo = spot.ctx - spot.n + t0;

@@ -18,13 +18,14 @@ static ChunkShape shape(const int* members, int n_kv, int group, int local, int 
     s.served[k * group / 32] |= (uint32_t)members[k] << (k * group % 32);
     const int n = chunk_bits(members[k]);
     s.n_served += n;
-    if (n) ++s.count[8 - chunk_shift(n)];
+    if (n) ++s.count[n - 1];
   }
+  for (int h = 1; h <= 8; ++h) s.per_tile[h - 1] = chunk_inverse(chunk_tokens(0, h));
   return s;
 }
 extern "C" void range_of(int n, int k, int S, int* out) { chunk_range(n, k, S, out, out + 1); }
-extern "C" int tiles_of(int n, int h) { return chunk_query_tiles(n, chunk_shift(h)); }
-extern "C" int tokens_of(int h) { return 1 << chunk_shift(h); }
+extern "C" int tiles_of(int n, int h, int fine) { return chunk_query_tiles(n, chunk_inverse(chunk_tokens(fine, h))); }
+extern "C" int tokens_of(int h, int fine) { return chunk_tokens(fine, h); }
 // The splits of every sequence; returns the units of cut tiles.
 extern "C" long plan(const int* members, int n_kv, int group, int local, int sink, int window, int cap, int places, int B, const int* n, const int* ctx,
                      int* splits, int* tiles) {
@@ -82,7 +83,7 @@ def ints(x):
     return (C.c_int * max(len(x), 1))(*x)
 
 
-TOKENS = [0, 256, 128, 64, 64, 32, 32, 32, 32]          # per tile, by the number of served heads
+TOKENS = [0, 256, 128, 85, 64, 51, 42, 36, 32]          # per tile, by the number of served heads
 MEMBERS = [([1], 1), ([15] * 8, 4), ([7, 15, 0, 13], 4), ([255], 8), ([1] * 16, 1), ([127, 31, 62, 3], 8), ([0, 2, 0, 1], 2)]
 
 
@@ -105,13 +106,14 @@ def test_every_unit_once(lib, members, group, n, S):
             assert [units[r + s * tiles[kv]] for s in range(S)] == [(kv, s, tile) for s in range(S)]
 
 
+@pytest.mark.parametrize("fine", [0, 3])
 @pytest.mark.parametrize("h", range(1, 9))
-def test_tiles(lib, h):
-    tok = TOKENS[h]
-    assert lib.tokens_of(h) == tok and h * tok <= 256 < 2 * h * tok
+def test_tiles(lib, h, fine):
+    tok, rows = TOKENS[h] if fine == 0 else 32 // h, 256 >> fine
+    assert lib.tokens_of(h, fine) == tok and h * tok <= rows < h * (tok + 1)
     rng = random.Random(h)
     for n in list(range(2000)) + [rng.randint(0, 1 << 24) for _ in range(5000)] + [(1 << 24) - k for k in range(600)] + [(1 << 24) // tok * tok + k for k in (-1, 0, 1)]:
-        assert lib.tiles_of(n, h) == -(-n // tok)
+        assert lib.tiles_of(n, h, fine) == -(-n // tok)
 
 
 def _plan(lib, heads, new, ctx, local=0, sink=4, window=64, cap=1024, places=256):
