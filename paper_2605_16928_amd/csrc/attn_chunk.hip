@@ -210,8 +210,11 @@ void serve(const rtp_layer_desc* L, const HeadTable& ht, int which, ChunkShape* 
       ++s->n_served;
     }
   for (int kv = 0; kv < s->n_kv; ++kv)
-    if (const int n = chunk_bits(chunk_members(*s, kv))) ++s->count[n - 1];
-  for (int kv = 0; kv < s->n_kv; ++kv) s->widest = std::max(s->widest, chunk_bits(chunk_members(*s, kv)));
+    if (const int n = chunk_bits(chunk_members(*s, kv))) {
+      ++s->count[n - 1];
+      ++s->kv_served;
+      s->widest = std::max(s->widest, n);
+    }
   s->local = which == kServeLocal;
   s->sink = L->sink;
   s->window = L->window;
@@ -254,8 +257,12 @@ ChunkSizes chunk_sizes(const ChunkShape& s, int32_t B, int64_t total_q, int64_t 
   const int64_t ranges = keys <= kUncutKeys ? 1 : std::min<int64_t>((keys + 2 * kCkK - 1) / (2 * kCkK), 289);
   z.cap = ranges > 1 ? std::min<int64_t>(z.tiles * ranges, 4 * (int64_t)compute_units()) : 0;
   z.part_rows = (int32_t)std::min<int64_t>(rows, max_q * widest);
-  // (a run: the tiles of one sequence, about)
-  for (z.run = 1; z.run < 32 && z.run * 2 <= (max_q + rows / 8 - 1) / (rows / 8);) z.run *= 2;
+  // so many runs that each die has two of a long sequence at least, one of long and one of short units; tiles of 32 rows are bound by the bytes
+  // of their keys, and those of a sequence stay together.  (Whole heads one after the other gave all long tiles to the same dies: a prompt of 8192
+  // tokens, 32 over 8 heads, 504 us and 712; 16384 behind 16384 5.5 and 7.0 ms; 16384 of 8 over 2 heads 486 and 779, without the turn 613.)
+  int64_t each = 0;
+  for (int k = 0; k < 8; ++k) each += s.count[k] * ((max_q + rows / (k + 1) - 1) / (rows / (k + 1)));
+  for (z.run = z.fine && max_q * widest > rows ? 2 : 1; z.run < 32 && z.run * 2 * 16 <= each;) z.run *= 2;
   z.again_bytes = z.narrow ? 0 : align_up((size_t)(z.tiles + z.cap + 8 * 32) * sizeof(int32_t), 256);
   z.plan_bytes = B > 64 ? align_up((size_t)(kPlanHead + 3 * ((int64_t)B + 1)) * sizeof(int32_t), 256) : 0;
   z.merge_bytes = z.cap > 0 ? align_up((size_t)z.tiles * sizeof(ChunkMerge), 256) : 0;
@@ -313,7 +320,10 @@ int32_t chunk_call(const char* who, int which, const rtp_layer_desc* layer, cons
   a.shape.total_q = chunk->total_q;
   a.shape.max_q = chunk->max_q;
   a.shape.fine = z.fine;
+  while ((1 << a.shape.run_shift) < z.run) ++a.shape.run_shift;
   for (int h = 1; h <= 8; ++h) a.shape.per_tile[h - 1] = chunk_inverse(chunk_tokens(z.fine, h));
+  for (int h = 8; h >= 1; --h)
+    if (a.shape.count[h - 1]) a.shape.per_most = a.shape.per_tile[h - 1];
   a.shape.cap = (int32_t)z.cap;
   a.shape.places = (float)(compute_units() * (kv4 && z.part_rows <= kCkSlimRows ? 3 : z.narrow ? 2 : 1));
   a.q = (const uint16_t*)q;
@@ -330,7 +340,6 @@ int32_t chunk_call(const char* who, int which, const rtp_layer_desc* layer, cons
   a.merge = z.cap > 0 ? (ChunkMerge*)((uint8_t*)ws + z.plan_bytes + z.again_bytes) : nullptr;
   a.n_merge = (int32_t)z.tiles;
   a.part = (float*)((uint8_t*)ws + z.plan_bytes + z.again_bytes + z.merge_bytes);
-  while ((1 << a.run_shift) < z.run) ++a.run_shift;
   a.part_rows = z.part_rows;
   a.f16 = layer->kv_dtype == RTP_DTYPE_FP16;
   if (chunk->B > 64) RTP_LAUNCH(chunk_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a);

@@ -3,7 +3,9 @@
 //
 // A KV head with h served query heads takes 256 / h tokens per query tile (an eighth of the rows where all sequences have few: `fine`); a tile's rows
 // are (token, head) pairs, the heads of a token side by side.  A tile's keys are cut into as many ranges as its sequence has splits; a unit is one
-// range of one tile.  A sequence's units are numbered (KV head, range, tile from the last to the first): those that read the same keys are neighbours.
+// range of one tile.  Units that read the same keys are neighbours, and long ones come before short ones: a sequence's units are numbered (group of
+// 2^run_shift tiles from the last to the first, KV head, range, tile from the last to the first), as far as every KV head has whole groups, and then
+// (KV head, range, tile) over the tiles that are left.
 //
 // One number, the candidate, fixes all splits: sequence b has ceil(candidate * key tiles of b / key tiles of the longest), so that the
 // ranges of all sequences are about equally long.
@@ -31,6 +33,8 @@ struct ChunkShape {
   int32_t cap;                           // most units of tiles that are cut into ranges
   float places;                          // workgroups that run at the same time
   int32_t n_served, widest;              // served query heads; the most of one KV head
+  int32_t kv_served, run_shift;          // KV heads with served heads; 2^run_shift units in a row go to one die
+  uint32_t per_most;                     // of the KV head with the fewest served heads: the largest tokens per tile
   uint32_t served[4];                    // bit h: query head h is one of them
   int32_t count[8];                      // KV heads with 1 .. 8 of them
   uint32_t per_tile[8];                  // 2^32 / tokens per tile of such a head, as chunk_inverse has it
@@ -134,10 +138,27 @@ struct ChunkUnit {
   int kv, heads;                         // KV head, its served heads
   int split, tile;
   int tiles, before;                     // query tiles of this KV head, and of those before it
+  int step;                              // from a tile's range to its next one, in units
 };
 // Unit r of a sequence with n new tokens and S splits.  Its tile is the (before + tiles - 1 - tile)-th of the sequence.
 __host__ __device__ __forceinline__ ChunkUnit chunk_unit(const ChunkShape& s, int n, int S, int r) {
-  ChunkUnit u = {0, 1, 0, 0, 1, 0};
+  ChunkUnit u = {0, 1, 0, 0, 1, 0, 1};
+  const int groups = chunk_query_tiles(n, s.per_most) >> s.run_shift, block = S << s.run_shift;
+  int grouped = 0, group = 0, nth = 0;                                    // tiles of a KV head in groups; the unit's group, its KV head
+  bool in_group = false;
+  if (groups > 1) {
+    grouped = groups << s.run_shift;
+    const int units = groups * block * s.kv_served;
+    in_group = r < units;
+    if (in_group) {
+      const int k = (int)((uint32_t)r / (uint32_t)block);
+      r -= k * block;
+      group = (int)((uint32_t)k / (uint32_t)s.kv_served);
+      nth = k - group * s.kv_served;
+    } else {
+      r -= units;
+    }
+  }
   for (; u.kv < s.n_kv; ++u.kv) {
     u.heads = chunk_bits(chunk_members(s, u.kv));
     if (u.heads == 0) continue;
@@ -145,12 +166,21 @@ __host__ __device__ __forceinline__ ChunkUnit chunk_unit(const ChunkShape& s, in
 #pragma unroll
     for (int k = 1; k < 8; ++k) inverse = u.heads == k + 1 ? s.per_tile[k] : inverse;
     u.tiles = chunk_query_tiles(n, inverse);
-    if (r < u.tiles * S) break;
-    r -= u.tiles * S;
+    const int mine = (u.tiles - grouped) * S;
+    if (in_group ? nth == 0 : r < mine) break;
+    r -= in_group ? 0 : mine;
+    --nth;
     u.before += u.tiles;
   }
-  u.split = (int)((uint32_t)r / (uint32_t)u.tiles);
-  u.tile = u.tiles - 1 - (r - u.split * u.tiles);
+  if (in_group) {
+    u.split = r >> s.run_shift;
+    u.tile = u.tiles - 1 - (group << s.run_shift) - (r & ((1 << s.run_shift) - 1));
+    u.step = 1 << s.run_shift;
+  } else {
+    u.step = u.tiles - grouped;
+    u.split = (int)((uint32_t)r / (uint32_t)u.step);
+    u.tile = u.step - 1 - (r - u.split * u.step);
+  }
   return u;
 }
 

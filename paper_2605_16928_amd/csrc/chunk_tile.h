@@ -30,7 +30,6 @@ struct ChunkArgs {
   float* lse;
   float* part;                 // [units of cut tiles, part_rows, kCkPart]
   int32_t part_rows;           // rows of a partial result: what a tile can have
-  int32_t run_shift;           // 2^run_shift units in a row go to one die
   struct ChunkMerge* merge;    // [n_merge]: the tiles, for the merge launch (NULL: nothing is cut)
   int32_t n_merge;
   int32_t* plan;               // B > 64: what chunk_plan_kernel leaves, kPlanHead ints and three lists of B + 1
@@ -193,12 +192,13 @@ __device__ __forceinline__ int chunk_head(const ChunkArgs& a, const ChunkTile& t
 }
 __device__ __forceinline__ int chunk_row_pos(const ChunkTile& t, int row) { return t.m_lo + ((row * t.over) >> 16); }
 
-// A workgroup's unit (false: there is none).  Workgroups are dealt to the eight dies in turn; 2^run_shift units in a row go to one die.
+// A workgroup's unit (false: there is none).  Workgroups are dealt to the eight dies in turn; 2^run_shift units in a row go to one die, and every
+// other deal goes the other way round, since what comes first is longer.
 template <bool LOCAL, bool KV4>
 __device__ __forceinline__ bool chunk_tile(const ChunkArgs& a, int workgroup, ChunkTile* t) {
   const ChunkShape& s = a.shape;
-  const int k8 = workgroup >> 3, in_run = k8 & ((1 << a.run_shift) - 1);
-  const ChunkSpot spot = chunk_find(a, ((((k8 >> a.run_shift) * 8 + (workgroup & 7)) << a.run_shift) + in_run));
+  const int k8 = workgroup >> 3, in_run = k8 & ((1 << s.run_shift) - 1), deal = k8 >> s.run_shift, die = (workgroup & 7) ^ ((deal & 1) * 7);
+  const ChunkSpot spot = chunk_find(a, ((deal * 8 + die) << s.run_shift) + in_run);
   if (spot.b < 0) {
     // (there are as many workgroups without a unit as there may be tiles that are not there)
     if (a.merge && threadIdx.x == 0 && spot.tile0 + spot.rel < a.n_merge) a.merge[spot.tile0 + spot.rel].rows = 0;
@@ -231,7 +231,7 @@ __device__ __forceinline__ bool chunk_tile(const ChunkArgs& a, int workgroup, Ch
   t->part = spot.part0 + spot.rel;
   if (a.merge && u.split == 0 && threadIdx.x == 0)
     a.merge[spot.tile0 + u.before + u.tiles - 1 - u.tile] =
-        ChunkMerge{spot.splits > 1 ? t->rows : 0, spot.splits, t->part, u.tiles, u.heads, t->members, u.kv, (int)t->q0};
+        ChunkMerge{spot.splits > 1 ? t->rows : 0, spot.splits, t->part, u.step, u.heads, t->members, u.kv, (int)t->q0};
   // (the same in every lane, which the compiler does not see everywhere)
   int* const whole[] = {&t->nh, &t->over, &t->kvh, &t->members, &t->rows, &t->m_lo, &t->m_hi, &t->kend, &t->sink_tiles, &t->gap, &t->it_lo, &t->it_hi,
                         &t->splits, &t->part};

@@ -18,9 +18,10 @@ static ChunkShape shape(const int* members, int n_kv, int group, int local, int 
     s.served[k * group / 32] |= (uint32_t)members[k] << (k * group % 32);
     const int n = chunk_bits(members[k]);
     s.n_served += n;
-    if (n) ++s.count[n - 1];
+    if (n) { ++s.count[n - 1]; ++s.kv_served; }
   }
   for (int h = 1; h <= 8; ++h) s.per_tile[h - 1] = chunk_inverse(chunk_tokens(0, h));
+  for (int h = 8; h >= 1; --h) if (s.count[h - 1]) s.per_most = s.per_tile[h - 1];
   return s;
 }
 extern "C" void range_of(int n, int k, int S, int* out) { chunk_range(n, k, S, out, out + 1); }
@@ -57,10 +58,11 @@ extern "C" long plan(const int* members, int n_kv, int group, int local, int sin
   }
   return cut;
 }
-extern "C" void unit(const int* members, int n_kv, int group, int n, int S, int r, int* out) {
-  const ChunkShape s = shape(members, n_kv, group, 0, 0, 0, 0, 1);
+extern "C" void unit(const int* members, int n_kv, int group, int n, int S, int r, int run_shift, int* out) {
+  ChunkShape s = shape(members, n_kv, group, 0, 0, 0, 0, 1);
+  s.run_shift = run_shift;
   const ChunkUnit u = chunk_unit(s, n, S, r);
-  out[0] = u.kv; out[1] = u.split; out[2] = u.tile; out[3] = u.heads; out[4] = u.tiles; out[5] = u.before;
+  out[0] = u.kv; out[1] = u.split; out[2] = u.tile; out[3] = u.heads; out[4] = u.tiles; out[5] = u.before; out[6] = u.step;
 }
 """
 
@@ -89,21 +91,30 @@ MEMBERS = [([1], 1), ([15] * 8, 4), ([7, 15, 0, 13], 4), ([255], 8), ([1] * 16, 
 
 @pytest.mark.parametrize("members,group", MEMBERS)
 @pytest.mark.parametrize("n,S", [(1, 1), (1, 7), (31, 2), (32, 3), (33, 1), (300, 5), (5000, 1)])
-def test_every_unit_once(lib, members, group, n, S):
+@pytest.mark.parametrize("run_shift", [0, 1, 4])
+def test_every_unit_once(lib, members, group, n, S, run_shift):
     heads = [bin(m).count("1") for m in members]
     tiles = [-(-n // TOKENS[h]) if h else 0 for h in heads]
-    units, numbers, out = [], set(), (C.c_int * 6)()
+    units, steps, numbers, out = [], [], set(), (C.c_int * 7)()
     for r in range(sum(tiles) * S):
-        lib.unit(ints(members), len(members), group, n, S, r, out)
-        kv, split, tile, h, mine, before = out
+        lib.unit(ints(members), len(members), group, n, S, r, run_shift, out)
+        kv, split, tile, h, mine, before, step = out
         assert 0 <= split < S and 0 <= tile < tiles[kv] and h == heads[kv] and mine == tiles[kv] and before == sum(tiles[:kv])
         units.append((kv, split, tile))
-        if split == 0:                                  # the ranges of a tile are `tiles` units apart; every tile has a number of its own
+        steps.append(step)
+        if split == 0:                                  # every tile has a number of its own
             numbers.add(before + mine - 1 - tile)
     assert len(set(units)) == sum(tiles) * S and numbers == set(range(sum(tiles)))
     for r, (kv, split, tile) in enumerate(units):
-        if split == 0:
-            assert [units[r + s * tiles[kv]] for s in range(S)] == [(kv, s, tile) for s in range(S)]
+        if split == 0:                                  # the ranges of a tile are as far apart as the unit says
+            assert [units[r + s * steps[r]] for s in range(S)] == [(kv, s, tile) for s in range(S)]
+    groups = min(t for t in tiles if t) >> run_shift    # whole groups: those of later tiles first, of every KV head in turn
+    if groups > 1:
+        block, served = S << run_shift, [kv for kv, t in enumerate(tiles) if t]
+        for j in range(groups * len(served)):
+            g, kv = j // len(served), served[j % len(served)]
+            mine = {(kv, s, tiles[kv] - 1 - (g << run_shift) - k) for s in range(S) for k in range(1 << run_shift)}
+            assert set(units[j * block:(j + 1) * block]) == mine
 
 
 @pytest.mark.parametrize("fine", [0, 3])
