@@ -216,8 +216,8 @@ void serve(const rtp_layer_desc* L, const HeadTable& ht, int which, ChunkShape* 
       s->widest = std::max(s->widest, n);
     }
   s->local = which == kServeLocal;
-  s->sink = L->sink;
-  s->window = L->window;
+  s->sink = std::min(L->sink, kMostContext);           // (as good as any larger: no position is behind it, and sums of two stay in 32 bits)
+  s->window = std::min(L->window, kMostContext);
 }
 
 // Contexts up to here are not cut: a workgroup is through with them by the time that the results of ranges would be merged.  One call, whole and cut:

@@ -19,6 +19,7 @@
 namespace rtp {
 
 constexpr int kChunkRows = 256;          // rows of a query tile
+constexpr int kMostContext = 1 << 30;
 constexpr int kChunkMostKeyTiles = 1 << 22;
 constexpr int kChunkCandidates = 64;
 // What a unit costs beside its key tiles, in key tiles: its way to the first product and from the last; a launch's, that results are merged; and

@@ -57,7 +57,7 @@ __device__ __forceinline__ ChunkLane chunk_lane(const ChunkArgs& a, int b) {
     const NewTokens nt = new_tokens(a.q_offset, b, a.shape.total_q, a.shape.max_q);
     s.n = nt.n;
     s.q0 = nt.q0;
-    s.ctx = max(a.ctx_len[b], 0);
+    s.ctx = min(max(a.ctx_len[b], 0), kMostContext);
     s.tiles = chunk_tiles(a.shape, nt.n);
     s.key_tiles = nt.n > 0 ? chunk_key_tiles(a.shape, nt.n, s.ctx) : 1;
   }
@@ -205,6 +205,7 @@ __device__ __forceinline__ bool chunk_tile(const ChunkArgs& a, int workgroup, Ch
     return false;
   }
   const ChunkUnit u = chunk_unit(s, spot.n, spot.splits, spot.rel);
+  if (u.kv >= s.n_kv) return false;                                    // (offsets that do not ascend)
   t->nh = u.heads;
   t->over = chunk_row_factor(u.heads);
   t->kvh = u.kv;
@@ -223,14 +224,15 @@ __device__ __forceinline__ bool chunk_tile(const ChunkArgs& a, int workgroup, Ch
   t->sink_tiles = t->gap = 0;
   if (LOCAL) {
     t->sink_tiles = (min(s.sink, t->kend) + kCkK - 1) / kCkK;
-    t->gap = max((s.window > 0 ? max(t->m_lo - s.window + 1, 0) / kCkK : all) - t->sink_tiles, 0);
+    t->gap = max((s.window > 0 ? min(max(t->m_lo - s.window + 1, 0) / kCkK, all) : all) - t->sink_tiles, 0);      // (kend may end before the band)
   }
   const int n_tiles = all - t->gap;
   chunk_range(n_tiles, u.split, spot.splits, &t->it_lo, &t->it_hi);
   t->splits = spot.splits;
   t->part = spot.part0 + spot.rel;
-  if (a.merge && u.split == 0 && threadIdx.x == 0)
-    a.merge[spot.tile0 + u.before + u.tiles - 1 - u.tile] =
+  const int number = spot.tile0 + u.before + u.tiles - 1 - u.tile;
+  if (a.merge && u.split == 0 && threadIdx.x == 0 && number < a.n_merge)
+    a.merge[number] =
         ChunkMerge{spot.splits > 1 ? t->rows : 0, spot.splits, t->part, u.step, u.heads, t->members, u.kv, (int)t->q0};
   // (the same in every lane, which the compiler does not see everywhere)
   int* const whole[] = {&t->nh, &t->over, &t->kvh, &t->members, &t->rows, &t->m_lo, &t->m_hi, &t->kend, &t->sink_tiles, &t->gap, &t->it_lo, &t->it_hi,

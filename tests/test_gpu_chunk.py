@@ -174,6 +174,29 @@ def test_positions_before_the_first_and_behind_the_table():
     check(b, want, out, lse, MARK)
 
 
+@pytest.mark.parametrize("cache", ["16", "4"])
+@pytest.mark.parametrize("new", [3, 40])
+@pytest.mark.parametrize("sink,window", [(0, 8), (4, 16), (20, 200), (40, 0)])
+def test_windows_behind_the_end_of_the_table(sink, window, new, cache):
+    """Contexts that are longer than the table: what it does not hold is left out, and a band that lies behind it is empty."""
+    b = Batch(new=[new, 1], past=[300, 500], seed=12, cache=cache)
+    q, c, chunk = b.device()
+    c.pt_stride, chunk.max_ctx = 2, 32
+    b.table = b.table.flatten()[:4].view(2, 2)
+    out, lse, want = run(b, "local", sink=sink, window=window, prepared=(q, c, chunk))
+    check(b, want, out, lse, MARK)
+
+
+@pytest.mark.parametrize("cache", ["16", "4"])
+@pytest.mark.parametrize("new", [7, 40])
+def test_the_largest_sinks_and_windows(new, cache):
+    most = 2 ** 31 - 1
+    b = Batch(new=[new, 1, 2], past=None, ctx=[new - 3, 700, 150], seed=13, cache=cache)       # (three rows have no position)
+    for sink, window in ((0, most), (most, 0), (most, most)):
+        out, lse, want = run(b, "local", sink=sink, window=window)
+        check(b, want, out, lse, MARK)
+
+
 def test_bounds_may_be_larger_than_what_is_there():
     b = Batch(new=[6, 1, 0], past=[70, 300, 9], seed=10)
     q, cache, chunk = b.device()
