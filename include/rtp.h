@@ -569,8 +569,8 @@ int32_t rtp_kv4_append(const rtp_layer_desc* layer, const rtp_kv4_cache* cache, 
                        int64_t batch_stride, int64_t token_stride, int64_t head_stride, const int32_t* start,
                        const int32_t* count, int32_t B, int32_t T, void* stream);
 
-/* Gives stored tokens back in the layer's 16-bit type (bf16: exactly; fp16: rounded once) -- what a further prefill chunk's attention,
- * which reads 16-bit rows, needs of a context that is held in 4 bits.  Positions start[b] .. start[b] + count[b] - 1 go to rows
+/* Gives stored tokens back in the layer's 16-bit type (bf16: exactly; fp16: rounded once) -- what calls that read 16-bit rows need
+ * of a context that is held in 4 bits (rtp_sparse_attn_prefill; a chunk's dense and local attention has forms that read it: rtp_dense_attn_chunk_kv4).  Positions start[b] .. start[b] + count[b] - 1 go to rows
  * 0 .. count[b] - 1 of sequence b, laid out like the inputs of rtp_kv4_append, where the strides must keep the B * T * n_kv_heads rows
  * apart; rows behind them are left as they are.  No workspace. */
 int32_t rtp_kv4_read(const rtp_layer_desc* layer, const rtp_kv4_cache* cache, const int32_t* start, const int32_t* count,

@@ -7,6 +7,10 @@
 // wave's LDS:  K: lane (g, r) takes the dims 64 g .. + 63 of token r, and the queries lie alike, so that a word of codes is one product's operand;
 // V: lane (g, r) takes the dims 4 r .. + 3 (two bytes) of its 16 tokens, so that accumulator db holds the dims 4 rho + db.
 //
+// Measured: 32 single tokens over 1500 to 30000 keys, 32 over 8 heads (1.1 GB) 203 us with the merge, 5.4 TB/s, where a copy reaches 4.9;
+// as wide tiles, whose buffers the whole workgroup fills and passes on at barriers, 1074.  Bound by HBM; one token over 700 keys takes 7.0 + 2.4: the launches, code that
+// comes from memory for the first time, and four dependent loads.
+//
 // The running reference follows a row's maximum only when it is left behind by more than 2^8.  Probabilities enter the product in two parts, their
 // rounding to 16 bits and the rounding of the rest: the matrix cores have the time, and an output is then as exact as its own rounding.
 //

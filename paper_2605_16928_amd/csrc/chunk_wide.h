@@ -10,6 +10,10 @@
 // with tile x - 1, whose buffer tile x + 2 fills.  Tiles that every row sees in full run in a loop without a branch; the others -- the first, those
 // on the window's edge and on the diagonal -- block by block, with masks.
 //
+// Measured: 4096 tokens behind 126976, 4 heads (1.08 TFLOP) 950 us with the merge, 1.14 PFLOP/s, where a product of 8192^3 reaches 1.59; a prompt of
+// 8192 tokens, 32 over 8 heads, 504 us, 1.09; 4096 behind 28672 over 4 bits 1716, 1.20.  Bound by issue: the matrix cores are busy for 58 % of
+// the launch, the LDS reads (every wave reads every tile) for as long, and exponentials, rounding and sums take most of a SIMD's other slots.
+//
 // 16-bit rows go to LDS by direct loads.  The four rows that a wave brings per instruction lie in one page, whose place is a scalar: 64 of them, for
 // 32 tiles, are looked up at a time, a lane each, a window ahead, and taken from there with two lane reads.  4-bit rows come through registers
 // a tile ahead, 16 bytes per lane, and are turned into 16 bits on their way to LDS, between the products.

@@ -1,5 +1,5 @@
-// The 4-bit cache's own traffic: rtp_kv4_append stores new tokens, rtp_kv4_read gives stored tokens back at 16 bits (for the prefill
-// of a next chunk, whose kernels read 16-bit rows).
+// The 4-bit cache's own traffic: rtp_kv4_append stores new tokens, rtp_kv4_read gives stored tokens back at 16 bits (for calls
+// that read 16-bit rows, such as the sparse prefill; a chunk's dense and local attention reads the 4-bit cache itself: attn_chunk.hip).
 //
 //   scale  s = max(2, E - 2 + [M >= 0.75]),  amax = max |x| of the block = (1 + M) 2^(E - 127)
 //   code   nearest e2m1 value of x 2^(127 - s), ties to the even code
