@@ -145,6 +145,19 @@ __device__ __forceinline__ void chunk_put_records(unsigned char* mine, const Cod
   *reinterpret_cast<uint32_t*>(mine + kCkScalesAt + lane * 4) = x.scales;
   chunk_wave_fence();
 }
+// Blocks of this scale and above may hold values that are infinite in 16 bits: 4 or 6 times it (fp16: 2^16, the largest is 65504; bf16: 2^128).
+template <bool F16>
+constexpr float kKv4Large = F16 ? 0x1p14f : 0x1p126f;
+// Scale of a block of token n's V; infinite: the block is not a number.
+__device__ __forceinline__ float chunk_value_scale(const unsigned char* mine, int n, int block) {
+  return __uint_as_float((uint32_t)mine[kCkScalesAt + (n >> 2) * kKv4Group + 16 + block * 4 + (n & 3)] << 23);
+}
+// Token n (the same for the whole wave) has such a block that is a number.
+template <bool F16>
+__device__ __forceinline__ bool chunk_large(const unsigned char* mine, int n) {
+  const float f = chunk_value_scale(mine, n, threadIdx.x & 3);
+  return __ballot(f >= kKv4Large<F16> && f < __builtin_huge_valf()) != 0ull;
+}
 
 template <bool F16, bool LOCAL, bool KV4, int NW, bool CARE>
 struct ChunkNarrow {
@@ -223,9 +236,9 @@ struct ChunkNarrow {
         const uint32_t x = *reinterpret_cast<const uint16_t*>(mine + chunk_record_at(n, 4 + (r >> 3)) + (r & 7) * 2);
         const uint32_t y = *reinterpret_cast<const uint16_t*>(mine + chunk_record_at(n + 1, 4 + (r >> 3)) + (r & 7) * 2);
         float fx = kv4_scale(sc, j), fy = kv4_scale(sc, j + 1);
-        if constexpr (CARE) {                                               // (not_numbers() has the blocks that are none)
-          fx = fx < __builtin_huge_valf() ? fx : 0.f;
-          fy = fy < __builtin_huge_valf() ? fy : 0.f;
+        if constexpr (CARE) {                                               // (large_values() and not_numbers() have these blocks)
+          fx = fx < kKv4Large<F16> ? fx : 0.f;
+          fy = fy < kKv4Large<F16> ? fy : 0.f;
         }
         const int w = 2 * e + (j >> 1);
         if constexpr (F16) {
@@ -249,6 +262,26 @@ struct ChunkNarrow {
     }
   }
 
+  // The blocks of V that may hold infinities, token by token and over the seen ones alone.
+  __device__ __forceinline__ void large_values(uint32_t seen, const uint32_t (&P)[8], const uint32_t (&R)[8]) {
+    const uint32_t seen_other = (uint32_t)__shfl_xor((int)seen, 32);
+#pragma unroll 1
+    for (int k = 0; k < 32; ++k) {                                          // key 8 (i / 4) + 4 half + i % 4
+      const int i = k >> 1, half = k & 1, n = 8 * (i >> 2) + 4 * half + (i & 3);
+      if (!chunk_large<F16>(mine, n)) continue;
+      const float p_own = chunk_probability<F16>(P, R, i), p_other = __shfl_xor(p_own, 32), p = half == g ? p_own : p_other;
+      const bool ok = ((half == g ? seen : seen_other) >> i) & 1u;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {                                        // dims 4 rho .. + 3
+        const int rho = 8 * (e >> 2) + 4 * g + (e & 3);
+        const float f = chunk_value_scale(mine, n, rho >> 3);
+        const u32x4 v = decode8<F16>(*reinterpret_cast<const uint16_t*>(mine + chunk_record_at(n, 4 + (rho >> 3)) + (rho & 7) * 2), f);
+        const float x[4] = {lo16<F16>(v[0]), hi16<F16>(v[0]), lo16<F16>(v[1]), hi16<F16>(v[1])};
+#pragma unroll
+        for (int db = 0; db < 4; ++db) O[db][e] = ok && f >= kKv4Large<F16> && f < __builtin_huge_valf() ? fmaf(p, x[db], O[db][e]) : O[db][e];
+      }
+    }
+  }
   // Rows that see a token whose V has a block that is not a number have none there either.
   __device__ __forceinline__ void not_numbers(uint32_t seen) {
     uint32_t hit = 0;                                                       // bit: block of 32 dims
@@ -336,10 +369,7 @@ struct ChunkNarrow {
 #pragma unroll
         for (int e = 0; e < 8; ++e) any |= chunk_not_finite<F16>(chunk_read_v(mine + kCkBlockBytes / 2, rd, e >> 2, e & 3));
         odd = __ballot(any != 0u) != 0ull;
-        if (odd) {
-          chunk_pv_seen<F16>(mine + kCkBlockBytes / 2, seen, P, O);
-          chunk_pv_seen<F16>(mine + kCkBlockBytes / 2, seen, R, O);
-        }
+        if (odd) chunk_pv_seen<F16>(mine + kCkBlockBytes / 2, seen, P, R, O);
       }
 #pragma unroll
       for (int tt = 0; tt < 2 && !odd; ++tt) {
@@ -382,7 +412,10 @@ struct ChunkNarrow {
         values4(tt, v);
         pv(v, tt, P, R);
       }
-      if constexpr (CARE) not_numbers(seen);
+      if constexpr (CARE) {
+        large_values(seen, P, R);
+        not_numbers(seen);
+      }
     };
     while (at[0] < blocks.count) {
       step(x[0], at[0], at[1]);

@@ -111,7 +111,7 @@ struct ChunkSlim {
         R[2 * s + (i >> 1)] = pack16<F16>(p0 - lo16<F16>(w), p1 - hi16<F16>(w));
       }
     // ---- V: 8 tokens x 8 dims ----
-    uint32_t v[2][4], vs[2], none = 0;
+    uint32_t v[2][4], vs[2];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       vs[s] = *reinterpret_cast<const uint32_t*>(sc + (4 * s + g) * kKv4Group + 16 + (c >> 2) * 4);
@@ -124,7 +124,7 @@ struct ChunkSlim {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         f[s][i] = kv4_scale(vs[s], i);
-        if constexpr (CARE) f[s][i] = f[s][i] < __builtin_huge_valf() ? f[s][i] : 0.f;
+        if constexpr (CARE) f[s][i] = f[s][i] < kKv4Large<F16> ? f[s][i] : 0.f;
       }
 #define RTP_SLIM_PV(B)                                                                                                                \
   {                                                                                                                                   \
@@ -153,6 +153,27 @@ struct ChunkSlim {
     RTP_SLIM_PV(3)
 #undef RTP_SLIM_PV
     if constexpr (CARE) {
+      // the blocks of V that may hold infinities, token by token and over the seen ones alone: dims 32 g + 8 e + n, block g
+#pragma unroll 1
+      for (int k = 0; k < 32; ++k) {                                        // key 16 s + 4 (from's g) + i
+        if (!chunk_large<F16>(mine, k)) continue;
+        const int i = k & 3, own = 4 * (k >> 4) + i, from = ((k >> 2) & 3) * 16 + c;
+        uint32_t w = P[0], x = R[0];
+#pragma unroll
+        for (int e = 1; e < 4; ++e) {
+          w = e == (own >> 1) ? P[e] : w;
+          x = e == (own >> 1) ? R[e] : x;
+        }
+        const float p = __shfl((i & 1) ? hi16<F16>(w) + hi16<F16>(x) : lo16<F16>(w) + lo16<F16>(x), from);
+        const float f_own = chunk_value_scale(mine, k, g);
+        const bool ok = (((uint32_t)__shfl((int)seen, from) >> own) & 1u) && f_own >= kKv4Large<F16> && f_own < __builtin_huge_valf();
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const u32x4 y = decode8<F16>(*reinterpret_cast<const uint32_t*>(mine + chunk_record_at(k, 4 + g) + e * 4), f_own);
+#pragma unroll
+          for (int n = 0; n < 8; ++n) O[n][e] = ok ? fmaf(p, (n & 1) ? hi16<F16>(y[n >> 1]) : lo16<F16>(y[n >> 1]), O[n][e]) : O[n][e];
+        }
+      }
       // rows that see a token whose V has a block that is not a number have none there either: dims 32 g + 8 i + n, block g
       uint32_t hit = 0;                                                     // of the lane's own tokens, bit: block
 #pragma unroll
@@ -169,7 +190,6 @@ struct ChunkSlim {
 #pragma unroll
         for (int i = 0; i < 4; ++i) O[n][i] = (hit >> g) & 1u ? __builtin_nanf("") : O[n][i];
     }
-    (void)none;
   }
 
   // true: a page was not there or a result is not finite (never with CARE)

@@ -342,10 +342,21 @@ __device__ __forceinline__ uint32_t chunk_not_finite(const u32x4 v) {      // no
   for (int w = 0; w < 4; ++w) any |= ((v[w] & kExp) + kOne) & 0x80008000u;
   return any;
 }
-// O^T += V^T P^T over the seen keys alone, one by one: a key that a row does not see has probability 0, and 0 times a value that is not
-// finite would not be 0.  seen: bit i = the lane's i-th key, 8 (i / 4) + 4 g + i % 4.
+// A lane's i-th probability of a block: its rounding P, and the rounding of the rest R.
 template <bool F16>
-__device__ __forceinline__ void chunk_pv_seen(const unsigned char* v_rows, uint32_t seen, const uint32_t (&P)[8], f32x16 (&O)[4]) {
+__device__ __forceinline__ float chunk_probability(const uint32_t (&P)[8], const uint32_t (&R)[8], int i) {      // the lane's i-th
+  uint32_t w = P[0], x = R[0];
+#pragma unroll
+  for (int e = 1; e < 8; ++e) {
+    w = e == (i >> 1) ? P[e] : w;
+    x = e == (i >> 1) ? R[e] : x;
+  }
+  return (i & 1) ? hi16<F16>(w) + hi16<F16>(x) : lo16<F16>(w) + lo16<F16>(x);
+}
+// O^T += V^T (P + R)^T over the seen keys alone, one by one: a key that a row does not see has probability 0, and 0 times a value that is not
+// finite would not be 0; nor would R, which is 0 where P is exact.  seen: bit i = the lane's i-th key, 8 (i / 4) + 4 g + i % 4.
+template <bool F16>
+__device__ __forceinline__ void chunk_pv_seen(const unsigned char* v_rows, uint32_t seen, const uint32_t (&P)[8], const uint32_t (&R)[8], f32x16 (&O)[4]) {
   const int g = (threadIdx.x & 63) >> 5;
   const uint32_t seen_other = (uint32_t)__shfl_xor((int)seen, 32);
 #pragma unroll
@@ -353,10 +364,7 @@ __device__ __forceinline__ void chunk_pv_seen(const unsigned char* v_rows, uint3
 #pragma unroll 1
     for (int k = 0; k < 32; ++k) {                                         // key 8 (i / 4) + 4 half + i % 4
       const int i = k >> 1, half = k & 1, n = 8 * (i >> 2) + 4 * half + (i & 3);
-      uint32_t w = P[0];
-#pragma unroll
-      for (int e = 1; e < 8; ++e) w = e == (i >> 1) ? P[e] : w;
-      const float p_own = (i & 1) ? hi16<F16>(w) : lo16<F16>(w), p_other = __shfl_xor(p_own, 32), p = half == g ? p_own : p_other;
+      const float p_own = chunk_probability<F16>(P, R, i), p_other = __shfl_xor(p_own, 32), p = half == g ? p_own : p_other;
       const bool ok = ((half == g ? seen : seen_other) >> i) & 1u;
 #pragma unroll
       for (int i4 = 0; i4 < 4; ++i4) {

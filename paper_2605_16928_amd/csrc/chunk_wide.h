@@ -440,6 +440,7 @@ struct ChunkWide {
     const float ninf = -__builtin_huge_valf();
     f32x16 S;
     uint32_t P[8];
+    const uint32_t none[8] = {};
     clear();
     m = ninf;
     __syncthreads();
@@ -488,7 +489,7 @@ struct ChunkWide {
           for (int k = 0; k < 8; ++k) odd |= chunk_not_finite<F16>(chunk_read_v(v_rows, rd, k >> 2, k & 3));
         }
         if (__ballot(odd != 0u) == 0ull) pv(tile, kb, P);
-        else chunk_pv_seen<F16>(v_rows, seen, P, O);
+        else chunk_pv_seen<F16>(v_rows, seen, P, none, O);
       }
       __syncthreads();
     }

@@ -144,6 +144,28 @@ def test_what_a_row_does_not_see_does_not_change_it(cache, what):
     check(b, {k: v for k, v in want.items() if not 25 <= k[0] < 35}, out, lse)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("cache", ["16", "4"])
+@pytest.mark.parametrize("new", [3, 5, 40])
+def test_infinite_values_reach_the_rows_that_see_them(new, cache, dtype):
+    """V of the last token of a draft, a short run and a chunk, infinite in three of four blocks; in 4 bits by a scale that the 16-bit type does not
+    hold six times."""
+    b = Batch(new=[new, 1], past=[100, 30], cache=cache, dtype=DT[dtype], seed=14 + new)
+    page, slot = b.spot(0, b.ctx[0] - 1)
+    b.rows[1][:, page, slot, 32:] = math.inf
+    if cache == "4":
+        b.code[1][:, page, slot, 32:] = 7
+        b.scale[1][:, page, slot, 1:] = 253 if dtype == "bf16" else 141
+    for which, kw in (("all", {}), ("local", dict(sink=3, window=30))):
+        out, lse, want = run(b, which, **kw)
+        hit = {k: v for k, v in want.items() if k[0] == new - 1}
+        check(b, {k: v for k, v in want.items() if k not in hit}, out, lse)
+        for k, (o, z, tol, tol_z) in hit.items():
+            got = out[k].double().cpu()
+            assert (got[32:] == math.inf).all()
+            assert ((got[:32] - o[:32]).abs() <= tol[:32]).all() and abs(float(lse[k]) - z) <= tol_z
+
+
 def test_large_logits_and_references():
     """Scores far from those of a range's first tile: sums that 32 bits do not hold against one reference."""
     for dtype in (torch.bfloat16, torch.float16):
