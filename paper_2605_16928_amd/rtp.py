@@ -173,13 +173,15 @@ def _on_one_device(who: str, descriptors, tensors):
             raise RtpError(RTP_ERR_INVALID_ARG, f"{who}: tensors on devices {sorted(set(at))}, the current one is {current}")
 
 
-def _rows(who: str, t, total: int, heads: int, name: str):
-    """A tensor of packed rows [total or more, heads, 128] whose tokens are a stride apart and whose heads are not."""
+def _rows(who: str, t, total: int, heads: int, name: str, stride: int):
+    """A tensor of packed rows [total or more, heads, 128] whose tokens are `stride` apart and whose heads are not."""
     if hasattr(t, "stride"):
         n = t.shape
         if len(n) != 3 or n[0] < total or n[1] != heads or n[2] != 128 or t.element_size() != 2 \
                 or (total and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != 128))):
             raise RtpError(RTP_ERR_INVALID_ARG, f"{who}: {name} of 16 bits [{total} or more, {heads}, 128] expected, a token's rows contiguous")
+        if total > 1 and t.stride(0) != stride:
+            raise RtpError(RTP_ERR_INVALID_ARG, f"{who}: {name} with tokens {stride} elements apart expected, they are {t.stride(0)}")
 
 
 class rtp_page_map(C.Structure):
@@ -687,8 +689,9 @@ def rtp_kv_append(layer, cache, chunk, rope, q, q_stride, k, k_stride, v, v_stri
     who = "rtp_kv_append"
     _held(who, layer, cache, chunk.B)
     _on_one_device(who, (cache, chunk, rope), (q, k, v, q_out))
-    for t, heads, name in ((q, layer.n_q_heads, "q"), (k, layer.n_kv_heads, "k"), (v, layer.n_kv_heads, "v"), (q_out, layer.n_q_heads, "q_out")):
-        _rows(who, t, chunk.total_q, heads, name)
+    for t, heads, name, stride in ((q, layer.n_q_heads, "q", q_stride), (k, layer.n_kv_heads, "k", k_stride), (v, layer.n_kv_heads, "v", v_stride),
+                                   (q_out, layer.n_q_heads, "q_out", q_out_stride)):
+        _rows(who, t, chunk.total_q, heads, name, stride)
     _check(lib().rtp_kv_append(C.byref(layer), C.byref(cache), C.byref(chunk), None if rope is None else C.byref(rope), _ptr(q), q_stride,
                                _ptr(k), k_stride, _ptr(v), v_stride, _ptr(q_out), q_out_stride, _stream(stream)))
 
@@ -704,10 +707,10 @@ def rtp_local_attn_chunk_workspace_bytes(layer, B, total_q, max_q, max_ctx) -> i
 def _chunk_attn(who, layer, q, q_stride, cache, chunk, heads, out, lse, ws, stream):
     _held(who, layer, cache, chunk.B)
     _on_one_device(who, (cache, chunk), (q, out, lse, ws))
-    _rows(who, q, chunk.total_q, layer.n_q_heads, "q")
-    _rows(who, out, chunk.total_q, layer.n_q_heads, "out")
-    if hasattr(lse, "numel") and lse.numel() < chunk.total_q * layer.n_q_heads:
-        raise RtpError(RTP_ERR_INVALID_ARG, f"{who}: lse [{chunk.total_q}, {layer.n_q_heads}] expected")
+    _rows(who, q, chunk.total_q, layer.n_q_heads, "q", q_stride)
+    _rows(who, out, chunk.total_q, layer.n_q_heads, "out", layer.n_q_heads * 128)
+    if hasattr(lse, "numel") and (lse.numel() < chunk.total_q * layer.n_q_heads or lse.element_size() != 4 or not lse.is_contiguous()):
+        raise RtpError(RTP_ERR_INVALID_ARG, f"{who}: contiguous fp32 lse [{chunk.total_q}, {layer.n_q_heads}] expected")
     _check(getattr(lib(), who)(C.byref(layer), _ptr(q), q_stride, C.byref(cache), C.byref(chunk), *heads, _ptr(out), _ptr(lse), _ptr(ws),
                                _nbytes(ws), _stream(stream)))
 

@@ -172,3 +172,29 @@ def test_calls_over_more_than_the_tensors_hold():
             with pytest.raises(rtp.RtpError) as e:
                 call(**args)
             assert "a cache of" in str(e.value)
+
+
+class Rows:
+    """A tensor that says nothing of its device."""
+
+    def __init__(self, t):
+        self.shape, self.stride, self.element_size, self.data_ptr, self.numel, self.is_contiguous = t.shape, t.stride, t.element_size, (lambda: A), t.numel, t.is_contiguous
+
+
+def test_tensors_lie_as_the_calls_take_them():
+    """Tokens as far apart as the call says; outputs contiguous, log-sums contiguous in 32 bits."""
+    fused, plain, short = (torch.zeros(n, dtype=torch.bfloat16) for n in ((50, 12, 128), (50, 8, 128), (49, 8, 128)))
+    q = fused[:, :8]
+    lse = torch.zeros((50, 8))
+    for name in ("dense", "local", "dense4", "local4"):
+        call, args = _calls()[name]
+        for bad in (dict(q=Rows(q), q_stride=1024), dict(q=Rows(plain)), dict(q=Rows(short), q_stride=1024), dict(q=Rows(q.transpose(1, 2))), dict(q=Rows(q[:, :4])),
+                    dict(q=Rows(q.float())), dict(out=Rows(q)), dict(out=Rows(short)), dict(out=Rows(torch.zeros((8, 50, 128), dtype=torch.half).transpose(0, 1))),
+                    dict(lse=Rows(lse.half())), dict(lse=Rows(lse[:49])), dict(lse=Rows(torch.zeros((8, 50)).T)), dict(lse=Rows(torch.zeros((50, 12))[:, :8]))):
+            with pytest.raises(rtp.RtpError, match="expected"):
+                call(**dict(args, **bad))
+    call, args = _calls()["append"]
+    for bad in (dict(q=Rows(plain)), dict(k=Rows(plain[:, :2])), dict(v=Rows(fused[:, 10:]), v_stride=256), dict(q_out=Rows(q)), dict(k=Rows(fused[:, 8:])),
+                dict(v=Rows(fused[:49, 10:]))):
+        with pytest.raises(rtp.RtpError, match="expected"):
+            call(**dict(args, **bad))
