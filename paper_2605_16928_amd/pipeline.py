@@ -519,8 +519,12 @@ class ServeRun:
         total, grown = sum(new), [n + c for n, c in zip(new, self.ctx_len)]
         if len(new) != self.B or min(new) < 0 or total > self.max_tokens:
             self._refuse(f"{self.B} counts of at most {self.max_tokens} tokens together expected")
-        if any(x.dim() != 3 or x.shape[0] != total for x in (q, k, v)):
-            self._refuse(f"rows of {total} tokens expected")
+        L = self.layer
+        for x, heads in ((q, L.n_q_heads), (k, L.n_kv_heads), (v, L.n_kv_heads)):
+            if x.shape != (total, heads, 128) or x.dtype != self.K.dtype or x.device != self.K.device:
+                self._refuse(f"rows of {total} tokens in the layer's type expected, on its device")
+            if total and (x.stride(2) != 1 or (heads > 1 and x.stride(1) != 128) or x.stride(0) < heads * 128 or x.stride(0) % 8 or x.data_ptr() % 16):
+                self._refuse("a token's rows contiguous, tokens a multiple of 8 elements apart, 16-byte aligned")
         if max(grown) > self.max_ctx or sum(map(self.pages, grown)) > self.n_pages:
             self._refuse("no room for these tokens")
         if total == 0:

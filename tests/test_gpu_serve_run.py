@@ -103,6 +103,23 @@ def test_steps_without_room_are_refused_and_change_nothing():
     s.step((33, 7))
 
 
+def test_rows_that_a_step_cannot_take_change_nothing():
+    """Other heads, types, strides, alignments and devices are refused before pages are handed out."""
+    s = Server(_layer(), seqs=2, n_pages=6, page_size=16, max_ctx=56, max_tokens=50)
+    s.step((15, 3))
+    table, refs, lens = s.run.page_table.clone(), s.run.page_refs.clone(), list(s.run.ctx_len)
+    fine = {name: torch.zeros((5, heads, 128), dtype=torch.bfloat16, device=DEV) for name, heads in (("q", 8), ("k", 2), ("v", 2))}
+    wide = torch.zeros((5, 8, 136), dtype=torch.bfloat16, device=DEV)
+    odd = torch.zeros((5, 2 * 128 + 4), dtype=torch.bfloat16, device=DEV)
+    for bad in (dict(q=fine["k"]), dict(k=fine["q"]), dict(v=fine["v"][..., :64]), dict(q=fine["q"].half()), dict(k=fine["k"].float()), dict(v=fine["v"].cpu()),
+                dict(q=wide[..., :128]), dict(k=odd[:, :256].unflatten(1, (2, 128))), dict(v=odd.flatten()[4:1284].view(5, 2, 128)),
+                dict(k=fine["k"][:1].expand(5, 2, 128)), dict(v=fine["v"].flatten(1))):
+        with pytest.raises(rtp.RtpError):
+            s.run.step(*{**fine, **bad}.values(), [4, 1])
+    assert torch.equal(table, s.run.page_table) and torch.equal(refs, s.run.page_refs) and s.run.ctx_len == lens
+    s.step((4, 1))
+
+
 @pytest.mark.parametrize("kw", [dict(), dict(n_q_heads=4, n_kv_heads=4, ret_heads=(0, 3), window=700, kv_dtype="fp16")], ids=["g4", "g1_fp16"])
 @pytest.mark.parametrize("T", [1, 4])
 def test_drafts_over_four_bits(kw, T):
