@@ -224,10 +224,15 @@ void serve(const rtp_layer_desc* L, const HeadTable& ht, int which, ChunkShape* 
 // one token of 32 heads over 8 KV heads, 500 keys 10.9 and 11.2 us, 1000 keys 13.9 and 11.2; 512 tokens, 500 keys 25.9 and 27.6, 2000 keys 62 and 45.
 constexpr int kUncutKeys = 512;
 
-// Up to this many rows of a KV head to a sequence, its tiles have 32 rows, whose waves need not wait for each other; two that read the same keys are
-// neighbours on a die and share its L2.  8 contexts of 8000, 64 over 8 heads, 8 new tokens (64 rows) 53 us and 61 as one tile, 12 tokens 90 and 64;
-// 30000 in 4 bits, 8 tokens 143 and 166, 16 tokens 260 and 185.
+// Tiles of 32 rows, whose waves need not wait for each other and which need no second launch for what has to be taken again, are taken in two cases.
+// Up to this many rows of a KV head to a sequence: two that read the same keys are neighbours on a die and share its L2.  8 contexts of 8000, 64 over
+// 8 heads, 8 new tokens (64 rows) 53 us and 61 as one tile, 12 tokens 90 and 64; 30000 in 4 bits, 8 tokens 143 and 166, 16 tokens 260 and 185.
 constexpr int kFineRows = 64;
+// And where they all have a place at once, two to a compute unit, and read no more than so many keys together, as wide tiles would leave most of
+// the compute units without work.  32 over 8 heads, fine and wide: 60 tokens over as many 9 us and 15; 4 x 60 (256 tiles of 32 rows) over 500 keys 13
+// and 25, over 4000 (2^20) 45 and 46, over 8000 73 and 59; 16 x 60 (1024) over 500 32 and 27; 64 over 8 heads, 4 x 60 (480) over 2000 40 and 45, over
+// 4000 66 and 58; 4 x 20 (160) over 4000 40 and 39.
+constexpr int64_t kFineKeys = 3 << 18;
 
 struct ChunkSizes {
   int64_t tiles;               // query tiles that the bounds allow
@@ -239,21 +244,35 @@ struct ChunkSizes {
   size_t plan_bytes, again_bytes, merge_bytes, part_bytes;
   size_t total() const { return plan_bytes + again_bytes + merge_bytes + part_bytes; }
 };
-ChunkSizes chunk_sizes(const ChunkShape& s, int32_t B, int64_t total_q, int64_t max_q, int64_t max_ctx) {
+// Query tiles that the bounds allow, of so many rows: a sequence of n tokens has ceil(n / tok), at most n of them, at most one more than its share.
+int64_t chunk_most_tiles(const ChunkShape& s, int32_t B, int64_t total_q, int64_t max_q, int rows) {
+  int64_t tiles = 0;
+  for (int k = 0; k < 8; ++k) {
+    const int64_t tok = rows / (k + 1), per_seq = (max_q + tok - 1) / tok;
+    tiles += s.count[k] * std::min(std::min(total_q, total_q / tok + B), per_seq * B);
+  }
+  return tiles;
+}
+int64_t chunk_most_keys(const ChunkShape& s, int64_t max_ctx) {       // that a tile reads
+  return s.local ? std::min<int64_t>(max_ctx, (int64_t)s.sink + s.window + 64) : max_ctx;
+}
+bool chunk_fine(const ChunkShape& s, int32_t B, int64_t total_q, int64_t max_q, int64_t max_ctx) {
+  max_q = std::max<int64_t>(1, std::min(max_q, total_q));
+  if (max_q * std::max(s.widest, 1) <= kFineRows) return true;
+  const int64_t tiles = chunk_most_tiles(s, B, total_q, max_q, kCkNarrowRows);
+  return tiles <= 2 * (int64_t)compute_units() && tiles * chunk_most_keys(s, max_ctx) <= kFineKeys;
+}
+// most: there are no more tiles.
+ChunkSizes chunk_sizes(const ChunkShape& s, int32_t B, int64_t total_q, int64_t max_q, int64_t max_ctx, bool fine, int64_t most) {
   ChunkSizes z = {};
   max_q = std::max<int64_t>(1, std::min(max_q, total_q));
   const int widest = std::max(s.widest, 1);
-  z.narrow = max_q * widest <= kFineRows;
+  z.narrow = fine;
   z.fine = z.narrow ? 3 : 0;
   const int rows = kChunkRows >> z.fine;
-  for (int k = 0; k < 8; ++k) {
-    // a sequence of n tokens has ceil(n / tok) tiles: at most n of them, at most one more than its share
-    const int64_t tok = rows / (k + 1), per_seq = (max_q + tok - 1) / tok;
-    z.tiles += s.count[k] * std::min(std::min(total_q, total_q / tok + B), per_seq * B);
-  }
+  z.tiles = std::min(chunk_most_tiles(s, B, total_q, max_q, rows), most);
   // ranges of two key tiles and more, at most four per compute unit
-  int64_t keys = max_ctx;
-  if (s.local) keys = std::min<int64_t>(keys, (int64_t)s.sink + s.window + 64);
+  const int64_t keys = chunk_most_keys(s, max_ctx);
   const int64_t ranges = keys <= kUncutKeys ? 1 : std::min<int64_t>((keys + 2 * kCkK - 1) / (2 * kCkK), 289);
   z.cap = ranges > 1 ? std::min<int64_t>(z.tiles * ranges, 4 * (int64_t)compute_units()) : 0;
   z.part_rows = (int32_t)std::min<int64_t>(rows, max_q * widest);
@@ -270,10 +289,12 @@ ChunkSizes chunk_sizes(const ChunkShape& s, int32_t B, int64_t total_q, int64_t 
   return z;
 }
 
-// What a call needs, and every one with smaller bounds: finer tiles among them.
+// What a call needs, and every one with smaller bounds: finer tiles, for either reason, among them.
 size_t chunk_bytes(const ChunkShape& s, int32_t B, int64_t total_q, int64_t max_q, int64_t max_ctx) {
-  const size_t bytes = std::max<size_t>(256, chunk_sizes(s, B, total_q, max_q, max_ctx).total());
-  return std::max(bytes, chunk_sizes(s, B, total_q, std::min<int64_t>(max_q, kFineRows / std::max(s.widest, 1)), max_ctx).total());
+  const int64_t any = INT64_MAX;
+  size_t bytes = std::max<size_t>(256, chunk_sizes(s, B, total_q, max_q, max_ctx, chunk_fine(s, B, total_q, max_q, max_ctx), any).total());
+  bytes = std::max(bytes, chunk_sizes(s, B, total_q, std::min<int64_t>(max_q, kFineRows / std::max(s.widest, 1)), max_ctx, true, any).total());
+  return std::max(bytes, chunk_sizes(s, B, total_q, max_q, max_ctx, true, 2 * (int64_t)compute_units()).total());
 }
 
 size_t chunk_workspace(const rtp_layer_desc* layer, int which, int32_t B, int32_t total_q, int32_t max_q, int64_t max_ctx) {
@@ -309,7 +330,8 @@ int32_t chunk_call(const char* who, int which, const rtp_layer_desc* layer, cons
     clear_error();
     return RTP_OK;
   }
-  const ChunkSizes z = chunk_sizes(a.shape, chunk->B, chunk->total_q, chunk->max_q, chunk->max_ctx);
+  const bool fine = chunk_fine(a.shape, chunk->B, chunk->total_q, chunk->max_q, chunk->max_ctx);
+  const ChunkSizes z = chunk_sizes(a.shape, chunk->B, chunk->total_q, chunk->max_q, chunk->max_ctx, fine, INT64_MAX);
   const size_t bytes = chunk_bytes(a.shape, chunk->B, chunk->total_q, chunk->max_q, chunk->max_ctx);
   if (!ws || ((uintptr_t)ws & 255) || ws_bytes < bytes)
     return fail(RTP_ERR_WORKSPACE, "%s: workspace of %zu bytes, 256-byte aligned, needed", who, bytes);

@@ -1,5 +1,7 @@
 """Refusals of the calls over new tokens in a paged cache, all on the host."""
 import ctypes as C
+import math
+import random
 
 import pytest
 import torch
@@ -198,3 +200,16 @@ def test_tensors_lie_as_the_calls_take_them():
                 dict(v=Rows(fused[:49, 10:]))):
         with pytest.raises(rtp.RtpError, match="expected"):
             call(**dict(args, **bad))
+
+
+def test_a_workspace_serves_every_smaller_call():
+    """Whichever tiles the smaller bounds are taken in."""
+    rng = random.Random(4)
+    for _ in range(400):
+        hq, hkv = rng.choice([(8, 2), (32, 8), (64, 8), (16, 16), (4, 1)])
+        layer = _layer(n_q_heads=hq, n_kv_heads=hkv, ret_heads=sorted(rng.sample(range(hq), 2)), window=rng.choice([0, 16, 500, 8192]))
+        bounds = [int(2 ** rng.uniform(0, top)) for top in (8, 13, 12, 18)]
+        less = [int(2 ** rng.uniform(0, math.log2(n))) for n in bounds]
+        for size in (lambda *b: rtp.rtp_local_attn_chunk_workspace_bytes(layer, *b), lambda *b: rtp.rtp_dense_attn_chunk_workspace_bytes(layer, *b, 0),
+                     lambda *b: rtp.rtp_dense_attn_chunk_workspace_bytes(layer, *b, 1)):
+            assert size(*less) <= size(*bounds), (hq, hkv, less, bounds)
