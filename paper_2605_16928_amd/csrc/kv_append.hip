@@ -10,7 +10,7 @@
 // is read twice, and the queries may be rotated in place.  A lane's eight angles are those of its place in the row, the same for every head, so they
 // are computed once per token and kept in registers while the wave goes through the token's rows.  Up to 1024 tokens four waves share one.
 // Measured: 4096 tokens of 32 + 8 + 8 heads (101 MB read and written) 17.8 us, 5.7 TB/s, where a copy of 4 GiB reaches 4.9; one token for each of 32
-// sequences 5.0, of which the launch and the chain offsets -> length -> page -> row are all; a call in a row of calls 8.4, the host's time.
+// sequences 5.0, of which the launch and the chain offsets -> length -> page -> row are all; a call in a row of calls 7.2, the host's time.
 #include "kv16_cache.h"
 #include "mfma_tile.h"
 
