@@ -27,12 +27,6 @@ constexpr int kCkBlockBytes = 2 * 32 * kHeadDim * 2;                        // K
 constexpr int chunk_narrow_lds(int waves) { return waves * (kCkBlockBytes + kCkNarrowRows * 2 * 4); }
 constexpr int kCkLds = chunk_narrow_lds(kCkWaves) > kCkWideLds ? chunk_narrow_lds(kCkWaves) : kCkWideLds;
 
-// LDS words that only the own wave writes and reads.
-__device__ __forceinline__ void chunk_wave_fence() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
 // The blocks of 32 keys that a wave takes, and where their rows lie: block k of wave w is block w + NW k of the range.
 template <bool LOCAL, bool KV4, int NW>
 struct ChunkBlocks {

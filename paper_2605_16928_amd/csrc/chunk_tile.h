@@ -378,6 +378,12 @@ __device__ __forceinline__ void chunk_pv_seen(const unsigned char* v_rows, uint3
   }
 }
 
+// LDS words that only the own wave writes and reads.
+__device__ __forceinline__ void chunk_wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // 16 bytes per lane from global memory to LDS, 1 KiB per wave.  (Assembly, since through the compiler's intrinsic every later LDS read waits for
 // all outstanding loads; whoever reads the rows waits for them itself.)
 __device__ __forceinline__ void chunk_load_lds(uint32_t dst, const uint8_t* base, uint32_t offset) {

@@ -57,11 +57,6 @@ struct ChunkWide {
         row(wave * 32 + r), qok(row < t_.rows), w_lo(wave * 32 < t_.rows ? chunk_row_pos(t_, wave * 32) : -1),
         w_hi(wave * 32 < t_.rows ? chunk_row_pos(t_, min(wave * 32 + 31, t_.rows - 1)) : -1), c(a_.scale_log2), rd(chunk_reads()),
         sight(chunk_sight(a_.shape, t_, row)), lost(false), n_tiles(t_.it_hi - t_.it_lo), n_full(0), n_moved(0) {
-    // (rows behind the tile's last repeat it)
-    const int row_c = min(row, t.rows - 1), rt = (row_c * t.over) >> 16;
-    const uint16_t* src = a.q + (t.q0 + rt) * a.q_stride + chunk_head(a, t, row_c, rt) * kHeadDim + g * 8;
-#pragma unroll
-    for (int kk = 0; kk < 8; ++kk) q[kk] = *reinterpret_cast<const u32x4*>(src + kk * 16);
     if constexpr (KV4) {
       base0 = a.c4.codes + (int64_t)t.kvh * a.c4.code_head_stride;
       base1 = a.c4.scales + (int64_t)t.kvh * a.c4.scale_head_stride;
@@ -182,6 +177,11 @@ struct ChunkWide {
   }
   __device__ __forceinline__ void begin() {                                 // before the first bring()
     look_up(0);
+    // (behind the first pages, which the first rows wait for.  Rows behind the tile's last repeat it.)
+    const int row_c = min(row, t.rows - 1), rt = (row_c * t.over) >> 16;
+    const uint16_t* src = a.q + (t.q0 + rt) * a.q_stride + chunk_head(a, t, row_c, rt) * kHeadDim + g * 8;
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) q[kk] = *reinterpret_cast<const u32x4*>(src + kk * 16);
     if constexpr (KV4) {
       advance(0);
       fetch_codes(0, true);
@@ -493,10 +493,38 @@ struct ChunkWide {
       }
       __syncthreads();
     }
+    landed();                                                               // (what the last tile sent for)
+    __syncthreads();
   }
 
+  // Outputs go by way of the wave's LDS, to be written as whole rows: group u of four outputs of row r at u ^ 2 (r % 16).  (All waves are done with
+  // the tiles.)
   __device__ __forceinline__ void store() {
     const float sum = l + __shfl_xor(l, 32), full = F + __shfl_xor(F, 32);
+    if (t.splits == 1) {
+      unsigned char* const mine = smem + wave * 32 * 256;
+      const bool none = sum == 0.f;
+      const float inv = none ? 0.f : 1.f / sum;
+#pragma unroll
+      for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) {
+          const u32x2 w = {pack16<F16>(O[db][i4 * 4] * inv, O[db][i4 * 4 + 1] * inv), pack16<F16>(O[db][i4 * 4 + 2] * inv, O[db][i4 * 4 + 3] * inv)};
+          *reinterpret_cast<u32x2*>(mine + r * 256 + (((db * 8 + i4 * 2 + g) ^ (2 * (r & 15))) << 3)) = none ? (u32x2){0u, 0u} : w;
+        }
+      if (a.lse && g == 0 && qok) {
+        const int rt = (row * t.over) >> 16;
+        a.lse[(t.q0 + rt) * a.n_q_heads + chunk_head(a, t, row, rt)] = none ? -__builtin_huge_valf() : m * a.scale + logf(full);
+      }
+      chunk_wave_fence();
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int n = 4 * i + (lane >> 4), to = wave * 32 + n, rt = (to * t.over) >> 16, piece = lane & 15;
+        const u32x4 w = *reinterpret_cast<const u32x4*>(mine + n * 256 + ((piece ^ (n & 15)) << 4));
+        if (to < t.rows) *reinterpret_cast<u32x4*>(a.out + ((t.q0 + rt) * a.n_q_heads + chunk_head(a, t, to, rt)) * kHeadDim + piece * 8) = w;
+      }
+      return;
+    }
     if (!qok) return;
 #pragma unroll
     for (int db = 0; db < 4; ++db)
