@@ -22,9 +22,11 @@ constexpr int kChunkRows = 256;          // rows of a query tile
 constexpr int kMostContext = 1 << 30;
 constexpr int kChunkMostKeyTiles = 1 << 22;
 constexpr int kChunkCandidates = 64;
-// What a unit costs beside its key tiles, in key tiles: its way to the first product and from the last; a launch's, that results are merged; and
-// the rows of partial results, written and read, that take as long as a key tile per place (two passes over 528 bytes, 32 KiB a tile).
-constexpr int kChunkUnitCost = 3, kChunkMergeCost = 4, kChunkRowsPerTile = 31;
+// What a unit costs beside its key tiles, in key tiles: its way to the first product and from the last, 12 us where a wide tile of keys takes 1.9
+// (plan 1.6, first pages, queries and keys 4.3, reference 0.9, end of the sums and outputs 3, the next workgroup's beginning 2.5; at 3 in place of 6 a
+// batch of 12 sequences, 0 to 500 tokens behind 0 to 16001, 172 us and 155); a launch's, that results are merged; and the rows of partial results,
+// written and read, that take as long as a key tile per place (two passes over 528 bytes, 32 KiB a tile).
+constexpr int kChunkUnitCost = 6, kChunkMergeCost = 4, kChunkRowsPerTile = 31;
 
 struct ChunkShape {
   int32_t B, total_q, max_q;
