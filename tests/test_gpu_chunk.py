@@ -260,3 +260,17 @@ def test_the_same_twice_and_from_a_graph():
         eager, lse3, want = run(b, prepared=(q, cache, chunk))
         check(b, want, o, z)
         assert torch.equal(o[:b.total], eager[:b.total]) and torch.equal(z[:b.total], lse3[:b.total])
+
+
+@pytest.mark.parametrize("cache", ["16", "4"])
+def test_rows_in_front_of_the_first_sequence(cache):
+    """Offsets that begin behind the first row: the rows in front belong to no sequence.  Two sequences read the same pages."""
+    b = Batch(new=[6, 0, 40], past=[70, 30, 300], cache=cache, seed=17)
+    b.table[1, :6], b.ctx[1], b.new[1] = b.table[0, :6], 70, 2               # (one prompt, two drafts: the second's are the first's last ones)
+    b.off, b.total = [2, 8, 10, 50], 50
+    b.q = torch.randn((52, b.hq, 128), generator=torch.Generator().manual_seed(18)).to(b.dtype)
+    q, c, chunk = b.device()
+    out, lse, want = run(b, prepared=(q, c, chunk))
+    check(b, want, out, lse, MARK)
+    out, lse, want = run(b, "local", ret=[1], sink=3, window=40, prepared=(q, c, chunk))
+    check(b, want, out, lse, MARK)
