@@ -3,7 +3,7 @@
 // Nothing hides latency by itself at two waves per SIMD, so the loop is pipelined over blocks of 32 keys by hand: while the probabilities of a
 // block are computed on the vector ALU, the matrix pipe runs the PV product of the block before and the score product of the one behind.  For that
 // nothing may touch the accumulators in between, so there is no running maximum: every row takes its largest score in the range's first tile for a
-// reference, and a range after whose pass some row's sum or output says that this did not do (out of the middle of fp32's range, or not finite), or
+// reference, and a range after whose pass some row's sum or output says that this did not do (chunk_reach.h; or not finite), or
 // which met a page that is not there, is left to a launch that goes through such ranges with a running maximum (exact_pass).
 //
 // K/V tiles rotate through three LDS buffers with one barrier per tile, in its middle: it publishes tile x + 1, and behind it every wave is done
@@ -20,6 +20,7 @@
 #pragma once
 
 #include "chunk_tile.h"
+#include "chunk_reach.h"
 
 namespace rtp {
 
@@ -312,6 +313,18 @@ struct ChunkWide {
     // (of what the row sees there, if it does see anything)
     float any = ninf;
     m = ninf;
+    // fp16, a window: rows that see a part of the first tile, or nothing of it, take the first tile that every row sees in full as well.  (A few keys'
+    // best may be 2^16 below the row's: a chunk of 4096 tokens, sink 0, 1210 us and 517, all units having been taken again.)
+    if constexpr (F16 && LOCAL) {
+      if (n_full > 0 && !all_seen(n0_of(0), kCkK)) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          scores(tile_of(slot_next), kb, S);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) m = fmaxf(m, S[i]);
+        }
+      }
+    }
 #pragma unroll
     for (int kb = 1; kb >= 0; --kb) {
       scores(smem, kb, S);
@@ -324,7 +337,8 @@ struct ChunkWide {
     }
     m = fmaxf(m, __shfl_xor(m, 32));
     any = fmaxf(any, __shfl_xor(any, 32));
-    m = m > ninf ? m : any;
+    const bool held = m > ninf;
+    m = held ? m : any;
     // At the start of half hf of tile x: S holds the scores of that block if the wave has a row that sees one of its keys; if `pend`, the
     // probabilities of the block before wait in P1 (hf = 0, V in the tile before) or P0; tiles x and x + 1 are in LDS.
     bool pend = false;
@@ -415,8 +429,7 @@ struct ChunkWide {
     while (x < n_tiles) edge_tile();
     if (pend) pv(tile_of(slot_before), 1, P1);
     landed();
-    // Was every reference within reach?  A row that sees a key of the range has a sum in the middle of fp32's range (fp16: nothing above 65504 is
-    // finite; where the largest probability is below 2^-6 most of the mass may be in subnormals), and outputs are finite.
+    // Was every reference within reach, and are the outputs finite?  (A row's keys are counted where its sum alone does not say so.)
     const float sum = l + __shfl_xor(l, 32);
     float z = 0.f;
 #pragma unroll
@@ -424,13 +437,11 @@ struct ChunkWide {
 #pragma unroll
       for (int i = 0; i < 16; ++i) z = fmaf(O[db][i], 0.f, z);
     bool bad = lost || !(z == 0.f) || !(sum < 0x1p100f);
-    if (qok && sight.hi >= 0 && !(sum > (F16 ? 0x1p-6f : 0x1p-60f))) {
-      // does the row see a key of the range?  Of the sink's tiles ...
-      const int first = chunk_tile_n0(t, t.it_lo), end = min(chunk_tile_n0(t, t.it_hi - 1) + kCkK, t.kend);
-      const int band = t.it_lo < t.sink_tiles ? chunk_tile_n0(t, t.sink_tiles) : first;
-      bool sees = !LOCAL && first <= sight.hi;
-      if (LOCAL) sees = first <= min(min(a.shape.sink - 1, sight.hi), end - 1) || max(max(first, sight.lo + 1), t.gap > 0 ? band : 0) <= min(end - 1, sight.hi);
-      bad = bad || sees;
+    if (qok && sight.hi >= 0 && !chunk_surely_in_reach(F16, held, sum)) {
+      const int split = max(t.it_lo, min(t.it_hi, t.sink_tiles));           // the range's tiles in front of the gap, and those behind it
+      const int seen = chunk_seen_among(t.it_lo * kCkK, split * kCkK, LOCAL, a.shape.sink, sight.lo, sight.hi) +
+                       chunk_seen_among((split + t.gap) * kCkK, (t.it_hi + t.gap) * kCkK, LOCAL, a.shape.sink, sight.lo, sight.hi);
+      bad = bad || !chunk_in_reach(F16, held, sum, seen);
     }
     return __syncthreads_or(bad ? 1 : 0) != 0;
   }
