@@ -12,7 +12,9 @@
 // comes from memory for the first time, and four dependent loads.
 //
 // The running reference follows a row's maximum only when it is left behind by more than 2^8.  Probabilities enter the product in two parts, their
-// rounding to 16 bits and the rounding of the rest: the matrix cores have the time, and an output is then as exact as its own rounding.
+// rounding to 16 bits and the rounding of the rest: the matrix cores have the time, and an output is then as exact as its own rounding.  fp16 ends
+// at 2^16 and at 2^-24, where nothing is left for a second part: there probabilities are taken times 2^13, against a reference that follows at 2^2, so
+// that one is whole down to 2^-27 of its row's largest and gone below 2^-38 (all of 2^20 tokens together then 2^-18 of it).
 //
 // Where a page was not there or a result is not finite, the tile is taken again with care: keys are masked by their pages too, and what a row does
 // not see does not reach it, whatever it holds.
@@ -139,6 +141,25 @@ __device__ __forceinline__ void chunk_put_records(unsigned char* mine, const Cod
   *reinterpret_cast<uint32_t*>(mine + kCkScalesAt + lane * 4) = x.scales;
   chunk_wave_fence();
 }
+// The reference is raised when it is left behind by more than 2^kCkLag; probabilities are taken times 2^kCkLift, results by as much less.
+template <bool F16>
+constexpr float kCkLag = F16 ? 2.f : 8.f;
+template <bool F16>
+constexpr float kCkLift = F16 ? 13.f : 0.f;
+template <bool F16>
+constexpr float kCkLower = F16 ? 0x1p-13f : 1.f;
+
+template <bool F16, int N>
+__device__ __forceinline__ void chunk_lower(float& L, float (&o)[N][4]) {
+  if constexpr (F16) {
+    L *= kCkLower<F16>;
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[e][i] *= kCkLower<F16>;
+  }
+}
+
 // Blocks of this scale and above may hold values that are infinite in 16 bits: 4 or 6 times it (fp16: 2^16, the largest is 65504; bf16: 2^128).
 template <bool F16>
 constexpr float kKv4Large = F16 ? 0x1p14f : 0x1p126f;
@@ -307,7 +328,7 @@ struct ChunkNarrow {
     float mx = fmaxf(S[0], S[1]);
 #pragma unroll
     for (int i = 2; i < 16; ++i) mx = fmaxf(mx, S[i]);
-    if (__ballot((mx - m) * c > 8.f || (m == ninf && mx > ninf)) != 0ull) {
+    if (__ballot((mx - m) * c > kCkLag<F16> || (m == ninf && mx > ninf)) != 0ull) {
       const float m_new = fmaxf(m, fmaxf(mx, __shfl_xor(mx, 32)));
       const float corr = m_new == ninf ? 1.f : fast_exp2((m - m_new) * c);
       m = m_new;
@@ -317,7 +338,7 @@ struct ChunkNarrow {
 #pragma unroll
         for (int i = 0; i < 16; ++i) O[db][i] *= corr;
     }
-    const float mc = m == ninf ? 0.f : m * c;
+    const float mc = (m == ninf ? 0.f : m * c) - kCkLift<F16>;
 #pragma unroll
     for (int i = 0; i < 16; i += 2) {
       const float p0 = fast_exp2(fmaf(S[i], c, -mc)), p1 = fast_exp2(fmaf(S[i + 1], c, -mc));
@@ -481,6 +502,7 @@ struct ChunkNarrow {
         }
       }
     }
+    chunk_lower<F16>(L, o);
 #pragma unroll
     for (int e = 0; e < kEach; ++e) chunk_store4<F16>(a, t, row, 4 * (d0 + kLanes * e), M, L, L, o[e]);
     return false;

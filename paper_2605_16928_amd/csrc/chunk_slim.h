@@ -89,7 +89,7 @@ struct ChunkSlim {
       }
     }
     float mx = fmaxf(fmaxf(fmaxf(S[0][0], S[0][1]), fmaxf(S[0][2], S[0][3])), fmaxf(fmaxf(S[1][0], S[1][1]), fmaxf(S[1][2], S[1][3])));
-    if (__ballot((mx - m) * scale > 8.f || (m == ninf && mx > ninf)) != 0ull) {
+    if (__ballot((mx - m) * scale > kCkLag<F16> || (m == ninf && mx > ninf)) != 0ull) {
       mx = fmaxf(mx, __shfl_xor(mx, 16));
       mx = fmaxf(mx, __shfl_xor(mx, 32));
       const float m_new = fmaxf(m, mx), corr = m_new == ninf ? 1.f : fast_exp2((m - m_new) * scale);
@@ -98,7 +98,7 @@ struct ChunkSlim {
 #pragma unroll
       for (int n = 0; n < 8; ++n) O[n] *= corr;
     }
-    const float mc = m == ninf ? 0.f : m * scale;
+    const float mc = (m == ninf ? 0.f : m * scale) - kCkLift<F16>;
     u32x4 P, R;
 #pragma unroll
     for (int s = 0; s < 2; ++s)
@@ -259,6 +259,7 @@ struct ChunkSlim {
         o[e][3] = fmaf(v.w, cw, o[e][3]);
       }
     }
+    chunk_lower<F16>(L, o);
 #pragma unroll
     for (int e = 0; e < kEach; ++e) chunk_store4<F16>(a, t, row, 4 * (d0 + kLanes * e), M, L, L, o[e]);
     return false;

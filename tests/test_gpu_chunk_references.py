@@ -55,3 +55,22 @@ def test_a_strong_key_in_front_of_the_window(cache):
     out, lse, _ = run(b, "local", sink=0, window=window)
     rows = [(t, h) for t in (0, 1, 2, 3, 31, 62, 63, 64, 100, 2047) for h in (0, 5, 31)]
     check_rows(b, out, lse, rows, sink=0, window=window, faint=2.0 ** -25, off_reference=2.0 ** -12)
+
+
+@pytest.mark.parametrize("again", [False, True], ids=["plain", "taken_again"])
+@pytest.mark.parametrize("cache", ["16", "4"])
+@pytest.mark.parametrize("new", [1, 3, 6])
+def test_dominant_keys_in_tiles_of_few_rows(new, cache, again):
+    """Every 32nd token has nearly all of the softmax and a value of 0; the others' probabilities are 2^-26 of theirs."""
+    b = Batch(new=[new], past=[1500], dtype=torch.float16, cache=cache, seed=26 + new)
+    u = alike(b, 27)
+    put(b, 0, slice(None), torch.zeros((2, b.n_pages, b.page, 128)))
+    put(b, 1, slice(None), torch.full((2, b.n_pages, b.page, 128), 1024.0))
+    for pos in range(7, b.ctx[0], 32):
+        page, slot = b.spot(0, pos)
+        put(b, 0, (slice(None), page, slot), 18.0 * 128 ** 0.5 * u / u.square().sum(1, keepdim=True))
+        put(b, 1, (slice(None), page, slot), torch.zeros((2, 128)))
+    if again:
+        b.table[0, 40] = -1
+    out, lse, _ = run(b)
+    check_rows(b, out, lse, [(t, h) for t in range(new) for h in range(8)], parts=2, faint=2.0 ** -38)
