@@ -1,10 +1,10 @@
 // Whether the probabilities of a row were good enough against a fixed reference (chunk_wide.h), from their sum.  Apart from the kernels so that it also
 // compiles for the host.
 //
-// The reference is the row's largest score in its range's first tile (fp16, a window: and in the first tile that every row sees in full), or, where the
-// row sees nothing there, the largest of what it does not see, which says nothing of what it sees.  bf16 has the range of fp32: only sums near its ends need another reference.  fp16 ends at 65504, which the sum shows as
+// The reference is the row's largest score in its range's first tile (fp16: or in the first tile that every row sees in full), or, where the row sees
+// nothing there, the largest of what it does not see, which says nothing of what it sees.  bf16 has the range of fp32: only sums near its ends need another reference.  fp16 ends at 65504, which the sum shows as
 // an infinity, and below 2^-14 a probability is off by up to 2^-25 whatever its size: n of them by n 2^-25 together, which is within 2^-12 of a
-// sum of n 2^-13.  A row that sees its reference (`held`) needs no such sum: no other reference would serve it better.
+// sum of n 2^-13.  A row that sees its reference (`held`) needs no such sum: most of its probabilities are not that much smaller.
 #pragma once
 
 #include <stdint.h>

@@ -288,6 +288,7 @@ struct ChunkWide {
     end_block();
   }
 
+  static constexpr float kOutstanding = 12.f;    // (in the logarithm to the base of 2)
   // ---- the pass against fixed references; true: some row needs another ----
   __device__ __forceinline__ bool fast_pass() {
     const float ninf = -__builtin_huge_valf();
@@ -313,16 +314,20 @@ struct ChunkWide {
     // (of what the row sees there, if it does see anything)
     float any = ninf;
     m = ninf;
-    // fp16, a window: rows that see a part of the first tile, or nothing of it, take the first tile that every row sees in full as well.  (A few keys'
-    // best may be 2^16 below the row's: a chunk of 4096 tokens, sink 0, 1210 us and 517, all units having been taken again.)
-    if constexpr (F16 && LOCAL) {
-      if (n_full > 0 && !all_seen(n0_of(0), kCkK)) {
+    // fp16: of the first tile that every row sees in full, if there is one, and of the range's first tile what is more than 2^12 above that.  A
+    // context's first token often has most of the softmax, at 2^15 or more above the others, and fp16 has 14 binades below the reference in which a
+    // probability is whole, 16 above.  (A window: rows see a part of the first tile, or nothing, and a few keys' best may be 2^16 below the
+    // row's.  A chunk of 4096 tokens, sink 0, 1210 us and 517, all units having been taken again.)
+    float full = ninf;
+    if constexpr (F16) {
+      if (n_full > 0) {
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
           scores(tile_of(slot_next), kb, S);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) m = fmaxf(m, S[i]);
+          for (int i = 0; i < 16; ++i) full = fmaxf(full, S[i]);
         }
+        full = fmaxf(full, __shfl_xor(full, 32));
       }
     }
 #pragma unroll
@@ -337,8 +342,8 @@ struct ChunkWide {
     }
     m = fmaxf(m, __shfl_xor(m, 32));
     any = fmaxf(any, __shfl_xor(any, 32));
-    const bool held = m > ninf;
-    m = held ? m : any;
+    const bool held = m > ninf || full > ninf;
+    m = !held ? any : full > ninf ? fmaxf(full, m - kOutstanding / c) : m;
     // At the start of half hf of tile x: S holds the scores of that block if the wave has a row that sees one of its keys; if `pend`, the
     // probabilities of the block before wait in P1 (hf = 0, V in the tile before) or P0; tiles x and x + 1 are in LDS.
     bool pend = false;
@@ -446,7 +451,9 @@ struct ChunkWide {
     return __syncthreads_or(bad ? 1 : 0) != 0;
   }
 
-  // ---- running maximum, accumulators rescaled in place, keys masked by their pages too (apart from the pass above: its registers are its own) ----
+  // ---- running maximum, accumulators rescaled in place, keys masked by their pages too (apart from the pass above: its registers are its own).
+  // fp16: probabilities are taken times 2^15, the most that it holds, and results by as much less. ----
+  static constexpr float kLift = F16 ? 15.f : 0.f, kLower = F16 ? 0x1p-15f : 1.f;
   __device__ __forceinline__ void exact_pass() {
     const float ninf = -__builtin_huge_valf();
     f32x16 S;
@@ -477,11 +484,11 @@ struct ChunkWide {
           mx = fmaxf(mx, S[i]);
         }
         mx = fmaxf(mx, __shfl_xor(mx, 32));
-        const float m_new = fmaxf(m, mx), ref = m_new == ninf ? 0.f : m_new, corr = fast_exp2((m - ref) * c);
+        const float m_new = fmaxf(m, mx), ref = m_new == ninf ? 0.f : m_new, corr = fast_exp2((m - ref) * c), mc = ref * c - kLift;
         float sum = 0.f, full = 0.f;
 #pragma unroll
         for (int i = 0; i < 16; i += 2) {
-          const float p0 = fast_exp2(fmaf(S[i], c, -ref * c)), p1 = fast_exp2(fmaf(S[i + 1], c, -ref * c));
+          const float p0 = fast_exp2(fmaf(S[i], c, -mc)), p1 = fast_exp2(fmaf(S[i + 1], c, -mc));
           P[i >> 1] = pack16<F16>(p0, p1);
           full += p0 + p1;
           sum += lo16<F16>(P[i >> 1]) + hi16<F16>(P[i >> 1]);
@@ -506,6 +513,14 @@ struct ChunkWide {
     }
     landed();                                                               // (what the last tile sent for)
     __syncthreads();
+    if constexpr (F16) {
+      l *= kLower;
+      F *= kLower;
+#pragma unroll
+      for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) O[db][i] *= kLower;
+    }
   }
 
   // Outputs go by way of the wave's LDS, to be written as whole rows: group u of four outputs of row r at u ^ 2 (r % 16).  (All waves are done with

@@ -59,6 +59,27 @@ def test_a_strong_key_in_front_of_the_window(cache):
 
 @pytest.mark.parametrize("again", [False, True], ids=["plain", "taken_again"])
 @pytest.mark.parametrize("cache", ["16", "4"])
+def test_a_dominant_key_without_a_value(cache, again):
+    """One of a context's first tokens has nearly all of the softmax and a value of 0, as the first token of a prompt often has: the outputs are
+    sums of probabilities 16 below it, 2^-23 of it each.  Wide tiles, whose keys are not cut; with a page that is not there they are taken again."""
+    b = Batch(new=[2048], past=[6000], hq=32, hkv=8, dtype=torch.float16, page=64, cache=cache, seed=23)
+    u = alike(b, 24)
+    put(b, 0, slice(None), 0.05 * torch.randn((8, b.n_pages, b.page, 128), generator=torch.Generator().manual_seed(25)))
+    page, slot = b.spot(0, 5)
+    put(b, 0, (slice(None), page, slot), 16.0 * 128 ** 0.5 * u / u.square().sum(1, keepdim=True))
+    strong = (b.rows[0][:, page, slot].double() * u.double()).sum(1) * 128.0 ** -0.5
+    assert 14.0 < strong.min() < strong.max() < 17.0
+    against(b, u, strong, 2.0 ** -24)
+    put(b, 1, (slice(None), page, slot), torch.zeros((8, 128)))
+    if again:
+        b.table[0, 70] = -1
+    b.expected = lambda *a: {}
+    out, lse, _ = run(b)
+    check_rows(b, out, lse, [(t, h) for t in (0, 1, 63, 64, 1000, 2047) for h in (0, 5, 31)], faint=2.0 ** -37)
+
+
+@pytest.mark.parametrize("again", [False, True], ids=["plain", "taken_again"])
+@pytest.mark.parametrize("cache", ["16", "4"])
 @pytest.mark.parametrize("new", [1, 3, 6])
 def test_dominant_keys_in_tiles_of_few_rows(new, cache, again):
     """Every 32nd token has nearly all of the softmax and a value of 0; the others' probabilities are 2^-26 of theirs."""
