@@ -5,7 +5,7 @@
 
 namespace rtp {
 
-// The kernels.  ANY: tiles of any size; what has to be taken again is noted by workgroup, for AGAIN.  NARROW: where the host knows that no tile has
+// The kernels.  ANY: tiles of any size; what has to be taken again is noted by workgroup, for AGAIN, each size in its own way.  NARROW: where the host knows that no tile has
 // more than 32 rows; takes its tiles again itself.  Workgroups of four waves, two to a compute unit, whose beginnings and ends lie beside the other's
 // middle; of eight where there are no more units than compute units (`few`): one token of 2 KV heads over 700 keys, whole, 11.7 us with eight and 13.6 with four.
 #define RTP_CHUNK_KERNELS(ANY, AGAIN, NARROW, KV4)                                                                      \
@@ -39,9 +39,13 @@ namespace rtp {
       ChunkTile t;                                                                                                      \
       if (a.again[i] == 0 || !chunk_tile<LOCAL, KV4>(a, i, &t)) continue;                                               \
       __syncthreads();                                                                                                  \
-      ChunkWide<F16, LOCAL, KV4, true> w(a, t, smem);                                                                   \
-      w.exact_pass();                                                                                                   \
-      w.store();                                                                                                        \
+      if (t.rows <= kCkNarrowRows) {                                                                                    \
+        (void)ChunkNarrow<F16, LOCAL, KV4, kCkWaves, true>(a, t, smem).run();                                           \
+      } else {                                                                                                          \
+        ChunkWide<F16, LOCAL, KV4, true> w(a, t, smem);                                                                 \
+        w.exact_pass();                                                                                                 \
+        w.store();                                                                                                      \
+      }                                                                                                                 \
     }                                                                                                                   \
   }                                                                                                                     \
   template <bool F16, bool LOCAL, int NW>                                                                               \
