@@ -72,7 +72,7 @@ class rtp_kv4_cache(C.Structure):
         ("page_table", C.c_void_p), ("pt_stride", C.c_int64), ("page_size", C.c_int32), ("n_pages", C.c_int32),
     ]
     n_heads = n_seqs = 1 << 31                      # KV heads of the pools, rows of the table: known where kv4_cache made it
-    _device = None                                  # and of which device
+    _device = _dtype = None                         # and of which device and (16-bit rows) type
 
 
 def _held(who: str, layer, cache, B: int):
@@ -111,7 +111,7 @@ class rtp_kv_cache(C.Structure):
         ("page_table", C.c_void_p), ("pt_stride", C.c_int64), ("page_size", C.c_int32), ("n_pages", C.c_int32),
     ]
     n_heads = n_seqs = 1 << 31                      # as in rtp_kv4_cache
-    _device = None
+    _device = _dtype = None
 
 
 class rtp_chunk(C.Structure):
@@ -128,7 +128,7 @@ class rtp_rope(C.Structure):
 def kv_cache(K, V, page_table) -> rtp_kv_cache:
     """Descriptor of a 16-bit cache in torch tensors: K and V [n_kv_heads, n_pages, page_size, 128] of the same strides (any but the
     last's: a pool with the pages, or the tokens, in front as a permuted view), page_table int32 [B, pages].  Calls over more KV heads or
-    sequences than these tensors hold are refused."""
+    sequences than these tensors hold, or of a layer of another type, are refused."""
     ok = K.dim() == 4 and K.shape[3] == 128 and min(K.shape) > 0 and K.element_size() == 2 and K.stride(3) == 1 and K.dtype == V.dtype \
         and K.shape == V.shape and K.stride() == V.stride() and page_table.dim() == 2 and _int32(page_table) \
         and K.device == V.device == page_table.device
@@ -138,7 +138,7 @@ def kv_cache(K, V, page_table) -> rtp_kv_cache:
     c = rtp_kv_cache(K.data_ptr(), V.data_ptr(), K.stride(2), K.stride(1), K.stride(0), page_table.data_ptr(), page_table.shape[1], K.shape[2],
                      K.shape[1])
     c.n_heads, c.n_seqs = K.shape[0], page_table.shape[0]
-    c._keepalive, c._device = (K, V, page_table), K.get_device()
+    c._keepalive, c._device, c._dtype = (K, V, page_table), K.get_device(), K.dtype
     return c
 
 
@@ -174,8 +174,23 @@ def _on_one_device(who: str, descriptors, tensors):
             raise RtpError(RTP_ERR_INVALID_ARG, f"{who}: tensors on devices {sorted(set(at))}, the current one is {current}")
 
 
-def _rows(who: str, t, total: int, heads: int, name: str, stride: int):
-    """The address of packed rows [total or more, heads, 128], whose tokens are `stride` apart and whose heads are not."""
+_torch_types = None
+
+
+def _type_of(who: str, layer, cache):
+    """The layer's 16-bit type as torch names it (None: a layer that the call refuses), which is the cache's."""
+    global _torch_types
+    if _torch_types is None:
+        import torch
+        _torch_types = {RTP_DTYPE_BF16: torch.bfloat16, RTP_DTYPE_FP16: torch.float16, "lse": torch.float32}
+    kind = _torch_types.get(layer.kv_dtype)
+    if cache._dtype is not kind and cache._dtype is not None and kind is not None:
+        raise RtpError(RTP_ERR_INVALID_ARG, f"{who}: a cache of {kind} expected, as the layer's type is; it is of {cache._dtype}")
+    return kind
+
+
+def _rows(who: str, t, total: int, heads: int, name: str, stride: int, kind):
+    """The address of packed rows [total or more, heads, 128] of type `kind`, whose tokens are `stride` apart and whose heads are not."""
     if t is None or t.__class__ is int:
         return t
     n, s = t.shape, t.stride()
@@ -184,6 +199,8 @@ def _rows(who: str, t, total: int, heads: int, name: str, stride: int):
         raise RtpError(RTP_ERR_INVALID_ARG, f"{who}: {name} of 16 bits [{total} or more, {heads}, 128] expected, a token's rows contiguous")
     if total > 1 and s[0] != stride:
         raise RtpError(RTP_ERR_INVALID_ARG, f"{who}: {name} with tokens {stride} elements apart expected, they are {s[0]}")
+    if t.dtype is not kind and kind is not None:
+        raise RtpError(RTP_ERR_INVALID_ARG, f"{who}: {name} of {kind} expected, as the layer's type is; it is of {t.dtype}")
     return t.data_ptr()
 
 
@@ -696,14 +713,15 @@ def rtp_kv_pages_copy(pools, n_pages, src, dst, n, count=None, stream=None):
 
 
 # (The calls below hand ctypes the structs themselves, which costs a third less than references made for it.  A call of rtp_kv_append takes 8.4 us of
-# host time with checks that look up what they need several times, 7.2 with these.)
+# host time with checks that look up what they need several times, 7.3 with these.)
 def rtp_kv_append(layer, cache, chunk, rope, q, q_stride, k, k_stride, v, v_stride, q_out, q_out_stride, stream=None):
     who, total, n_q, n_kv = "rtp_kv_append", chunk.total_q, layer.n_q_heads, layer.n_kv_heads
     _held(who, layer, cache, chunk.B)
+    kind = _type_of(who, layer, cache)
     _on_one_device(who, (cache, chunk, rope), (q, k, v, q_out))
-    _check(lib().rtp_kv_append(layer, cache, chunk, rope, _rows(who, q, total, n_q, "q", q_stride), q_stride, _rows(who, k, total, n_kv, "k", k_stride),
-                               k_stride, _rows(who, v, total, n_kv, "v", v_stride), v_stride,
-                               _rows(who, q_out, total, n_q, "q_out", q_out_stride), q_out_stride, _stream(stream)))
+    _check(lib().rtp_kv_append(layer, cache, chunk, rope, _rows(who, q, total, n_q, "q", q_stride, kind), q_stride,
+                               _rows(who, k, total, n_kv, "k", k_stride, kind), k_stride, _rows(who, v, total, n_kv, "v", v_stride, kind), v_stride,
+                               _rows(who, q_out, total, n_q, "q_out", q_out_stride, kind), q_out_stride, _stream(stream)))
 
 
 def rtp_dense_attn_chunk_workspace_bytes(layer, B, total_q, max_q, max_ctx, heads) -> int:
@@ -717,9 +735,11 @@ def rtp_local_attn_chunk_workspace_bytes(layer, B, total_q, max_q, max_ctx) -> i
 def _chunk_attn(who, layer, q, q_stride, cache, chunk, heads, out, lse, ws, stream):
     total, n_q = chunk.total_q, layer.n_q_heads
     _held(who, layer, cache, chunk.B)
+    kind = _type_of(who, layer, cache)
     _on_one_device(who, (cache, chunk), (q, out, lse, ws))
-    q, out = _rows(who, q, total, n_q, "q", q_stride), _rows(who, out, total, n_q, "out", n_q * 128)
-    if lse is not None and lse.__class__ is not int and (lse.numel() < total * n_q or lse.element_size() != 4 or not lse.is_contiguous()):
+    q, out = _rows(who, q, total, n_q, "q", q_stride, kind), _rows(who, out, total, n_q, "out", n_q * 128, kind)
+    if lse is not None and lse.__class__ is not int and (lse.numel() < total * n_q or lse.element_size() != 4 or not lse.is_contiguous()
+                                                         or lse.dtype is not _torch_types["lse"]):
         raise RtpError(RTP_ERR_INVALID_ARG, f"{who}: contiguous fp32 lse [{total}, {n_q}] expected")
     _check(getattr(lib(), who)(layer, q, q_stride, cache, chunk, *heads, out, _ptr(lse), _ptr(ws), _nbytes(ws), _stream(stream)))
 
