@@ -40,7 +40,7 @@ struct ChunkBlocks {
   const uint8_t* base1;
   uint32_t at_lo, at_hi, sc_lo, sc_hi;           // places of half blocks (16 keys lie in one page), two per block, of 32 blocks
   int next_page, window;
-  bool lost;                                     // a page was not there; the first was taken for it
+  bool lost;                                     // a page that some row sees was not there; the first was taken for it
 
   __device__ __forceinline__ ChunkBlocks(const ChunkArgs& a_, const ChunkTile& t_)
       : a(a_), t(t_), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), g(lane >> 5),
@@ -82,7 +82,7 @@ struct ChunkBlocks {
     const int n = half_n0(w * 32 + (lane >> 1), lane & 1);
     const bool there = (uint32_t)next_page < (uint32_t)(KV4 ? a.c4.n_pages : a.c16.n_pages);
     const uint32_t page = there ? (uint32_t)next_page : 0u, slot = n & ((1 << (KV4 ? a.c4.page_shift : a.c16.page_shift)) - 1);
-    lost = lost || __ballot(!there) != 0ull;
+    lost = lost || __ballot(!there && (!LOCAL || chunk_any_seen<LOCAL>(a.shape, t, t.m_lo, t.m_hi, n, 16))) != 0ull;
     uint64_t at;
     if constexpr (KV4) {
       at = (uint64_t)page * a.c4.code_page16 * 16u + (uint64_t)slot * kKv4Row;

@@ -99,13 +99,13 @@ struct ChunkWide {
   __device__ __forceinline__ void look_up(int window) {
     next_page = t.pt[piece_row(window * 64 + lane) >> (KV4 ? a.c4.page_shift : a.c16.page_shift)];
   }
-  // (an entry that names no page is taken for the first page; the range is repeated)
+  // (an entry that names no page is taken for the first page; the range is repeated if some row sees these keys)
   __device__ __forceinline__ void take_window(int window) {
     const int n = piece_row(window * 64 + lane);
     const bool there = (uint32_t)next_page < (uint32_t)(KV4 ? a.c4.n_pages : a.c16.n_pages);
     const uint32_t page = there ? (uint32_t)next_page : 0u;
     const uint32_t slot = n & ((1 << (KV4 ? a.c4.page_shift : a.c16.page_shift)) - 1);
-    lost = lost || __ballot(!there) != 0ull;
+    lost = lost || __ballot(!there && (!LOCAL || chunk_any_seen<LOCAL>(a.shape, t, t.m_lo, t.m_hi, n, kRowsEach))) != 0ull;
     uint64_t at;
     if constexpr (KV4) {
       at = (uint64_t)page * a.c4.code_page16 * 16u + (uint64_t)slot * kKv4Row;

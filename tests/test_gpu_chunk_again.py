@@ -43,3 +43,24 @@ def test_few_rows_beside_a_chunk(why, cache, dtype):
         few, many = [0, 1, 73] if why == "not_finite" else [0, 1, 2, 73], range(3, 72, 6)
         check_rows(b, out, lse, [(i, h) for i in few for h in range(8)], parts=2, faint=faint, **how)
         check_rows(b, out, lse, [(i, h) for i in many for h in range(8)], faint=2.0 ** 13 * faint, **how)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("cache", ["16", "4"])
+@pytest.mark.parametrize("sink", [0, 20])
+def test_pages_that_nobody_sees(sink, cache, dtype):
+    """Pages between the sink and the first window are given back, as a server does with them: their tiles of keys, which the window's edge and the sink
+    share with what is seen, are not taken again -- the results are those of before to the bit (sink 20: every row sees its reference)."""
+    b = Batch(new=[70, 2], past=[1000, 777], cache=cache, dtype=DT[dtype], seed=34)
+    how = dict(sink=sink, window=300)
+    whole = [run(b, "local", **how)[:2] for run in (wide.run_small, wide.run)]
+    for s in range(2):
+        first = max(0, b.ctx[s] - b.new[s] - 300 + 1)
+        b.table[s, -(-sink // b.page):first // b.page] = -1
+    assert (b.table[0, :44] == -1).sum() >= 40
+    faint = 0.0 if dtype == "bf16" else 2.0 ** -25
+    for (out0, lse0), run in zip(whole, (wide.run_small, wide.run)):
+        out, lse, _ = run(b, "local", **how)
+        check_rows(b, out, lse, [(i, h) for i in range(0, 72, 5) for h in range(8)], faint=faint, **how)
+        same = bool((out == out0).all()) and bool((lse == lse0).all())
+        assert same or sink == 0
