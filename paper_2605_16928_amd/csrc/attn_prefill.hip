@@ -1965,12 +1965,12 @@ __global__ __launch_bounds__(kPwThreads, 2) void flash_prefill_wide_kernel(const
     const int n_kept = SPARSE ? sel_cnt + __shfl_xor(sel_cnt, 32) : 0;
     const bool sees_key = SPARSE ? n_kept > 0 : (qok && tile_n0(it_lo) <= mq);
     // (fp16 probabilities: nothing above 65504 -- a larger one is infinite and shows in the sum -- and a
-    // row whose largest probability is below 2^-6 may have most of its mass in subnormals.  Few kept keys may have a smaller sum: a subnormal is
-    // off by at most 2^-25, and n of those are within 2^-11 of a sum of n * 2^-14, as the rounding of n normal probabilities is.  A query
+    // row whose largest probability is below 2^-6 may have most of its mass in subnormals.  A subnormal is off by at most 2^-25, and n of those are within 2^-11
+    // of a sum of n * 2^-14, as the rounding of n normal probabilities is: in selecting mode, where the reference may be a key that the query does not
+    // keep, that is what a sum has to reach (half of what the reference itself adds is enough).  A query
     // that keeps a few keys of a range, all far below its first tile's best, is one of 256 in hundreds of tiles nearly always, and the whole range was
     // repeated for it.  Attention launch at 128K tokens, 333, 2000 and 4096 queries (clusters): 365 -> 150, 1547 -> 606, 1472 -> 939 us.)
-    float least = F16 ? 0x1p-6f : 0x1p-60f;
-    if (SPARSE && F16) least = fminf(least, (float)n_kept * 0x1p-14f);
+    const float least = !F16 ? 0x1p-60f : SPARSE ? fminf(0x1p-1f, (float)n_kept * 0x1p-14f) : 0x1p-6f;
     bad = bad || (sees_key && !(ltot > least && ltot < 0x1p100f));
     redo = __syncthreads_or(bad ? 1 : 0) != 0;
   }
