@@ -387,13 +387,17 @@ class Kv4DecodeRun(DecodeRun):
 
     def draft_attn(self, q, out=None, lse=None):
         """Attention of the last T tokens of every context (a draft that grow() added), q [B, T, n_q_heads, 128], as a verification
-        needs it: the retrieval heads over every token up to their own, the others over the sink and the window."""
+        needs it: the retrieval heads over every token up to their own, the others over the sink and the window.  (out [B, T, n_q_heads, 128],
+        lse [B, T, n_q_heads]), contiguous, the caller's or new."""
         L, B = self.w.layer, self.B
         if q.dim() != 4 or q.shape[0] != B or q.shape[1] < 1 or not q.is_contiguous():
             raise rtp.RtpError(rtp.RTP_ERR_INVALID_ARG, f"Kv4DecodeRun: contiguous queries of {B} contexts expected")
         T, q = q.shape[1], q.reshape(-1, *q.shape[2:])
         out = torch.zeros_like(q) if out is None else out
         lse = torch.zeros(q.shape[:2], dtype=torch.float32, device=DEV) if lse is None else lse
+        if out.numel() != q.numel() or lse.numel() != B * T * L.n_q_heads or not out.is_contiguous() or not lse.is_contiguous():
+            raise rtp.RtpError(rtp.RTP_ERR_INVALID_ARG, f"Kv4DecodeRun: contiguous outputs and log-sums of {B} x {T} tokens expected")
+        out, lse = out.view(q.shape), lse.view(-1, q.shape[1])
         chunk = rtp.chunk_desc(torch.arange(0, B * T + 1, T, dtype=torch.int32, device=DEV), self.ctx_len, B * T, T, self.max_ctx)
         if L.n_ret:
             ws = ws_alloc(rtp.rtp_dense_attn_chunk_workspace_bytes(self.desc, B, B * T, T, self.max_ctx, rtp.RTP_HEADS_RETRIEVAL))
