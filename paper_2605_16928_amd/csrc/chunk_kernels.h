@@ -20,9 +20,12 @@ namespace rtp {
         again = ChunkNarrow<F16, LOCAL, KV4, kCkWaves, false>(a, t, smem).run();                                        \
       } else {                                                                                                          \
         ChunkWide<F16, LOCAL, KV4, FULL> w(a, t, smem);                                                                 \
-        w.m = -__builtin_huge_valf();                                                                                   \
-        w.clear();                                                                                                      \
-        again = t.it_lo < t.it_hi && w.fast_pass();                                                                     \
+        if (t.it_lo < t.it_hi) {                                                                                        \
+          again = w.fast_pass();                                                                                        \
+        } else {                                                                                                        \
+          w.m = -__builtin_huge_valf();                                                                                 \
+          w.clear();                                                                                                    \
+        }                                                                                                               \
         if (!again) w.store();                                                                                          \
       }                                                                                                                 \
     }                                                                                                                   \

@@ -140,8 +140,7 @@ struct ChunkWide {
   __device__ __forceinline__ uint32_t edge_off(int p, bool second) const {
     const int left = t.kend - 1 - piece_row(p);
     if constexpr (KV4) {
-      const int n = min(lane >> 3, left), of = lane & 7, s4 = piece_row(p) & 3;
-      (void)s4;
+      const int n = min(lane >> 3, left), of = lane & 7;
       return second ? (uint32_t)((n >> 2) * kKv4Group + of * 4 + (n & 3)) : (uint32_t)(n * kKv4Row + of * 16);
     } else {
       const int sub = lane >> 4;
