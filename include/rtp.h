@@ -713,8 +713,8 @@ int32_t rtp_kv_append(const rtp_layer_desc* layer, const rtp_kv_cache* cache, co
  * (rtp_dense_attn_chunk: of every query head, or of the retrieval heads alone, as rtp_sparse_attn_prefill with p >= 1) or { n < sink } U
  * { m - window < n <= m } (rtp_local_attn_chunk: of every other head).  q [total_q, n_q_heads, 128] with tokens q_stride elements apart; out
  * [total_q, n_q_heads, 128] contiguous, not overlapping q; lse fp32 [total_q, n_q_heads] or NULL.  Rows of heads that the call does not serve are left as
- * they are.  A row that sees no token writes zeros and lse = -inf; what a row does not see (NaN and infinities there too) does not
- * change it.  The _kv4 forms read the 4-bit cache and take K and V as rtp_kv4_read gives them.
+ * they are.  A row that sees no token writes zeros and lse = -inf; what a row does not see (NaN and infinities there too, pages that are
+ * not there) does not change it beyond the rounding of its last bits.  The _kv4 forms read the 4-bit cache and take K and V as rtp_kv4_read gives them.
  * A workspace for (B, total_q, max_q, max_ctx) serves every call with smaller ones. */
 #define RTP_HEADS_ALL        0
 #define RTP_HEADS_RETRIEVAL  1

@@ -6,6 +6,10 @@
 // reference, and a range after whose pass some row's sum or output says that this did not do (chunk_reach.h; or not finite), or
 // which met a page that is not there, is left to a launch that goes through such ranges with a running maximum (exact_pass).
 //
+// Probabilities enter the product as 16 bits, once: outputs are off by 0.0023 (bf16, relative to their size) where 0.0017 is their own rounding.  The
+// second part of tiles of few rows would be half as many products again where the matrix cores are the bound: these alone, without the subtractions and
+// roundings, take 4096 tokens behind 126976 from 979 to 1262 us, a mixed batch from 161 to 197.
+//
 // K/V tiles rotate through three LDS buffers with one barrier per tile, in its middle: it publishes tile x + 1, and behind it every wave is done
 // with tile x - 1, whose buffer tile x + 2 fills.  Tiles that every row sees in full run in a loop without a branch; the others -- the first, those
 // on the window's edge and on the diagonal -- block by block, with masks.

@@ -484,8 +484,9 @@ class PrefillRun:
 class ServeRun:
     """One layer's attention in a server of `seqs` places: every step takes the new tokens of all places, packed -- a prompt's chunk beside
     drafts and single tokens, none where a place waits --, hands out pages of a 16-bit cache, rotates the rows and appends them, and attends:
-    the retrieval heads over every token, the others over the sink and the window.  The host knows the lengths, so that a step that
-    lacks pages or room is refused before anything changes."""
+    the retrieval heads over every token, single tokens' too, the others over the sink and the window.  No index keys are kept and no tokens selected: the
+    top-p step is DecodeRun's and Kv4DecodeRun's.  The host knows the lengths, so that a step that lacks pages or room is refused before
+    anything changes."""
 
     def __init__(self, layer: wl.Layer, seqs: int, n_pages: int, page_size: int = 64, max_ctx: int = 32768, max_tokens: int = 4096,
                  inv_freq=None, interleaved: bool = False):
