@@ -291,7 +291,7 @@ struct ChunkWide {
     end_block();
   }
 
-  static constexpr float kOutstanding = 12.f;    // (in the logarithm to the base of 2)
+  static constexpr float kOutstanding = 12.f, kAlike = 10.f;                // (in the logarithm to the base of 2)
   // ---- the pass against fixed references; true: some row needs another ----
   __device__ __forceinline__ bool fast_pass() {
     const float ninf = -__builtin_huge_valf();
@@ -317,9 +317,9 @@ struct ChunkWide {
     // (of what the row sees there, if it does see anything)
     float any = ninf;
     m = ninf;
-    // fp16: of the first tile that every row sees in full, if there is one, and of the range's first tile what is more than 2^12 above that.  A
-    // context's first token often has most of the softmax, at 2^15 or more above the others, and fp16 has 14 binades below the reference in which a
-    // probability is whole, 16 above.  (A window: rows see a part of the first tile, or nothing, and a few keys' best may be 2^16 below the
+    // fp16: of the first tile that every row sees in full, if there is one, unless one of the two tiles stands out: then 2^12 below its best, or near
+    // the other's.  A context's first token often has most of the softmax, at 2^15 or more above the others, and fp16 has 14 binades below the
+    // reference in which a probability is whole, 16 above.  (A window: rows see a part of the first tile, or nothing, and a few keys' best may be 2^16 below the
     // row's.  A chunk of 4096 tokens, sink 0, 1210 us and 517, all units having been taken again.)
     float full = ninf;
     if constexpr (F16) {
@@ -346,7 +346,8 @@ struct ChunkWide {
     m = fmaxf(m, __shfl_xor(m, 32));
     any = fmaxf(any, __shfl_xor(any, 32));
     const bool held = m > ninf || full > ninf;
-    m = !held ? any : full > ninf ? fmaxf(full, m - kOutstanding / c) : m;
+    if (full > ninf) m = m > ninf ? fmaxf(fminf(full, m + kAlike / c), fmaxf(full, m) - kOutstanding / c) : full;
+    else if (!held) m = any;
     // At the start of half hf of tile x: S holds the scores of that block if the wave has a row that sees one of its keys; if `pend`, the
     // probabilities of the block before wait in P1 (hf = 0, V in the tile before) or P0; tiles x and x + 1 are in LDS.
     bool pend = false;

@@ -60,12 +60,22 @@ def test_a_strong_key_in_front_of_the_window(cache):
 @pytest.mark.parametrize("again", [False, True], ids=["plain", "taken_again"])
 @pytest.mark.parametrize("cache", ["16", "4"])
 def test_a_dominant_key_without_a_value(cache, again):
-    """One of a context's first tokens has nearly all of the softmax and a value of 0, as the first token of a prompt often has: the outputs are
+    _dominant(5, cache, again)
+
+
+@pytest.mark.parametrize("cache", ["16", "4"])
+@pytest.mark.parametrize("pos", [63, 64, 127, 128, 3000])
+def test_a_dominant_key_anywhere(pos, cache):
+    _dominant(pos, cache, False)
+
+
+def _dominant(pos, cache, again):
+    """One of a context's tokens has nearly all of the softmax and a value of 0, as the first token of a prompt often has: the outputs are
     sums of probabilities 16 below it, 2^-23 of it each.  Wide tiles, whose keys are not cut; with a page that is not there they are taken again."""
     b = Batch(new=[2048], past=[6000], hq=32, hkv=8, dtype=torch.float16, page=64, cache=cache, seed=23)
     u = alike(b, 24)
     put(b, 0, slice(None), 0.05 * torch.randn((8, b.n_pages, b.page, 128), generator=torch.Generator().manual_seed(25)))
-    page, slot = b.spot(0, 5)
+    page, slot = b.spot(0, pos)
     put(b, 0, (slice(None), page, slot), 16.0 * 128 ** 0.5 * u / u.square().sum(1, keepdim=True))
     strong = (b.rows[0][:, page, slot].double() * u.double()).sum(1) * 128.0 ** -0.5
     assert 14.0 < strong.min() < strong.max() < 17.0
